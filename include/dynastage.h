@@ -539,6 +539,63 @@ ds_status ds_norm_bwd(int32_t dtype, int32_t rms, int32_t rows, int32_t d, const
                       float* dg, float* db, float* partial, int32_t accumulate, void* hip_stream);
 int64_t ds_norm_bwd_scratch_floats(int32_t rows, int32_t d);
 
+/* The joint between two blocks of a layer, in one pass over the rows (norms before and after a block, gate, residual scale):
+ *     z = N_post(h)   (post_g = NULL: z = h)
+ *     y = resid_scale * x + branch_scale * gate . z      (the stream; stored)
+ *     u = N_pre(y)    (of y as stored; pre_g = NULL: not computed)
+ * rms = 0: LayerNorm (gain and bias, eps 1e-5); 1: RMSNorm (gain only, eps 1e-6), for both norms.
+ * x, h, y, u: [rows, d] row-major, contiguous, d a multiple of 8, at most 8192; all tensors 16-byte aligned.
+ * gate_kind: DS_GATE_NONE (gate NULL), DS_GATE_COL ([d], one factor per column), DS_GATE_ROW ([rows, d]).
+ * row_valid: NULL, or DEVICE int32[rows]: where it is negative the inputs are not looked at (they may be NaN), y and u are
+ * written as zeros.  stats: float32 [4, rows], mean and rstd of the rows of h, then of y, for the backward pass.
+ * y may be x, and u may be h. */
+enum { DS_GATE_NONE = 0, DS_GATE_COL = 1, DS_GATE_ROW = 2 };
+ds_status ds_resid_norm_fwd(int32_t dtype, int32_t rms, int32_t rows, int32_t d, const void* x, const void* h,
+                            const int32_t* row_valid, const void* post_g, const void* post_b, int32_t gate_kind,
+                            const void* gate, float resid_scale, float branch_scale, const void* pre_g,
+                            const void* pre_b, void* y, void* u, float* stats, void* hip_stream);
+/* Backward: dy (may be NULL: no gradient of y but through u) and du (with pre_g) -> dx, dh and the gradients of the
+ * parameters.  y, h, gate, stats: as the forward pass read and left them.  dgate: float32 [d] (DS_GATE_COL) or a [rows, d]
+ * tensor (DS_GATE_ROW).  dpost_g, dpost_b, dpre_g, dpre_b: float32 [d]; those of a norm that is there must be given (biases:
+ * LayerNorm only).  accumulate = 1 adds to the float32 gradients.  Rows with negative row_valid: zeros in dx, dh and dgate,
+ * nothing in the sums.  dx may be dy, dh may be du or h.
+ * partial: float32 scratch of at least ds_resid_norm_bwd_scratch_floats(rows, d), 16-byte aligned; calls that share it must
+ * not overlap. */
+ds_status ds_resid_norm_bwd(int32_t dtype, int32_t rms, int32_t rows, int32_t d, const void* dy, const void* du,
+                            const void* y, const void* h, const int32_t* row_valid, const void* post_g,
+                            const void* post_b, int32_t gate_kind, const void* gate, float resid_scale,
+                            float branch_scale, const void* pre_g, const float* stats, void* dx, void* dh, void* dgate,
+                            float* dpost_g, float* dpost_b, float* dpre_g, float* dpre_b, float* partial,
+                            int32_t accumulate, void* hip_stream);
+int64_t ds_resid_norm_bwd_scratch_floats(int32_t rows, int32_t d);
+
+/* Rotary positions.  x: [rows, >= n_heads * head_dim] with row stride ldx (elements), heads consecutive column groups; of each
+ * head the first rot_dim columns are turned in pairs, (2p, 2p + 1) with interleaved = 1, (p, p + rot_dim / 2) with 0: pair p of
+ * row r by the angle pos[r] * freq[p],
+ *     (x0, x1) -> amplitude * (x0 cos - x1 sin, x1 cos + x0 sin);
+ * inverse = 1 turns by the negative angle with the same amplitude, which is the gradient.  The other columns of a head are
+ * copied.  pos: DEVICE int32[rows]; rows with a negative position are not touched.  freq: DEVICE float64[rot_dim / 2], radians
+ * per position (ds_rope_freqs); angles are taken in 64 bits.  y: like x, row stride ldy; y = x with ldy = ldx turns in place;
+ * other overlaps are not allowed.  Query and key heads that lie side by side (a packed QKV tensor) go in one call.
+ * Any even rot_dim and any alignment of the element type; with 16-byte aligned rows, head_dim % 8 == 0 and rot_dim % 16 == 0 the
+ * accesses are 16 bytes wide. */
+ds_status ds_rope(int32_t dtype, int32_t rows, int32_t n_heads, int32_t head_dim, int32_t rot_dim, int32_t interleaved,
+                  int32_t inverse, const int32_t* pos, const double* freq, float amplitude, const void* x, int64_t ldx,
+                  void* y, int64_t ldy, void* hip_stream);
+/* HOST: freq[p] = base^(-2p / rot_dim), p < rot_dim / 2, scaled for contexts longer than the one trained on:
+ *   PLAIN   as it is
+ *   LINEAR  divided by factor (positions interpolated)
+ *   BASE    base * factor^(rot_dim / (rot_dim - 2)) instead of base: the slowest pair is slowed by factor, the fastest not at all
+ *   BANDS   by turns over `context` (the length trained on): pairs that make at least high_turns stay, pairs that make at most
+ *           low_turns are divided by factor, those between are a weighted mean of both, linear in the turns
+ * Arguments that a kind does not name are not looked at.  Errors: DS_EINVAL. */
+enum { DS_ROPE_PLAIN = 0, DS_ROPE_LINEAR = 1, DS_ROPE_BASE = 2, DS_ROPE_BANDS = 3 };
+ds_status ds_rope_freqs(int32_t rot_dim, double base, int32_t scaling, double factor, double context, double low_turns,
+                        double high_turns, double* freq);
+/* HOST: pos[r], r < total_rows (which = 0) or total_rows_tgt (1): the position of stream row r within its sequence, -1 for
+ * padding rows.  Errors: DS_EINVAL, DS_ELAYOUT (no such stream). */
+ds_status ds_layout_positions(const ds_layout* layout, int32_t which, int32_t* pos);
+
 /* out[n] (float32) = sum_m x[m,n] (+ out[n] if accumulate).  partial as above (same size rule). */
 ds_status ds_colsum(int32_t dtype, int32_t rows, int32_t n, const void* x, float* out, float* partial,
                     int32_t accumulate, void* hip_stream);

@@ -18,6 +18,8 @@ DS_COST_POLY_GPT, DS_COST_POLY_T5, DS_COST_TABLE = 0, 1, 2
 DS_MODEL_GPT, DS_MODEL_T5 = 0, 1
 DS_DTYPE_F32, DS_DTYPE_BF16 = 0, 1
 DS_EPI_NONE, DS_EPI_GELU, DS_EPI_RESID, DS_EPI_DGELU, DS_EPI_ACC32, DS_EPI_GATE, DS_EPI_DGATE, DS_EPI_GELU_D, DS_EPI_MULR = range(9)
+DS_GATE_NONE, DS_GATE_COL, DS_GATE_ROW = range(3)
+DS_ROPE_PLAIN, DS_ROPE_LINEAR, DS_ROPE_BASE, DS_ROPE_BANDS = range(4)
 
 PROF_KINDS = ("gemm_fwd", "gemm_dgrad", "gemm_wgrad", "attn_fwd", "attn_bwd", "norm", "colsum", "other", "transpose")
 
@@ -29,6 +31,7 @@ EXPORTS = ["dp_plan", "dp_plan_sampled", "dp_plan_replicas", "ds_plan_recompute"
            "ds_stage_create", "ds_stage_destroy", "ds_stage_workspace_bytes", "ds_stage_workspace_need", "stage_fwd_bwd",
            "ds_stage_last_launch_count", "ds_stage_weights_unchanged", "ds_stage_profile_enable", "ds_stage_profile_read", "ds_pack", "ds_unpack", "ds_gemm", "ds_gemm_ws", "ds_attention_fwd",
            "ds_attention_bwd", "ds_attention_scratch_bytes", "ds_norm_fwd", "ds_norm_bwd", "ds_norm_bwd_scratch_floats", "ds_colsum", "ds_colsum_static",
+           "ds_resid_norm_fwd", "ds_resid_norm_bwd", "ds_resid_norm_bwd_scratch_floats", "ds_rope", "ds_rope_freqs", "ds_layout_positions",
            "ds_mfma_probe", "ds_version"]
 
 
@@ -113,6 +116,7 @@ def lib():
         _lib.ds_stage_workspace_need.restype = C.c_int64
         _lib.ds_norm_bwd_scratch_floats.restype = C.c_int64
         _lib.ds_attention_scratch_bytes.restype = C.c_int64
+        _lib.ds_resid_norm_bwd_scratch_floats.restype = C.c_int64
         _lib.ds_layout_free.restype = None
         _lib.ds_stage_destroy.restype = None
     return _lib
@@ -540,6 +544,114 @@ def ds_norm_bwd(dy, x, g, stats, resid, dx, dg, db, partial, rms=False, accumula
                            _dp(g), _dp(stats), _dp(resid), _dp(dx), _dp(dg), _dp(db), _dp(partial),
                            C.c_int32(int(accumulate)), _stream(stream))
     _check(rc, "ds_norm_bwd")
+
+
+def _tensor(t, name, shape, dtype, device):
+    """Pointer of a contiguous tensor of the given shape (a number: at least so many elements), element type and device; None stays None."""
+    if t is None:
+        return None
+    fits = t.numel() >= shape if isinstance(shape, int) else tuple(t.shape) == tuple(shape)
+    if not fits or t.dtype != dtype or t.device != device or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous %s tensor of %s on %s, got %s %s on %s" % (name, dtype, shape, device, t.dtype, tuple(t.shape), t.device))
+    return C.c_void_p(t.data_ptr())
+
+
+def _columns(t, name, rows, cols, dtype, device):
+    """(pointer, row stride) of a 2-D tensor with at least `rows` rows and `cols` columns that lie next to each other: a column range of a
+    wider tensor, for instance."""
+    if t.dim() != 2 or t.shape[0] < rows or t.shape[1] < cols or (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]) \
+            or t.dtype != dtype or t.device != device:
+        raise ValueError("%s must be a [>= %d, >= %d] %s tensor with consecutive columns on %s, got %s %s, strides %s, on %s"
+                         % (name, rows, cols, dtype, device, t.dtype, tuple(t.shape), t.stride(), t.device))
+    return C.c_void_p(t.data_ptr()), max(t.stride(0), t.shape[1]) if t.shape[0] == 1 else t.stride(0)
+
+
+def _current(t):
+    """The device of t; kernels go to the current device, so it has to be that one."""
+    import torch
+    if t.device.type != "cuda" or t.device.index != torch.cuda.current_device():
+        raise ValueError("tensors must be on the current GPU, got %s" % (t.device,))
+    return t.device
+
+
+def _gate(gate, rows, d):
+    if gate is None:
+        return DS_GATE_NONE, None
+    return (DS_GATE_COL, (d,)) if gate.dim() == 1 else (DS_GATE_ROW, (rows, d))
+
+
+def ds_resid_norm_fwd(x, h, y, stats, post_g=None, post_b=None, gate=None, pre_g=None, pre_b=None, u=None, resid_scale=1.0, branch_scale=1.0,
+                      row_valid=None, rms=False, stream=None):
+    """gate: None, [d] or [rows, d]."""
+    import torch
+    dev, dt = _current(x), x.dtype
+    code = _dtype_code(x)
+    rows, d = x.shape
+    kind, gate_shape = _gate(gate, rows, d)
+    rc = lib().ds_resid_norm_fwd(C.c_int32(code), C.c_int32(int(rms)), C.c_int32(rows), C.c_int32(d), _tensor(x, "x", (rows, d), dt, dev),
+                                 _tensor(h, "h", (rows, d), dt, dev), _tensor(row_valid, "row_valid", (rows,), torch.int32, dev),
+                                 _tensor(post_g, "post_g", (d,), dt, dev), _tensor(post_b, "post_b", (d,), dt, dev), C.c_int32(kind),
+                                 _tensor(gate, "gate", gate_shape, dt, dev), C.c_float(resid_scale), C.c_float(branch_scale),
+                                 _tensor(pre_g, "pre_g", (d,), dt, dev), _tensor(pre_b, "pre_b", (d,), dt, dev), _tensor(y, "y", (rows, d), dt, dev),
+                                 _tensor(u, "u", (rows, d), dt, dev), _tensor(stats, "stats", (4, rows), torch.float32, dev), _stream(stream))
+    _check(rc, "ds_resid_norm_fwd")
+
+
+def ds_resid_norm_bwd_scratch_floats(rows, d):
+    return lib().ds_resid_norm_bwd_scratch_floats(C.c_int32(rows), C.c_int32(d))
+
+
+def ds_resid_norm_bwd(dy, y, h, stats, dx, dh, partial, du=None, post_g=None, post_b=None, gate=None, pre_g=None, dgate=None, dpost_g=None,
+                      dpost_b=None, dpre_g=None, dpre_b=None, resid_scale=1.0, branch_scale=1.0, row_valid=None, rms=False, accumulate=False,
+                      stream=None):
+    import torch
+    dev, dt, f32 = _current(h), h.dtype, torch.float32
+    code = _dtype_code(h)
+    rows, d = h.shape
+    kind, gate_shape = _gate(gate, rows, d)
+    full, col = (rows, d), (d,)
+    rc = lib().ds_resid_norm_bwd(C.c_int32(code), C.c_int32(int(rms)), C.c_int32(rows), C.c_int32(d), _tensor(dy, "dy", full, dt, dev),
+                                 _tensor(du, "du", full, dt, dev), _tensor(y, "y", full, dt, dev), _tensor(h, "h", full, dt, dev),
+                                 _tensor(row_valid, "row_valid", (rows,), torch.int32, dev), _tensor(post_g, "post_g", col, dt, dev),
+                                 _tensor(post_b, "post_b", col, dt, dev), C.c_int32(kind), _tensor(gate, "gate", gate_shape, dt, dev),
+                                 C.c_float(resid_scale), C.c_float(branch_scale), _tensor(pre_g, "pre_g", col, dt, dev),
+                                 _tensor(stats, "stats", (4, rows), f32, dev), _tensor(dx, "dx", full, dt, dev), _tensor(dh, "dh", full, dt, dev),
+                                 _tensor(dgate, "dgate", gate_shape, dt if kind == DS_GATE_ROW else f32, dev) if kind != DS_GATE_NONE else None,
+                                 _tensor(dpost_g, "dpost_g", col, f32, dev), _tensor(dpost_b, "dpost_b", col, f32, dev),
+                                 _tensor(dpre_g, "dpre_g", col, f32, dev), _tensor(dpre_b, "dpre_b", col, f32, dev),
+                                 _tensor(partial, "partial", int(ds_resid_norm_bwd_scratch_floats(rows, d)), f32, dev), C.c_int32(int(accumulate)),
+                                 _stream(stream))
+    _check(rc, "ds_resid_norm_bwd")
+
+
+def ds_rope(x, y, pos, freq, n_heads, head_dim, rot_dim, interleaved=False, inverse=False, amplitude=1.0, stream=None):
+    """x, y: 2-D, one row per token, heads first; y may be x."""
+    import torch
+    dev = _current(x)
+    code = _dtype_code(x)
+    rows = int(pos.shape[0])
+    px, ldx = _columns(x, "x", rows, n_heads * head_dim, x.dtype, dev)
+    py, ldy = _columns(y, "y", rows, n_heads * head_dim, x.dtype, dev)
+    rc = lib().ds_rope(C.c_int32(code), C.c_int32(rows), C.c_int32(n_heads), C.c_int32(head_dim), C.c_int32(rot_dim), C.c_int32(int(interleaved)),
+                       C.c_int32(int(inverse)), _tensor(pos, "pos", (rows,), torch.int32, dev), _tensor(freq, "freq", rot_dim // 2, torch.float64, dev),
+                       C.c_float(amplitude), px, C.c_int64(ldx), py, C.c_int64(ldy), _stream(stream))
+    _check(rc, "ds_rope")
+
+
+def ds_rope_freqs(rot_dim, base=10000.0, scaling=DS_ROPE_PLAIN, factor=1.0, context=0.0, low_turns=1.0, high_turns=32.0):
+    """float64 [rot_dim / 2]: radians per position of each pair (host)."""
+    out = np.zeros(max(int(rot_dim) // 2, 1), dtype=np.float64)
+    rc = lib().ds_rope_freqs(C.c_int32(rot_dim), C.c_double(base), C.c_int32(scaling), C.c_double(factor), C.c_double(context), C.c_double(low_turns),
+                             C.c_double(high_turns), _vp(out))
+    _check(rc, "ds_rope_freqs")
+    return out
+
+
+def ds_layout_positions(layout, which=0):
+    """int32 [stream rows]: position within its sequence, -1 in padding rows (host)."""
+    out = np.zeros(max(layout.total_rows_tgt if which else layout.total_rows, 1), dtype=np.int32)
+    _check(lib().ds_layout_positions(layout.handle, C.c_int32(which), _vp(out)), "ds_layout_positions")
+    return out
 
 
 def ds_mfma_probe(operands, sink, n_groups, iters, stream=None):
