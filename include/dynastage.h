@@ -528,6 +528,38 @@ ds_status ds_attention_bwd(int32_t dtype, int32_t n_seq, int32_t n_heads, int32_
                            int32_t k_total_rows, void* scratch, int64_t scratch_bytes,
                            int32_t force_generic, void* hip_stream);
 
+/* Bytes of DEVICE scratch the calls below need.  Calls that share one scratch buffer must not overlap. */
+int64_t ds_diff_attention_scratch_bytes(int32_t n_heads, int32_t q_total_rows, int32_t k_total_rows, int32_t n_seq);
+
+/* Differential attention: the difference of two softmax maps with a learned weight per head.  Tables, tensors and mask as in
+ * ds_attention_fwd; the first half of a head's q and k columns makes the scores of map 1, the second half those of map 2:
+ *     P_i = softmax(Q_i K_i^T / sqrt(head_dim / 2)),   O2 = P_2 V,   O = P_1 V - lambda[h] O2.
+ * head_dim: a multiple of 16, at most 128.  lambda: DEVICE float32[n_heads].  o, o2: [q_total_rows, ...] with row stride ldo; o2 is
+ * what the backward pass needs beside o and may be NULL.  lse: float32 [2 * n_heads, q_total_rows], map m of head h at 2h + m.
+ * q_total_rows / k_total_rows: rows of the tensors holding the queries / the keys; max_q_len / max_k_len: upper bounds of the lengths.
+ * Rows not covered by any sequence are not touched; the sequences must not overlap; one with k_len[s] = 0 gets zero outputs.
+ * Strides and alignments of the element type are taken as they are.  scratch: DEVICE, 16-byte aligned, at least
+ * ds_diff_attention_scratch_bytes.  force_generic != 0 selects the kernels that compute in fp32 whatever the type.
+ * Values that are not finite: a row is affected by the rows it sees, and by rows that mask = 1 hides up to 127 tokens behind it, since
+ * whole blocks are multiplied by probabilities that are 0 there. */
+ds_status ds_diff_attention_fwd(int32_t dtype, int32_t n_seq, int32_t n_heads, int32_t head_dim, int32_t mask,
+                                const int32_t* q_row, const int32_t* q_len, const int32_t* k_row, const int32_t* k_len,
+                                int32_t max_q_len, int32_t max_k_len,
+                                const void* q, int32_t ldq, const void* k, int32_t ldk, const void* v, int32_t ldv,
+                                const float* lambda, void* o, void* o2, int32_t ldo, float* lse,
+                                int32_t q_total_rows, int32_t k_total_rows, void* scratch, int64_t scratch_bytes,
+                                int32_t force_generic, void* hip_stream);
+/* Backward: given dO, O, O2, lse produce dQ, dK, dV (same strides as q, k, v) and dlambda, float32[n_heads], overwritten or
+ * added to (accumulate). */
+ds_status ds_diff_attention_bwd(int32_t dtype, int32_t n_seq, int32_t n_heads, int32_t head_dim, int32_t mask,
+                                const int32_t* q_row, const int32_t* q_len, const int32_t* k_row, const int32_t* k_len,
+                                int32_t max_q_len, int32_t max_k_len,
+                                const void* q, int32_t ldq, const void* k, int32_t ldk, const void* v, int32_t ldv,
+                                const float* lambda, const void* o, const void* o2, const void* d_o, int32_t ldo,
+                                const float* lse, void* dq, void* dk, void* dv, float* dlambda, int32_t accumulate,
+                                int32_t q_total_rows, int32_t k_total_rows, void* scratch, int64_t scratch_bytes,
+                                int32_t force_generic, void* hip_stream);
+
 /* Row normalisation.  rms = 0: LayerNorm (gain g, bias b, eps 1e-5, stats = mean and rstd);
  * rms = 1: RMSNorm (gain only, eps 1e-6, stats = rstd).  stats: float32 [2, rows]. */
 ds_status ds_norm_fwd(int32_t dtype, int32_t rms, int32_t rows, int32_t d, const void* x,

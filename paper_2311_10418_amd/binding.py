@@ -31,6 +31,7 @@ EXPORTS = ["dp_plan", "dp_plan_sampled", "dp_plan_replicas", "ds_plan_recompute"
            "ds_stage_create", "ds_stage_destroy", "ds_stage_workspace_bytes", "ds_stage_workspace_need", "stage_fwd_bwd",
            "ds_stage_last_launch_count", "ds_stage_weights_unchanged", "ds_stage_profile_enable", "ds_stage_profile_read", "ds_pack", "ds_unpack", "ds_gemm", "ds_gemm_ws", "ds_attention_fwd",
            "ds_attention_bwd", "ds_attention_scratch_bytes", "ds_norm_fwd", "ds_norm_bwd", "ds_norm_bwd_scratch_floats", "ds_colsum", "ds_colsum_static",
+           "ds_diff_attention_fwd", "ds_diff_attention_bwd", "ds_diff_attention_scratch_bytes",
            "ds_resid_norm_fwd", "ds_resid_norm_bwd", "ds_resid_norm_bwd_scratch_floats", "ds_rope", "ds_rope_freqs", "ds_layout_positions",
            "ds_mfma_probe", "ds_version"]
 
@@ -117,6 +118,7 @@ def lib():
         _lib.ds_norm_bwd_scratch_floats.restype = C.c_int64
         _lib.ds_attention_scratch_bytes.restype = C.c_int64
         _lib.ds_resid_norm_bwd_scratch_floats.restype = C.c_int64
+        _lib.ds_diff_attention_scratch_bytes.restype = C.c_int64
         _lib.ds_layout_free.restype = None
         _lib.ds_stage_destroy.restype = None
     return _lib
@@ -622,6 +624,60 @@ def ds_resid_norm_bwd(dy, y, h, stats, dx, dh, partial, du=None, post_g=None, po
                                  _tensor(partial, "partial", int(ds_resid_norm_bwd_scratch_floats(rows, d)), f32, dev), C.c_int32(int(accumulate)),
                                  _stream(stream))
     _check(rc, "ds_resid_norm_bwd")
+
+
+def ds_diff_attention_scratch_bytes(n_heads, q_total_rows, k_total_rows, n_seq):
+    return lib().ds_diff_attention_scratch_bytes(C.c_int32(n_heads), C.c_int32(q_total_rows), C.c_int32(k_total_rows), C.c_int32(n_seq))
+
+
+def _diff_tensors(q, k, v, lam, lse, q_row, q_len, k_row, k_len, n_heads, head_dim, scratch):
+    """The arguments both directions share: (dtype code, tables, tensors with strides, lambda, lse, rows, scratch), checked."""
+    import torch
+    dev, dt = _current(q), q.dtype
+    code = _dtype_code(q)
+    n, wide, i32 = int(q_row.shape[0]), n_heads * head_dim, torch.int32
+    q_rows, k_rows = int(q.shape[0]), int(k.shape[0])
+    tables = [_tensor(t, name, (n,), i32, dev) for t, name in ((q_row, "q_row"), (q_len, "q_len"), (k_row, "k_row"), (k_len, "k_len"))]
+    (pq, ldq), (pk, ldk), (pv, ldv) = (_columns(t, name, rows, wide, dt, dev) for t, name, rows in ((q, "q", q_rows), (k, "k", k_rows), (v, "v", k_rows)))
+    return (C.c_int32(code), n, tables, [pq, C.c_int32(ldq), pk, C.c_int32(ldk), pv, C.c_int32(ldv), _tensor(lam, "lam", (n_heads,), torch.float32, dev)],
+            _tensor(lse, "lse", (2 * n_heads, q_rows), torch.float32, dev),
+            [C.c_int32(q_rows), C.c_int32(k_rows), _tensor(scratch, "scratch", int(ds_diff_attention_scratch_bytes(n_heads, q_rows, k_rows, n)), torch.uint8, dev),
+             C.c_int64(scratch.numel())])
+
+
+def ds_diff_attention_fwd(q, k, v, lam, o, lse, q_row, q_len, k_row, k_len, n_heads, head_dim, causal, max_q_len, max_k_len, scratch, o2=None,
+                          force_generic=False, stream=None):
+    """q, k, v, o, o2: 2-D, a row per token (column ranges of wider tensors are fine; o and o2 with the same row stride); scratch: uint8."""
+    code, n, tables, qkv, plse, rest = _diff_tensors(q, k, v, lam, lse, q_row, q_len, k_row, k_len, n_heads, head_dim, scratch)
+    wide = n_heads * head_dim
+    po, ldo = _columns(o, "o", q.shape[0], wide, q.dtype, q.device)
+    po2, ldo2 = _columns(o2, "o2", q.shape[0], wide, q.dtype, q.device) if o2 is not None else (None, ldo)
+    if ldo2 != ldo:
+        raise ValueError("o and o2 must have the same row stride, got %d and %d" % (ldo, ldo2))
+    rc = lib().ds_diff_attention_fwd(code, C.c_int32(n), C.c_int32(n_heads), C.c_int32(head_dim), C.c_int32(int(causal)), *tables, C.c_int32(max_q_len),
+                                     C.c_int32(max_k_len), *qkv, po, po2, C.c_int32(ldo), plse, *rest, C.c_int32(int(force_generic)), _stream(stream))
+    _check(rc, "ds_diff_attention_fwd")
+
+
+def ds_diff_attention_bwd(q, k, v, lam, o, o2, d_o, lse, dq, dk, dv, dlam, q_row, q_len, k_row, k_len, n_heads, head_dim, causal, max_q_len, max_k_len,
+                          scratch, accumulate=False, force_generic=False, stream=None):
+    """dq, dk, dv have the strides of q, k, v; o, o2 and d_o the same row stride."""
+    import torch
+    code, n, tables, qkv, plse, rest = _diff_tensors(q, k, v, lam, lse, q_row, q_len, k_row, k_len, n_heads, head_dim, scratch)
+    wide, dt, dev = n_heads * head_dim, q.dtype, q.device
+    (po, ldo), (po2, ldo2), (pdo, lddo) = (_columns(t, name, q.shape[0], wide, dt, dev) for t, name in ((o, "o"), (o2, "o2"), (d_o, "d_o")))
+    if not ldo == ldo2 == lddo:
+        raise ValueError("o, o2 and d_o must have the same row stride, got %d, %d and %d" % (ldo, ldo2, lddo))
+    grads = []
+    for t, name, like in ((dq, "dq", q), (dk, "dk", k), (dv, "dv", v)):
+        p, ld = _columns(t, name, like.shape[0], wide, dt, dev)
+        if t.stride(0) != like.stride(0) and like.shape[0] > 1:
+            raise ValueError("%s must have the row stride of %s, got %d and %d" % (name, name[1:], t.stride(0), like.stride(0)))
+        grads.append(p)
+    rc = lib().ds_diff_attention_bwd(code, C.c_int32(n), C.c_int32(n_heads), C.c_int32(head_dim), C.c_int32(int(causal)), *tables, C.c_int32(max_q_len),
+                                     C.c_int32(max_k_len), *qkv, po, po2, pdo, C.c_int32(ldo), plse, *grads, _tensor(dlam, "dlam", (n_heads,), torch.float32, dev),
+                                     C.c_int32(int(accumulate)), *rest, C.c_int32(int(force_generic)), _stream(stream))
+    _check(rc, "ds_diff_attention_bwd")
 
 
 def ds_rope(x, y, pos, freq, n_heads, head_dim, rot_dim, interleaved=False, inverse=False, amplitude=1.0, stream=None):

@@ -1,0 +1,27 @@
+// Arguments shared by the kernels of differential attention.
+//
+// Head h owns columns h * head_dim .. of q, k, v, o.  The first half of its q and k columns makes the scores of map 1, the second
+// half those of map 2:  P_i = softmax(Q_i K_i^T / sqrt(head_dim / 2)),  O_2 = P_2 V,  O = P_1 V - lambda_h O_2.
+// Backward, with G = dO V^T, D_2 = rowsum(dO O_2), D_1 = rowsum(dO O) + lambda_h D_2 (= rowsum(dO O_1)):
+//     dS_1 = P_1 (G - D_1),  dS_2 = -lambda_h P_2 (G - D_2),  dQ_i = s dS_i K_i,  dK_i = s dS_i^T Q_i,
+//     dV = (P_1 - lambda_h P_2)^T dO,  dlambda_h = - sum P_2 G.
+// (dlambda is summed from the probabilities themselves, in fp32, and not from O_2, which is rounded to the tensors' type.)
+#pragma once
+#include "attention.hpp"
+
+struct DiffAttnArgs : AttnArgs {                        // scale: 1 / sqrt(head_dim / 2); lse: [2 n_heads][lse_stride], map m of head h at row 2h + m
+    const float* lambda;                                // [n_heads]
+    void* o2;                                           // forward: NULL or where O_2 goes; backward: O_2
+    float* dlambda;
+    int32_t accumulate;
+    float *d1, *d2;                                     // general kernels: D_1, D_2, [n_heads][q_total_rows]
+    float* lam_part;                                    // sums of P_2 G of the queries of a wavefront, at the row of its first query
+    int32_t vec;                                        // general kernels: rows of four elements may be accessed at once
+    char* aug;                                          // matrix-core kernels: see diff_attention_mfma.hip
+};
+
+size_t diff_scratch_bytes(int n_heads, int q_total_rows, int k_total_rows, int n_seq);
+ds_status diff_fwd_general(const DiffAttnArgs& a, hipStream_t st);
+ds_status diff_bwd_general(const DiffAttnArgs& a, hipStream_t st);
+// dlambda[h] = (accumulate ? dlambda[h] : 0) - the sums in lam_part, which stand `queries` rows apart within a sequence
+ds_status diff_dlambda(const DiffAttnArgs& a, int queries, hipStream_t st);

@@ -1,0 +1,87 @@
+// C-ABI entry points and dispatch of differential attention.
+#include "diff_attention.hpp"
+#include <cmath>
+
+// Scratch: the work lists of the matrix-core kernels, then four arrays of [n_heads][q_total_rows] entries of 16 bytes that the dQ kernels
+// hand to the dK/dV kernels (the general ones use two of them as arrays of floats), then the parts of dlambda, one float each.
+static size_t lists_size(int q_total_rows, int k_total_rows, int n_seq) { return attn_scratch_bytes(0, 0, q_total_rows, k_total_rows, n_seq); }
+size_t diff_scratch_bytes(int n_heads, int q_total_rows, int k_total_rows, int n_seq) {
+    return lists_size(q_total_rows, k_total_rows, n_seq) + (size_t)n_heads * q_total_rows * (4 * 16 + 4);
+}
+
+static bool four_at_once(const void* p, size_t size) { return !p || (uintptr_t)p % (4 * size) == 0; }
+
+static ds_status check(DiffAttnArgs& a) {
+    if (a.n_seq <= 0 || a.n_heads <= 0 || a.head_dim <= 0 || a.head_dim > 128 || a.head_dim % 16) return DS_EINVAL;
+    if (a.dtype != DS_DTYPE_F32 && a.dtype != DS_DTYPE_BF16) return DS_EINVAL;
+    if (a.mask != 0 && a.mask != 1) return DS_EINVAL;
+    if (!a.q_row || !a.q_len || !a.k_row || !a.k_len || !a.q || !a.k || !a.v || !a.lambda || !a.o || !a.lse) return DS_EINVAL;
+    if (a.max_q_len <= 0 || a.max_k_len <= 0 || a.q_total_rows <= 0 || a.k_total_rows <= 0) return DS_EINVAL;
+    if (a.n_seq > 65535 || a.n_heads > 65535) return DS_EINVAL;
+    const long long wide = (long long)a.n_heads * a.head_dim;
+    if (a.ldq < wide || a.ldk < wide || a.ldv < wide || a.ldo < wide) return DS_EINVAL;
+    if (!a.scratch || (uintptr_t)a.scratch % 16 || a.scratch_bytes < diff_scratch_bytes(a.n_heads, a.q_total_rows, a.k_total_rows, a.n_seq)) return DS_EINVAL;
+    const size_t size = dtype_size(a.dtype);
+    for (const void* p : {a.q, a.k, a.v, (const void*)a.o, (const void*)a.o2, a.d_o, (const void*)a.dq, (const void*)a.dk, (const void*)a.dv})
+        if ((uintptr_t)p % size) return DS_EINVAL;
+    a.vec = four_at_once(a.q, size) && four_at_once(a.k, size) && four_at_once(a.v, size) && four_at_once(a.o, size) && four_at_once(a.o2, size) &&
+            four_at_once(a.d_o, size) && four_at_once(a.dq, size) && four_at_once(a.dk, size) && four_at_once(a.dv, size) &&
+            a.ldq % 4 == 0 && a.ldk % 4 == 0 && a.ldv % 4 == 0 && a.ldo % 4 == 0;
+    a.scale = 1.0f / sqrtf((float)(a.head_dim / 2));
+    char* after_lists = (char*)a.scratch + lists_size(a.q_total_rows, a.k_total_rows, a.n_seq);
+    const size_t entries = (size_t)a.n_heads * a.q_total_rows;
+    a.aug = after_lists;
+    a.d1 = (float*)after_lists;
+    a.d2 = a.d1 + entries;
+    a.lam_part = (float*)(after_lists + entries * 4 * 16);
+    return DS_OK;
+}
+
+extern "C" int64_t ds_diff_attention_scratch_bytes(int32_t n_heads, int32_t q_total_rows, int32_t k_total_rows, int32_t n_seq) {
+    if (n_heads <= 0 || q_total_rows <= 0 || k_total_rows <= 0 || n_seq <= 0) return 0;
+    return (int64_t)diff_scratch_bytes(n_heads, q_total_rows, k_total_rows, n_seq);
+}
+
+extern "C" ds_status ds_diff_attention_fwd(int32_t dtype, int32_t n_seq, int32_t n_heads, int32_t head_dim, int32_t mask, const int32_t* q_row,
+                                           const int32_t* q_len, const int32_t* k_row, const int32_t* k_len, int32_t max_q_len, int32_t max_k_len,
+                                           const void* q, int32_t ldq, const void* k, int32_t ldk, const void* v, int32_t ldv, const float* lambda,
+                                           void* o, void* o2, int32_t ldo, float* lse, int32_t q_total_rows, int32_t k_total_rows, void* scratch,
+                                           int64_t scratch_bytes, int32_t force_generic, void* hip_stream) {
+    DiffAttnArgs a = {};
+    a.dtype = dtype; a.n_seq = n_seq; a.n_heads = n_heads; a.head_dim = head_dim; a.mask = mask;
+    a.q_row = q_row; a.q_len = q_len; a.k_row = k_row; a.k_len = k_len;
+    a.max_q_len = max_q_len; a.max_k_len = max_k_len;
+    a.q = q; a.k = k; a.v = v; a.ldq = ldq; a.ldk = ldk; a.ldv = ldv;
+    a.lambda = lambda;
+    a.o = o; a.o2 = o2; a.ldo = ldo; a.lse = lse; a.lse_stride = q_total_rows;
+    a.q_total_rows = q_total_rows; a.k_total_rows = k_total_rows;
+    a.scratch = scratch; a.scratch_bytes = scratch_bytes < 0 ? 0 : (size_t)scratch_bytes;
+    const ds_status r = check(a);
+    if (r != DS_OK) return r;
+    (void)force_generic;
+    return diff_fwd_general(a, (hipStream_t)hip_stream);
+}
+
+extern "C" ds_status ds_diff_attention_bwd(int32_t dtype, int32_t n_seq, int32_t n_heads, int32_t head_dim, int32_t mask, const int32_t* q_row,
+                                           const int32_t* q_len, const int32_t* k_row, const int32_t* k_len, int32_t max_q_len, int32_t max_k_len,
+                                           const void* q, int32_t ldq, const void* k, int32_t ldk, const void* v, int32_t ldv, const float* lambda,
+                                           const void* o, const void* o2, const void* d_o, int32_t ldo, const float* lse, void* dq, void* dk, void* dv,
+                                           float* dlambda, int32_t accumulate, int32_t q_total_rows, int32_t k_total_rows, void* scratch,
+                                           int64_t scratch_bytes, int32_t force_generic, void* hip_stream) {
+    DiffAttnArgs a = {};
+    a.dtype = dtype; a.n_seq = n_seq; a.n_heads = n_heads; a.head_dim = head_dim; a.mask = mask;
+    a.q_row = q_row; a.q_len = q_len; a.k_row = k_row; a.k_len = k_len;
+    a.max_q_len = max_q_len; a.max_k_len = max_k_len;
+    a.q = q; a.k = k; a.v = v; a.ldq = ldq; a.ldk = ldk; a.ldv = ldv;
+    a.lambda = lambda;
+    a.o = const_cast<void*>(o); a.o2 = const_cast<void*>(o2); a.d_o = d_o; a.ldo = ldo;
+    a.lse = const_cast<float*>(lse); a.lse_stride = q_total_rows;
+    a.dq = dq; a.dk = dk; a.dv = dv; a.dlambda = dlambda; a.accumulate = accumulate;
+    a.q_total_rows = q_total_rows; a.k_total_rows = k_total_rows;
+    a.scratch = scratch; a.scratch_bytes = scratch_bytes < 0 ? 0 : (size_t)scratch_bytes;
+    const ds_status r = check(a);
+    if (r != DS_OK) return r;
+    if (!o2 || !d_o || !dq || !dk || !dv || !dlambda || (accumulate != 0 && accumulate != 1)) return DS_EINVAL;
+    (void)force_generic;
+    return diff_bwd_general(a, (hipStream_t)hip_stream);
+}

@@ -1,0 +1,440 @@
+// Differential attention for every type, head size, stride and alignment the entry points take: v_mfma_f32_16x16x4_f32 on fp32 values
+// (bf16 operands are widened as their tiles go to LDS), so that products, probabilities and sums are fp32 throughout.
+//
+// A wavefront owns 16 "column" items (queries in forward and dQ, keys in dK/dV) and computes transposed score blocks of both maps: 16
+// rows of the other side x its 16 columns, lane = (column lane % 16, rows 4 g + e with g = lane / 16, e = 0..3).  Per column values
+// are per-lane scalars, and register e of a block is, as it stands, the B operand of the second product for the rows {4 g + e}.
+// Tiles of the other side are kept in LDS row by row, every half head padded with zeros to HH columns (a multiple of 16), V and dO too:
+// the contraction over features does not see the order of the columns, and outputs go back through the same mapping.
+#include "diff_attention.hpp"
+
+namespace {
+
+constexpr float kLog2eG = 1.4426950408889634f;
+constexpr float kLn2G = 0.6931471805599453f;
+
+__device__ __forceinline__ f32x4_t mfma4(float a, float b, f32x4_t c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x4_t zero4() { f32x4_t z = {0.f, 0.f, 0.f, 0.f}; return z; }
+
+template <class T> __device__ __forceinline__ float4 load4(const T* p, bool vec);
+template <> __device__ __forceinline__ float4 load4<float>(const float* p, bool vec) {
+    return vec ? *reinterpret_cast<const float4*>(p) : make_float4(p[0], p[1], p[2], p[3]);
+}
+template <> __device__ __forceinline__ float4 load4<bf16_t>(const bf16_t* p, bool vec) {
+    if (vec) {
+        const bf16x4_t v = *reinterpret_cast<const bf16x4_t*>(p);
+        return make_float4((float)v[0], (float)v[1], (float)v[2], (float)v[3]);
+    }
+    return make_float4((float)p[0], (float)p[1], (float)p[2], (float)p[3]);
+}
+__device__ __forceinline__ void store4(float* p, const f32x4_t& v, bool vec) {
+    if (vec) *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+    else
+        for (int j = 0; j < 4; ++j) p[j] = v[j];
+}
+__device__ __forceinline__ void store4(bf16_t* p, const f32x4_t& v, bool vec) {
+    if (vec) {
+        bf16x4_t b;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) b[j] = (bf16_t)v[j];
+        *reinterpret_cast<bf16x4_t*>(p) = b;
+    } else
+        for (int j = 0; j < 4; ++j) p[j] = (bf16_t)v[j];
+}
+
+template <class T, int HH> struct Tile {
+    static constexpr int ROWS = HH <= 48 ? 64 : 32, HD = 2 * HH, LD = HD + 4, NV = ROWS * HD / 4 / 256;
+    static constexpr int FLOATS = ROWS * LD;
+    float4 v[NV];
+    __device__ __forceinline__ void load(const T* src, long long ld, int r0, int n_rows, int half, bool vec) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int u = threadIdx.x + 256 * i, r = r0 + u / (HD / 4), d = (u % (HD / 4)) * 4, m = d >= HH;
+            v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (r < n_rows && d - m * HH < half) v[i] = load4<T>(src + (long long)r * ld + m * half + (d - m * HH), vec);
+        }
+    }
+    __device__ __forceinline__ void store(float* tile) const {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int u = threadIdx.x + 256 * i;
+            *reinterpret_cast<float4*>(tile + (u / (HD / 4)) * LD + (u % (HD / 4)) * 4) = v[i];
+        }
+    }
+};
+
+// this lane's column item: features 16 s + 4 g .. + 3, padded like the tiles
+template <class T, int HH>
+__device__ __forceinline__ void load_column(const T* row, int half, int g, bool vec, float4 (&f)[HH / 8]) {
+#pragma unroll
+    for (int s = 0; s < HH / 8; ++s) {
+        const int m = s >= HH / 16, d = 16 * s + 4 * g - m * HH;
+        f[s] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (d < half) f[s] = load4<T>(row + m * half + d, vec);
+    }
+}
+template <class T, int HH>
+__device__ __forceinline__ void store_column(const f32x4_t (&acc)[HH / 8], float mul, T* row, int half, int g, bool vec) {
+#pragma unroll
+    for (int s = 0; s < HH / 8; ++s) {
+        const int m = s >= HH / 16, d = 16 * s + 4 * g - m * HH;
+        if (d < half) store4(row + m * half + d, acc[s] * mul, vec);
+    }
+}
+
+// rows rb .. rb+15 of a tile times this lane's column item, contracted over the feature steps S0 .. S1-1
+template <int HH, int S0, int S1>
+__device__ __forceinline__ f32x4_t first_product(const float* tile, int rb, int lane, const float4 (&f)[HH / 8]) {
+    const float* p = tile + (rb + (lane & 15)) * (2 * HH + 4) + 4 * (lane >> 4);
+    f32x4_t acc = zero4();
+#pragma unroll
+    for (int s = S0; s < S1; ++s) {
+        const float4 x = *reinterpret_cast<const float4*>(p + 16 * s);
+        acc = mfma4(x.x, f[s].x, acc);
+        acc = mfma4(x.y, f[s].y, acc);
+        acc = mfma4(x.z, f[s].z, acc);
+        acc = mfma4(x.w, f[s].w, acc);
+    }
+    return acc;
+}
+// out^T[feature step S0 .. S1-1][column] += tile[rows rb .. rb+15]^T * w
+template <int HH, int S0, int S1>
+__device__ __forceinline__ void second_product(const float* tile, int rb, int lane, const f32x4_t& w, f32x4_t (&out)[HH / 8]) {
+    const float* p = tile + (rb + 4 * (lane >> 4)) * (2 * HH + 4) + (lane & 15);
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int s = S0; s < S1; ++s) out[s] = mfma4(p[e * (2 * HH + 4) + 16 * s], w[e], out[s]);
+}
+
+__device__ __forceinline__ float groups_max(float v) { v = fmaxf(v, __shfl_xor(v, 16, 64)); return fmaxf(v, __shfl_xor(v, 32, 64)); }
+__device__ __forceinline__ float groups_sum(float v) { v += __shfl_xor(v, 16, 64); return v + __shfl_xor(v, 32, 64); }
+
+// A work-group's 64 columns: sequence, head, first column (negative: nothing to do).  Sequences last to first: a plan lists them by
+// ascending length, and the longest chains of tiles should start first.
+struct ColumnBlock { int s, h, first; };
+__device__ __forceinline__ ColumnBlock column_block(const AttnArgs& a, const int32_t* len, bool last_first) {
+    ColumnBlock c = {a.n_seq - 1 - (int)blockIdx.z, (int)blockIdx.y, -1};
+    const int n = (len[c.s] + 63) / 64, b = blockIdx.x;
+    if (b < n) c.first = 64 * (last_first ? n - 1 - b : b);
+    return c;
+}
+// an odd number of blocks per grid row: work-groups go to the eight XCDs in turn, and the longest of every sequence should not meet on one
+dim3 column_grid(const AttnArgs& a, int max_len) { return dim3(((max_len + 63) / 64) | 1, a.n_heads, a.n_seq); }
+
+// ---------------------------------------------------------------- forward
+template <class T, int HH>
+__global__ __launch_bounds__(256) void diff_fwd_kernel(DiffAttnArgs a) {
+    typedef Tile<T, HH> Tl;
+    constexpr int KT = Tl::ROWS, NB = KT / 16, NS = HH / 8;
+    __shared__ __attribute__((aligned(16))) float sK[Tl::FLOATS];
+    __shared__ __attribute__((aligned(16))) float sV[Tl::FLOATS];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4;
+    const ColumnBlock cb = column_block(a, a.q_len, a.mask != 0);
+    if (cb.first < 0) return;
+    const int s = cb.s, h = cb.h, q0 = cb.first, ql = a.q_len[s], kl = a.k_len[s], hd = a.head_dim, half = hd / 2;
+    const bool vec = a.vec;
+    const long long qrow0 = a.q_row[s], krow0 = a.k_row[s];
+    const T* K = (const T*)a.k + krow0 * a.ldk + (long long)h * hd;
+    const T* V = (const T*)a.v + krow0 * a.ldv + (long long)h * hd;
+    const int qw0 = q0 + wave * 16, qi = qw0 + (lane & 15), qi_c = qi < ql ? qi : ql - 1;
+    float4 qf[NS];
+    load_column<T, HH>((const T*)a.q + (qrow0 + qi_c) * a.ldq + (long long)h * hd, half, g, vec, qf);
+    f32x4_t o1[NS], o2[NS];
+#pragma unroll
+    for (int i = 0; i < NS; ++i) { o1[i] = zero4(); o2[i] = zero4(); }
+    const float c = a.scale * kLog2eG;
+    float m1 = -INFINITY, m2 = -INFINITY, l1 = 0.f, l2 = 0.f;          // running maxima (exp2 domain), this lane's part of the sums
+    const int kv_end = a.mask ? min(kl, q0 + 64) : kl;
+    const int wave_last = a.mask ? min(kl - 1, qw0 + 15) : kl - 1;     // last key this wavefront can see
+    Tl tk, tv;
+    if (kv_end > 0) {
+        tk.load(K, a.ldk, 0, kl, half, vec);
+        tv.load(V, a.ldv, 0, kl, half, vec);
+    }
+    for (int k0 = 0; k0 < kv_end; k0 += KT) {
+        __syncthreads();                                               // the previous tile has been read by everybody
+        tk.store(sK);
+        tv.store(sV);
+        __syncthreads();
+        if (k0 + KT < kv_end) {
+            tk.load(K, a.ldk, k0 + KT, kl, half, vec);
+            tv.load(V, a.ldv, k0 + KT, kl, half, vec);
+        }
+        if (k0 > wave_last || qw0 >= ql) continue;
+        f32x4_t p1[NB], p2[NB];
+        float x1 = -INFINITY, x2 = -INFINITY;
+#pragma unroll
+        for (int kt = 0; kt < NB; ++kt) {
+            p1[kt] = first_product<HH, 0, NS / 2>(sK, 16 * kt, lane, qf);
+            p2[kt] = first_product<HH, NS / 2, NS>(sK, 16 * kt, lane, qf);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int key = k0 + 16 * kt + 4 * g + e;
+                if (key >= kl || (a.mask && key > qi)) p1[kt][e] = p2[kt][e] = -INFINITY;
+                x1 = fmaxf(x1, p1[kt][e]);
+                x2 = fmaxf(x2, p2[kt][e]);
+            }
+        }
+        auto soften = [&](f32x4_t (&p)[NB], float x, float& m, float& l, f32x4_t (&o)[NS]) {
+            const float m_new = fmaxf(m, groups_max(x) * c), m_use = m_new == -INFINITY ? 0.f : m_new;
+            const float alpha = __builtin_amdgcn_exp2f(m - m_use);
+            float rs = 0.f;
+#pragma unroll
+            for (int kt = 0; kt < NB; ++kt)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    p[kt][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[kt][e], c, -m_use));
+                    rs += p[kt][e];
+                }
+            l = l * alpha + rs;
+            m = m_new;
+#pragma unroll
+            for (int i = 0; i < NS; ++i) o[i] *= alpha;
+#pragma unroll
+            for (int kt = 0; kt < NB; ++kt) second_product<HH, 0, NS>(sV, 16 * kt, lane, p[kt], o);
+        };
+        soften(p1, x1, m1, l1, o1);
+        soften(p2, x2, m2, l2, o2);
+    }
+    if (qi >= ql) return;
+    l1 = groups_sum(l1);
+    l2 = groups_sum(l2);
+    const float lam = a.lambda[h], r1 = kl > 0 ? 1.0f / l1 : 0.f, r2 = kl > 0 ? 1.0f / l2 : 0.f;      // (no keys: zeros)
+    const long long row = qrow0 + qi;
+#pragma unroll
+    for (int i = 0; i < NS; ++i) {
+        o2[i] *= r2;
+        o1[i] = o1[i] * r1 - o2[i] * lam;
+    }
+    store_column<T, HH>(o1, 1.0f, (T*)a.o + row * a.ldo + (long long)h * hd, half, g, vec);
+    if (a.o2) store_column<T, HH>(o2, 1.0f, (T*)a.o2 + row * a.ldo + (long long)h * hd, half, g, vec);
+    if (g == 0) {
+        a.lse[(size_t)(2 * h) * a.lse_stride + row] = (m1 + __builtin_amdgcn_logf(l1)) * kLn2G;
+        a.lse[(size_t)(2 * h + 1) * a.lse_stride + row] = (m2 + __builtin_amdgcn_logf(l2)) * kLn2G;
+    }
+}
+
+// ---------------------------------------------------------------- backward: dQ, D_1, D_2, the parts of dlambda
+template <class T, int HH>
+__global__ __launch_bounds__(256) void diff_bwd_dq_kernel(DiffAttnArgs a) {
+    typedef Tile<T, HH> Tl;
+    constexpr int KT = Tl::ROWS, NS = HH / 8;
+    __shared__ __attribute__((aligned(16))) float sK[Tl::FLOATS];
+    __shared__ __attribute__((aligned(16))) float sV[Tl::FLOATS];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4;
+    const ColumnBlock cb = column_block(a, a.q_len, a.mask != 0);
+    if (cb.first < 0) return;
+    const int s = cb.s, h = cb.h, q0 = cb.first, ql = a.q_len[s], kl = a.k_len[s], hd = a.head_dim, half = hd / 2;
+    const bool vec = a.vec;
+    const long long qrow0 = a.q_row[s], krow0 = a.k_row[s];
+    const T* K = (const T*)a.k + krow0 * a.ldk + (long long)h * hd;
+    const T* V = (const T*)a.v + krow0 * a.ldv + (long long)h * hd;
+    const int qw0 = q0 + wave * 16, qi = qw0 + (lane & 15), qi_c = qi < ql ? qi : ql - 1;
+    const long long row = qrow0 + qi_c;
+    const float lam = a.lambda[h];
+    float4 qf[NS], dof[NS];
+    load_column<T, HH>((const T*)a.q + row * a.ldq + (long long)h * hd, half, g, vec, qf);
+    load_column<T, HH>((const T*)a.d_o + row * a.ldo + (long long)h * hd, half, g, vec, dof);
+    float d1 = 0.f, d2 = 0.f;
+    {
+        float4 f[NS];
+        load_column<T, HH>((const T*)a.o + row * a.ldo + (long long)h * hd, half, g, vec, f);
+#pragma unroll
+        for (int i = 0; i < NS; ++i) d1 += (f[i].x * dof[i].x + f[i].y * dof[i].y) + (f[i].z * dof[i].z + f[i].w * dof[i].w);
+        load_column<T, HH>((const T*)a.o2 + row * a.ldo + (long long)h * hd, half, g, vec, f);
+#pragma unroll
+        for (int i = 0; i < NS; ++i) d2 += (f[i].x * dof[i].x + f[i].y * dof[i].y) + (f[i].z * dof[i].z + f[i].w * dof[i].w);
+        d2 = groups_sum(d2);
+        d1 = groups_sum(d1) + lam * d2;
+        if (g == 0 && qi < ql) {
+            a.d1[(size_t)h * a.q_total_rows + row] = d1;
+            a.d2[(size_t)h * a.q_total_rows + row] = d2;
+        }
+    }
+    const float e1 = a.lse[(size_t)(2 * h) * a.lse_stride + row] * kLog2eG, e2 = a.lse[(size_t)(2 * h + 1) * a.lse_stride + row] * kLog2eG;
+    const float c = a.scale * kLog2eG;
+    f32x4_t gacc[NS];
+#pragma unroll
+    for (int i = 0; i < NS; ++i) gacc[i] = zero4();
+    float lam_sum = 0.f;
+    const int kv_end = a.mask ? min(kl, q0 + 64) : kl;
+    const int wave_last = a.mask ? min(kl - 1, qw0 + 15) : kl - 1;
+    Tl tk, tv;
+    if (kv_end > 0) {
+        tk.load(K, a.ldk, 0, kl, half, vec);
+        tv.load(V, a.ldv, 0, kl, half, vec);
+    }
+    for (int k0 = 0; k0 < kv_end; k0 += KT) {
+        __syncthreads();
+        tk.store(sK);
+        tv.store(sV);
+        __syncthreads();
+        if (k0 + KT < kv_end) {
+            tk.load(K, a.ldk, k0 + KT, kl, half, vec);
+            tv.load(V, a.ldv, k0 + KT, kl, half, vec);
+        }
+        if (qw0 >= ql) continue;
+#pragma unroll
+        for (int kt = 0; kt < KT / 16; ++kt) {
+            if (k0 + 16 * kt > wave_last) break;
+            f32x4_t p1 = first_product<HH, 0, NS / 2>(sK, 16 * kt, lane, qf);
+            f32x4_t p2 = first_product<HH, NS / 2, NS>(sK, 16 * kt, lane, qf);
+            const f32x4_t gr = first_product<HH, 0, NS>(sV, 16 * kt, lane, dof);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int key = k0 + 16 * kt + 4 * g + e;
+                const bool hidden = key >= kl || (a.mask && key > qi);
+                const float u1 = __builtin_amdgcn_exp2f(__builtin_fmaf(p1[e], c, -e1)), u2 = __builtin_amdgcn_exp2f(__builtin_fmaf(p2[e], c, -e2));
+                p1[e] = hidden ? 0.f : u1 * (gr[e] - d1);
+                p2[e] = hidden ? 0.f : -lam * u2 * (gr[e] - d2);
+                lam_sum += hidden ? 0.f : u2 * gr[e];
+            }
+            second_product<HH, 0, NS / 2>(sK, 16 * kt, lane, p1, gacc);
+            second_product<HH, NS / 2, NS>(sK, 16 * kt, lane, p2, gacc);
+        }
+    }
+    lam_sum = wave_sum(qi < ql ? lam_sum : 0.f);
+    if (lane == 0 && qw0 < ql) a.lam_part[(size_t)h * a.q_total_rows + qrow0 + qw0] = lam_sum;
+    if (qi < ql) store_column<T, HH>(gacc, a.scale, (T*)a.dq + (qrow0 + qi) * a.ldq + (long long)h * hd, half, g, vec);
+}
+
+// ---------------------------------------------------------------- backward: dK, dV
+template <class T, int HH>
+__global__ __launch_bounds__(256) void diff_bwd_dkv_kernel(DiffAttnArgs a) {
+    typedef Tile<T, HH> Tl;
+    constexpr int QT = Tl::ROWS, NS = HH / 8;
+    __shared__ __attribute__((aligned(16))) float sQ[Tl::FLOATS];
+    __shared__ __attribute__((aligned(16))) float sO[Tl::FLOATS];
+    __shared__ __attribute__((aligned(16))) float stat[4][QT];         // log-sum-exps (exp2 domain), D_1, D_2 of the tile's queries
+    const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), g = lane >> 4;
+    const ColumnBlock cb = column_block(a, a.k_len, false);
+    if (cb.first < 0) return;
+    const int s = cb.s, h = cb.h, k0 = cb.first, ql = a.q_len[s], kl = a.k_len[s], hd = a.head_dim, half = hd / 2;
+    const bool vec = a.vec;
+    const long long qrow0 = a.q_row[s], krow0 = a.k_row[s];
+    const T* Q = (const T*)a.q + qrow0 * a.ldq + (long long)h * hd;
+    const T* dO = (const T*)a.d_o + qrow0 * a.ldo + (long long)h * hd;
+    const int kw0 = k0 + wave * 16, ki = kw0 + (lane & 15), ki_c = ki < kl ? ki : kl - 1;
+    float4 kf[NS], vf[NS];
+    load_column<T, HH>((const T*)a.k + (krow0 + ki_c) * a.ldk + (long long)h * hd, half, g, vec, kf);
+    load_column<T, HH>((const T*)a.v + (krow0 + ki_c) * a.ldv + (long long)h * hd, half, g, vec, vf);
+    const float c = a.scale * kLog2eG, lam = a.lambda[h];
+    f32x4_t dk[NS], dv[NS];
+#pragma unroll
+    for (int i = 0; i < NS; ++i) { dk[i] = zero4(); dv[i] = zero4(); }
+    const int q_begin = a.mask ? k0 : 0;                               // causal: only queries at or after the key see it
+    Tl tq, to;
+    float st[4];
+    auto fetch = [&](int q0) {
+        tq.load(Q, a.ldq, q0, ql, half, vec);
+        to.load(dO, a.ldo, q0, ql, half, vec);
+        const bool in = t < QT && q0 + t < ql;
+        const long long row = qrow0 + q0 + t;
+        st[0] = in ? a.lse[(size_t)(2 * h) * a.lse_stride + row] * kLog2eG : 0.f;
+        st[1] = in ? a.lse[(size_t)(2 * h + 1) * a.lse_stride + row] * kLog2eG : 0.f;
+        st[2] = in ? a.d1[(size_t)h * a.q_total_rows + row] : 0.f;
+        st[3] = in ? a.d2[(size_t)h * a.q_total_rows + row] : 0.f;
+    };
+    if (q_begin < ql) fetch(q_begin);
+    for (int q0 = q_begin; q0 < ql; q0 += QT) {
+        __syncthreads();
+        tq.store(sQ);
+        to.store(sO);
+        if (t < QT)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) stat[i][t] = st[i];
+        __syncthreads();
+        if (q0 + QT < ql) fetch(q0 + QT);
+        if (kw0 >= kl) continue;
+#pragma unroll
+        for (int qt = 0; qt < QT / 16; ++qt) {
+            const int qb = q0 + 16 * qt;
+            if (qb >= ql || (a.mask && qb + 15 < kw0)) continue;       // no visible query
+            f32x4_t p1 = first_product<HH, 0, NS / 2>(sQ, 16 * qt, lane, kf);
+            f32x4_t p2 = first_product<HH, NS / 2, NS>(sQ, 16 * qt, lane, kf);
+            const f32x4_t gr = first_product<HH, 0, NS>(sO, 16 * qt, lane, vf);
+            f32x4_t p;
+            const f32x4_t e1 = *reinterpret_cast<const f32x4_t*>(&stat[0][16 * qt + 4 * g]), e2 = *reinterpret_cast<const f32x4_t*>(&stat[1][16 * qt + 4 * g]);
+            const f32x4_t d1 = *reinterpret_cast<const f32x4_t*>(&stat[2][16 * qt + 4 * g]), d2 = *reinterpret_cast<const f32x4_t*>(&stat[3][16 * qt + 4 * g]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int q = qb + 4 * g + e;
+                const bool hidden = q >= ql || (a.mask && q < ki);
+                const float u1 = hidden ? 0.f : __builtin_amdgcn_exp2f(__builtin_fmaf(p1[e], c, -e1[e]));
+                const float u2 = hidden ? 0.f : lam * __builtin_amdgcn_exp2f(__builtin_fmaf(p2[e], c, -e2[e]));
+                p[e] = u1 - u2;
+                p1[e] = hidden ? 0.f : u1 * (gr[e] - d1[e]);
+                p2[e] = hidden ? 0.f : -u2 * (gr[e] - d2[e]);
+            }
+            second_product<HH, 0, NS>(sO, 16 * qt, lane, p, dv);
+            second_product<HH, 0, NS / 2>(sQ, 16 * qt, lane, p1, dk);
+            second_product<HH, NS / 2, NS>(sQ, 16 * qt, lane, p2, dk);
+        }
+    }
+    if (ki >= kl) return;
+    store_column<T, HH>(dk, a.scale, (T*)a.dk + (krow0 + ki) * a.ldk + (long long)h * hd, half, g, vec);
+    store_column<T, HH>(dv, 1.0f, (T*)a.dv + (krow0 + ki) * a.ldv + (long long)h * hd, half, g, vec);
+}
+
+// ---------------------------------------------------------------- dlambda: one work-group per head, a wavefront per sequence, fixed order
+__global__ __launch_bounds__(1024) void diff_dlambda_kernel(DiffAttnArgs a, int queries) {
+    __shared__ float part[16];
+    const int h = blockIdx.x, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const float* p = a.lam_part + (size_t)h * a.q_total_rows;
+    float sum = 0.f;
+    for (int s = wave; s < a.n_seq; s += 16) {
+        const int n = (a.q_len[s] + queries - 1) / queries;
+        const float* q = p + a.q_row[s];
+        for (int i = lane; i < n; i += 64) sum += q[(size_t)i * queries];
+    }
+    sum = wave_sum(sum);
+    if (lane == 0) part[wave] = sum;
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+    sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < 16; ++w) sum += part[w];
+    a.dlambda[h] = (a.accumulate ? a.dlambda[h] : 0.f) - sum;
+}
+
+template <class T, int HH> void fwd_launch(const DiffAttnArgs& a, hipStream_t st) {
+    hipLaunchKernelGGL((diff_fwd_kernel<T, HH>), column_grid(a, a.max_q_len), dim3(256), 0, st, a);
+}
+template <class T, int HH> void dq_launch(const DiffAttnArgs& a, hipStream_t st) {
+    hipLaunchKernelGGL((diff_bwd_dq_kernel<T, HH>), column_grid(a, a.max_q_len), dim3(256), 0, st, a);
+}
+template <class T, int HH> void dkv_launch(const DiffAttnArgs& a, hipStream_t st) {
+    hipLaunchKernelGGL((diff_bwd_dkv_kernel<T, HH>), column_grid(a, a.max_k_len), dim3(256), 0, st, a);
+}
+
+}  // namespace
+
+#define DS_DIFF_DISPATCH(launch)                                              \
+    do {                                                                      \
+        const bool bf = a.dtype == DS_DTYPE_BF16;                             \
+        if (a.head_dim <= 32) bf ? launch<bf16_t, 16>(a, st) : launch<float, 16>(a, st);      \
+        else if (a.head_dim <= 64) bf ? launch<bf16_t, 32>(a, st) : launch<float, 32>(a, st); \
+        else if (a.head_dim <= 96) bf ? launch<bf16_t, 48>(a, st) : launch<float, 48>(a, st); \
+        else bf ? launch<bf16_t, 64>(a, st) : launch<float, 64>(a, st);       \
+    } while (0)
+
+ds_status diff_fwd_general(const DiffAttnArgs& a, hipStream_t st) {
+    DS_DIFF_DISPATCH(fwd_launch);
+    DS_LAUNCH_CHECK();
+    return DS_OK;
+}
+
+ds_status diff_bwd_general(const DiffAttnArgs& a, hipStream_t st) {
+    DS_DIFF_DISPATCH(dq_launch);
+    DS_LAUNCH_CHECK();
+    DS_DIFF_DISPATCH(dkv_launch);
+    DS_LAUNCH_CHECK();
+    return diff_dlambda(a, 16, st);
+}
+
+ds_status diff_dlambda(const DiffAttnArgs& a, int queries, hipStream_t st) {
+    hipLaunchKernelGGL(diff_dlambda_kernel, dim3(a.n_heads), dim3(1024), 0, st, a, queries);
+    DS_LAUNCH_CHECK();
+    return DS_OK;
+}

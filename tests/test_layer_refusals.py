@@ -104,3 +104,33 @@ def test_the_binding_refuses_tensors_that_are_not_on_the_gpu():
         ds.ds_resid_norm_fwd(t, t, t.clone(), torch.zeros((4, 4)))
     with pytest.raises(ValueError):
         ds.ds_rope(t, t, torch.zeros(4, dtype=torch.int32), torch.zeros(32, dtype=torch.float64), 1, 64, 64)
+
+
+def _diff(back, **kw):
+    a = dict(dtype=1, n_seq=2, n_heads=2, head_dim=64, mask=1, q_row=P, q_len=P, k_row=P, k_len=P, max_q_len=8, max_k_len=8, q=P, ldq=128, k=P, ldk=128, v=P,
+             ldv=128, lam=P, o=P, o2=P)
+    if back:
+        a.update(d_o=P)
+    a.update(ldo=128, lse=P)
+    if back:
+        a.update(dq=P, dk=P, dv=P, dlam=P, accumulate=0)
+    a.update(q_total_rows=16, k_total_rows=16, scratch=P, scratch_bytes=0, force_generic=0, stream=None)
+    a.update(kw)                                                # (no scratch bytes: refused whatever else is right)
+    ints = ("dtype", "n_seq", "n_heads", "head_dim", "mask", "max_q_len", "max_k_len", "ldq", "ldk", "ldv", "ldo", "accumulate", "q_total_rows", "k_total_rows", "force_generic")
+    f = ds.lib().ds_diff_attention_bwd if back else ds.lib().ds_diff_attention_fwd
+    return f(*[v if k in ints else C.c_int64(v) if k == "scratch_bytes" else C.c_void_p(v) for k, v in a.items()])
+
+
+@pytest.mark.parametrize("back", [False, True])
+def test_differential_attention(back):
+    need = ds.ds_diff_attention_scratch_bytes(2, 16, 16, 2)
+    assert need > 0 and ds.ds_diff_attention_scratch_bytes(0, 16, 16, 2) == 0 and ds.ds_diff_attention_scratch_bytes(2, 16, 0, 2) == 0
+    assert _diff(back, scratch_bytes=need - 1) == BAD and _diff(back, scratch_bytes=-1) == BAD
+    bad = [dict(dtype=3), dict(n_seq=0), dict(n_heads=0), dict(head_dim=0), dict(head_dim=72), dict(head_dim=144), dict(mask=2), dict(q_row=None), dict(q_len=None),
+           dict(k_row=None), dict(k_len=None), dict(max_q_len=0), dict(max_k_len=0), dict(q=None), dict(k=None), dict(v=None), dict(ldq=127), dict(ldk=127),
+           dict(ldv=127), dict(ldo=127), dict(lam=None), dict(o=None), dict(lse=None), dict(q_total_rows=0), dict(k_total_rows=0), dict(scratch=None),
+           dict(scratch=P + 8), dict(q=P + 1), dict(k=P + 1), dict(v=P + 1), dict(o=P + 1), dict(o2=P + 1), dict(n_seq=70000), dict(n_heads=70000, head_dim=16, ldq=1 << 21, ldk=1 << 21, ldv=1 << 21, ldo=1 << 21)]
+    if back:
+        bad += [dict(o2=None), dict(d_o=None), dict(dq=None), dict(dk=None), dict(dv=None), dict(dlam=None), dict(accumulate=2), dict(dq=P + 1), dict(d_o=P + 1)]
+    for kw in bad:
+        assert _diff(back, **dict(dict(scratch_bytes=1 << 40), **kw)) == BAD, kw

@@ -55,3 +55,39 @@ def test_rope_closed_forms():
     for inter in (True, False):
         there = layer.rope(x, [5, 7, 100], freq, 2, 6, 4, inter, False, 2.0)
         assert np.allclose(layer.rope(there, [5, 7, 100], freq, 2, 6, 4, inter, True, 0.5), x)
+
+
+@pytest.mark.parametrize("causal", [False, True])
+def test_differential_attention_gradients_against_differences(causal):
+    rng = np.random.default_rng(5)
+    H, hd, lq, lk = 2, 4, 5, 5 if causal else 3
+    v = {"q": rng.standard_normal((lq, H * hd)), "k": rng.standard_normal((lk, H * hd)), "v": rng.standard_normal((lk, H * hd)), "lam": rng.standard_normal(H)}
+    d_o = rng.standard_normal((lq, H * hd))
+
+    def forward(v):
+        return layer.diff_attention(v["q"], v["k"], v["v"], v["lam"], H, causal)
+
+    o, o2, lse = forward(v)[:3]
+    g = layer.diff_attention_back(v["q"], v["k"], v["v"], v["lam"], o, o2, d_o, lse, H, causal)
+    for key in v:
+        for at in np.ndindex(v[key].shape):
+            hi, lo = dict(v), dict(v)
+            hi[key], lo[key] = v[key].copy(), v[key].copy()
+            hi[key][at] += 1e-6
+            lo[key][at] -= 1e-6
+            slope = ((forward(hi)[0] - forward(lo)[0]) * d_o).sum() / 2e-6
+            assert abs(slope - g["d" + key][at]) <= 1e-6 * (1 + abs(slope)), key
+
+
+def test_differential_attention_closed_forms():
+    rng = np.random.default_rng(6)
+    H, hd, l = 2, 8, 4
+    q, k, v = (rng.standard_normal((l, H * hd)) for _ in range(3))
+    lam = np.array([0.3, -0.5])
+    o, o2, lse = layer.diff_attention(q[:1], k[:1], v[:1], lam, H, True)[:3]          # one key: every probability is 1
+    assert np.allclose(o, v[:1] * np.repeat(1 - lam, hd)) and np.allclose(o2, v[:1])
+    o, o2, lse = layer.diff_attention(np.zeros_like(q), k, v, lam, H, False)[:3]      # uniform scores
+    assert np.allclose(o, np.tile(v.mean(axis=0) * np.repeat(1 - lam, hd), (l, 1))) and np.allclose(lse, np.log(l))
+    same = np.concatenate([np.concatenate([t[:, :hd // 2]] * 2, axis=1) for t in (q, k)], axis=0)      # both maps alike, lambda = 1: nothing is left
+    o = layer.diff_attention(same[:l], same[l:], v[:, :hd], np.ones(1), 1, True)[0]
+    assert np.allclose(o, 0)
