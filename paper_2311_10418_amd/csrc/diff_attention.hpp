@@ -23,5 +23,9 @@ struct DiffAttnArgs : AttnArgs {                        // scale: 1 / sqrt(head_
 size_t diff_scratch_bytes(int n_heads, int q_total_rows, int k_total_rows, int n_seq);
 ds_status diff_fwd_general(const DiffAttnArgs& a, hipStream_t st);
 ds_status diff_bwd_general(const DiffAttnArgs& a, hipStream_t st);
+// bf16 matrix-core kernels; what they do not take (see diff_mfma_supported) the general ones do
+bool diff_mfma_supported(const DiffAttnArgs& a);
+ds_status diff_fwd_mfma(const DiffAttnArgs& a, hipStream_t st);
+ds_status diff_bwd_mfma(const DiffAttnArgs& a, hipStream_t st);
 // dlambda[h] = (accumulate ? dlambda[h] : 0) - the sums in lam_part, which stand `queries` rows apart within a sequence
 ds_status diff_dlambda(const DiffAttnArgs& a, int queries, hipStream_t st);

@@ -58,7 +58,7 @@ extern "C" ds_status ds_diff_attention_fwd(int32_t dtype, int32_t n_seq, int32_t
     a.scratch = scratch; a.scratch_bytes = scratch_bytes < 0 ? 0 : (size_t)scratch_bytes;
     const ds_status r = check(a);
     if (r != DS_OK) return r;
-    (void)force_generic;
+    if (!force_generic && diff_mfma_supported(a)) return diff_fwd_mfma(a, (hipStream_t)hip_stream);
     return diff_fwd_general(a, (hipStream_t)hip_stream);
 }
 
@@ -82,6 +82,6 @@ extern "C" ds_status ds_diff_attention_bwd(int32_t dtype, int32_t n_seq, int32_t
     const ds_status r = check(a);
     if (r != DS_OK) return r;
     if (!o2 || !d_o || !dq || !dk || !dv || !dlambda || (accumulate != 0 && accumulate != 1)) return DS_EINVAL;
-    (void)force_generic;
+    if (!force_generic && diff_mfma_supported(a)) return diff_bwd_mfma(a, (hipStream_t)hip_stream);
     return diff_bwd_general(a, (hipStream_t)hip_stream);
 }

@@ -1,0 +1,582 @@
+// Differential attention in bf16 on the matrix cores (v_mfma_f32_32x32x16_bf16), head size 64 or 128 (maps of 32 or 64), causal or
+// unmasked, forward and backward.  Register layout, tiles, transpose reads and work lists are those of attention_mfma.hip: a wavefront
+// owns 32 columns (queries in forward and dQ, keys in dK/dV) and computes transposed score tiles, one set of accumulator registers
+// being the B operand of the next product as it stands.
+//
+// What two maps change.  The products that make scores contract over half a head each, so that both maps' scores cost what one map's
+// of the whole head do; dP = dO V^T is common to both, and so is dV (one product with P_1 - lambda P_2); dQ and dK of a map are half a
+// head wide.  Backward therefore takes the matrix instructions of ordinary attention, with twice the exponentials.  Forward cannot form
+// P_1 - lambda P_2 before both sums are known, so it keeps two accumulators and multiplies every fragment of V^T by both maps'
+// probabilities (6 instead of 4 products of a head's width; a first pass over the scores for the sums would cost the same).
+//
+// Probabilities, their difference and dS are rounded to bf16 as they become operands; scores, statistics, sums, dP and dlambda are fp32.
+#include "attention_tiles.hpp"
+#include "diff_attention.hpp"
+#include <type_traits>
+
+namespace {
+
+// ------------------------------------------------------------------------------------ forward
+// A tile of 64 keys goes in two halves of 32, so that both maps' scores (32 registers) and both accumulators (128 at head size 128) leave
+// room for two wavefronts per SIMD.
+template <int HD, bool CAUSAL>
+__global__ __launch_bounds__(256, 2) void diff_fwd_mfma_kernel(DiffAttnArgs a) {
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    constexpr int TILE = 64 * HD * 2, NS = HD / 16, ND = HD / 32;
+    const uint32_t lds0 = lds_address(smem);
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int col = lane & 31, g = lane >> 5;
+    const int item = blockIdx.x / a.n_heads, h = blockIdx.x - item * a.n_heads;
+    const int2 it = a.items_q[item];
+    if (item >= a.n_items[0]) return;
+    const int s = it.x, q0 = it.y * 128;
+    const int ql = a.q_len[s], kl = a.k_len[s];
+    const long long qrow0 = a.q_row[s];
+    const bf16_t* Q = (const bf16_t*)a.q + qrow0 * a.ldq + h * HD;
+    const bf16_t* K = (const bf16_t*)a.k + (long long)a.k_row[s] * a.ldk + h * HD;
+    const bf16_t* V = (const bf16_t*)a.v + (long long)a.k_row[s] * a.ldv + h * HD;
+    const int qw0 = q0 + wave * 32;
+    const int qi = qw0 + col;
+    const int qi_c = qi < ql ? qi : ql - 1;
+
+    bf16x8_t qf[NS];
+#pragma unroll
+    for (int ks = 0; ks < NS; ++ks) qf[ks] = *reinterpret_cast<const bf16x8_t*>(Q + (long long)qi_c * a.ldq + ks * 16 + g * 8);
+
+    BufferTileLoader<HD> ldK, ldV;
+    ldK.setup(K, a.ldk, kl, wave, lane);
+    ldV.setup(V, a.ldv, kl, wave, lane);
+    TrOffsets<HD> tro;
+    tro.init(lane);
+    const int rbase = col * (HD * 2);
+    const int rsw = swz<HD>(col);
+
+    f32x16_t o1[ND], o2[ND];
+#pragma unroll
+    for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) { o1[dt][e] = 0.f; o2[dt][e] = 0.f; }
+    float m1 = -INFINITY, m2 = -INFINITY, l1 = 0.f, l2 = 0.f;          // running maxima (in the exp2 domain) and sums
+    const float c = a.scale * kLog2e;
+
+    const int kv_end = CAUSAL ? min(kl, q0 + 128) : kl;
+    const int wave_last = CAUSAL ? min(kl - 1, qw0 + 31) : kl - 1;     // last key this wavefront can see
+    const int nb = (kv_end + 63) / 64;
+    if (nb > 0) {                                       // (a sequence without keys: zero output, nothing to fetch)
+        ldK.issue(lds0, 0);
+        ldV.issue(lds0 + TILE, 0);
+    }
+    // scores -> probabilities of one map in place; its accumulator is rescaled only when some column's maximum moved
+    auto soften = [&](f32x16_t& p, float& m, float& l, f32x16_t (&o)[ND]) {
+        float mx = -INFINITY;
+#pragma unroll
+        for (int e = 0; e < 16; e += 2) mx = max3f(mx, p[e], p[e + 1]);
+        const float m_new = max3f(m, mx * c, __shfl_xor(mx, 32, 64) * c);
+        float rs = 0.f;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[e], c, -m_new));
+            rs += p[e];
+        }
+        const float alpha = __builtin_amdgcn_exp2f(m - m_new);
+        l = l * alpha + rs;
+        if (__builtin_amdgcn_ballot_w64(m_new > m) != 0) {
+#pragma unroll
+            for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[dt][e] *= alpha;
+        }
+        m = m_new;
+    };
+    for (int b = 0; b < nb; ++b) {
+        const int kv0 = b * 64;
+        const char* sK = smem + (b & 1) * (2 * TILE);
+        const char* sV = sK + TILE;
+        wait_tiles_and_sync();                          // block b has landed; the other stage is free
+        if (b + 1 < nb) {
+            const uint32_t n = lds0 + ((b + 1) & 1) * (2 * TILE);
+            ldK.issue(n, kv0 + 64);
+            ldV.issue(n + TILE, kv0 + 64);
+        }
+        if (kv0 > wave_last || qw0 >= ql) continue;
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt) {
+            if (kv0 + kt * 32 > wave_last) continue;    // the half beyond the last key this wavefront sees
+            f32x16_t p1, p2;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) { p1[e] = 0.f; p2[e] = 0.f; }
+#pragma unroll
+            for (int ks = 0; ks < NS; ++ks) {
+                const bf16x8_t fk = *reinterpret_cast<const bf16x8_t*>(sK + kt * (32 * HD * 2) + rbase + (((ks * 2 + g) ^ rsw) << 4));
+                if (ks < NS / 2) p1 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fk, qf[ks], p1, 0, 0, 0);
+                else p2 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fk, qf[ks], p2, 0, 0, 0);
+            }
+            if (kv0 + kt * 32 + 32 > kl || (CAUSAL && kv0 + kt * 32 + 31 > qw0)) {
+                int kbase = kv0 + kt * 32;              // (one real branch around the whole mask: see attention_mfma.hip)
+                asm volatile("" : "+s"(kbase));
+                const int last = (CAUSAL ? min(kl - 1, qi) : kl - 1) - kbase - 4 * g;      // last visible row, as this lane counts them
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    if (8 * (e >> 2) + (e & 3) > last) { p1[e] = -INFINITY; p2[e] = -INFINITY; }
+            }
+            soften(p1, m1, l1, o1);
+            soften(p2, m2, l2, o2);
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const bf16x8_t f1 = frag_from_acc(p1, u), f2 = frag_from_acc(p2, u);
+#pragma unroll
+                for (int dt = 0; dt < ND; ++dt) {
+                    const bf16x8_t fv = read_tr<HD>(sV, tro, 2 * kt + u, dt);
+                    o1[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fv, f1, o1[dt], 0, 0, 0);
+                    o2[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fv, f2, o2[dt], 0, 0, 0);
+                }
+            }
+        }
+    }
+    l1 += __shfl_xor(l1, 32, 64);
+    l2 += __shfl_xor(l2, 32, 64);
+    if (qi < ql) {
+        const long long row = qrow0 + qi;
+        const float r1 = l1 > 0.f ? 1.0f / l1 : 0.f, r2 = l2 > 0.f ? 1.0f / l2 : 0.f, lam = a.lambda[h];
+#pragma unroll
+        for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                o2[dt][e] *= r2;
+                o1[dt][e] = o1[dt][e] * r1 - lam * o2[dt][e];
+            }
+        store_cols<HD>(o1, 1.0f, (bf16_t*)a.o + row * a.ldo + h * HD, g);
+        if (a.o2) store_cols<HD>(o2, 1.0f, (bf16_t*)a.o2 + row * a.ldo + h * HD, g);
+        if (g == 0) {
+            a.lse[(size_t)(2 * h) * a.lse_stride + row] = (m1 + __builtin_amdgcn_logf(l1)) * kLn2;
+            a.lse[(size_t)(2 * h + 1) * a.lse_stride + row] = (m2 + __builtin_amdgcn_logf(l2)) * kLn2;
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------ backward: dQ (and the statistics, the parts of dlambda)
+// For the dK/dV kernel a query leaves one entry of eight bf16 values, the {hi, lo} splits of lse_1 / scale, lse_2 / scale, D_1 and D_2.
+template <int HD, bool CAUSAL>
+__global__ __launch_bounds__(256, 2) void diff_bwd_dq_mfma_kernel(DiffAttnArgs a) {
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    constexpr int TILE = 64 * HD * 2, NS = HD / 16, ND = HD / 32;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int col = lane & 31, g = lane >> 5;
+    const int item = blockIdx.x / a.n_heads, h = blockIdx.x - item * a.n_heads;
+    if (item >= a.n_items[0]) return;
+    const int2 it = a.items_q[item];
+    const int s = it.x, q0 = it.y * 128;
+    const int ql = a.q_len[s], kl = a.k_len[s];
+    const long long qrow0 = a.q_row[s];
+    const bf16_t* Q = (const bf16_t*)a.q + qrow0 * a.ldq + h * HD;
+    const bf16_t* dO = (const bf16_t*)a.d_o + qrow0 * a.ldo + h * HD;
+    const bf16_t* O = (const bf16_t*)a.o + qrow0 * a.ldo + h * HD;
+    const bf16_t* O2 = (const bf16_t*)a.o2 + qrow0 * a.ldo + h * HD;
+    const bf16_t* K = (const bf16_t*)a.k + (long long)a.k_row[s] * a.ldk + h * HD;
+    const bf16_t* V = (const bf16_t*)a.v + (long long)a.k_row[s] * a.ldv + h * HD;
+    const int qw0 = q0 + wave * 32;
+    const int qi = qw0 + col;
+    const int qi_c = qi < ql ? qi : ql - 1;
+
+    const uint32_t lds0 = lds_address(smem);
+    TileLoader<HD> ldK, ldV;
+    ldK.setup(K, a.ldk, kl, wave, lane);
+    ldV.setup(V, a.ldv, kl, wave, lane);
+    if (kl > 0) {
+        ldK.issue(lds0, 0);
+        ldV.issue(lds0 + TILE, 0);
+    }
+
+    const float lam = a.lambda[h];
+    bf16x8_t qf[NS], dof[NS];
+    float d1 = 0.f, d2 = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < NS; ++ks) {
+        qf[ks] = *reinterpret_cast<const bf16x8_t*>(Q + (long long)qi_c * a.ldq + ks * 16 + g * 8);
+        dof[ks] = *reinterpret_cast<const bf16x8_t*>(dO + (long long)qi_c * a.ldo + ks * 16 + g * 8);
+        const bf16x8_t of = *reinterpret_cast<const bf16x8_t*>(O + (long long)qi_c * a.ldo + ks * 16 + g * 8);
+        const bf16x8_t of2 = *reinterpret_cast<const bf16x8_t*>(O2 + (long long)qi_c * a.ldo + ks * 16 + g * 8);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            d1 = __builtin_fmaf((float)of[j], (float)dof[ks][j], d1);
+            d2 = __builtin_fmaf((float)of2[j], (float)dof[ks][j], d2);
+        }
+    }
+    d2 += __shfl_xor(d2, 32, 64);
+    d1 += __shfl_xor(d1, 32, 64);
+    d1 += lam * d2;
+    const float lse1 = a.lse[(size_t)(2 * h) * a.lse_stride + qrow0 + qi_c], lse2 = a.lse[(size_t)(2 * h + 1) * a.lse_stride + qrow0 + qi_c];
+    if (g == 0 && qi < ql)
+        reinterpret_cast<uint4*>(a.aug)[(size_t)h * a.q_total_rows + qrow0 + qi] =
+            make_uint4(split_hi_lo(lse1 * (1.0f / a.scale)), split_hi_lo(lse2 * (1.0f / a.scale)), split_hi_lo(d1), split_hi_lo(d2));
+    const float e1 = lse1 * kLog2e, e2 = lse2 * kLog2e;
+    const float c = a.scale * kLog2e;
+
+    TrOffsets<HD> tro;
+    tro.init(lane);
+    const int rbase = col * (HD * 2);
+    const int rsw = swz<HD>(col);
+
+    f32x16_t gacc[ND];
+#pragma unroll
+    for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) gacc[dt][e] = 0.f;
+    float lam_sum = 0.f;
+
+    const int kv_end = CAUSAL ? min(kl, q0 + 128) : kl;
+    const int wave_last = CAUSAL ? min(kl - 1, qw0 + 31) : kl - 1;
+    const int nb = (kv_end + 63) / 64;
+    for (int b = 0; b < nb; ++b) {
+        const int kv0 = b * 64;
+        const char* sK = smem + (b & 1) * (2 * TILE);
+        const char* sV = sK + TILE;
+        wait_tiles_and_sync();
+        if (b + 1 < nb) {
+            const uint32_t n = lds0 + ((b + 1) & 1) * (2 * TILE);
+            ldK.issue(n, kv0 + 64);
+            ldV.issue(n + TILE, kv0 + 64);
+        }
+        if (kv0 > wave_last || qw0 >= ql) continue;
+        const bool need_mask = (kv0 + 64 > kl) || (CAUSAL && kv0 + 63 > qw0);
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt) {
+            if (kv0 + kt * 32 > wave_last) continue;                    // the half beyond the last key this wavefront sees
+            f32x16_t p1, p2, gr;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) { p1[e] = 0.f; p2[e] = 0.f; gr[e] = 0.f; }
+#pragma unroll
+            for (int ks = 0; ks < NS; ++ks) {
+                const int o = kt * (32 * HD * 2) + rbase + (((ks * 2 + g) ^ rsw) << 4);
+                const bf16x8_t fk = *reinterpret_cast<const bf16x8_t*>(sK + o);
+                const bf16x8_t fv = *reinterpret_cast<const bf16x8_t*>(sV + o);
+                if (ks < NS / 2) p1 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fk, qf[ks], p1, 0, 0, 0);
+                else p2 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fk, qf[ks], p2, 0, 0, 0);
+                gr = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fv, dof[ks], gr, 0, 0, 0);
+            }
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                p1[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(p1[e], c, -e1));
+                p2[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(p2[e], c, -e2));
+            }
+            if (need_mask) {
+                int kbase = kv0 + kt * 32;
+                asm volatile("" : "+s"(kbase));
+                const int last = (CAUSAL ? min(kl - 1, qi) : kl - 1) - kbase - 4 * g;  // last visible row, as this lane counts them
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    if (8 * (e >> 2) + (e & 3) > last) { p1[e] = 0.f; p2[e] = 0.f; gr[e] = 0.f; }
+            }
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                lam_sum = __builtin_fmaf(p2[e], gr[e], lam_sum);
+                p1[e] *= gr[e] - d1;                                  // dS_1^T
+                p2[e] *= gr[e] - d2;                                  // dS_2^T / -lambda
+            }
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const bf16x8_t f1 = frag_from_acc(p1, u), f2 = frag_from_acc(p2, u);
+#pragma unroll
+                for (int dt = 0; dt < ND; ++dt) {
+                    const bf16x8_t kt_f = read_tr<HD>(sK, tro, 2 * kt + u, dt);
+                    gacc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kt_f, dt < ND / 2 ? f1 : f2, gacc[dt], 0, 0, 0);
+                }
+            }
+        }
+    }
+    lam_sum = wave_sum(qi < ql ? lam_sum : 0.f);
+    if (lane == 0 && qw0 < ql) a.lam_part[(size_t)h * a.q_total_rows + qrow0 + qw0] = lam_sum;
+    if (qi < ql) {
+#pragma unroll
+        for (int dt = ND / 2; dt < ND; ++dt)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) gacc[dt][e] *= -lam;
+        store_cols<HD>(gacc, a.scale, (bf16_t*)a.dq + (qrow0 + qi) * a.ldq + h * HD, g);
+    }
+}
+
+// ------------------------------------------------------------------------------------ backward: dK, dV
+// A ring of four stages of Q tile, dO tile ([64][HD]) and statistics tile ([64 queries][8] bf16, see above), three blocks in flight.  One matrix
+// instruction with the statistics as its A operand and -1 in the two slots of a value subtracts it: score_i - lse_i / scale and, from the one dP,
+// dP - D_1 and dP - D_2.  At head size 128 work-groups are persistent, one to a compute unit (see attention_mfma.hip).
+template <int HD, bool CAUSAL>
+__global__ __launch_bounds__(256, HD == 64 ? 2 : 1) void diff_bwd_dkv_mfma_kernel(DiffAttnArgs a) {
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    constexpr int TILE = 64 * HD * 2;
+    constexpr int STAGE = 2 * TILE + 1024;
+    constexpr int NS = 4;
+    constexpr bool PS = HD == 128;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int col = lane & 31, g = lane >> 5;
+    const uint32_t lds0 = lds_address(smem);
+    volatile int* s_next = reinterpret_cast<volatile int*>(smem + NS * STAGE);      // two words used in turn (an item without steps has one barrier only)
+    int turn = 0;
+    char* s_zero = smem + NS * STAGE + 64;              // 32 rows of zeros
+    TileLoader<HD> ldQ, ldO;
+    ldQ.setup(nullptr, a.ldq, 0, wave, lane);
+    ldO.setup(nullptr, a.ldo, 0, wave, lane);
+    WorkDraw draw(a, 1);
+    int kw0, ki, kl, ql, h, q_begin, nb;
+    long long krow0;
+    const char* aug_src;
+    float lam;
+    bf16x8_t kf[HD / 16], vf[HD / 16];
+    // block blk -> stage blk % 4 by direct transfers (the statistics by wavefront 0); indices past the last block are clamped
+    auto issue_block = [&](int blk) {
+        const uint32_t n = lds0 + (blk & (NS - 1)) * STAGE;
+        const int bc = blk < nb ? blk : nb - 1;
+        const int q0 = q_begin + bc * 64;
+        ldQ.issue(n, q0);
+        ldO.issue(n + TILE, q0);
+        if (wave == 0) {
+            int r = q0 + lane;
+            r = r < ql ? r : ql - 1;
+            lds_dma16_at(aug_src + (size_t)r * 16, n + 2 * TILE);
+        }
+    };
+    auto begin_item = [&] {
+        const int item = draw.index() / a.n_heads;
+        h = draw.index() - item * a.n_heads;
+        const int2 it = a.items_k[item];
+        const int s = __builtin_amdgcn_readfirstlane(it.x), k0 = __builtin_amdgcn_readfirstlane(it.y) * 128;
+        ql = __builtin_amdgcn_readfirstlane(a.q_len[s]);
+        kl = __builtin_amdgcn_readfirstlane(a.k_len[s]);
+        const long long qrow0 = __builtin_amdgcn_readfirstlane(a.q_row[s]);
+        krow0 = __builtin_amdgcn_readfirstlane(a.k_row[s]);
+        lam = a.lambda[h];
+        kw0 = k0 + wave * 32;
+        ki = kw0 + col;
+        q_begin = CAUSAL ? k0 : 0;
+        nb = (ql - q_begin + 63) / 64;                  // (none: keys beyond the last query of a causal sequence)
+        ldQ.base = reinterpret_cast<const char*>((const bf16_t*)a.q + qrow0 * a.ldq + h * HD);
+        ldO.base = reinterpret_cast<const char*>((const bf16_t*)a.d_o + qrow0 * a.ldo + h * HD);
+        ldQ.n_valid = ldO.n_valid = ql;
+        aug_src = a.aug + ((size_t)h * a.q_total_rows + qrow0) * 16;
+        if (nb > 0) {
+            issue_block(0);
+            issue_block(1);
+            issue_block(2);
+        }
+        const int ki_c = ki < kl ? ki : kl - 1;
+        const bf16_t* K = (const bf16_t*)a.k + (krow0 + ki_c) * a.ldk + h * HD;
+        const bf16_t* V = (const bf16_t*)a.v + (krow0 + ki_c) * a.ldv + h * HD;
+#pragma unroll
+        for (int ks = 0; ks < HD / 16; ++ks) {
+            kf[ks] = *reinterpret_cast<const bf16x8_t*>(K + ks * 16 + g * 8);
+            vf[ks] = *reinterpret_cast<const bf16x8_t*>(V + ks * 16 + g * 8);
+        }
+    };
+    if (!draw.valid()) {
+        if (PS) draw.finish();
+        return;
+    }
+    begin_item();
+    for (int i = tid; i < 64 * HD / 16; i += 256) reinterpret_cast<uint4*>(s_zero)[i] = make_uint4(0u, 0u, 0u, 0u);
+    bf16x8_t minus[4];                                  // -1 in the contraction slots of value i (lane half 0), which hold its hi and lo
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) minus[i][j] = (bf16_t)((g == 0 && j / 2 == i) ? -1.0f : 0.0f);
+    const float c = a.scale * kLog2e;
+
+    TrOffsets<HD> tro;
+    tro.init(lane);
+    const int rbase = col * (HD * 2);
+    const int rsw = swz<HD>(col);
+
+    f32x16_t dkacc[HD / 32], dvacc[HD / 32];
+    for (;;) {
+#pragma unroll
+    for (int dt = 0; dt < HD / 32; ++dt)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) { dkacc[dt][e] = 0.f; dvacc[dt][e] = 0.f; }
+
+    int next = 0;
+    if (PS) next = draw.take();                         // (needed after the loop)
+    // ordinary loads and stores are complete before the loop (left to the compiler its waits would sit inside it), and so are the zeros of s_zero
+    __builtin_amdgcn_s_waitcnt(0x0070);
+    const bool wave_has_keys = kw0 < kl;
+    // one step = one 64-query block, straight code, with the mask as selects or without (see attention_mfma.hip)
+    auto step = [&](int b, auto masked_t) {
+        constexpr bool MASKED = decltype(masked_t)::value;
+        const int q0 = q_begin + b * 64;
+        const char* sQ = smem + (b & (NS - 1)) * STAGE;
+        const char* sdO = sQ + TILE;
+        const char* s_stat = sdO + TILE;
+        // block b has landed for this wavefront (the two newest may still be in flight), then for everybody; the stage read before is free
+        if (wave == 0) __builtin_amdgcn_s_waitcnt(vmcnt_imm(2 * (2 * (HD / 32) + 1)));
+        else __builtin_amdgcn_s_waitcnt(vmcnt_imm(2 * (2 * (HD / 32))));
+        __builtin_amdgcn_s_barrier();
+        issue_block(b + 3);
+        if (!wave_has_keys) return;
+        if (MASKED && CAUSAL && q0 + 63 < kw0) return;
+        // queries of the block that see this lane's key, as this lane counts its rows: first .. first + visible - 1
+        const int first = (CAUSAL ? max(ki - q0, 0) : 0) - 4 * g;
+        const unsigned visible = (unsigned)max(ql - q0 - 4 * g - first, 0);
+        // two 32-query halves: the exponentials of half 0 between the first products of half 1, those of half 1 between the second products of half 0
+        constexpr int NA = HD / 16, AHEAD = 3, ND = 2 * (HD / 32), AHEAD_D = 2;
+        f32x16_t sa[2], sb[2], ga[2], gb[2];
+        bf16x8_t fq[NA], fo[NA], td[ND], tq[ND], pf[2], f1[2], f2[2];
+        auto read_a = [&](int qt, int i) {
+            const int o = qt * (32 * HD * 2) + rbase + (((i * 2 + g) ^ rsw) << 4);
+            fq[i] = *reinterpret_cast<const bf16x8_t*>(sQ + o);
+            fo[i] = *reinterpret_cast<const bf16x8_t*>(sdO + o);
+        };
+        auto soften2 = [&](int qt, int e0) {          // two elements of half qt: P_1 - lambda P_2 (sa), dS_1 (ga) and dS_2 (gb) in place
+#pragma unroll
+            for (int e = e0; e < e0 + 2; ++e) {
+                const bool out = MASKED && (unsigned)(qt * 32 + 8 * (e >> 2) + (e & 3) - first) >= visible;
+                float p1 = __builtin_amdgcn_exp2f(sa[qt][e] * c), p2 = lam * __builtin_amdgcn_exp2f(sb[qt][e] * c);
+                sa[qt][e] = out ? 0.f : p1 - p2;
+                ga[qt][e] = out ? 0.f : p1 * ga[qt][e];
+                gb[qt][e] = out ? 0.f : -p2 * gb[qt][e];
+            }
+        };
+        auto phase_a = [&](int qt, bool with_prev) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) { sa[qt][e] = 0.f; sb[qt][e] = 0.f; ga[qt][e] = 0.f; }
+            const bf16x8_t fs = *reinterpret_cast<const bf16x8_t*>(s_stat + (qt * 32 + col) * 16);
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) read_a(qt, i);
+#pragma unroll
+            for (int i = 0; i < NA; ++i) {
+                if (i + AHEAD < NA) read_a(qt, i + AHEAD);
+                __builtin_amdgcn_sched_barrier(kFence);
+                if (i < NA / 2) sa[qt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fq[i], kf[i], sa[qt], 0, 0, 0);
+                else sb[qt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fq[i], kf[i], sb[qt], 0, 0, 0);
+                ga[qt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fo[i], vf[i], ga[qt], 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(kFence);
+                if (with_prev) {
+#pragma unroll
+                    for (int e = i * (16 / NA); e < (i + 1) * (16 / NA); e += 2) soften2(qt ^ 1, e);
+                }
+            }
+            sa[qt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fs, minus[0], sa[qt], 0, 0, 0);
+            sb[qt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fs, minus[1], sb[qt], 0, 0, 0);
+            gb[qt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fs, minus[3], ga[qt], 0, 0, 0);
+            ga[qt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fs, minus[2], ga[qt], 0, 0, 0);
+        };
+        auto phase_d = [&](int qt, bool with_next) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) { pf[u] = frag_from_acc(sa[qt], u); f1[u] = frag_from_acc(ga[qt], u); f2[u] = frag_from_acc(gb[qt], u); }
+            // a half that no key of this wavefront sees: zeros instead of its rows, which may hold infinities (0 x Inf is NaN)
+            const bool hidden = MASKED && (qt ? q0 + 32 >= ql : CAUSAL && q0 + 31 < kw0);
+            const char* rO = hidden ? s_zero - qt * (32 * HD * 2) : sdO;
+            const char* rQ = hidden ? s_zero - qt * (32 * HD * 2) : sQ;
+            auto read_d = [&](int j) {
+                td[j] = read_tr<HD>(rO, tro, 2 * qt + j / (HD / 32), j % (HD / 32));
+                tq[j] = read_tr<HD>(rQ, tro, 2 * qt + j / (HD / 32), j % (HD / 32));
+            };
+#pragma unroll
+            for (int j = 0; j < AHEAD_D; ++j) read_d(j);
+#pragma unroll
+            for (int j = 0; j < ND; ++j) {
+                if (j + AHEAD_D < ND) read_d(j + AHEAD_D);
+                __builtin_amdgcn_sched_barrier(kFence);
+                const int dt = j % (HD / 32), u = j / (HD / 32);
+                dvacc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(td[j], pf[u], dvacc[dt], 0, 0, 0);
+                dkacc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tq[j], dt < HD / 64 ? f1[u] : f2[u], dkacc[dt], 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(kFence);
+                if (with_next) {
+#pragma unroll
+                    for (int e = j * (16 / ND); e < (j + 1) * (16 / ND); e += 2) soften2(qt ^ 1, e);
+                }
+            }
+        };
+        phase_a(0, false);
+        phase_a(1, true);
+        phase_d(0, true);
+        phase_d(1, false);
+    };
+    const int n_diag = CAUSAL ? min(2, nb) : 0;         // causal: queries k0 .. k0+127 meet this block's own keys
+    const int n_full = (ql - q_begin) / 64;             // blocks b < n_full have all their 64 rows
+    int b = 0;
+    for (; b < n_diag; ++b) step(b, std::true_type{});
+    for (; b < n_full; ++b) step(b, std::false_type{});
+    for (; b < nb; ++b) step(b, std::true_type{});
+    __builtin_amdgcn_s_waitcnt(0x0F70);                 // no transfer may still be writing LDS ...
+    const bool store = ki < kl;
+    bf16_t* dk = (bf16_t*)a.dk + (krow0 + ki) * a.ldk + h * HD;
+    bf16_t* dv = (bf16_t*)a.dv + (krow0 + ki) * a.ldv + h * HD;
+    bool more = false;
+    if constexpr (PS) {
+        if (tid == 0) s_next[turn] = next;
+        __builtin_amdgcn_s_waitcnt(0xC07F);             // lgkmcnt(0)
+        __builtin_amdgcn_s_barrier();                   // ... and nobody is reading it any more
+        draw.advance(__builtin_amdgcn_readfirstlane(s_next[turn]));
+        turn ^= 1;
+        more = draw.valid();
+        if (more) begin_item();
+    }
+    if (store) {
+        store_cols<HD>(dkacc, a.scale, dk, g);
+        store_cols<HD>(dvacc, 1.0f, dv, g);
+    }
+    if (!more) break;
+    }   // for (;;): the next item
+    if (PS) draw.finish();
+}
+
+template <int HD, bool CAUSAL>
+ds_status fwd_launch(const DiffAttnArgs& a, hipStream_t st) {
+    static bool attr = false;
+    auto kern = diff_fwd_mfma_kernel<HD, CAUSAL>;
+    const int smem = 4 * (64 * HD * 2);
+    const ds_status r = set_smem(kern, smem, attr);
+    if (r != DS_OK) return r;
+    hipLaunchKernelGGL(kern, dim3((unsigned)a.max_items_q * a.n_heads), dim3(256), smem, st, a);
+    DS_LAUNCH_CHECK();
+    return DS_OK;
+}
+
+template <int HD, bool CAUSAL>
+ds_status bwd_launch(const DiffAttnArgs& a, hipStream_t st) {
+    static bool attr_q = false, attr_kv = false;
+    auto kq = diff_bwd_dq_mfma_kernel<HD, CAUSAL>;
+    auto kkv = diff_bwd_dkv_mfma_kernel<HD, CAUSAL>;
+    const int smem_q = 4 * (64 * HD * 2);
+    const int smem_kv = 4 * (2 * (64 * HD * 2) + 1024) + 64 + 64 * HD;      // stages, draws, zeros
+    ds_status r = set_smem(kq, smem_q, attr_q);
+    if (r != DS_OK) return r;
+    r = set_smem(kkv, smem_kv, attr_kv);
+    if (r != DS_OK) return r;
+    hipLaunchKernelGGL(kq, dim3((unsigned)a.max_items_q * a.n_heads), dim3(256), smem_q, st, a);
+    DS_LAUNCH_CHECK();
+    const unsigned items_kv = (unsigned)a.max_items_k * a.n_heads;
+    hipLaunchKernelGGL(kkv, dim3(HD == 128 ? persistent_grid(items_kv) : items_kv), dim3(256), smem_kv, st, a);
+    DS_LAUNCH_CHECK();
+    return diff_dlambda(a, 32, st);
+}
+
+}  // namespace
+
+// what the matrix-core kernels ask beside a scratch that is large enough: 16-byte accesses, 64 rows of a tile within a 31-bit byte offset
+bool diff_mfma_supported(const DiffAttnArgs& a) {
+    if (a.dtype != DS_DTYPE_BF16 || (a.head_dim != 64 && a.head_dim != 128)) return false;
+    const long long ld_max = 1LL << 23;
+    for (const long long ld : {a.ldq, a.ldk, a.ldv, a.ldo})
+        if (ld % 8 || ld >= ld_max) return false;
+    for (const void* p : {a.q, a.k, a.v, (const void*)a.o, (const void*)a.o2, a.d_o, (const void*)a.dq, (const void*)a.dk, (const void*)a.dv})
+        if ((uintptr_t)p & 15) return false;
+    // the grids: one work-group per (block of 128 rows, head)
+    return ((long long)a.q_total_rows / 128 + a.n_seq) * a.n_heads <= 0x7fffffffLL && ((long long)a.k_total_rows / 128 + a.n_seq) * a.n_heads <= 0x7fffffffLL;
+}
+
+ds_status diff_fwd_mfma(const DiffAttnArgs& a0, hipStream_t st) {
+    DiffAttnArgs a = a0;
+    const ds_status r = attn_prepare_lists(a, false, st);
+    if (r != DS_OK) return r;
+    if (a.head_dim == 128) return a.mask ? fwd_launch<128, true>(a, st) : fwd_launch<128, false>(a, st);
+    return a.mask ? fwd_launch<64, true>(a, st) : fwd_launch<64, false>(a, st);
+}
+
+ds_status diff_bwd_mfma(const DiffAttnArgs& a0, hipStream_t st) {
+    DiffAttnArgs a = a0;
+    const ds_status r = attn_prepare_lists(a, true, st);
+    if (r != DS_OK) return r;
+    if (a.head_dim == 128) return a.mask ? bwd_launch<128, true>(a, st) : bwd_launch<128, false>(a, st);
+    return a.mask ? bwd_launch<64, true>(a, st) : bwd_launch<64, false>(a, st);
+}
