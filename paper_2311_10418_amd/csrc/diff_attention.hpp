@@ -17,7 +17,7 @@ struct DiffAttnArgs : AttnArgs {                        // scale: 1 / sqrt(head_
     float *d1, *d2;                                     // general kernels: D_1, D_2, [n_heads][q_total_rows]
     float* lam_part;                                    // sums of P_2 G of the queries of a wavefront, at the row of its first query
     int32_t vec;                                        // general kernels: rows of four elements may be accessed at once
-    char* aug;                                          // matrix-core kernels: see diff_attention_mfma.hip
+    char* aug;                                          // matrix-core kernels: see diff_attention_bwd.hip
 };
 
 size_t diff_scratch_bytes(int n_heads, int q_total_rows, int k_total_rows, int n_seq);

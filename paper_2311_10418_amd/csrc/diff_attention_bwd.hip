@@ -1,166 +1,17 @@
-// Differential attention in bf16 on the matrix cores (v_mfma_f32_32x32x16_bf16), head size 64 or 128 (maps of 32 or 64), causal or
-// unmasked, forward and backward.  Register layout, tiles, transpose reads and work lists are those of attention_mfma.hip: a wavefront
-// owns 32 columns (queries in forward and dQ, keys in dK/dV) and computes transposed score tiles, one set of accumulator registers
-// being the B operand of the next product as it stands.
+// The backward pass of diff_attention_fwd.hip, which says how two maps share the products.
 //
-// What two maps change.  The products that make scores contract over half a head each, so that both maps' scores cost what one map's
-// of the whole head do; dP = dO V^T is common to both, and so is dV (one product with P_1 - lambda P_2); dQ and dK of a map are half a
-// head wide.  Backward therefore takes the matrix instructions of ordinary attention, with twice the exponentials.  Forward cannot form
-// P_1 - lambda P_2 before both sums are known, so it keeps two accumulators and multiplies every fragment of V^T by both maps'
-// probabilities (6 instead of 4 products of a head's width; a first pass over the scores for the sums would cost the same).
-//
-// Probabilities, their difference and dS are rounded to bf16 as they become operands; scores, statistics, sums, dP and dlambda are fp32.
-#include "attention_tiles.hpp"
-#include "diff_attention.hpp"
+// Split into a dQ kernel and a dK/dV kernel, so that every result has one owner: no atomics, the same result every time.
+#include "diff_attention_tiles.hpp"
 #include <type_traits>
 
 namespace {
-
-// ------------------------------------------------------------------------------------ forward
-// A tile of 64 keys goes in two halves of 32, so that both maps' scores (32 registers) and both accumulators (128 at head size 128) leave
-// room for two wavefronts per SIMD.
-template <int HD, bool CAUSAL>
-__global__ __launch_bounds__(256, 2) void diff_fwd_mfma_kernel(DiffAttnArgs a) {
-    extern __shared__ __attribute__((aligned(16))) char smem[];
-    constexpr int TILE = 64 * HD * 2, NS = HD / 16, ND = HD / 32;
-    const uint32_t lds0 = lds_address(smem);
-    const int tid = threadIdx.x, lane = tid & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int col = lane & 31, g = lane >> 5;
-    const int item = blockIdx.x / a.n_heads, h = blockIdx.x - item * a.n_heads;
-    const int2 it = a.items_q[item];
-    if (item >= a.n_items[0]) return;
-    const int s = it.x, q0 = it.y * 128;
-    const int ql = a.q_len[s], kl = a.k_len[s];
-    const long long qrow0 = a.q_row[s];
-    const bf16_t* Q = (const bf16_t*)a.q + qrow0 * a.ldq + h * HD;
-    const bf16_t* K = (const bf16_t*)a.k + (long long)a.k_row[s] * a.ldk + h * HD;
-    const bf16_t* V = (const bf16_t*)a.v + (long long)a.k_row[s] * a.ldv + h * HD;
-    const int qw0 = q0 + wave * 32;
-    const int qi = qw0 + col;
-    const int qi_c = qi < ql ? qi : ql - 1;
-
-    bf16x8_t qf[NS];
-#pragma unroll
-    for (int ks = 0; ks < NS; ++ks) qf[ks] = *reinterpret_cast<const bf16x8_t*>(Q + (long long)qi_c * a.ldq + ks * 16 + g * 8);
-
-    BufferTileLoader<HD> ldK, ldV;
-    ldK.setup(K, a.ldk, kl, wave, lane);
-    ldV.setup(V, a.ldv, kl, wave, lane);
-    TrOffsets<HD> tro;
-    tro.init(lane);
-    const int rbase = col * (HD * 2);
-    const int rsw = swz<HD>(col);
-
-    f32x16_t o1[ND], o2[ND];
-#pragma unroll
-    for (int dt = 0; dt < ND; ++dt)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) { o1[dt][e] = 0.f; o2[dt][e] = 0.f; }
-    float m1 = -INFINITY, m2 = -INFINITY, l1 = 0.f, l2 = 0.f;          // running maxima (in the exp2 domain) and sums
-    const float c = a.scale * kLog2e;
-
-    const int kv_end = CAUSAL ? min(kl, q0 + 128) : kl;
-    const int wave_last = CAUSAL ? min(kl - 1, qw0 + 31) : kl - 1;     // last key this wavefront can see
-    const int nb = (kv_end + 63) / 64;
-    if (nb > 0) {                                       // (a sequence without keys: zero output, nothing to fetch)
-        ldK.issue(lds0, 0);
-        ldV.issue(lds0 + TILE, 0);
-    }
-    // scores -> probabilities of one map in place; its accumulator is rescaled only when some column's maximum moved
-    auto soften = [&](f32x16_t& p, float& m, float& l, f32x16_t (&o)[ND]) {
-        float mx = -INFINITY;
-#pragma unroll
-        for (int e = 0; e < 16; e += 2) mx = max3f(mx, p[e], p[e + 1]);
-        const float m_new = max3f(m, mx * c, __shfl_xor(mx, 32, 64) * c);
-        float rs = 0.f;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[e], c, -m_new));
-            rs += p[e];
-        }
-        const float alpha = __builtin_amdgcn_exp2f(m - m_new);
-        l = l * alpha + rs;
-        if (__builtin_amdgcn_ballot_w64(m_new > m) != 0) {
-#pragma unroll
-            for (int dt = 0; dt < ND; ++dt)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) o[dt][e] *= alpha;
-        }
-        m = m_new;
-    };
-    for (int b = 0; b < nb; ++b) {
-        const int kv0 = b * 64;
-        const char* sK = smem + (b & 1) * (2 * TILE);
-        const char* sV = sK + TILE;
-        wait_tiles_and_sync();                          // block b has landed; the other stage is free
-        if (b + 1 < nb) {
-            const uint32_t n = lds0 + ((b + 1) & 1) * (2 * TILE);
-            ldK.issue(n, kv0 + 64);
-            ldV.issue(n + TILE, kv0 + 64);
-        }
-        if (kv0 > wave_last || qw0 >= ql) continue;
-#pragma unroll
-        for (int kt = 0; kt < 2; ++kt) {
-            if (kv0 + kt * 32 > wave_last) continue;    // the half beyond the last key this wavefront sees
-            f32x16_t p1, p2;
-#pragma unroll
-            for (int e = 0; e < 16; ++e) { p1[e] = 0.f; p2[e] = 0.f; }
-#pragma unroll
-            for (int ks = 0; ks < NS; ++ks) {
-                const bf16x8_t fk = *reinterpret_cast<const bf16x8_t*>(sK + kt * (32 * HD * 2) + rbase + (((ks * 2 + g) ^ rsw) << 4));
-                if (ks < NS / 2) p1 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fk, qf[ks], p1, 0, 0, 0);
-                else p2 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fk, qf[ks], p2, 0, 0, 0);
-            }
-            if (kv0 + kt * 32 + 32 > kl || (CAUSAL && kv0 + kt * 32 + 31 > qw0)) {
-                int kbase = kv0 + kt * 32;              // (one real branch around the whole mask: see attention_mfma.hip)
-                asm volatile("" : "+s"(kbase));
-                const int last = (CAUSAL ? min(kl - 1, qi) : kl - 1) - kbase - 4 * g;      // last visible row, as this lane counts them
-#pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    if (8 * (e >> 2) + (e & 3) > last) { p1[e] = -INFINITY; p2[e] = -INFINITY; }
-            }
-            soften(p1, m1, l1, o1);
-            soften(p2, m2, l2, o2);
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const bf16x8_t f1 = frag_from_acc(p1, u), f2 = frag_from_acc(p2, u);
-#pragma unroll
-                for (int dt = 0; dt < ND; ++dt) {
-                    const bf16x8_t fv = read_tr<HD>(sV, tro, 2 * kt + u, dt);
-                    o1[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fv, f1, o1[dt], 0, 0, 0);
-                    o2[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fv, f2, o2[dt], 0, 0, 0);
-                }
-            }
-        }
-    }
-    l1 += __shfl_xor(l1, 32, 64);
-    l2 += __shfl_xor(l2, 32, 64);
-    if (qi < ql) {
-        const long long row = qrow0 + qi;
-        const float r1 = l1 > 0.f ? 1.0f / l1 : 0.f, r2 = l2 > 0.f ? 1.0f / l2 : 0.f, lam = a.lambda[h];
-#pragma unroll
-        for (int dt = 0; dt < ND; ++dt)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                o2[dt][e] *= r2;
-                o1[dt][e] = o1[dt][e] * r1 - lam * o2[dt][e];
-            }
-        store_cols<HD>(o1, 1.0f, (bf16_t*)a.o + row * a.ldo + h * HD, g);
-        if (a.o2) store_cols<HD>(o2, 1.0f, (bf16_t*)a.o2 + row * a.ldo + h * HD, g);
-        if (g == 0) {
-            a.lse[(size_t)(2 * h) * a.lse_stride + row] = (m1 + __builtin_amdgcn_logf(l1)) * kLn2;
-            a.lse[(size_t)(2 * h + 1) * a.lse_stride + row] = (m2 + __builtin_amdgcn_logf(l2)) * kLn2;
-        }
-    }
-}
 
 // ------------------------------------------------------------------------------------ backward: dQ (and the statistics, the parts of dlambda)
 // For the dK/dV kernel a query leaves one entry of eight bf16 values, the {hi, lo} splits of lse_1 / scale, lse_2 / scale, D_1 and D_2.
 template <int HD, bool CAUSAL>
 __global__ __launch_bounds__(256, 2) void diff_bwd_dq_mfma_kernel(DiffAttnArgs a) {
     extern __shared__ __attribute__((aligned(16))) char smem[];
-    constexpr int TILE = 64 * HD * 2, NS = HD / 16, ND = HD / 32;
+    constexpr int TILE = 64 * HD * 2, NS = HD / 16, ND = HD / 32, AHEAD = 2;
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 31, g = lane >> 5;
@@ -181,7 +32,7 @@ __global__ __launch_bounds__(256, 2) void diff_bwd_dq_mfma_kernel(DiffAttnArgs a
     const int qi_c = qi < ql ? qi : ql - 1;
 
     const uint32_t lds0 = lds_address(smem);
-    TileLoader<HD> ldK, ldV;
+    PieceLoader<HD> ldK, ldV;
     ldK.setup(K, a.ldk, kl, wave, lane);
     ldV.setup(V, a.ldv, kl, wave, lane);
     if (kl > 0) {
@@ -214,10 +65,8 @@ __global__ __launch_bounds__(256, 2) void diff_bwd_dq_mfma_kernel(DiffAttnArgs a
     const float e1 = lse1 * kLog2e, e2 = lse2 * kLog2e;
     const float c = a.scale * kLog2e;
 
-    TrOffsets<HD> tro;
-    tro.init(lane);
-    const int rbase = col * (HD * 2);
-    const int rsw = swz<HD>(col);
+    FragOffsets<HD> at;
+    at.init(lane);
 
     f32x16_t gacc[ND];
 #pragma unroll
@@ -232,7 +81,6 @@ __global__ __launch_bounds__(256, 2) void diff_bwd_dq_mfma_kernel(DiffAttnArgs a
     for (int b = 0; b < nb; ++b) {
         const int kv0 = b * 64;
         const char* sK = smem + (b & 1) * (2 * TILE);
-        const char* sV = sK + TILE;
         wait_tiles_and_sync();
         if (b + 1 < nb) {
             const uint32_t n = lds0 + ((b + 1) & 1) * (2 * TILE);
@@ -247,14 +95,22 @@ __global__ __launch_bounds__(256, 2) void diff_bwd_dq_mfma_kernel(DiffAttnArgs a
             f32x16_t p1, p2, gr;
 #pragma unroll
             for (int e = 0; e < 16; ++e) { p1[e] = 0.f; p2[e] = 0.f; gr[e] = 0.f; }
+            const char* tK = sK + kt * (32 * HD * 2);
+            bf16x8_t fk[NS], fv[NS];
+            auto read_kv = [&](int ks) {
+                fk[ks] = at.row(tK, ks);
+                fv[ks] = at.row(tK + TILE, ks);
+            };
+#pragma unroll
+            for (int ks = 0; ks < AHEAD; ++ks) read_kv(ks);
 #pragma unroll
             for (int ks = 0; ks < NS; ++ks) {
-                const int o = kt * (32 * HD * 2) + rbase + (((ks * 2 + g) ^ rsw) << 4);
-                const bf16x8_t fk = *reinterpret_cast<const bf16x8_t*>(sK + o);
-                const bf16x8_t fv = *reinterpret_cast<const bf16x8_t*>(sV + o);
-                if (ks < NS / 2) p1 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fk, qf[ks], p1, 0, 0, 0);
-                else p2 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fk, qf[ks], p2, 0, 0, 0);
-                gr = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fv, dof[ks], gr, 0, 0, 0);
+                if (ks + AHEAD < NS) read_kv(ks + AHEAD);
+                __builtin_amdgcn_sched_barrier(kFence);
+                if (ks < NS / 2) p1 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fk[ks], qf[ks], p1, 0, 0, 0);
+                else p2 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fk[ks], qf[ks], p2, 0, 0, 0);
+                gr = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fv[ks], dof[ks], gr, 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(kFence);
             }
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
@@ -280,7 +136,7 @@ __global__ __launch_bounds__(256, 2) void diff_bwd_dq_mfma_kernel(DiffAttnArgs a
                 const bf16x8_t f1 = frag_from_acc(p1, u), f2 = frag_from_acc(p2, u);
 #pragma unroll
                 for (int dt = 0; dt < ND; ++dt) {
-                    const bf16x8_t kt_f = read_tr<HD>(sK, tro, 2 * kt + u, dt);
+                    const bf16x8_t kt_f = at.turned(tK + u * (16 * HD * 2), dt);
                     gacc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kt_f, dt < ND / 2 ? f1 : f2, gacc[dt], 0, 0, 0);
                 }
             }
@@ -288,13 +144,12 @@ __global__ __launch_bounds__(256, 2) void diff_bwd_dq_mfma_kernel(DiffAttnArgs a
     }
     lam_sum = wave_sum(qi < ql ? lam_sum : 0.f);
     if (lane == 0 && qw0 < ql) a.lam_part[(size_t)h * a.q_total_rows + qrow0 + qw0] = lam_sum;
-    if (qi < ql) {
+    if (qw0 >= ql) return;
 #pragma unroll
-        for (int dt = ND / 2; dt < ND; ++dt)
+    for (int dt = ND / 2; dt < ND; ++dt)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) gacc[dt][e] *= -lam;
-        store_cols<HD>(gacc, a.scale, (bf16_t*)a.dq + (qrow0 + qi) * a.ldq + h * HD, g);
-    }
+        for (int e = 0; e < 16; ++e) gacc[dt][e] *= -lam;
+    store_cols16<HD>(gacc, a.scale, (bf16_t*)a.dq + (qrow0 + qi) * a.ldq + h * HD, g, qi < ql);
 }
 
 // ------------------------------------------------------------------------------------ backward: dK, dV
@@ -511,25 +366,13 @@ __global__ __launch_bounds__(256, HD == 64 ? 2 : 1) void diff_bwd_dkv_mfma_kerne
         more = draw.valid();
         if (more) begin_item();
     }
-    if (store) {
-        store_cols<HD>(dkacc, a.scale, dk, g);
-        store_cols<HD>(dvacc, 1.0f, dv, g);
+    if (wave_has_keys) {
+        store_cols16<HD>(dkacc, a.scale, dk, g, store);
+        store_cols16<HD>(dvacc, 1.0f, dv, g, store);
     }
     if (!more) break;
     }   // for (;;): the next item
     if (PS) draw.finish();
-}
-
-template <int HD, bool CAUSAL>
-ds_status fwd_launch(const DiffAttnArgs& a, hipStream_t st) {
-    static bool attr = false;
-    auto kern = diff_fwd_mfma_kernel<HD, CAUSAL>;
-    const int smem = 4 * (64 * HD * 2);
-    const ds_status r = set_smem(kern, smem, attr);
-    if (r != DS_OK) return r;
-    hipLaunchKernelGGL(kern, dim3((unsigned)a.max_items_q * a.n_heads), dim3(256), smem, st, a);
-    DS_LAUNCH_CHECK();
-    return DS_OK;
 }
 
 template <int HD, bool CAUSAL>
@@ -552,26 +395,6 @@ ds_status bwd_launch(const DiffAttnArgs& a, hipStream_t st) {
 }
 
 }  // namespace
-
-// what the matrix-core kernels ask beside a scratch that is large enough: 16-byte accesses, 64 rows of a tile within a 31-bit byte offset
-bool diff_mfma_supported(const DiffAttnArgs& a) {
-    if (a.dtype != DS_DTYPE_BF16 || (a.head_dim != 64 && a.head_dim != 128)) return false;
-    const long long ld_max = 1LL << 23;
-    for (const long long ld : {a.ldq, a.ldk, a.ldv, a.ldo})
-        if (ld % 8 || ld >= ld_max) return false;
-    for (const void* p : {a.q, a.k, a.v, (const void*)a.o, (const void*)a.o2, a.d_o, (const void*)a.dq, (const void*)a.dk, (const void*)a.dv})
-        if ((uintptr_t)p & 15) return false;
-    // the grids: one work-group per (block of 128 rows, head)
-    return ((long long)a.q_total_rows / 128 + a.n_seq) * a.n_heads <= 0x7fffffffLL && ((long long)a.k_total_rows / 128 + a.n_seq) * a.n_heads <= 0x7fffffffLL;
-}
-
-ds_status diff_fwd_mfma(const DiffAttnArgs& a0, hipStream_t st) {
-    DiffAttnArgs a = a0;
-    const ds_status r = attn_prepare_lists(a, false, st);
-    if (r != DS_OK) return r;
-    if (a.head_dim == 128) return a.mask ? fwd_launch<128, true>(a, st) : fwd_launch<128, false>(a, st);
-    return a.mask ? fwd_launch<64, true>(a, st) : fwd_launch<64, false>(a, st);
-}
 
 ds_status diff_bwd_mfma(const DiffAttnArgs& a0, hipStream_t st) {
     DiffAttnArgs a = a0;

@@ -1,0 +1,203 @@
+// Differential attention in bf16 on the matrix cores (v_mfma_f32_32x32x16_bf16), head size 64 or 128 (maps of 32 or 64), causal or
+// unmasked, forward and backward.  Register layout, tiles, transpose reads and work lists are those of attention_mfma.hip: a wavefront
+// owns 32 columns (queries in forward and dQ, keys in dK/dV) and computes transposed score tiles, one set of accumulator registers
+// being the B operand of the next product as it stands.
+//
+// What two maps change.  The products that make scores contract over half a head each, so that both maps' scores cost what one map's
+// of the whole head do; dP = dO V^T is common to both, and so is dV (one product with P_1 - lambda P_2); dQ and dK of a map are half a
+// head wide.  Backward therefore takes the matrix instructions of ordinary attention, with twice the exponentials.  Forward cannot form
+// P_1 - lambda P_2 before both sums are known, so it keeps two accumulators and multiplies every fragment of V^T by both maps'
+// probabilities (6 instead of 4 products of a head's width; a first pass over the scores for the sums would cost the same).
+//
+// Probabilities, their difference and dS are rounded to bf16 as they become operands; scores, statistics, sums, dP and dlambda are fp32.
+#include "diff_attention_tiles.hpp"
+#include <type_traits>
+
+namespace {
+
+constexpr float kSlack = 8.0f;                          // see diff_fwd_mfma_kernel
+
+// ------------------------------------------------------------------------------------ forward
+// A tile of 64 keys goes in two steps of 32, so that both maps' scores (32 registers) and both accumulators (128 at head size 128) leave room
+// for two wavefronts per SIMD, whose vector work and matrix instructions then overlap.
+template <int HD, bool CAUSAL>
+__global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void diff_fwd_mfma_kernel(DiffAttnArgs a) {
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    constexpr int TILE = 64 * HD * 2, NS = HD / 16, ND = HD / 32, AHEAD = 2, AHEAD_V = 1;
+    const uint32_t lds0 = lds_address(smem);
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int col = lane & 31, g = lane >> 5;
+    const int item = blockIdx.x / a.n_heads, h = blockIdx.x - item * a.n_heads;
+    const int2 it = a.items_q[item];
+    if (item >= a.n_items[0]) return;
+    const int s = it.x, q0 = it.y * 128;
+    const int ql = a.q_len[s], kl = a.k_len[s];
+    const long long qrow0 = a.q_row[s];
+    const bf16_t* Q = (const bf16_t*)a.q + qrow0 * a.ldq + h * HD;
+    const bf16_t* K = (const bf16_t*)a.k + (long long)a.k_row[s] * a.ldk + h * HD;
+    const bf16_t* V = (const bf16_t*)a.v + (long long)a.k_row[s] * a.ldv + h * HD;
+    const int qw0 = q0 + wave * 32;
+    const int qi = qw0 + col;
+    const int qi_c = qi < ql ? qi : ql - 1;
+
+    bf16x8_t qf[NS];
+#pragma unroll
+    for (int ks = 0; ks < NS; ++ks) qf[ks] = *reinterpret_cast<const bf16x8_t*>(Q + (long long)qi_c * a.ldq + ks * 16 + g * 8);
+
+    PieceLoader<HD> ldK, ldV;
+    ldK.setup(K, a.ldk, kl, wave, lane);
+    ldV.setup(V, a.ldv, kl, wave, lane);
+    FragOffsets<HD> at;
+    at.init(lane);
+
+    f32x16_t o[2][ND];
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[m][dt][e] = 0.f;
+    float top[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};          // running maxima (in the exp2 domain) and sums
+    const float c = a.scale * kLog2e;
+
+    const int kv_end = CAUSAL ? min(kl, q0 + 128) : kl;
+    const int wave_last = CAUSAL ? min(kl - 1, qw0 + 31) : kl - 1;     // last key this wavefront can see
+    const int nb = (kv_end + 63) / 64;
+    if (nb > 0) {                                       // (a sequence without keys: zero output, nothing to fetch)
+        ldK.issue(lds0, 0);
+        ldV.issue(lds0 + TILE, 0);
+    }
+    // scores -> probabilities of map m in place.  The running maximum is raised, and what was summed so far rescaled, only where a score exceeds it
+    // by more than kSlack: probabilities are then at most 2^kSlack times what they are relative to the true maximum, which costs no digits, and a
+    // lane needs nothing of the lane that holds the other half of its column.
+    auto soften = [&](f32x16_t& p, int m) {
+        float x = -INFINITY;
+#pragma unroll
+        for (int e = 0; e < 16; e += 2) x = max3f(x, p[e], p[e + 1]);
+        x *= c;
+        if (__builtin_amdgcn_ballot_w64(x > top[m] + kSlack) != 0) {
+            const float up = max3f(top[m], x, __shfl_xor(x, 32, 64));
+            const float alpha = __builtin_amdgcn_exp2f(top[m] - up);
+            l[m] *= alpha;
+            top[m] = up;
+#pragma unroll
+            for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[m][dt][e] *= alpha;
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[e], c, -top[m]));
+            l[m] += p[e];
+        }
+    };
+    for (int b = 0; b < nb; ++b) {
+        const int kv0 = b * 64;
+        const char* sK = smem + (b & 1) * (2 * TILE);
+        wait_tiles_and_sync();                          // block b has landed; the other stage is free
+        if (b + 1 < nb) {
+            const uint32_t n = lds0 + ((b + 1) & 1) * (2 * TILE);
+            ldK.issue(n, kv0 + 64);
+            ldV.issue(n + TILE, kv0 + 64);
+        }
+        if (kv0 > wave_last || qw0 >= ql) continue;
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt) {
+            if (kv0 + kt * 32 > wave_last) continue;    // the half beyond the last key this wavefront sees
+            const char* tK = sK + kt * (32 * HD * 2);
+            const char* tV = tK + TILE;
+            f32x16_t p[2];
+#pragma unroll
+            for (int m = 0; m < 2; ++m)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) p[m][e] = 0.f;
+            bf16x8_t fk[NS], fv[2 * ND];
+            auto read_k = [&](int i) { fk[i] = at.row(tK, i); };
+            auto read_v = [&](int i) { fv[i] = at.turned(tV + (i / ND) * (16 * HD * 2), i % ND); };
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) read_k(i);
+#pragma unroll
+            for (int i = 0; i < NS; ++i) {
+                if (i + AHEAD < NS) read_k(i + AHEAD);
+                __builtin_amdgcn_sched_barrier(kFence);
+                p[i >= NS / 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fk[i], qf[i], p[i >= NS / 2], 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(kFence);
+            }
+            if (kv0 + kt * 32 + 32 > kl || (CAUSAL && kv0 + kt * 32 + 31 > qw0)) {
+                int kbase = kv0 + kt * 32;              // (one real branch around the whole mask: see attention_mfma.hip)
+                asm volatile("" : "+s"(kbase));
+                const int last = (CAUSAL ? min(kl - 1, qi) : kl - 1) - kbase - 4 * g;      // last visible row, as this lane counts them
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    if (8 * (e >> 2) + (e & 3) > last) { p[0][e] = -INFINITY; p[1][e] = -INFINITY; }
+            }
+            soften(p[0], 0);
+            soften(p[1], 1);
+#pragma unroll
+            for (int i = 0; i < AHEAD_V; ++i) read_v(i);
+            bf16x8_t f1, f2;
+#pragma unroll
+            for (int i = 0; i < 2 * ND; ++i) {
+                if (i + AHEAD_V < 2 * ND) read_v(i + AHEAD_V);
+                if (i % ND == 0) { f1 = frag_from_acc(p[0], i / ND); f2 = frag_from_acc(p[1], i / ND); }
+                __builtin_amdgcn_sched_barrier(kFence);
+                o[0][i % ND] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fv[i], f1, o[0][i % ND], 0, 0, 0);
+                o[1][i % ND] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fv[i], f2, o[1][i % ND], 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(kFence);
+            }
+        }
+    }
+#pragma unroll
+    for (int m = 0; m < 2; ++m) l[m] += __shfl_xor(l[m], 32, 64);
+    if (qw0 >= ql) return;
+    const long long row = qrow0 + qi;
+    const float r1 = l[0] > 0.f ? 1.0f / l[0] : 0.f, r2 = l[1] > 0.f ? 1.0f / l[1] : 0.f, lam = a.lambda[h];
+#pragma unroll
+    for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            o[1][dt][e] *= r2;
+            o[0][dt][e] = o[0][dt][e] * r1 - lam * o[1][dt][e];
+        }
+    store_cols16<HD>(o[0], 1.0f, (bf16_t*)a.o + row * a.ldo + h * HD, g, qi < ql);
+    if (a.o2) store_cols16<HD>(o[1], 1.0f, (bf16_t*)a.o2 + row * a.ldo + h * HD, g, qi < ql);
+    if (g == 0 && qi < ql) {
+        a.lse[(size_t)(2 * h) * a.lse_stride + row] = (top[0] + __builtin_amdgcn_logf(l[0])) * kLn2;
+        a.lse[(size_t)(2 * h + 1) * a.lse_stride + row] = (top[1] + __builtin_amdgcn_logf(l[1])) * kLn2;
+    }
+}
+
+template <int HD, bool CAUSAL>
+ds_status fwd_launch(const DiffAttnArgs& a, hipStream_t st) {
+    static bool attr = false;
+    auto kern = diff_fwd_mfma_kernel<HD, CAUSAL>;
+    const int smem = 4 * (64 * HD * 2);
+    const ds_status r = set_smem(kern, smem, attr);
+    if (r != DS_OK) return r;
+    hipLaunchKernelGGL(kern, dim3((unsigned)a.max_items_q * a.n_heads), dim3(256), smem, st, a);
+    DS_LAUNCH_CHECK();
+    return DS_OK;
+}
+
+}  // namespace
+
+// what the matrix-core kernels ask beside a scratch that is large enough: 16-byte accesses, 64 rows of a tile within a 31-bit byte offset
+bool diff_mfma_supported(const DiffAttnArgs& a) {
+    if (a.dtype != DS_DTYPE_BF16 || (a.head_dim != 64 && a.head_dim != 128)) return false;
+    const long long ld_max = 1LL << 23;
+    for (const long long ld : {a.ldq, a.ldk, a.ldv, a.ldo})
+        if (ld % 8 || ld >= ld_max) return false;
+    for (const void* p : {a.q, a.k, a.v, (const void*)a.o, (const void*)a.o2, a.d_o, (const void*)a.dq, (const void*)a.dk, (const void*)a.dv})
+        if ((uintptr_t)p & 15) return false;
+    // the grids: one work-group per (block of 128 rows, head)
+    return ((long long)a.q_total_rows / 128 + a.n_seq) * a.n_heads <= 0x7fffffffLL && ((long long)a.k_total_rows / 128 + a.n_seq) * a.n_heads <= 0x7fffffffLL;
+}
+
+ds_status diff_fwd_mfma(const DiffAttnArgs& a0, hipStream_t st) {
+    DiffAttnArgs a = a0;
+    const ds_status r = attn_prepare_lists(a, false, st);
+    if (r != DS_OK) return r;
+    if (a.head_dim == 128) return a.mask ? fwd_launch<128, true>(a, st) : fwd_launch<128, false>(a, st);
+    return a.mask ? fwd_launch<64, true>(a, st) : fwd_launch<64, false>(a, st);
+}

@@ -1,0 +1,77 @@
+// What the matrix-core kernels of differential attention share beside attention_tiles.hpp.
+#pragma once
+#include "attention_tiles.hpp"
+#include "diff_attention.hpp"
+
+namespace {
+
+// Transfers of 64-row tiles, 1 KB (4 rows of 128 columns or 8 of 64) at a time, HD / 32 per wavefront and tile, through a raw buffer that ends
+// at the last valid row: rows past it arrive as zeros.  The swizzled chunk of a lane in transfer i is that of transfer 0 with i
+// (HD = 128) or 2 i flipped in, so that one register per tensor and one for the chunk make every offset.
+template <int HD> struct PieceLoader {
+    static constexpr int PW = HD / 32, ROWS = 512 / HD;               // transfers, rows per transfer
+    const char* base;
+    int ld2, n_valid;
+    uint32_t row0, chunk0, lds_off;
+    __device__ __forceinline__ void setup(const bf16_t* base_, long long ld_, int n_valid_, int wave, int lane) {
+        base = (const char*)base_; ld2 = (int)ld_ * 2; n_valid = n_valid_; lds_off = wave * (PW * 1024);
+        const int u = wave * PW * 64 + lane;
+        row0 = (uint32_t)(TileLoader<HD>::row_of(u) * ld2);
+        chunk0 = (uint32_t)TileLoader<HD>::chunk_of(u) * 16;
+    }
+    // rows r0 .. r0+63 -> the tile at LDS address lds_tile
+    __device__ __forceinline__ void issue(uint32_t lds_tile, int r0) const {
+        const i32x4_t buf = make_raw_buffer(base + (long long)r0 * ld2, (uint32_t)max(0, min(64, n_valid - r0)) * (uint32_t)ld2);
+#pragma unroll
+        for (int i = 0; i < PW; ++i)
+            lds_dma16_buffer(buf, row0 + (uint32_t)(i * ROWS * ld2) + (chunk0 ^ (uint32_t)(i * (HD == 128 ? 16 : 32))), lds_tile + lds_off + i * 1024);
+    }
+};
+
+// This lane's offset in a tile for the fragments of the first product, and for transpose reads; the k-th 16 features or the dt-th 32 features are
+// the same with k << 5 or dt << 6 flipped in: three registers instead of one per fragment.
+template <int HD> struct FragOffsets {
+    uint32_t rows, lo, hi;
+    __device__ __forceinline__ void init(int lane) {
+        const int col = lane & 31, g = lane >> 5;
+        rows = (uint32_t)(col * (HD * 2) + ((g ^ swz<HD>(col)) << 4));
+        TrOffsets<HD> t;
+        t.init(lane);
+        lo = t.lo[0];
+        hi = t.hi[0];
+    }
+    // features 16 k .. of the 32 rows at t
+    __device__ __forceinline__ bf16x8_t row(const char* t, int k) const { return *reinterpret_cast<const bf16x8_t*>(t + (rows ^ (uint32_t)(k << 5))); }
+    // features 32 dt .. of the 16 rows at t, turned
+    __device__ __forceinline__ bf16x8_t turned(const char* t, int dt) const {
+        const s16x4_t a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(t + (lo ^ (uint32_t)(dt << 6))));
+        const s16x4_t b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(t + (hi ^ (uint32_t)(dt << 6))));
+        const s16x8_t v = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+        return __builtin_bit_cast(bf16x8_t, v);
+    }
+};
+
+// Stores a transposed [HD x 32] accumulator block times mul: lane column = row `row` of the output.  A lane holds 4 of every 8 features, the lane 32
+// further on the other 4: they swap, so that each has 8 of every 16 and the stores are 16 bytes wide.  Every lane of the wavefront takes part;
+// `on` says whether this lane's row is stored.
+template <int HD>
+__device__ __forceinline__ void store_cols16(const f32x16_t (&acc)[HD / 32], float mul, bf16_t* __restrict__ row, int g, bool on) {
+#pragma unroll
+    for (int dt = 0; dt < HD / 32; ++dt)
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            uint32_t x[2][2];                           // [8-feature group][two packed pairs]
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                bf16x4_t v;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[j] = (bf16_t)(acc[dt][8 * q + 4 * i + j] * mul);
+                __builtin_memcpy(x[i], &v, 8);
+            }
+            const auto a = __builtin_amdgcn_permlane32_swap(x[0][0], x[1][0], false, false);
+            const auto b = __builtin_amdgcn_permlane32_swap(x[0][1], x[1][1], false, false);
+            if (on) *reinterpret_cast<uint4*>(row + dt * 32 + q * 16 + g * 8) = make_uint4(a[0], b[0], a[1], b[1]);
+        }
+}
+
+}  // namespace
