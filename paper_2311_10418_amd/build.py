@@ -18,6 +18,9 @@ CPP_SOURCES = ["planner.cpp", "schedule.cpp", "recompute.cpp"]
 
 HIPCC_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function", "-Wno-inline-asm",
                "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
+# Results of matrix instructions in ordinary vector registers: with more than 256 registers per lane the compiler's own choice is accumulation
+# registers for all of them, and the dK/dV kernel of differential attention would move every score over before its exponential
+FILE_FLAGS = {"diff_attention_bwd.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
 CXX_FLAGS = ["-O2", "-std=c++17", "-fPIC", "-Wall", "-Wextra", "-ffp-contract=off"]
 
 
@@ -38,7 +41,7 @@ def _compile(args):
     if not force and not _deps_newer(obj):
         return src, 0, ""
     if src.endswith(".hip"):
-        cmd = ["hipcc"] + HIPCC_FLAGS + ["-c", os.path.join(CSRC, src), "-o", obj]
+        cmd = ["hipcc"] + HIPCC_FLAGS + FILE_FLAGS.get(src, []) + ["-c", os.path.join(CSRC, src), "-o", obj]
     else:
         cmd = ["g++"] + CXX_FLAGS + ["-c", os.path.join(CSRC, src), "-o", obj]
     p = subprocess.run(cmd, capture_output=True, text=True)

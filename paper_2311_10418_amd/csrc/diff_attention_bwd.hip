@@ -7,7 +7,7 @@
 namespace {
 
 // ------------------------------------------------------------------------------------ backward: dQ (and the statistics, the parts of dlambda)
-// For the dK/dV kernel a query leaves one entry of eight bf16 values, the {hi, lo} splits of lse_1 / scale, lse_2 / scale, D_1 and D_2.
+// For the dK/dV kernel a query leaves one entry of eight bf16 values, the {hi, lo} splits of lse_1 / scale, lse_2 / scale, D_1 and D_2 - D_1.
 template <int HD, bool CAUSAL>
 __global__ __launch_bounds__(256, 2) void diff_bwd_dq_mfma_kernel(DiffAttnArgs a) {
     extern __shared__ __attribute__((aligned(16))) char smem[];
@@ -61,7 +61,7 @@ __global__ __launch_bounds__(256, 2) void diff_bwd_dq_mfma_kernel(DiffAttnArgs a
     const float lse1 = a.lse[(size_t)(2 * h) * a.lse_stride + qrow0 + qi_c], lse2 = a.lse[(size_t)(2 * h + 1) * a.lse_stride + qrow0 + qi_c];
     if (g == 0 && qi < ql)
         reinterpret_cast<uint4*>(a.aug)[(size_t)h * a.q_total_rows + qrow0 + qi] =
-            make_uint4(split_hi_lo(lse1 * (1.0f / a.scale)), split_hi_lo(lse2 * (1.0f / a.scale)), split_hi_lo(d1), split_hi_lo(d2));
+            make_uint4(split_hi_lo(lse1 * (1.0f / a.scale)), split_hi_lo(lse2 * (1.0f / a.scale)), split_hi_lo(d1), split_hi_lo(d2 - d1));
     const float e1 = lse1 * kLog2e, e2 = lse2 * kLog2e;
     const float c = a.scale * kLog2e;
 
@@ -145,11 +145,7 @@ __global__ __launch_bounds__(256, 2) void diff_bwd_dq_mfma_kernel(DiffAttnArgs a
     lam_sum = wave_sum(qi < ql ? lam_sum : 0.f);
     if (lane == 0 && qw0 < ql) a.lam_part[(size_t)h * a.q_total_rows + qrow0 + qw0] = lam_sum;
     if (qw0 >= ql) return;
-#pragma unroll
-    for (int dt = ND / 2; dt < ND; ++dt)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) gacc[dt][e] *= -lam;
-    store_cols16<HD>(gacc, a.scale, (bf16_t*)a.dq + (qrow0 + qi) * a.ldq + h * HD, g, qi < ql);
+    store_cols16<HD>(gacc, a.scale, -lam * a.scale, (bf16_t*)a.dq + (qrow0 + qi) * a.ldq + h * HD, g, qi < ql);
 }
 
 // ------------------------------------------------------------------------------------ backward: dK, dV
@@ -170,7 +166,7 @@ __global__ __launch_bounds__(256, HD == 64 ? 2 : 1) void diff_bwd_dkv_mfma_kerne
     volatile int* s_next = reinterpret_cast<volatile int*>(smem + NS * STAGE);      // two words used in turn (an item without steps has one barrier only)
     int turn = 0;
     char* s_zero = smem + NS * STAGE + 64;              // 32 rows of zeros
-    TileLoader<HD> ldQ, ldO;
+    PieceLoader<HD> ldQ, ldO;
     ldQ.setup(nullptr, a.ldq, 0, wave, lane);
     ldO.setup(nullptr, a.ldo, 0, wave, lane);
     WorkDraw draw(a, 1);
@@ -179,18 +175,14 @@ __global__ __launch_bounds__(256, HD == 64 ? 2 : 1) void diff_bwd_dkv_mfma_kerne
     const char* aug_src;
     float lam;
     bf16x8_t kf[HD / 16], vf[HD / 16];
-    // block blk -> stage blk % 4 by direct transfers (the statistics by wavefront 0); indices past the last block are clamped
+    // block blk -> stage blk % 4 by direct transfers (the statistics by wavefront 0).  Queries past the last one are zeros in
+    // all three: P is 1 there, and multiplies zeros (dV), and dS is 1 (0 - 0): no mask
     auto issue_block = [&](int blk) {
         const uint32_t n = lds0 + (blk & (NS - 1)) * STAGE;
-        const int bc = blk < nb ? blk : nb - 1;
-        const int q0 = q_begin + bc * 64;
+        const int q0 = q_begin + blk * 64;
         ldQ.issue(n, q0);
         ldO.issue(n + TILE, q0);
-        if (wave == 0) {
-            int r = q0 + lane;
-            r = r < ql ? r : ql - 1;
-            lds_dma16_at(aug_src + (size_t)r * 16, n + 2 * TILE);
-        }
+        if (wave == 0) lds_dma16_buffer(make_raw_buffer(aug_src + (long long)q0 * 16, (uint32_t)max(0, min(64, ql - q0)) * 16), (uint32_t)lane * 16, n + 2 * TILE);
     };
     auto begin_item = [&] {
         const int item = draw.index() / a.n_heads;
@@ -230,17 +222,13 @@ __global__ __launch_bounds__(256, HD == 64 ? 2 : 1) void diff_bwd_dkv_mfma_kerne
     }
     begin_item();
     for (int i = tid; i < 64 * HD / 16; i += 256) reinterpret_cast<uint4*>(s_zero)[i] = make_uint4(0u, 0u, 0u, 0u);
-    bf16x8_t minus[4];                                  // -1 in the contraction slots of value i (lane half 0), which hold its hi and lo
+    bf16x8_t minus;                                     // -1 in the contraction slots 0 and 1 (lane half 0), where a statistic's hi and lo are put
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) minus[i][j] = (bf16_t)((g == 0 && j / 2 == i) ? -1.0f : 0.0f);
+    for (int j = 0; j < 8; ++j) minus[j] = (bf16_t)((g == 0 && j < 2) ? -1.0f : 0.0f);
     const float c = a.scale * kLog2e;
 
-    TrOffsets<HD> tro;
-    tro.init(lane);
-    const int rbase = col * (HD * 2);
-    const int rsw = swz<HD>(col);
+    FragOffsets<HD> at;
+    at.init(lane);
 
     f32x16_t dkacc[HD / 32], dvacc[HD / 32];
     for (;;) {
@@ -267,77 +255,84 @@ __global__ __launch_bounds__(256, HD == 64 ? 2 : 1) void diff_bwd_dkv_mfma_kerne
         __builtin_amdgcn_s_barrier();
         issue_block(b + 3);
         if (!wave_has_keys) return;
-        if (MASKED && CAUSAL && q0 + 63 < kw0) return;
-        // queries of the block that see this lane's key, as this lane counts its rows: first .. first + visible - 1
-        const int first = (CAUSAL ? max(ki - q0, 0) : 0) - 4 * g;
-        const unsigned visible = (unsigned)max(ql - q0 - 4 * g - first, 0);
+        if (MASKED && q0 + 63 < kw0) return;
+        const int first = ki - q0 - 4 * g;             // the first query of the block that sees this lane's key, as this lane counts its rows
         // two 32-query halves: the exponentials of half 0 between the first products of half 1, those of half 1 between the second products of half 0
-        constexpr int NA = HD / 16, AHEAD = 3, ND = 2 * (HD / 32), AHEAD_D = 2;
-        f32x16_t sa[2], sb[2], ga[2], gb[2];
-        bf16x8_t fq[NA], fo[NA], td[ND], tq[ND], pf[2], f1[2], f2[2];
-        auto read_a = [&](int qt, int i) {
-            const int o = qt * (32 * HD * 2) + rbase + (((i * 2 + g) ^ rsw) << 4);
-            fq[i] = *reinterpret_cast<const bf16x8_t*>(sQ + o);
-            fo[i] = *reinterpret_cast<const bf16x8_t*>(sdO + o);
+        // (without the freedom to move vector instructions across, the register allocation of the causal kernel at head size 128 copies fewer
+        // accumulators: 407 us against 452 at 8 sequences of up to 2048, 16 heads; the unmasked one is better with it, 8.6 against 9.5 us per 32 keys)
+        constexpr int FENCE = HD == 128 && !CAUSAL ? kFence : 0;
+        constexpr int NA = HD / 16, AHEAD = 2, ND = 2 * (HD / 32), AHEAD_D = 2;
+        f32x16_t sa[2], sb[2], ga[2];
+        u32x4_t fs[2];
+        bf16x8_t fq[NA], fo[NA], td[ND], tq[ND], pf[2][2], f1[2][2], f2[2][2];
+        auto less = [&](f32x16_t x, uint32_t hi_lo) {   // x minus a statistic of its rows
+            const u32x4_t f = {hi_lo, 0u, 0u, 0u};
+            return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, f), minus, x, 0, 0, 0);
         };
-        auto soften2 = [&](int qt, int e0) {          // two elements of half qt: P_1 - lambda P_2 (sa), dS_1 (ga) and dS_2 (gb) in place
-#pragma unroll
-            for (int e = e0; e < e0 + 2; ++e) {
-                const bool out = MASKED && (unsigned)(qt * 32 + 8 * (e >> 2) + (e & 3) - first) >= visible;
-                float p1 = __builtin_amdgcn_exp2f(sa[qt][e] * c), p2 = lam * __builtin_amdgcn_exp2f(sb[qt][e] * c);
-                sa[qt][e] = out ? 0.f : p1 - p2;
-                ga[qt][e] = out ? 0.f : p1 * ga[qt][e];
-                gb[qt][e] = out ? 0.f : -p2 * gb[qt][e];
+        auto read_a = [&](int qt, int i) {
+            fq[i] = at.row(sQ + qt * (32 * HD * 2), i);
+            fo[i] = at.row(sdO + qt * (32 * HD * 2), i);
+        };
+        auto hidden = [&](int qt, int e) { return MASKED && qt * 32 + 8 * (e >> 2) + (e & 3) < first; };
+        // scores and dP of half qt to operands, in 32 pieces: P_1 and dS_1 first (16), then P_2, the difference and dS_2
+        auto soften = [&](int qt, int i) {
+            const int e = i & 15;
+            if (i < 16) {
+                sa[qt][e] = __builtin_amdgcn_exp2f(sa[qt][e] * c);
+                const float d = hidden(qt, e) ? 0.f : sa[qt][e] * ga[qt][e];
+                f1[qt][e >> 3][e & 7] = (bf16_t)d;
+            } else {
+                const float p2 = __builtin_amdgcn_exp2f(sb[qt][e] * c);
+                pf[qt][e >> 3][e & 7] = (bf16_t)(hidden(qt, e) ? 0.f : __builtin_fmaf(-lam, p2, sa[qt][e]));
+                f2[qt][e >> 3][e & 7] = (bf16_t)(hidden(qt, e) ? 0.f : p2 * ga[qt][e]);      // dS_2 / -lambda
             }
+            if (i == 15) ga[qt] = less(ga[qt], fs[qt][3]);       // dP - D_2: the fourth value is D_2 - D_1
         };
         auto phase_a = [&](int qt, bool with_prev) {
 #pragma unroll
             for (int e = 0; e < 16; ++e) { sa[qt][e] = 0.f; sb[qt][e] = 0.f; ga[qt][e] = 0.f; }
-            const bf16x8_t fs = *reinterpret_cast<const bf16x8_t*>(s_stat + (qt * 32 + col) * 16);
+            fs[qt] = *reinterpret_cast<const u32x4_t*>(s_stat + (qt * 32 + col) * 16);
 #pragma unroll
             for (int i = 0; i < AHEAD; ++i) read_a(qt, i);
 #pragma unroll
             for (int i = 0; i < NA; ++i) {
                 if (i + AHEAD < NA) read_a(qt, i + AHEAD);
-                __builtin_amdgcn_sched_barrier(kFence);
+                __builtin_amdgcn_sched_barrier(FENCE);
                 if (i < NA / 2) sa[qt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fq[i], kf[i], sa[qt], 0, 0, 0);
                 else sb[qt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fq[i], kf[i], sb[qt], 0, 0, 0);
                 ga[qt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fo[i], vf[i], ga[qt], 0, 0, 0);
-                __builtin_amdgcn_sched_barrier(kFence);
+                __builtin_amdgcn_sched_barrier(FENCE);
                 if (with_prev) {
 #pragma unroll
-                    for (int e = i * (16 / NA); e < (i + 1) * (16 / NA); e += 2) soften2(qt ^ 1, e);
+                    for (int e = i * (32 / NA); e < (i + 1) * (32 / NA); ++e) soften(qt ^ 1, e);
                 }
             }
-            sa[qt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fs, minus[0], sa[qt], 0, 0, 0);
-            sb[qt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fs, minus[1], sb[qt], 0, 0, 0);
-            gb[qt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fs, minus[3], ga[qt], 0, 0, 0);
-            ga[qt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fs, minus[2], ga[qt], 0, 0, 0);
+            sa[qt] = less(sa[qt], fs[qt][0]);
+            sb[qt] = less(sb[qt], fs[qt][1]);
+            ga[qt] = less(ga[qt], fs[qt][2]);
         };
         auto phase_d = [&](int qt, bool with_next) {
-#pragma unroll
-            for (int u = 0; u < 2; ++u) { pf[u] = frag_from_acc(sa[qt], u); f1[u] = frag_from_acc(ga[qt], u); f2[u] = frag_from_acc(gb[qt], u); }
             // a half that no key of this wavefront sees: zeros instead of its rows, which may hold infinities (0 x Inf is NaN)
-            const bool hidden = MASKED && (qt ? q0 + 32 >= ql : CAUSAL && q0 + 31 < kw0);
-            const char* rO = hidden ? s_zero - qt * (32 * HD * 2) : sdO;
-            const char* rQ = hidden ? s_zero - qt * (32 * HD * 2) : sQ;
+            const bool none = MASKED && q0 + 32 * qt + 31 < kw0;
+            const char* rO = none ? s_zero : sdO + qt * (32 * HD * 2);
+            const char* rQ = none ? s_zero : sQ + qt * (32 * HD * 2);
             auto read_d = [&](int j) {
-                td[j] = read_tr<HD>(rO, tro, 2 * qt + j / (HD / 32), j % (HD / 32));
-                tq[j] = read_tr<HD>(rQ, tro, 2 * qt + j / (HD / 32), j % (HD / 32));
+                td[j] = at.turned(rO + (j / (HD / 32)) * (16 * HD * 2), j % (HD / 32));
+                tq[j] = at.turned(rQ + (j / (HD / 32)) * (16 * HD * 2), j % (HD / 32));
             };
 #pragma unroll
             for (int j = 0; j < AHEAD_D; ++j) read_d(j);
 #pragma unroll
             for (int j = 0; j < ND; ++j) {
                 if (j + AHEAD_D < ND) read_d(j + AHEAD_D);
-                __builtin_amdgcn_sched_barrier(kFence);
+                __builtin_amdgcn_sched_barrier(FENCE);
                 const int dt = j % (HD / 32), u = j / (HD / 32);
-                dvacc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(td[j], pf[u], dvacc[dt], 0, 0, 0);
-                dkacc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tq[j], dt < HD / 64 ? f1[u] : f2[u], dkacc[dt], 0, 0, 0);
-                __builtin_amdgcn_sched_barrier(kFence);
+                dvacc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(td[j], pf[qt][u], dvacc[dt], 0, 0, 0);
+                dkacc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tq[j], dt < HD / 64 ? f1[qt][u] : f2[qt][u], dkacc[dt], 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(FENCE);
                 if (with_next) {
 #pragma unroll
-                    for (int e = j * (16 / ND); e < (j + 1) * (16 / ND); e += 2) soften2(qt ^ 1, e);
+                    for (int e = j * (32 / ND); e < (j + 1) * (32 / ND); ++e) soften(qt ^ 1, e);
                 }
             }
         };
@@ -347,13 +342,13 @@ __global__ __launch_bounds__(256, HD == 64 ? 2 : 1) void diff_bwd_dkv_mfma_kerne
         phase_d(1, false);
     };
     const int n_diag = CAUSAL ? min(2, nb) : 0;         // causal: queries k0 .. k0+127 meet this block's own keys
-    const int n_full = (ql - q_begin) / 64;             // blocks b < n_full have all their 64 rows
     int b = 0;
-    for (; b < n_diag; ++b) step(b, std::true_type{});
-    for (; b < n_full; ++b) step(b, std::false_type{});
-    for (; b < nb; ++b) step(b, std::true_type{});
+    if constexpr (CAUSAL)
+        for (; b < n_diag; ++b) step(b, std::true_type{});
+    for (; b < nb; ++b) step(b, std::false_type{});
     __builtin_amdgcn_s_waitcnt(0x0F70);                 // no transfer may still be writing LDS ...
     const bool store = ki < kl;
+    const float lam_of_item = lam;                      // (begin_item moves on)
     bf16_t* dk = (bf16_t*)a.dk + (krow0 + ki) * a.ldk + h * HD;
     bf16_t* dv = (bf16_t*)a.dv + (krow0 + ki) * a.ldv + h * HD;
     bool more = false;
@@ -367,8 +362,8 @@ __global__ __launch_bounds__(256, HD == 64 ? 2 : 1) void diff_bwd_dkv_mfma_kerne
         if (more) begin_item();
     }
     if (wave_has_keys) {
-        store_cols16<HD>(dkacc, a.scale, dk, g, store);
-        store_cols16<HD>(dvacc, 1.0f, dv, g, store);
+        store_cols16<HD>(dkacc, a.scale, -lam_of_item * a.scale, dk, g, store);
+        store_cols16<HD>(dvacc, 1.0f, 1.0f, dv, g, store);
     }
     if (!more) break;
     }   // for (;;): the next item

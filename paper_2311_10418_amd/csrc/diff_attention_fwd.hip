@@ -160,8 +160,8 @@ __global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void diff_fwd_mfma_kernel(Di
             o[1][dt][e] *= r2;
             o[0][dt][e] = o[0][dt][e] * r1 - lam * o[1][dt][e];
         }
-    store_cols16<HD>(o[0], 1.0f, (bf16_t*)a.o + row * a.ldo + h * HD, g, qi < ql);
-    if (a.o2) store_cols16<HD>(o[1], 1.0f, (bf16_t*)a.o2 + row * a.ldo + h * HD, g, qi < ql);
+    store_cols16<HD>(o[0], 1.0f, 1.0f, (bf16_t*)a.o + row * a.ldo + h * HD, g, qi < ql);
+    if (a.o2) store_cols16<HD>(o[1], 1.0f, 1.0f, (bf16_t*)a.o2 + row * a.ldo + h * HD, g, qi < ql);
     if (g == 0 && qi < ql) {
         a.lse[(size_t)(2 * h) * a.lse_stride + row] = (top[0] + __builtin_amdgcn_logf(l[0])) * kLn2;
         a.lse[(size_t)(2 * h + 1) * a.lse_stride + row] = (top[1] + __builtin_amdgcn_logf(l[1])) * kLn2;

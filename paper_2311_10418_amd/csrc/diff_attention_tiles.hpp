@@ -5,6 +5,12 @@
 
 namespace {
 
+// One direct transfer of 64 x 4 bytes (see lds_dma16_at): lane i's dword lands at lds_addr + 4 i.
+__device__ __forceinline__ void lds_dma4(const void* gptr, uint32_t lds_addr) {
+    const uint32_t m0v = __builtin_amdgcn_readfirstlane(lds_addr);
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" : : "v"(gptr), "s"(m0v) : "memory", "m0");
+}
+
 // Transfers of 64-row tiles, 1 KB (4 rows of 128 columns or 8 of 64) at a time, HD / 32 per wavefront and tile, through a raw buffer that ends
 // at the last valid row: rows past it arrive as zeros.  The swizzled chunk of a lane in transfer i is that of transfer 0 with i
 // (HD = 128) or 2 i flipped in, so that one register per tensor and one for the chunk make every offset.
@@ -19,12 +25,15 @@ template <int HD> struct PieceLoader {
         row0 = (uint32_t)(TileLoader<HD>::row_of(u) * ld2);
         chunk0 = (uint32_t)TileLoader<HD>::chunk_of(u) * 16;
     }
-    // rows r0 .. r0+63 -> the tile at LDS address lds_tile
+    // rows r0 .. r0+63 -> the tile at LDS address lds_tile, one transfer or all
+    __device__ __forceinline__ i32x4_t rows(int r0) const { return make_raw_buffer(base + (long long)r0 * ld2, (uint32_t)max(0, min(64, n_valid - r0)) * (uint32_t)ld2); }
+    __device__ __forceinline__ void piece(i32x4_t buf, int i, uint32_t lds_tile) const {
+        lds_dma16_buffer(buf, row0 + (uint32_t)(i * ROWS * ld2) + (chunk0 ^ (uint32_t)(i * (HD == 128 ? 16 : 32))), lds_tile + lds_off + i * 1024);
+    }
     __device__ __forceinline__ void issue(uint32_t lds_tile, int r0) const {
-        const i32x4_t buf = make_raw_buffer(base + (long long)r0 * ld2, (uint32_t)max(0, min(64, n_valid - r0)) * (uint32_t)ld2);
+        const i32x4_t buf = rows(r0);
 #pragma unroll
-        for (int i = 0; i < PW; ++i)
-            lds_dma16_buffer(buf, row0 + (uint32_t)(i * ROWS * ld2) + (chunk0 ^ (uint32_t)(i * (HD == 128 ? 16 : 32))), lds_tile + lds_off + i * 1024);
+        for (int i = 0; i < PW; ++i) piece(buf, i, lds_tile);
     }
 };
 
@@ -51,11 +60,11 @@ template <int HD> struct FragOffsets {
     }
 };
 
-// Stores a transposed [HD x 32] accumulator block times mul: lane column = row `row` of the output.  A lane holds 4 of every 8 features, the lane 32
+// Stores a transposed [HD x 32] accumulator block times mul (first half of the features) or mul2 (second half): lane column = row `row` of the output.  A lane holds 4 of every 8 features, the lane 32
 // further on the other 4: they swap, so that each has 8 of every 16 and the stores are 16 bytes wide.  Every lane of the wavefront takes part;
 // `on` says whether this lane's row is stored.
 template <int HD>
-__device__ __forceinline__ void store_cols16(const f32x16_t (&acc)[HD / 32], float mul, bf16_t* __restrict__ row, int g, bool on) {
+__device__ __forceinline__ void store_cols16(const f32x16_t (&acc)[HD / 32], float mul, float mul2, bf16_t* __restrict__ row, int g, bool on) {
 #pragma unroll
     for (int dt = 0; dt < HD / 32; ++dt)
 #pragma unroll
@@ -65,7 +74,7 @@ __device__ __forceinline__ void store_cols16(const f32x16_t (&acc)[HD / 32], flo
             for (int i = 0; i < 2; ++i) {
                 bf16x4_t v;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) v[j] = (bf16_t)(acc[dt][8 * q + 4 * i + j] * mul);
+                for (int j = 0; j < 4; ++j) v[j] = (bf16_t)(acc[dt][8 * q + 4 * i + j] * (dt < HD / 64 ? mul : mul2));
                 __builtin_memcpy(x[i], &v, 8);
             }
             const auto a = __builtin_amdgcn_permlane32_swap(x[0][0], x[1][0], false, false);
