@@ -576,7 +576,7 @@ int64_t ds_norm_bwd_scratch_floats(int32_t rows, int32_t d);
  *     y = resid_scale * x + branch_scale * gate . z      (the stream; stored)
  *     u = N_pre(y)    (of y as stored; pre_g = NULL: not computed)
  * rms = 0: LayerNorm (gain and bias, eps 1e-5); 1: RMSNorm (gain only, eps 1e-6), for both norms.
- * x, h, y, u: [rows, d] row-major, contiguous, d a multiple of 8, at most 8192; all tensors 16-byte aligned.
+ * x, h, y, u: [rows, d] row-major, contiguous, d a multiple of 8, at most 4096; all tensors 16-byte aligned.
  * gate_kind: DS_GATE_NONE (gate NULL), DS_GATE_COL ([d], one factor per column), DS_GATE_ROW ([rows, d]).
  * row_valid: NULL, or DEVICE int32[rows]: where it is negative the inputs are not looked at (they may be NaN), y and u are
  * written as zeros.  stats: float32 [4, rows], mean and rstd of the rows of h, then of y, for the backward pass.

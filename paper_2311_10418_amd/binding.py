@@ -117,8 +117,15 @@ def lib():
         _lib.ds_stage_workspace_need.restype = C.c_int64
         _lib.ds_norm_bwd_scratch_floats.restype = C.c_int64
         _lib.ds_attention_scratch_bytes.restype = C.c_int64
-        _lib.ds_resid_norm_bwd_scratch_floats.restype = C.c_int64
-        _lib.ds_diff_attention_scratch_bytes.restype = C.c_int64
+        i, l, f, d, p = C.c_int32, C.c_int64, C.c_float, C.c_double, C.c_void_p
+        for name, args in (("ds_resid_norm_fwd", [i] * 4 + [p] * 5 + [i, p, f, f] + [p] * 6),
+                           ("ds_resid_norm_bwd", [i] * 4 + [p] * 7 + [i, p, f, f] + [p] * 10 + [i, p]),
+                           ("ds_rope", [i] * 7 + [p, p, f, p, l, p, l, p]), ("ds_rope_freqs", [i, d, i, d, d, d, d, p]), ("ds_layout_positions", [p, i, p]),
+                           ("ds_diff_attention_fwd", [i] * 5 + [p] * 4 + [i, i] + [p, i] * 3 + [p, p, p, i, p, i, i, p, l, i, p]),
+                           ("ds_diff_attention_bwd", [i] * 5 + [p] * 4 + [i, i] + [p, i] * 3 + [p, p, p, p, i] + [p] * 5 + [i, i, i, p, l, i, p])):
+            getattr(_lib, name).argtypes = args
+        _lib.ds_resid_norm_bwd_scratch_floats.argtypes, _lib.ds_resid_norm_bwd_scratch_floats.restype = [i, i], l
+        _lib.ds_diff_attention_scratch_bytes.argtypes, _lib.ds_diff_attention_scratch_bytes.restype = [i] * 4, l
         _lib.ds_layout_free.restype = None
         _lib.ds_stage_destroy.restype = None
     return _lib
@@ -548,32 +555,45 @@ def ds_norm_bwd(dy, x, g, stats, resid, dx, dg, db, partial, rms=False, accumula
     _check(rc, "ds_norm_bwd")
 
 
+# The entry points below take their pointers and numbers as they are (argtypes in lib()), and look their tensors over before the call: at the
+# smallest sizes a call is little else.
+def _refuse(t, name, what, dtype, device):
+    raise ValueError("%s must be a %s %s tensor on GPU %d, got %s %s, strides %s, on %s" % (name, what, dtype, device, t.dtype, tuple(t.shape), t.stride(), t.device))
+
+
 def _tensor(t, name, shape, dtype, device):
-    """Pointer of a contiguous tensor of the given shape (a number: at least so many elements), element type and device; None stays None."""
+    """Address of a contiguous tensor of the given shape (a number: at least so many elements), element type and GPU; None stays None."""
     if t is None:
         return None
-    fits = t.numel() >= shape if isinstance(shape, int) else tuple(t.shape) == tuple(shape)
-    if not fits or t.dtype != dtype or t.device != device or not t.is_contiguous():
-        raise ValueError("%s must be a contiguous %s tensor of %s on %s, got %s %s on %s" % (name, dtype, shape, device, t.dtype, tuple(t.shape), t.device))
-    return C.c_void_p(t.data_ptr())
+    if t.dtype is not dtype or not (t.numel() >= shape if type(shape) is int else t.shape == shape) or t.get_device() != device or not t.is_contiguous():
+        _refuse(t, name, "contiguous %s" % (shape,), dtype, device)
+    return t.data_ptr()
 
 
 def _columns(t, name, rows, cols, dtype, device):
-    """(pointer, row stride) of a 2-D tensor with at least `rows` rows and `cols` columns that lie next to each other: a column range of a
+    """(address, row stride) of a 2-D tensor with at least `rows` rows and `cols` columns that lie next to each other: a column range of a
     wider tensor, for instance."""
-    if t.dim() != 2 or t.shape[0] < rows or t.shape[1] < cols or (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]) \
-            or t.dtype != dtype or t.device != device:
-        raise ValueError("%s must be a [>= %d, >= %d] %s tensor with consecutive columns on %s, got %s %s, strides %s, on %s"
-                         % (name, rows, cols, dtype, device, t.dtype, tuple(t.shape), t.stride(), t.device))
-    return C.c_void_p(t.data_ptr()), max(t.stride(0), t.shape[1]) if t.shape[0] == 1 else t.stride(0)
+    if t.dim() != 2 or t.dtype is not dtype or t.get_device() != device:
+        _refuse(t, name, "[>= %d, >= %d]" % (rows, cols), dtype, device)
+    have, wide = t.shape
+    ld, step = t.stride()
+    if have < rows or wide < cols or (wide > 1 and step != 1) or (have > 1 and ld < wide):
+        _refuse(t, name, "[>= %d, >= %d] (consecutive columns)" % (rows, cols), dtype, device)
+    return t.data_ptr(), ld if have > 1 else max(ld, wide)
 
 
 def _current(t):
-    """The device of t; kernels go to the current device, so it has to be that one."""
+    """(torch, dtype code, number of the GPU) of a tensor; kernels go to the current GPU, so it has to be there."""
     import torch
-    if t.device.type != "cuda" or t.device.index != torch.cuda.current_device():
+    code = _dtype_code(t)
+    device = t.get_device()
+    if device < 0 or device != torch.cuda.current_device():
         raise ValueError("tensors must be on the current GPU, got %s" % (t.device,))
-    return t.device
+    return torch, code, device
+
+
+def _raw_stream(torch, stream):
+    return torch.cuda.current_stream().cuda_stream if stream is None else stream
 
 
 def _gate(gate, rows, d):
@@ -585,128 +605,118 @@ def _gate(gate, rows, d):
 def ds_resid_norm_fwd(x, h, y, stats, post_g=None, post_b=None, gate=None, pre_g=None, pre_b=None, u=None, resid_scale=1.0, branch_scale=1.0,
                       row_valid=None, rms=False, stream=None):
     """gate: None, [d] or [rows, d]."""
-    import torch
-    dev, dt = _current(x), x.dtype
-    code = _dtype_code(x)
-    rows, d = x.shape
+    torch, code, dev = _current(x)
+    dt, full = x.dtype, x.shape
+    rows, d = full
     kind, gate_shape = _gate(gate, rows, d)
-    rc = lib().ds_resid_norm_fwd(C.c_int32(code), C.c_int32(int(rms)), C.c_int32(rows), C.c_int32(d), _tensor(x, "x", (rows, d), dt, dev),
-                                 _tensor(h, "h", (rows, d), dt, dev), _tensor(row_valid, "row_valid", (rows,), torch.int32, dev),
-                                 _tensor(post_g, "post_g", (d,), dt, dev), _tensor(post_b, "post_b", (d,), dt, dev), C.c_int32(kind),
-                                 _tensor(gate, "gate", gate_shape, dt, dev), C.c_float(resid_scale), C.c_float(branch_scale),
-                                 _tensor(pre_g, "pre_g", (d,), dt, dev), _tensor(pre_b, "pre_b", (d,), dt, dev), _tensor(y, "y", (rows, d), dt, dev),
-                                 _tensor(u, "u", (rows, d), dt, dev), _tensor(stats, "stats", (4, rows), torch.float32, dev), _stream(stream))
+    col = (d,)
+    rc = lib().ds_resid_norm_fwd(code, int(rms), rows, d, _tensor(x, "x", full, dt, dev), _tensor(h, "h", full, dt, dev),
+                                 _tensor(row_valid, "row_valid", (rows,), torch.int32, dev), _tensor(post_g, "post_g", col, dt, dev),
+                                 _tensor(post_b, "post_b", col, dt, dev), kind, _tensor(gate, "gate", gate_shape, dt, dev), resid_scale, branch_scale,
+                                 _tensor(pre_g, "pre_g", col, dt, dev), _tensor(pre_b, "pre_b", col, dt, dev), _tensor(y, "y", full, dt, dev),
+                                 _tensor(u, "u", full, dt, dev), _tensor(stats, "stats", (4, rows), torch.float32, dev), _raw_stream(torch, stream))
     _check(rc, "ds_resid_norm_fwd")
 
 
 def ds_resid_norm_bwd_scratch_floats(rows, d):
-    return lib().ds_resid_norm_bwd_scratch_floats(C.c_int32(rows), C.c_int32(d))
+    return lib().ds_resid_norm_bwd_scratch_floats(rows, d)
 
 
 def ds_resid_norm_bwd(dy, y, h, stats, dx, dh, partial, du=None, post_g=None, post_b=None, gate=None, pre_g=None, dgate=None, dpost_g=None,
                       dpost_b=None, dpre_g=None, dpre_b=None, resid_scale=1.0, branch_scale=1.0, row_valid=None, rms=False, accumulate=False,
                       stream=None):
-    import torch
-    dev, dt, f32 = _current(h), h.dtype, torch.float32
-    code = _dtype_code(h)
-    rows, d = h.shape
+    torch, code, dev = _current(h)
+    dt, f32, full = h.dtype, torch.float32, h.shape
+    rows, d = full
     kind, gate_shape = _gate(gate, rows, d)
-    full, col = (rows, d), (d,)
-    rc = lib().ds_resid_norm_bwd(C.c_int32(code), C.c_int32(int(rms)), C.c_int32(rows), C.c_int32(d), _tensor(dy, "dy", full, dt, dev),
-                                 _tensor(du, "du", full, dt, dev), _tensor(y, "y", full, dt, dev), _tensor(h, "h", full, dt, dev),
-                                 _tensor(row_valid, "row_valid", (rows,), torch.int32, dev), _tensor(post_g, "post_g", col, dt, dev),
-                                 _tensor(post_b, "post_b", col, dt, dev), C.c_int32(kind), _tensor(gate, "gate", gate_shape, dt, dev),
-                                 C.c_float(resid_scale), C.c_float(branch_scale), _tensor(pre_g, "pre_g", col, dt, dev),
+    col = (d,)
+    rc = lib().ds_resid_norm_bwd(code, int(rms), rows, d, _tensor(dy, "dy", full, dt, dev), _tensor(du, "du", full, dt, dev), _tensor(y, "y", full, dt, dev),
+                                 _tensor(h, "h", full, dt, dev), _tensor(row_valid, "row_valid", (rows,), torch.int32, dev),
+                                 _tensor(post_g, "post_g", col, dt, dev), _tensor(post_b, "post_b", col, dt, dev), kind,
+                                 _tensor(gate, "gate", gate_shape, dt, dev), resid_scale, branch_scale, _tensor(pre_g, "pre_g", col, dt, dev),
                                  _tensor(stats, "stats", (4, rows), f32, dev), _tensor(dx, "dx", full, dt, dev), _tensor(dh, "dh", full, dt, dev),
                                  _tensor(dgate, "dgate", gate_shape, dt if kind == DS_GATE_ROW else f32, dev) if kind != DS_GATE_NONE else None,
                                  _tensor(dpost_g, "dpost_g", col, f32, dev), _tensor(dpost_b, "dpost_b", col, f32, dev),
                                  _tensor(dpre_g, "dpre_g", col, f32, dev), _tensor(dpre_b, "dpre_b", col, f32, dev),
-                                 _tensor(partial, "partial", int(ds_resid_norm_bwd_scratch_floats(rows, d)), f32, dev), C.c_int32(int(accumulate)),
-                                 _stream(stream))
+                                 _tensor(partial, "partial", ds_resid_norm_bwd_scratch_floats(rows, d), f32, dev), int(accumulate), _raw_stream(torch, stream))
     _check(rc, "ds_resid_norm_bwd")
 
 
 def ds_diff_attention_scratch_bytes(n_heads, q_total_rows, k_total_rows, n_seq):
-    return lib().ds_diff_attention_scratch_bytes(C.c_int32(n_heads), C.c_int32(q_total_rows), C.c_int32(k_total_rows), C.c_int32(n_seq))
+    return lib().ds_diff_attention_scratch_bytes(n_heads, q_total_rows, k_total_rows, n_seq)
 
 
-def _diff_tensors(q, k, v, lam, lse, q_row, q_len, k_row, k_len, n_heads, head_dim, scratch):
-    """The arguments both directions share: (dtype code, tables, tensors with strides, lambda, lse, rows, scratch), checked."""
-    import torch
-    dev, dt = _current(q), q.dtype
-    code = _dtype_code(q)
-    n, wide, i32 = int(q_row.shape[0]), n_heads * head_dim, torch.int32
-    q_rows, k_rows = int(q.shape[0]), int(k.shape[0])
-    tables = [_tensor(t, name, (n,), i32, dev) for t, name in ((q_row, "q_row"), (q_len, "q_len"), (k_row, "k_row"), (k_len, "k_len"))]
-    (pq, ldq), (pk, ldk), (pv, ldv) = (_columns(t, name, rows, wide, dt, dev) for t, name, rows in ((q, "q", q_rows), (k, "k", k_rows), (v, "v", k_rows)))
-    return (C.c_int32(code), n, tables, [pq, C.c_int32(ldq), pk, C.c_int32(ldk), pv, C.c_int32(ldv), _tensor(lam, "lam", (n_heads,), torch.float32, dev)],
-            _tensor(lse, "lse", (2 * n_heads, q_rows), torch.float32, dev),
-            [C.c_int32(q_rows), C.c_int32(k_rows), _tensor(scratch, "scratch", int(ds_diff_attention_scratch_bytes(n_heads, q_rows, k_rows, n)), torch.uint8, dev),
-             C.c_int64(scratch.numel())])
+def _diff_tensors(torch, dev, q, k, v, lam, lse, q_row, q_len, k_row, k_len, n_heads, head_dim, scratch):
+    """The arguments both directions share, checked: (number of sequences, tables, tensors with strides and lambda, lse, row counts and scratch)."""
+    dt = q.dtype
+    n, wide, i32 = q_row.shape[0], n_heads * head_dim, torch.int32
+    q_rows, k_rows = q.shape[0], k.shape[0]
+    tables = (_tensor(q_row, "q_row", (n,), i32, dev), _tensor(q_len, "q_len", (n,), i32, dev), _tensor(k_row, "k_row", (n,), i32, dev),
+              _tensor(k_len, "k_len", (n,), i32, dev))
+    qkv = (*_columns(q, "q", q_rows, wide, dt, dev), *_columns(k, "k", k_rows, wide, dt, dev), *_columns(v, "v", k_rows, wide, dt, dev),
+           _tensor(lam, "lam", (n_heads,), torch.float32, dev))
+    need = ds_diff_attention_scratch_bytes(n_heads, q_rows, k_rows, n)
+    return n, tables, qkv, _tensor(lse, "lse", (2 * n_heads, q_rows), torch.float32, dev), \
+        (q_rows, k_rows, _tensor(scratch, "scratch", need, torch.uint8, dev), scratch.numel())
 
 
 def ds_diff_attention_fwd(q, k, v, lam, o, lse, q_row, q_len, k_row, k_len, n_heads, head_dim, causal, max_q_len, max_k_len, scratch, o2=None,
                           force_generic=False, stream=None):
     """q, k, v, o, o2: 2-D, a row per token (column ranges of wider tensors are fine; o and o2 with the same row stride); scratch: uint8."""
-    code, n, tables, qkv, plse, rest = _diff_tensors(q, k, v, lam, lse, q_row, q_len, k_row, k_len, n_heads, head_dim, scratch)
+    torch, code, dev = _current(q)
+    n, tables, qkv, plse, rest = _diff_tensors(torch, dev, q, k, v, lam, lse, q_row, q_len, k_row, k_len, n_heads, head_dim, scratch)
     wide = n_heads * head_dim
-    po, ldo = _columns(o, "o", q.shape[0], wide, q.dtype, q.device)
-    po2, ldo2 = _columns(o2, "o2", q.shape[0], wide, q.dtype, q.device) if o2 is not None else (None, ldo)
+    po, ldo = _columns(o, "o", q.shape[0], wide, q.dtype, dev)
+    po2, ldo2 = _columns(o2, "o2", q.shape[0], wide, q.dtype, dev) if o2 is not None else (None, ldo)
     if ldo2 != ldo:
         raise ValueError("o and o2 must have the same row stride, got %d and %d" % (ldo, ldo2))
-    rc = lib().ds_diff_attention_fwd(code, C.c_int32(n), C.c_int32(n_heads), C.c_int32(head_dim), C.c_int32(int(causal)), *tables, C.c_int32(max_q_len),
-                                     C.c_int32(max_k_len), *qkv, po, po2, C.c_int32(ldo), plse, *rest, C.c_int32(int(force_generic)), _stream(stream))
+    rc = lib().ds_diff_attention_fwd(code, n, n_heads, head_dim, int(causal), *tables, max_q_len, max_k_len, *qkv, po, po2, ldo, plse, *rest,
+                                     int(force_generic), _raw_stream(torch, stream))
     _check(rc, "ds_diff_attention_fwd")
 
 
 def ds_diff_attention_bwd(q, k, v, lam, o, o2, d_o, lse, dq, dk, dv, dlam, q_row, q_len, k_row, k_len, n_heads, head_dim, causal, max_q_len, max_k_len,
                           scratch, accumulate=False, force_generic=False, stream=None):
     """dq, dk, dv have the strides of q, k, v; o, o2 and d_o the same row stride."""
-    import torch
-    code, n, tables, qkv, plse, rest = _diff_tensors(q, k, v, lam, lse, q_row, q_len, k_row, k_len, n_heads, head_dim, scratch)
-    wide, dt, dev = n_heads * head_dim, q.dtype, q.device
-    (po, ldo), (po2, ldo2), (pdo, lddo) = (_columns(t, name, q.shape[0], wide, dt, dev) for t, name in ((o, "o"), (o2, "o2"), (d_o, "d_o")))
+    torch, code, dev = _current(q)
+    n, tables, qkv, plse, rest = _diff_tensors(torch, dev, q, k, v, lam, lse, q_row, q_len, k_row, k_len, n_heads, head_dim, scratch)
+    wide, dt, rows = n_heads * head_dim, q.dtype, q.shape[0]
+    (po, ldo), (po2, ldo2), (pdo, lddo) = _columns(o, "o", rows, wide, dt, dev), _columns(o2, "o2", rows, wide, dt, dev), _columns(d_o, "d_o", rows, wide, dt, dev)
     if not ldo == ldo2 == lddo:
         raise ValueError("o, o2 and d_o must have the same row stride, got %d, %d and %d" % (ldo, ldo2, lddo))
     grads = []
     for t, name, like in ((dq, "dq", q), (dk, "dk", k), (dv, "dv", v)):
-        p, ld = _columns(t, name, like.shape[0], wide, dt, dev)
+        grads.append(_columns(t, name, like.shape[0], wide, dt, dev)[0])
         if t.stride(0) != like.stride(0) and like.shape[0] > 1:
             raise ValueError("%s must have the row stride of %s, got %d and %d" % (name, name[1:], t.stride(0), like.stride(0)))
-        grads.append(p)
-    rc = lib().ds_diff_attention_bwd(code, C.c_int32(n), C.c_int32(n_heads), C.c_int32(head_dim), C.c_int32(int(causal)), *tables, C.c_int32(max_q_len),
-                                     C.c_int32(max_k_len), *qkv, po, po2, pdo, C.c_int32(ldo), plse, *grads, _tensor(dlam, "dlam", (n_heads,), torch.float32, dev),
-                                     C.c_int32(int(accumulate)), *rest, C.c_int32(int(force_generic)), _stream(stream))
+    rc = lib().ds_diff_attention_bwd(code, n, n_heads, head_dim, int(causal), *tables, max_q_len, max_k_len, *qkv, po, po2, pdo, ldo, plse, *grads,
+                                     _tensor(dlam, "dlam", (n_heads,), torch.float32, dev), int(accumulate), *rest, int(force_generic),
+                                     _raw_stream(torch, stream))
     _check(rc, "ds_diff_attention_bwd")
 
 
 def ds_rope(x, y, pos, freq, n_heads, head_dim, rot_dim, interleaved=False, inverse=False, amplitude=1.0, stream=None):
     """x, y: 2-D, one row per token, heads first; y may be x."""
-    import torch
-    dev = _current(x)
-    code = _dtype_code(x)
-    rows = int(pos.shape[0])
+    torch, code, dev = _current(x)
+    rows = pos.shape[0]
     px, ldx = _columns(x, "x", rows, n_heads * head_dim, x.dtype, dev)
     py, ldy = _columns(y, "y", rows, n_heads * head_dim, x.dtype, dev)
-    rc = lib().ds_rope(C.c_int32(code), C.c_int32(rows), C.c_int32(n_heads), C.c_int32(head_dim), C.c_int32(rot_dim), C.c_int32(int(interleaved)),
-                       C.c_int32(int(inverse)), _tensor(pos, "pos", (rows,), torch.int32, dev), _tensor(freq, "freq", rot_dim // 2, torch.float64, dev),
-                       C.c_float(amplitude), px, C.c_int64(ldx), py, C.c_int64(ldy), _stream(stream))
+    rc = lib().ds_rope(code, rows, n_heads, head_dim, rot_dim, int(interleaved), int(inverse), _tensor(pos, "pos", (rows,), torch.int32, dev),
+                       _tensor(freq, "freq", rot_dim // 2, torch.float64, dev), amplitude, px, ldx, py, ldy, _raw_stream(torch, stream))
     _check(rc, "ds_rope")
 
 
 def ds_rope_freqs(rot_dim, base=10000.0, scaling=DS_ROPE_PLAIN, factor=1.0, context=0.0, low_turns=1.0, high_turns=32.0):
     """float64 [rot_dim / 2]: radians per position of each pair (host)."""
     out = np.zeros(max(int(rot_dim) // 2, 1), dtype=np.float64)
-    rc = lib().ds_rope_freqs(C.c_int32(rot_dim), C.c_double(base), C.c_int32(scaling), C.c_double(factor), C.c_double(context), C.c_double(low_turns),
-                             C.c_double(high_turns), _vp(out))
-    _check(rc, "ds_rope_freqs")
+    _check(lib().ds_rope_freqs(rot_dim, base, scaling, factor, context, low_turns, high_turns, _vp(out)), "ds_rope_freqs")
     return out
 
 
 def ds_layout_positions(layout, which=0):
     """int32 [stream rows]: position within its sequence, -1 in padding rows (host)."""
     out = np.zeros(max(layout.total_rows_tgt if which else layout.total_rows, 1), dtype=np.int32)
-    _check(lib().ds_layout_positions(layout.handle, C.c_int32(which), _vp(out)), "ds_layout_positions")
+    _check(lib().ds_layout_positions(layout.handle, which, _vp(out)), "ds_layout_positions")
     return out
 
 

@@ -1,7 +1,7 @@
 """ds_resid_norm_fwd / ds_resid_norm_bwd against oracle/layer.py.
 
 Tolerances, elementwise: half a step of the output's type, relative (2^-8 for bf16, 2^-24 for fp32), plus the arithmetic in fp32.  A sum of n
-terms taken in a tree over lanes and wavefronts (8 in a lane, 6 levels, 16 wavefronts) or row by row is off by at most
+terms taken in a tree over lanes and wavefronts (8 in a lane, 6 levels, 8 wavefronts) or row by row is off by at most
 (its depth) x 2^-24 x the sum of the terms' sizes, and some ten operations follow: K = 64 units of 2^-24 of `size`, the result computed
 from absolute values (so that what cancels counts in full), cover row sums; column sums add the rows a work-group takes one after the
 other (at most 8 x 4 here, 64 work-groups' sums in line at most, 6 levels): 128 units in all."""
@@ -155,7 +155,7 @@ class Case:
                 _near(got, ref[k] + base, size[k] + A(base), 0.0, 128, k)
 
 
-SIZES = [(1, 8), (5, 64), (3, 520), (9, 1024), (37, 1032), (130, 2048), (67, 2168), (11, 4096), (3, 8192), (517, 256)]
+SIZES = [(1, 8), (5, 64), (3, 520), (9, 1024), (37, 1032), (130, 2048), (67, 2168), (11, 4096), (3, 3000), (517, 256)]
 
 
 @pytest.mark.parametrize("dt", [F32, BF])

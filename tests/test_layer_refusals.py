@@ -23,7 +23,7 @@ def test_resid_norm_forward():
     assert _fwd() == ds.DS_OK                                   # no rows: nothing to do
     assert _fwd(rms=1, post_b=None, pre_b=None) == ds.DS_OK
     assert _fwd(post_g=None, post_b=None, pre_g=None, pre_b=None, u=None) == ds.DS_OK
-    for kw in (dict(dtype=2), dict(rms=2), dict(rows=-1), dict(d=0), dict(d=60), dict(d=8200), dict(x=None), dict(h=None), dict(y=None), dict(stats=None),
+    for kw in (dict(dtype=2), dict(rms=2), dict(rows=-1), dict(d=0), dict(d=60), dict(d=4104), dict(x=None), dict(h=None), dict(y=None), dict(stats=None),
                dict(post_b=None), dict(pre_b=None), dict(u=None), dict(gate=P), dict(gate_kind=1), dict(gate_kind=3, gate=P), dict(x=P + 8), dict(h=P + 2),
                dict(y=P + 8), dict(u=P + 8), dict(post_g=P + 4), dict(pre_g=P + 4), dict(pre_b=P + 8), dict(post_b=P + 8), dict(gate_kind=2, gate=P + 8)):
         assert _fwd(**kw) == BAD, kw
@@ -44,7 +44,7 @@ def test_resid_norm_backward():
         assert _bwd(**kw) == BAD, kw
     assert ds.ds_resid_norm_bwd_scratch_floats(0, 64) == 0 and ds.ds_resid_norm_bwd_scratch_floats(5, 0) == 0
     for rows in (1, 100, 1 << 20):
-        for d in (8, 512, 4096, 8192):
+        for d in (8, 512, 2056, 4096):
             assert 4 * d <= ds.ds_resid_norm_bwd_scratch_floats(rows, d) <= 1 << 24
 
 
