@@ -592,8 +592,9 @@ def _current(t):
     return torch, code, device
 
 
-def _raw_stream(torch, stream):
-    return torch.cuda.current_stream().cuda_stream if stream is None else stream
+def _raw_stream(torch, stream, device):
+    """The stream given or torch's current one (without the Stream object that torch.cuda.current_stream makes: 0.1 instead of 2.9 us)."""
+    return torch._C._cuda_getCurrentRawStream(device) if stream is None else stream
 
 
 def _gate(gate, rows, d):
@@ -614,7 +615,7 @@ def ds_resid_norm_fwd(x, h, y, stats, post_g=None, post_b=None, gate=None, pre_g
                                  _tensor(row_valid, "row_valid", (rows,), torch.int32, dev), _tensor(post_g, "post_g", col, dt, dev),
                                  _tensor(post_b, "post_b", col, dt, dev), kind, _tensor(gate, "gate", gate_shape, dt, dev), resid_scale, branch_scale,
                                  _tensor(pre_g, "pre_g", col, dt, dev), _tensor(pre_b, "pre_b", col, dt, dev), _tensor(y, "y", full, dt, dev),
-                                 _tensor(u, "u", full, dt, dev), _tensor(stats, "stats", (4, rows), torch.float32, dev), _raw_stream(torch, stream))
+                                 _tensor(u, "u", full, dt, dev), _tensor(stats, "stats", (4, rows), torch.float32, dev), _raw_stream(torch, stream, dev))
     _check(rc, "ds_resid_norm_fwd")
 
 
@@ -638,7 +639,7 @@ def ds_resid_norm_bwd(dy, y, h, stats, dx, dh, partial, du=None, post_g=None, po
                                  _tensor(dgate, "dgate", gate_shape, dt if kind == DS_GATE_ROW else f32, dev) if kind != DS_GATE_NONE else None,
                                  _tensor(dpost_g, "dpost_g", col, f32, dev), _tensor(dpost_b, "dpost_b", col, f32, dev),
                                  _tensor(dpre_g, "dpre_g", col, f32, dev), _tensor(dpre_b, "dpre_b", col, f32, dev),
-                                 _tensor(partial, "partial", ds_resid_norm_bwd_scratch_floats(rows, d), f32, dev), int(accumulate), _raw_stream(torch, stream))
+                                 _tensor(partial, "partial", ds_resid_norm_bwd_scratch_floats(rows, d), f32, dev), int(accumulate), _raw_stream(torch, stream, dev))
     _check(rc, "ds_resid_norm_bwd")
 
 
@@ -671,7 +672,7 @@ def ds_diff_attention_fwd(q, k, v, lam, o, lse, q_row, q_len, k_row, k_len, n_he
     if ldo2 != ldo:
         raise ValueError("o and o2 must have the same row stride, got %d and %d" % (ldo, ldo2))
     rc = lib().ds_diff_attention_fwd(code, n, n_heads, head_dim, int(causal), *tables, max_q_len, max_k_len, *qkv, po, po2, ldo, plse, *rest,
-                                     int(force_generic), _raw_stream(torch, stream))
+                                     int(force_generic), _raw_stream(torch, stream, dev))
     _check(rc, "ds_diff_attention_fwd")
 
 
@@ -691,7 +692,7 @@ def ds_diff_attention_bwd(q, k, v, lam, o, o2, d_o, lse, dq, dk, dv, dlam, q_row
             raise ValueError("%s must have the row stride of %s, got %d and %d" % (name, name[1:], t.stride(0), like.stride(0)))
     rc = lib().ds_diff_attention_bwd(code, n, n_heads, head_dim, int(causal), *tables, max_q_len, max_k_len, *qkv, po, po2, pdo, ldo, plse, *grads,
                                      _tensor(dlam, "dlam", (n_heads,), torch.float32, dev), int(accumulate), *rest, int(force_generic),
-                                     _raw_stream(torch, stream))
+                                     _raw_stream(torch, stream, dev))
     _check(rc, "ds_diff_attention_bwd")
 
 
@@ -702,7 +703,7 @@ def ds_rope(x, y, pos, freq, n_heads, head_dim, rot_dim, interleaved=False, inve
     px, ldx = _columns(x, "x", rows, n_heads * head_dim, x.dtype, dev)
     py, ldy = _columns(y, "y", rows, n_heads * head_dim, x.dtype, dev)
     rc = lib().ds_rope(code, rows, n_heads, head_dim, rot_dim, int(interleaved), int(inverse), _tensor(pos, "pos", (rows,), torch.int32, dev),
-                       _tensor(freq, "freq", rot_dim // 2, torch.float64, dev), amplitude, px, ldx, py, ldy, _raw_stream(torch, stream))
+                       _tensor(freq, "freq", rot_dim // 2, torch.float64, dev), amplitude, px, ldx, py, ldy, _raw_stream(torch, stream, dev))
     _check(rc, "ds_rope")
 
 
