@@ -8,10 +8,11 @@ namespace {
 
 // ------------------------------------------------------------------------------------ backward: dQ (and the statistics, the parts of dlambda)
 // For the dK/dV kernel a query leaves one entry of eight bf16 values, the {hi, lo} splits of lse_1 / scale, lse_2 / scale, D_1 and D_2 - D_1.
-template <int HD, bool CAUSAL>
+template <int HD, bool CAUSAL, int KS>
 __global__ __launch_bounds__(256, 2) void diff_bwd_dq_mfma_kernel(DiffAttnArgs a) {
     extern __shared__ __attribute__((aligned(16))) char smem[];
     constexpr int TILE = 64 * HD * 2, NS = HD / 16, ND = HD / 32, AHEAD = 2;
+    constexpr int RING = KeySplit<KS>::RING;
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 31, g = lane >> 5;
@@ -27,7 +28,9 @@ __global__ __launch_bounds__(256, 2) void diff_bwd_dq_mfma_kernel(DiffAttnArgs a
     const bf16_t* O2 = (const bf16_t*)a.o2 + qrow0 * a.ldo + h * HD;
     const bf16_t* K = (const bf16_t*)a.k + (long long)a.k_row[s] * a.ldk + h * HD;
     const bf16_t* V = (const bf16_t*)a.v + (long long)a.k_row[s] * a.ldv + h * HD;
-    const int qw0 = q0 + wave * 32;
+    KeySplit<KS> ks;
+    ks.init(wave);
+    const int qw0 = q0 + ks.group * 32;
     const int qi = qw0 + col;
     const int qi_c = qi < ql ? qi : ql - 1;
 
@@ -35,31 +38,38 @@ __global__ __launch_bounds__(256, 2) void diff_bwd_dq_mfma_kernel(DiffAttnArgs a
     PieceLoader<HD> ldK, ldV;
     ldK.setup(K, a.ldk, kl, wave, lane);
     ldV.setup(V, a.ldv, kl, wave, lane);
-    if (kl > 0) {
-        ldK.issue(lds0, 0);
-        ldV.issue(lds0 + TILE, 0);
-    }
+    const int kv_end = CAUSAL ? min(kl, q0 + 128) : kl;
+    const int wave_last = CAUSAL ? min(kl - 1, qw0 + 31) : kl - 1;
+    const int nb = (kv_end + 63) / 64;
+    auto fetch = [&](int b) {                           // (of a block past the last one every row is past the end)
+        const uint32_t n = lds0 + (b % RING) * (2 * TILE);
+        ldK.issue(n, b * 64);
+        ldV.issue(n + TILE, b * 64);
+    };
+    if (nb > 0)
+#pragma unroll
+        for (int b = 0; b < RING - 1; ++b) fetch(b);
 
     const float lam = a.lambda[h];
     bf16x8_t qf[NS], dof[NS];
     float d1 = 0.f, d2 = 0.f;
 #pragma unroll
-    for (int ks = 0; ks < NS; ++ks) {
-        qf[ks] = *reinterpret_cast<const bf16x8_t*>(Q + (long long)qi_c * a.ldq + ks * 16 + g * 8);
-        dof[ks] = *reinterpret_cast<const bf16x8_t*>(dO + (long long)qi_c * a.ldo + ks * 16 + g * 8);
-        const bf16x8_t of = *reinterpret_cast<const bf16x8_t*>(O + (long long)qi_c * a.ldo + ks * 16 + g * 8);
-        const bf16x8_t of2 = *reinterpret_cast<const bf16x8_t*>(O2 + (long long)qi_c * a.ldo + ks * 16 + g * 8);
+    for (int i = 0; i < NS; ++i) {
+        qf[i] = *reinterpret_cast<const bf16x8_t*>(Q + (long long)qi_c * a.ldq + i * 16 + g * 8);
+        dof[i] = *reinterpret_cast<const bf16x8_t*>(dO + (long long)qi_c * a.ldo + i * 16 + g * 8);
+        const bf16x8_t of = *reinterpret_cast<const bf16x8_t*>(O + (long long)qi_c * a.ldo + i * 16 + g * 8);
+        const bf16x8_t of2 = *reinterpret_cast<const bf16x8_t*>(O2 + (long long)qi_c * a.ldo + i * 16 + g * 8);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            d1 = __builtin_fmaf((float)of[j], (float)dof[ks][j], d1);
-            d2 = __builtin_fmaf((float)of2[j], (float)dof[ks][j], d2);
+            d1 = __builtin_fmaf((float)of[j], (float)dof[i][j], d1);
+            d2 = __builtin_fmaf((float)of2[j], (float)dof[i][j], d2);
         }
     }
     d2 += __shfl_xor(d2, 32, 64);
     d1 += __shfl_xor(d1, 32, 64);
     d1 += lam * d2;
     const float lse1 = a.lse[(size_t)(2 * h) * a.lse_stride + qrow0 + qi_c], lse2 = a.lse[(size_t)(2 * h + 1) * a.lse_stride + qrow0 + qi_c];
-    if (g == 0 && qi < ql)
+    if (g == 0 && qi < ql && ks.split == 0)
         reinterpret_cast<uint4*>(a.aug)[(size_t)h * a.q_total_rows + qrow0 + qi] =
             make_uint4(split_hi_lo(lse1 * (1.0f / a.scale)), split_hi_lo(lse2 * (1.0f / a.scale)), split_hi_lo(d1), split_hi_lo(d2 - d1));
     const float e1 = lse1 * kLog2e, e2 = lse2 * kLog2e;
@@ -75,41 +85,34 @@ __global__ __launch_bounds__(256, 2) void diff_bwd_dq_mfma_kernel(DiffAttnArgs a
         for (int e = 0; e < 16; ++e) gacc[dt][e] = 0.f;
     float lam_sum = 0.f;
 
-    const int kv_end = CAUSAL ? min(kl, q0 + 128) : kl;
-    const int wave_last = CAUSAL ? min(kl - 1, qw0 + 31) : kl - 1;
-    const int nb = (kv_end + 63) / 64;
     for (int b = 0; b < nb; ++b) {
         const int kv0 = b * 64;
-        const char* sK = smem + (b & 1) * (2 * TILE);
-        wait_tiles_and_sync();
-        if (b + 1 < nb) {
-            const uint32_t n = lds0 + ((b + 1) & 1) * (2 * TILE);
-            ldK.issue(n, kv0 + 64);
-            ldV.issue(n + TILE, kv0 + 64);
-        }
+        const char* sK = smem + (b % RING) * (2 * TILE);
+        ring_wait<RING, 2 * (HD / 32)>();               // block b has landed; the stage of the block before is free
+        if (RING > 2 || b + 1 < nb) fetch(b + RING - 1);
         if (kv0 > wave_last || qw0 >= ql) continue;
         const bool need_mask = (kv0 + 64 > kl) || (CAUSAL && kv0 + 63 > qw0);
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt) {
-            if (kv0 + kt * 32 > wave_last) continue;                    // the half beyond the last key this wavefront sees
+            if (kv0 + kt * 32 > wave_last || !ks.mine(2 * b + kt)) continue;      // the half beyond the last key this wavefront sees
             f32x16_t p1, p2, gr;
 #pragma unroll
             for (int e = 0; e < 16; ++e) { p1[e] = 0.f; p2[e] = 0.f; gr[e] = 0.f; }
             const char* tK = sK + kt * (32 * HD * 2);
             bf16x8_t fk[NS], fv[NS];
-            auto read_kv = [&](int ks) {
-                fk[ks] = at.row(tK, ks);
-                fv[ks] = at.row(tK + TILE, ks);
+            auto read_kv = [&](int i) {
+                fk[i] = at.row(tK, i);
+                fv[i] = at.row(tK + TILE, i);
             };
 #pragma unroll
-            for (int ks = 0; ks < AHEAD; ++ks) read_kv(ks);
+            for (int i = 0; i < AHEAD; ++i) read_kv(i);
 #pragma unroll
-            for (int ks = 0; ks < NS; ++ks) {
-                if (ks + AHEAD < NS) read_kv(ks + AHEAD);
+            for (int i = 0; i < NS; ++i) {
+                if (i + AHEAD < NS) read_kv(i + AHEAD);
                 __builtin_amdgcn_sched_barrier(kFence);
-                if (ks < NS / 2) p1 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fk[ks], qf[ks], p1, 0, 0, 0);
-                else p2 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fk[ks], qf[ks], p2, 0, 0, 0);
-                gr = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fv[ks], dof[ks], gr, 0, 0, 0);
+                if (i < NS / 2) p1 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fk[i], qf[i], p1, 0, 0, 0);
+                else p2 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fk[i], qf[i], p2, 0, 0, 0);
+                gr = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fv[i], dof[i], gr, 0, 0, 0);
                 __builtin_amdgcn_sched_barrier(kFence);
             }
 #pragma unroll
@@ -141,6 +144,21 @@ __global__ __launch_bounds__(256, 2) void diff_bwd_dq_mfma_kernel(DiffAttnArgs a
                 }
             }
         }
+    }
+    if constexpr (KS > 1) {
+        __builtin_amdgcn_s_waitcnt(0x0F70);             // no transfer may still be writing LDS
+        join_splits<KS, ND * 16 + 1>(smem, ks, lane,
+            [&](float* p) {
+                p[0] = lam_sum;
+#pragma unroll
+                for (int i = 0; i < ND * 16; ++i) p[(1 + i) * 64] = gacc[i / 16][i % 16];
+            },
+            [&](const float* p) {
+                lam_sum += p[0];
+#pragma unroll
+                for (int i = 0; i < ND * 16; ++i) gacc[i / 16][i % 16] += p[(1 + i) * 64];
+            });
+        if (ks.split != 0) return;
     }
     lam_sum = wave_sum(qi < ql ? lam_sum : 0.f);
     if (lane == 0 && qw0 < ql) a.lam_part[(size_t)h * a.q_total_rows + qrow0 + qw0] = lam_sum;
@@ -370,12 +388,12 @@ __global__ __launch_bounds__(256, HD == 64 ? 2 : 1) void diff_bwd_dkv_mfma_kerne
     if (PS) draw.finish();
 }
 
-template <int HD, bool CAUSAL>
+template <int HD, bool CAUSAL, int KS>
 ds_status bwd_launch(const DiffAttnArgs& a, hipStream_t st) {
     static bool attr_q = false, attr_kv = false;
-    auto kq = diff_bwd_dq_mfma_kernel<HD, CAUSAL>;
+    auto kq = diff_bwd_dq_mfma_kernel<HD, CAUSAL, KS>;
     auto kkv = diff_bwd_dkv_mfma_kernel<HD, CAUSAL>;
-    const int smem_q = 4 * (64 * HD * 2);
+    const int smem_q = KeySplit<KS>::RING * 2 * (64 * HD * 2);
     const int smem_kv = 4 * (2 * (64 * HD * 2) + 1024) + 64 + 64 * HD;      // stages, draws, zeros
     ds_status r = set_smem(kq, smem_q, attr_q);
     if (r != DS_OK) return r;
@@ -395,6 +413,5 @@ ds_status diff_bwd_mfma(const DiffAttnArgs& a0, hipStream_t st) {
     DiffAttnArgs a = a0;
     const ds_status r = attn_prepare_lists(a, true, st);
     if (r != DS_OK) return r;
-    if (a.head_dim == 128) return a.mask ? bwd_launch<128, true>(a, st) : bwd_launch<128, false>(a, st);
-    return a.mask ? bwd_launch<64, true>(a, st) : bwd_launch<64, false>(a, st);
+    return diff_by_kind(a, [&](auto hd, auto causal, auto split) { return bwd_launch<decltype(hd)::value, decltype(causal)::value, decltype(split)::value>(a, st); });
 }

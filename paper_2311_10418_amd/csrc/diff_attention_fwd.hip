@@ -16,14 +16,16 @@
 namespace {
 
 constexpr float kSlack = 8.0f;                          // see diff_fwd_mfma_kernel
+constexpr float kLowest = -1e30f;                       // a maximum of nothing: finite, so that a step in which a query sees no key adds nothing
 
 // ------------------------------------------------------------------------------------ forward
 // A tile of 64 keys goes in two steps of 32, so that both maps' scores (32 registers) and both accumulators (128 at head size 128) leave room
 // for two wavefronts per SIMD, whose vector work and matrix instructions then overlap.
-template <int HD, bool CAUSAL>
-__global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void diff_fwd_mfma_kernel(DiffAttnArgs a) {
+template <int HD, bool CAUSAL, int KS>
+__global__ __launch_bounds__(256, HD == 64 && KS == 1 ? 3 : 2) void diff_fwd_mfma_kernel(DiffAttnArgs a) {
     extern __shared__ __attribute__((aligned(16))) char smem[];
     constexpr int TILE = 64 * HD * 2, NS = HD / 16, ND = HD / 32, AHEAD = 2, AHEAD_V = 1;
+    constexpr int RING = KeySplit<KS>::RING;
     const uint32_t lds0 = lds_address(smem);
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -37,13 +39,15 @@ __global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void diff_fwd_mfma_kernel(Di
     const bf16_t* Q = (const bf16_t*)a.q + qrow0 * a.ldq + h * HD;
     const bf16_t* K = (const bf16_t*)a.k + (long long)a.k_row[s] * a.ldk + h * HD;
     const bf16_t* V = (const bf16_t*)a.v + (long long)a.k_row[s] * a.ldv + h * HD;
-    const int qw0 = q0 + wave * 32;
+    KeySplit<KS> ks;
+    ks.init(wave);
+    const int qw0 = q0 + ks.group * 32;
     const int qi = qw0 + col;
     const int qi_c = qi < ql ? qi : ql - 1;
 
     bf16x8_t qf[NS];
 #pragma unroll
-    for (int ks = 0; ks < NS; ++ks) qf[ks] = *reinterpret_cast<const bf16x8_t*>(Q + (long long)qi_c * a.ldq + ks * 16 + g * 8);
+    for (int i = 0; i < NS; ++i) qf[i] = *reinterpret_cast<const bf16x8_t*>(Q + (long long)qi_c * a.ldq + i * 16 + g * 8);
 
     PieceLoader<HD> ldK, ldV;
     ldK.setup(K, a.ldk, kl, wave, lane);
@@ -58,16 +62,20 @@ __global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void diff_fwd_mfma_kernel(Di
         for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
             for (int e = 0; e < 16; ++e) o[m][dt][e] = 0.f;
-    float top[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};          // running maxima (in the exp2 domain) and sums
+    float top[2] = {kLowest, kLowest}, l[2] = {0.f, 0.f};              // running maxima (in the exp2 domain) and sums
     const float c = a.scale * kLog2e;
 
     const int kv_end = CAUSAL ? min(kl, q0 + 128) : kl;
     const int wave_last = CAUSAL ? min(kl - 1, qw0 + 31) : kl - 1;     // last key this wavefront can see
     const int nb = (kv_end + 63) / 64;
-    if (nb > 0) {                                       // (a sequence without keys: zero output, nothing to fetch)
-        ldK.issue(lds0, 0);
-        ldV.issue(lds0 + TILE, 0);
-    }
+    auto fetch = [&](int b) {                           // (of a block past the last one every row is past the end)
+        const uint32_t n = lds0 + (b % RING) * (2 * TILE);
+        ldK.issue(n, b * 64);
+        ldV.issue(n + TILE, b * 64);
+    };
+    if (nb > 0)                                         // (a sequence without keys: zero output, nothing to fetch)
+#pragma unroll
+        for (int b = 0; b < RING - 1; ++b) fetch(b);
     // scores -> probabilities of map m in place.  The running maximum is raised, and what was summed so far rescaled, only where a score exceeds it
     // by more than kSlack: probabilities are then at most 2^kSlack times what they are relative to the true maximum, which costs no digits, and a
     // lane needs nothing of the lane that holds the other half of its column.
@@ -94,17 +102,13 @@ __global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void diff_fwd_mfma_kernel(Di
     };
     for (int b = 0; b < nb; ++b) {
         const int kv0 = b * 64;
-        const char* sK = smem + (b & 1) * (2 * TILE);
-        wait_tiles_and_sync();                          // block b has landed; the other stage is free
-        if (b + 1 < nb) {
-            const uint32_t n = lds0 + ((b + 1) & 1) * (2 * TILE);
-            ldK.issue(n, kv0 + 64);
-            ldV.issue(n + TILE, kv0 + 64);
-        }
+        const char* sK = smem + (b % RING) * (2 * TILE);
+        ring_wait<RING, 2 * (HD / 32)>();               // block b has landed; the stage of the block before is free
+        if (RING > 2 || b + 1 < nb) fetch(b + RING - 1);
         if (kv0 > wave_last || qw0 >= ql) continue;
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt) {
-            if (kv0 + kt * 32 > wave_last) continue;    // the half beyond the last key this wavefront sees
+            if (kv0 + kt * 32 > wave_last || !ks.mine(2 * b + kt)) continue;      // the half beyond the last key this wavefront sees
             const char* tK = sK + kt * (32 * HD * 2);
             const char* tV = tK + TILE;
             f32x16_t p[2];
@@ -148,6 +152,32 @@ __global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void diff_fwd_mfma_kernel(Di
             }
         }
     }
+    if constexpr (KS > 1) {
+        __builtin_amdgcn_s_waitcnt(0x0F70);             // no transfer may still be writing LDS
+        constexpr int N = 2 * ND * 16 + 4;
+        join_splits<KS, N>(smem, ks, lane,
+            [&](float* p) {
+#pragma unroll
+                for (int m = 0; m < 2; ++m) {
+                    p[(2 * m) * 64] = top[m];
+                    p[(2 * m + 1) * 64] = l[m];
+#pragma unroll
+                    for (int i = 0; i < ND * 16; ++i) p[(4 + m * ND * 16 + i) * 64] = o[m][i / 16][i % 16];
+                }
+            },
+            [&](const float* p) {
+#pragma unroll
+                for (int m = 0; m < 2; ++m) {
+                    const float other = p[(2 * m) * 64], up = fmaxf(top[m], other);
+                    const float mine = __builtin_amdgcn_exp2f(top[m] - up), theirs = __builtin_amdgcn_exp2f(other - up);
+                    l[m] = l[m] * mine + p[(2 * m + 1) * 64] * theirs;
+                    top[m] = up;
+#pragma unroll
+                    for (int i = 0; i < ND * 16; ++i) o[m][i / 16][i % 16] = o[m][i / 16][i % 16] * mine + p[(4 + m * ND * 16 + i) * 64] * theirs;
+                }
+            });
+        if (ks.split != 0) return;
+    }
 #pragma unroll
     for (int m = 0; m < 2; ++m) l[m] += __shfl_xor(l[m], 32, 64);
     if (qw0 >= ql) return;
@@ -168,11 +198,11 @@ __global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void diff_fwd_mfma_kernel(Di
     }
 }
 
-template <int HD, bool CAUSAL>
+template <int HD, bool CAUSAL, int KS>
 ds_status fwd_launch(const DiffAttnArgs& a, hipStream_t st) {
     static bool attr = false;
-    auto kern = diff_fwd_mfma_kernel<HD, CAUSAL>;
-    const int smem = 4 * (64 * HD * 2);
+    auto kern = diff_fwd_mfma_kernel<HD, CAUSAL, KS>;
+    const int smem = KeySplit<KS>::RING * 2 * (64 * HD * 2);
     const ds_status r = set_smem(kern, smem, attr);
     if (r != DS_OK) return r;
     hipLaunchKernelGGL(kern, dim3((unsigned)a.max_items_q * a.n_heads), dim3(256), smem, st, a);
@@ -198,6 +228,5 @@ ds_status diff_fwd_mfma(const DiffAttnArgs& a0, hipStream_t st) {
     DiffAttnArgs a = a0;
     const ds_status r = attn_prepare_lists(a, false, st);
     if (r != DS_OK) return r;
-    if (a.head_dim == 128) return a.mask ? fwd_launch<128, true>(a, st) : fwd_launch<128, false>(a, st);
-    return a.mask ? fwd_launch<64, true>(a, st) : fwd_launch<64, false>(a, st);
+    return diff_by_kind(a, [&](auto hd, auto causal, auto split) { return fwd_launch<decltype(hd)::value, decltype(causal)::value, decltype(split)::value>(a, st); });
 }

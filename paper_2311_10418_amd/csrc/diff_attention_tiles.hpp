@@ -2,6 +2,7 @@
 #pragma once
 #include "attention_tiles.hpp"
 #include "diff_attention.hpp"
+#include <type_traits>
 
 namespace {
 
@@ -60,6 +61,39 @@ template <int HD> struct FragOffsets {
     }
 };
 
+// Short queries (at most 64 or 32 in every sequence): a work-group's four wavefronts hold two or one blocks of 32 queries, and KS = 2 or 4 of them
+// share one, each taking every KS-th step of 32 keys; what they have is joined through LDS in the end.  Tiles then come in a ring of four, three
+// blocks of keys in flight: with few queries nothing else hides the transfers.
+template <int KS> struct KeySplit {
+    static constexpr int RING = KS > 1 ? 4 : 2, GROUPS = 4 / KS;       // stages; blocks of 32 queries
+    int split, group;
+    __device__ __forceinline__ void init(int wave) {
+        group = wave % GROUPS;
+        split = wave / GROUPS;
+    }
+    __device__ __forceinline__ bool mine(int step) const { return KS == 1 || step % KS == split; }
+};
+// Waits until block b of a ring has landed for everybody, `transfers` per wavefront and block; the stage before is free then.
+template <int RING, int TRANSFERS> __device__ __forceinline__ void ring_wait() {
+    if constexpr (RING == 2) __builtin_amdgcn_s_waitcnt(0x0F70);
+    else __builtin_amdgcn_s_waitcnt(vmcnt_imm((RING - 2) * TRANSFERS));
+    __builtin_amdgcn_s_barrier();
+}
+// The wavefronts of splits KS / 2 .. write N registers per lane each, those of the lower half read and `join` them, then a quarter and so on.
+// lds: two wavefronts write at a time at most: 2 x N x 256 bytes.  Every wavefront of the work-group calls it.
+template <int KS, int N, class Put, class Join>
+__device__ __forceinline__ void join_splits(char* lds, const KeySplit<KS>& ks, int lane, Put put, Join join) {
+    constexpr int GROUPS = 4 / KS;
+#pragma unroll
+    for (int half = KS / 2; half >= 1; half /= 2) {
+        __syncthreads();                                // what the memory held before has been read
+        float* p = reinterpret_cast<float*>(lds) + (size_t)((ks.split % half) * GROUPS + ks.group) * N * 64 + lane;
+        if (ks.split >= half && ks.split < 2 * half) put(p);
+        __syncthreads();
+        if (ks.split < half) join(p);
+    }
+}
+
 // Stores a transposed [HD x 32] accumulator block times mul (first half of the features) or mul2 (second half): lane column = row `row` of the output.  A lane holds 4 of every 8 features, the lane 32
 // further on the other 4: they swap, so that each has 8 of every 16 and the stores are 16 bytes wide.  Every lane of the wavefront takes part;
 // `on` says whether this lane's row is stored.
@@ -81,6 +115,17 @@ __device__ __forceinline__ void store_cols16(const f32x16_t (&acc)[HD / 32], flo
             const auto b = __builtin_amdgcn_permlane32_swap(x[0][1], x[1][1], false, false);
             if (on) *reinterpret_cast<uint4*>(row + dt * 32 + q * 16 + g * 8) = make_uint4(a[0], b[0], a[1], b[1]);
         }
+}
+
+// f(head size, causal, wavefronts that share a block of queries) with the template arguments of a call
+template <class F> ds_status diff_by_kind(const DiffAttnArgs& a, F f) {
+    auto by_split = [&](auto hd, auto causal) {
+        if (a.max_q_len <= 32) return f(hd, causal, std::integral_constant<int, 4>{});
+        if (a.max_q_len <= 64) return f(hd, causal, std::integral_constant<int, 2>{});
+        return f(hd, causal, std::integral_constant<int, 1>{});
+    };
+    auto by_mask = [&](auto hd) { return a.mask ? by_split(hd, std::true_type{}) : by_split(hd, std::false_type{}); };
+    return a.head_dim == 128 ? by_mask(std::integral_constant<int, 128>{}) : by_mask(std::integral_constant<int, 64>{});
 }
 
 }  // namespace

@@ -148,6 +148,16 @@ def test_other_sequences_and_none(dt, generic, causal, hd):
 
 
 @pytest.mark.parametrize("dt,generic", KINDS)
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("hd", [64, 128])
+def test_short_queries(dt, generic, causal, hd):
+    """At most 32 or 64 queries (a work-group then shares the keys out): fewer steps of 32 keys than wavefronts, many, one key, no query or none."""
+    for q in ([1, 32, 0, 17, 5, 31, 9], [64, 33, 0, 1, 40, 64, 63]):
+        Case(hd + q[0], dt, 2, hd, q, [700, 1, 40, 0, 97, 64, 129], causal).run(generic)
+        Case(hd + q[0], dt, 8, hd, q[:1], [33], causal).run(generic)
+
+
+@pytest.mark.parametrize("dt,generic", KINDS)
 @pytest.mark.parametrize("hd,pad", [(64, 8), (64, 4), (64, 1), (128, 3), (128, 64), (16, 2)])
 def test_columns_of_wider_tensors(dt, generic, hd, pad):
     """Row strides and first columns that allow accesses of 16, 8, or only 2 or 4 bytes."""
