@@ -2,11 +2,11 @@
 #include "diff_attention.hpp"
 #include <cmath>
 
-// Scratch: the work lists of the matrix-core kernels, then four arrays of [n_heads][q_total_rows] entries of 16 bytes that the dQ kernels
-// hand to the dK/dV kernels (the general ones use two of them as arrays of floats), then the parts of dlambda, one float each.
+// Scratch: the work lists of the matrix-core kernels, then what the dQ kernels hand to the dK/dV kernels, 16 bytes for each query of a head
+// (the general ones use 8 of them, as two arrays of floats), then the parts of dlambda, one float each.
 static size_t lists_size(int q_total_rows, int k_total_rows, int n_seq) { return attn_scratch_bytes(0, 0, q_total_rows, k_total_rows, n_seq); }
 size_t diff_scratch_bytes(int n_heads, int q_total_rows, int k_total_rows, int n_seq) {
-    return lists_size(q_total_rows, k_total_rows, n_seq) + (size_t)n_heads * q_total_rows * (4 * 16 + 4);
+    return lists_size(q_total_rows, k_total_rows, n_seq) + (size_t)n_heads * q_total_rows * (16 + 4);
 }
 
 static bool four_at_once(const void* p, size_t size) { return !p || (uintptr_t)p % (4 * size) == 0; }
@@ -33,7 +33,7 @@ static ds_status check(DiffAttnArgs& a) {
     a.aug = after_lists;
     a.d1 = (float*)after_lists;
     a.d2 = a.d1 + entries;
-    a.lam_part = (float*)(after_lists + entries * 4 * 16);
+    a.lam_part = (float*)(after_lists + entries * 16);
     return DS_OK;
 }
 

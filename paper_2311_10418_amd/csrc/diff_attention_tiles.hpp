@@ -6,12 +6,6 @@
 
 namespace {
 
-// One direct transfer of 64 x 4 bytes (see lds_dma16_at): lane i's dword lands at lds_addr + 4 i.
-__device__ __forceinline__ void lds_dma4(const void* gptr, uint32_t lds_addr) {
-    const uint32_t m0v = __builtin_amdgcn_readfirstlane(lds_addr);
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" : : "v"(gptr), "s"(m0v) : "memory", "m0");
-}
-
 // Transfers of 64-row tiles, 1 KB (4 rows of 128 columns or 8 of 64) at a time, HD / 32 per wavefront and tile, through a raw buffer that ends
 // at the last valid row: rows past it arrive as zeros.  The swizzled chunk of a lane in transfer i is that of transfer 0 with i
 // (HD = 128) or 2 i flipped in, so that one register per tensor and one for the chunk make every offset.
@@ -61,9 +55,9 @@ template <int HD> struct FragOffsets {
     }
 };
 
-// Short queries (at most 64 or 32 in every sequence): a work-group's four wavefronts hold two or one blocks of 32 queries, and KS = 2 or 4 of them
-// share one, each taking every KS-th step of 32 keys; what they have is joined through LDS in the end.  Tiles then come in a ring of four, three
-// blocks of keys in flight: with few queries nothing else hides the transfers.
+// Short queries (at most 64 or 32 in every sequence) of few sequences and heads: a work-group's four wavefronts hold two or one blocks of 32
+// queries, and KS = 2 or 4 of them share one, each taking every KS-th step of 32 keys; what they have is joined through LDS in the end.  Tiles then
+// come in a ring of four, three blocks of keys in flight: with few queries nothing else hides the transfers.  diff_by_kind has the rule.
 template <int KS> struct KeySplit {
     static constexpr int RING = KS > 1 ? 4 : 2, GROUPS = 4 / KS;       // stages; blocks of 32 queries
     int split, group;
@@ -118,8 +112,16 @@ __device__ __forceinline__ void store_cols16(const f32x16_t (&acc)[HD / 32], flo
 }
 
 // f(head size, causal, wavefronts that share a block of queries) with the template arguments of a call
+//
+// Sharing (KeySplit) pays where there is about one work-group for a compute unit or less, and costs where others would hide the transfers anyway:
+// its ring takes twice the LDS.  One wavefront to a block of queries -> sharing, forward, 16 heads of 64 / of 128, us a call:
+//     1 sequence,   1 query,   4096 keys:  79 ->  55 / 108 ->  83      16 sequences, 33 queries, 1019 keys:  28 -> 26 / 37 -> 37
+//     4 sequences,  1 query,   2048 keys:  44 ->  36 /  59 ->  50      16 sequences, 20 queries, 1019 keys:  26 -> 26 / 35 -> 38
+//    64 sequences, 33 queries,  500 keys:  36 ->  38 /  61 ->  82     200 sequences, 20 queries,  300 keys:  52 -> 78 / 122 -> 208
 template <class F> ds_status diff_by_kind(const DiffAttnArgs& a, F f) {
+    const bool few = (long long)a.n_seq * a.n_heads * a.head_dim <= 64LL * gemm_cu_count();
     auto by_split = [&](auto hd, auto causal) {
+        if (!few) return f(hd, causal, std::integral_constant<int, 1>{});
         if (a.max_q_len <= 32) return f(hd, causal, std::integral_constant<int, 4>{});
         if (a.max_q_len <= 64) return f(hd, causal, std::integral_constant<int, 2>{});
         return f(hd, causal, std::integral_constant<int, 1>{});
