@@ -1,0 +1,273 @@
+"""The layer parts together, as a block uses them: norm, QKV product, rotary positions on both maps, differential attention, RMSNorm per head, output
+product, and the joint that ends the block (norm of the branch, gate, residual, the next block's norm); forward and backward on a padded layout, against
+the same formulas in float64 with automatic differentiation; captured into a graph; and token by token on a cache.
+
+Tolerances (normwise, and elementwise in the terms of helpers.check).  On the way to a result lie at most 9 roundings of tensors forward and 9 backward
+(u, qkv, the turned qk, P, o, its norm, the branch, y, u and their gradients).  A per-head norm divides a difference of two averages by its own size,
+so that what is rounded before it counts as much more as the averages are larger than their difference: below 3 here (lambda <= 0.6 and hundreds of
+independent values).  The roundings are independent: sqrt(18) x 3 x 2^-8 in bf16 < 5.0e-2.  In fp32 a product of K <= 512 terms (768 in one of them) errs by at most
+sqrt(512) x 2^-24 of its terms, whose sum of squares is what the result is made of: sqrt(18) x 3 x 22.7 x 2^-24 < 1.8e-5."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2311_10418_amd import binding as ds
+from paper_2311_10418_amd import workload as wl
+from helpers import DEV, check, to_np
+
+pytestmark = pytest.mark.gpu
+
+BF, F32, F64 = torch.bfloat16, torch.float32, torch.float64
+TOL = {BF: 5.0e-2, F32: 1.8e-5}
+PARAMS = ("wqkv", "wo", "lam", "pre_g", "pre_b", "head_g", "post_g", "post_b", "gate", "next_g", "next_b")
+A_R, A_B = 0.9, 1.1
+
+
+def _norm64(t, g, b=None):
+    if b is None:
+        return t * torch.rsqrt((t * t).mean(-1, keepdim=True) + 1e-6) * g
+    c = t - t.mean(-1, keepdim=True)
+    return c * torch.rsqrt((c * c).mean(-1, keepdim=True) + 1e-5) * g + b
+
+
+def _turn64(t, freq):
+    """[l, heads, hd]: pairs (i, i + hd / 2) turned by position x freq[i]."""
+    a = torch.arange(t.shape[0], dtype=F64)[:, None, None] * freq
+    c, s = torch.cos(a), torch.sin(a)
+    u, v = t.chunk(2, dim=-1)
+    return torch.cat([u * c - v * s, v * c + u * s], dim=-1)
+
+
+def block64(x, p, heads, freq, causal=True):
+    """One sequence, float64 [l, d] -> y, u."""
+    l, d = x.shape
+    q, k, v = (_norm64(x, p["pre_g"], p["pre_b"]) @ p["wqkv"]).chunk(3, dim=1)
+    hide = torch.full((l, l), -math.inf, dtype=F64).triu(1) if causal else torch.zeros((l, l), dtype=F64)
+    maps = lambda t: _turn64(t.reshape(l, 2 * heads, -1), freq).reshape(l, heads, 2, -1).permute(1, 2, 0, 3)  # noqa: E731
+    s = maps(q) @ maps(k).transpose(2, 3) / math.sqrt(d // heads // 2) + hide
+    pr = torch.softmax(s, dim=-1)
+    both = pr[:, 0] - p["lam"][:, None, None] * pr[:, 1]
+    o = _norm64((both @ v.reshape(l, heads, -1).transpose(0, 1)).transpose(0, 1), p["head_g"]).reshape(l, d)
+    y = A_R * x + A_B * p["gate"] * _norm64(o @ p["wo"], p["post_g"], p["post_b"])
+    return y, _norm64(y, p["next_g"], p["next_b"])
+
+
+class Block:
+    """The block on the rows of a layout, all buffers made here: forward() and backward() only call the library."""
+
+    def __init__(self, lay, p, x, dy, du, heads, dt):
+        self.rows, self.d = x.shape
+        self.heads, self.hd, self.dt = heads, self.d // heads, dt
+        n, d = self.rows, self.d
+        dev = lambda a, t: torch.as_tensor(np.asarray(a), device=DEV).to(t).contiguous()  # noqa: E731
+        self.p = {k: v.to(F32 if k == "lam" else dt).to(DEV) for k, v in p.items()}
+        self.x, self.dy, self.du = (t.to(dt).to(DEV) for t in (x, dy, du))
+        pos = ds.ds_layout_positions(lay)
+        self.pos = dev(pos, torch.int32)
+        self.freq = dev(ds.ds_rope_freqs(self.hd // 2), F64)
+        self.tables = [dev(a, torch.int32) for a in (lay.seq_row, lay.seq_len)] * 2
+        self.longest = int(max(lay.seq_len))
+        new = lambda *s, t=dt: torch.zeros(s, dtype=t, device=DEV)  # noqa: E731
+        f = lambda *s: new(*s, t=F32)  # noqa: E731
+        self.u0, self.qkv, self.o, self.o2, self.on, self.branch, self.y, self.u = new(n, d), new(n, 3 * d), new(n, d), new(n, d), new(n, d), new(n, d), new(n, d), new(n, d)
+        self.st0, self.st1, self.st, self.lse = f(2, n), f(2, n * heads), f(4, n), f(2 * heads, n)
+        self.scratch = new(int(ds.ds_diff_attention_scratch_bytes(heads, n, n, len(lay.seq_len))), t=torch.uint8)
+        self.dres, self.dbranch, self.don, self.do, self.dqkv, self.du0, self.dx = new(n, d), new(n, d), new(n, d), new(n, d), new(n, 3 * d), new(n, d), new(n, d)
+        self.grads = {k: f(*v.shape) for k, v in self.p.items()}
+        self.joint_scratch = f(int(ds.ds_resid_norm_bwd_scratch_floats(n, d)))
+        self.norm_scratch = f(max(int(ds.ds_norm_bwd_scratch_floats(n, d)), int(ds.ds_norm_bwd_scratch_floats(n * heads, self.hd))))
+
+    def parts(self, t):
+        return [t[:, i * self.d:(i + 1) * self.d] for i in range(3)]
+
+    def turn(self, t, inverse, st):
+        """Both maps of every head of q and k, in place."""
+        qk = t[:, :2 * self.d]
+        ds.ds_rope(qk, qk, self.pos, self.freq, 4 * self.heads, self.hd // 2, self.hd // 2, inverse=inverse, stream=st)
+
+    def forward(self, st=None):
+        p, n, d, per_head = self.p, self.rows, self.d, lambda t: t.view(-1, self.hd)
+        ds.ds_norm_fwd(self.x, p["pre_g"], p["pre_b"], self.u0, self.st0, stream=st)
+        ds.ds_gemm(self.u0, p["wqkv"], self.qkv, n, 3 * d, d, stream=st)
+        self.turn(self.qkv, False, st)
+        q, k, v = self.parts(self.qkv)
+        ds.ds_diff_attention_fwd(q, k, v, p["lam"], self.o, self.lse, *self.tables, self.heads, self.hd, True, self.longest, self.longest, self.scratch, o2=self.o2,
+                                 stream=st)
+        ds.ds_norm_fwd(per_head(self.o), p["head_g"], None, per_head(self.on), self.st1, rms=True, stream=st)
+        ds.ds_gemm(self.on, p["wo"], self.branch, n, d, d, stream=st)
+        ds.ds_resid_norm_fwd(self.x, self.branch, self.y, self.st, p["post_g"], p["post_b"], p["gate"], p["next_g"], p["next_b"], self.u, A_R, A_B, self.pos, stream=st)
+
+    def backward(self, st=None):
+        p, g, n, d, per_head = self.p, self.grads, self.rows, self.d, lambda t: t.view(-1, self.hd)
+        ds.ds_resid_norm_bwd(self.dy, self.y, self.branch, self.st, self.dres, self.dbranch, self.joint_scratch, self.du, p["post_g"], p["post_b"], p["gate"],
+                             p["next_g"], g["gate"], g["post_g"], g["post_b"], g["next_g"], g["next_b"], A_R, A_B, self.pos, stream=st)
+        ds.ds_gemm(self.on, self.dbranch, g["wo"], d, d, n, trans_a=True, epilogue=ds.DS_EPI_ACC32, stream=st)
+        ds.ds_gemm(self.dbranch, p["wo"], self.don, n, d, d, trans_b=True, stream=st)
+        ds.ds_norm_bwd(per_head(self.don), per_head(self.o), p["head_g"], self.st1, None, per_head(self.do), g["head_g"], None, self.norm_scratch, rms=True, stream=st)
+        q, k, v = self.parts(self.qkv)
+        ds.ds_diff_attention_bwd(q, k, v, p["lam"], self.o, self.o2, self.do, self.lse, *self.parts(self.dqkv), g["lam"], *self.tables, self.heads, self.hd, True,
+                                 self.longest, self.longest, self.scratch, stream=st)
+        self.turn(self.dqkv, True, st)
+        ds.ds_gemm(self.u0, self.dqkv, g["wqkv"], d, 3 * d, n, trans_a=True, epilogue=ds.DS_EPI_ACC32, stream=st)
+        ds.ds_gemm(self.dqkv, p["wqkv"], self.du0, n, d, 3 * d, trans_b=True, stream=st)
+        ds.ds_norm_bwd(self.du0, self.x, p["pre_g"], self.st0, self.dres, self.dx, g["pre_g"], g["pre_b"], self.norm_scratch, stream=st)
+
+    def results(self):
+        return [t.clone() for t in (self.y, self.u, self.dx, *self.grads.values())]
+
+
+def _problem(seed, lens, cuts, heads, hd, dt):
+    """-> layout, parameters, x and the gradients of y and u: float64 on the grid of dt, padding rows zero."""
+    rng = np.random.default_rng(seed)
+    lay, d = ds.ds_layout_from_cuts(lens, cuts), heads * hd
+
+    def rnd(*shape, scale=1.0, mean=0.0):
+        a = (mean + scale * rng.standard_normal(shape)).astype(np.float32)
+        return torch.from_numpy((wl.to_bf16_grid(a) if dt == BF else a).astype(np.float64))
+
+    p = dict(wqkv=rnd(d, 3 * d, scale=d ** -0.5), wo=rnd(d, d, scale=d ** -0.5),
+             lam=torch.from_numpy(rng.uniform(0.1, 0.6, heads).astype(np.float32).astype(np.float64)), pre_g=rnd(d, scale=0.1, mean=1.0), pre_b=rnd(d, scale=0.1),
+             head_g=rnd(hd, scale=0.1, mean=0.8), post_g=rnd(d, scale=0.1, mean=1.0), post_b=rnd(d, scale=0.1), gate=rnd(d, scale=0.2, mean=0.5),
+             next_g=rnd(d, scale=0.1, mean=1.0), next_b=rnd(d, scale=0.1))
+    on = torch.from_numpy(ds.ds_layout_positions(lay) >= 0)[:, None]
+    x, dy, du = (rnd(lay.total_rows, d) * on for _ in range(3))
+    return lay, p, x, dy, du
+
+
+def _exact(lay, p, x, dy, du, heads, hd):
+    p = {k: v.clone().requires_grad_(True) for k, v in p.items()}
+    x = x.clone().requires_grad_(True)
+    freq = torch.from_numpy(ds.ds_rope_freqs(hd // 2))
+    y, u, loss = torch.zeros_like(x), torch.zeros_like(x), 0.0
+    for r, n in zip(lay.seq_row, lay.seq_len):
+        ys, us = block64(x[r:r + n], p, heads, freq)
+        loss = loss + (ys * dy[r:r + n]).sum() + (us * du[r:r + n]).sum()
+        y[r:r + n], u[r:r + n] = ys, us
+    grads = torch.autograd.grad(loss, [x] + [p[k] for k in PARAMS])
+    return y.detach(), u.detach(), grads[0], dict(zip(PARAMS, grads[1:]))
+
+
+# lengths (3 and 1 padded to the longest of their micro-batch), micro-batch cuts, heads, head size
+SHAPES = [([130, 3, 77, 1], [0, 2, 4], 4, 64), ([65, 129], [0, 2], 2, 128), ([19, 40], [0, 1, 2], 3, 32)]
+
+
+@pytest.mark.parametrize("dt", [F32, BF])
+@pytest.mark.parametrize("lens,cuts,heads,hd", SHAPES)
+def test_block(dt, lens, cuts, heads, hd):
+    prob = _problem(sum(lens), lens, cuts, heads, hd, dt)
+    lay = prob[0]
+    y, u, dx, grads = _exact(*prob, heads, hd)
+    b = Block(*prob, heads, dt)
+    b.forward()
+    b.backward()
+    torch.cuda.synchronize()
+    for name, got, ref in (("y", b.y, y), ("u", b.u, u), ("dx", b.dx, dx)):
+        for r, n in zip(lay.seq_row, lay.seq_len):
+            check(to_np(got)[r:r + n], ref[r:r + n].numpy(), TOL[dt], "%s rows %d" % (name, r))
+    off = torch.from_numpy(ds.ds_layout_positions(lay) < 0).to(DEV)
+    assert not b.y[off].any() and not b.u[off].any() and not b.dx[off].any()
+    for name in PARAMS:
+        check(to_np(b.grads[name]), grads[name].numpy(), TOL[dt], "d" + name)
+
+
+@pytest.mark.parametrize("dt", [F32, BF])
+def test_block_gradients_against_differences(dt):
+    """The library's gradients along one direction of all parameters and x, against a central difference of the formulas in float64."""
+    heads, hd = 4, 64
+    lay, p, x, dy, du = _problem(5, [33, 60], [0, 2], heads, hd, dt)
+    b = Block(lay, p, x, dy, du, heads, dt)
+    b.forward()
+    b.backward()
+    torch.cuda.synchronize()
+    freq = torch.from_numpy(ds.ds_rope_freqs(hd // 2))
+    got = dict(b.grads, x=b.dx)
+    point = dict(p, x=x)
+    # along the gradient itself, whose slope is its length: a direction that no cancellation makes small
+    step = {k: got[k].double().cpu() for k in point}
+    length = math.sqrt(sum(float((v * v).sum()) for v in step.values()))
+
+    def loss(t):
+        at = {k: point[k] + t * step[k] / length for k in point}
+        total = 0.0
+        for r, n in zip(lay.seq_row, lay.seq_len):
+            y, u = block64(at["x"][r:r + n], at, heads, freq)
+            total += float((y * dy[r:r + n]).sum() + (u * du[r:r + n]).sum())
+        return total
+
+    h = 1e-4                                            # a step far below the parameters' sizes: the error h^2 is far below the tolerances
+    slope = (loss(h) - loss(-h)) / (2 * h)
+    assert abs(slope - length) <= TOL[dt] * length, (slope, length)
+
+
+@pytest.mark.parametrize("dt", [F32, BF])
+def test_block_in_a_graph(dt):
+    """Forward and backward captured once: every replay gives the eager call's bits, with other calls on the same buffers in between."""
+    prob = _problem(9, [70, 20, 33], [0, 2, 3], 4, 64, dt)
+    b = Block(*prob, 4, dt)
+    b.forward()
+    b.backward()
+    torch.cuda.synchronize()
+    want = b.results()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        st = torch.cuda.current_stream().cuda_stream
+        b.forward(st)
+        b.backward(st)
+    x = b.x.clone()
+    for i in range(4):
+        b.x.copy_(x * 0.5)                              # the same buffers, workspaces too, used eagerly with other values
+        b.forward()
+        b.backward()
+        torch.cuda.synchronize()
+        assert not torch.equal(b.y, want[0])
+        b.x.copy_(x)
+        for t in (b.y, b.u, b.dx):
+            t.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        for name, got, ref in zip(("y", "u", "dx", *b.grads), b.results(), want):
+            assert torch.equal(got, ref), (i, name)
+
+
+@pytest.mark.parametrize("dt", [F32, BF])
+@pytest.mark.parametrize("heads,hd", [(4, 64), (2, 128)])
+def test_token_by_token(dt, heads, hd):
+    """A cache of turned keys and of values, one row per position: the last tokens of three sequences, one at a time, against the formulas on whole
+    sequences.  What lies behind a sequence's last key in the cache is NaN."""
+    lens, room, first = [40, 7, 133], 136, 3           # tokens, rows of a sequence in the cache, tokens left for the steps
+    d, n = heads * hd, len(lens)
+    lay, p, x, _, _ = _problem(11, lens, [0, 3], heads, hd, dt)
+    freq = torch.from_numpy(ds.ds_rope_freqs(hd // 2))
+    exact = [block64(x[r:r + m], p, heads, freq) for r, m in zip(lay.seq_row, lay.seq_len)]
+    whole = Block(lay, p, x, torch.zeros_like(x), torch.zeros_like(x), heads, dt)
+    whole.forward()
+    torch.cuda.synchronize()
+    cache_k, cache_v = (torch.full((n * room, d), math.nan, dtype=dt, device=DEV) for _ in range(2))
+    for s, (r, m) in enumerate(zip(lay.seq_row, lay.seq_len)):
+        cache_k[s * room:s * room + m - first], cache_v[s * room:s * room + m - first] = (t[r:r + m - first] for t in whole.parts(whole.qkv)[1:])
+    i32 = lambda a: torch.tensor(a, dtype=torch.int32, device=DEV)  # noqa: E731
+    w = whole.p
+    scratch = torch.zeros(int(ds.ds_diff_attention_scratch_bytes(heads, n, n * room, n)), dtype=torch.uint8, device=DEV)
+    for step in range(first):
+        at = [int(m) - first + step for m in lay.seq_len]
+        xs = torch.stack([whole.x[r + t] for r, t in zip(lay.seq_row, at)])
+        u0, qkv, o, on, branch, y, u = (torch.zeros((n, c), dtype=dt, device=DEV) for c in (d, 3 * d, d, d, d, d, d))
+        lse, st, st1 = torch.zeros((2 * heads, n), device=DEV), torch.zeros((4, n), device=DEV), torch.zeros((2, n * heads), device=DEV)
+        ds.ds_norm_fwd(xs, w["pre_g"], w["pre_b"], u0, st, stream=None)
+        ds.ds_gemm(u0, w["wqkv"], qkv, n, 3 * d, d)
+        qk = qkv[:, :2 * d]
+        ds.ds_rope(qk, qk, i32(at), whole.freq, 4 * heads, hd // 2, hd // 2)
+        slots = torch.tensor([s * room + t for s, t in enumerate(at)], device=DEV)
+        cache_k[slots], cache_v[slots] = qkv[:, d:2 * d], qkv[:, 2 * d:]
+        ds.ds_diff_attention_fwd(qkv[:, :d], cache_k, cache_v, w["lam"], o, lse, i32(list(range(n))), i32([1] * n), i32([s * room for s in range(n)]),
+                                 i32([t + 1 for t in at]), heads, hd, False, 1, room, scratch)
+        ds.ds_norm_fwd(o.view(-1, hd), w["head_g"], None, on.view(-1, hd), st1, rms=True)
+        ds.ds_gemm(on, w["wo"], branch, n, d, d)
+        ds.ds_resid_norm_fwd(xs, branch, y, st, w["post_g"], w["post_b"], w["gate"], w["next_g"], w["next_b"], u, A_R, A_B)
+        torch.cuda.synchronize()
+        for name, got, which in (("y", y, 0), ("u", u, 1)):
+            check(to_np(got), torch.stack([e[which][t] for e, t in zip(exact, at)]).numpy(), TOL[dt], "%s step %d" % (name, step))
