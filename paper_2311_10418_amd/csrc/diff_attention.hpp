@@ -18,7 +18,27 @@ struct DiffAttnArgs : AttnArgs {                        // scale: 1 / sqrt(head_
     float* lam_part;                                    // sums of P_2 G of the queries of a wavefront, at the row of its first query
     int32_t vec;                                        // general kernels: rows of four elements may be accessed at once
     char* aug;                                          // matrix-core kernels: see diff_attention_bwd.hip
+    int32_t k_splits;                                   // forward: work-groups that share the keys of a head (1: one has them all)
+    float* split_part;                                  // what each of them found: see SplitPart
 };
+
+// Few short queries over long keys (single tokens on a cache): the keys of a sequence and head are dealt out to k_splits work-groups, in runs of
+// whole tiles, and each leaves for every query its maxima and sums (exp2 domain) and its two unscaled outputs; diff_join_kernel puts them together.
+struct SplitPart {
+    float *stat, *o[2];                                 // {maximum 1, sum 1, maximum 2, sum 2}; [head_dim] each
+};
+__device__ __forceinline__ SplitPart split_part(const DiffAttnArgs& a, int h, long long row, int split) {
+    float* p = a.split_part + ((size_t)(h * (long long)a.q_total_rows + row) * a.k_splits + split) * (2 * a.head_dim + 4);
+    return {p, {p + 4, p + 4 + a.head_dim}};
+}
+// keys first .. first + count - 1 of kl are those of work-group `split`
+struct KeyRange { int first, count; };
+__device__ __forceinline__ KeyRange split_keys(const DiffAttnArgs& a, int kl, int split) {
+    if (a.k_splits == 1) return {0, kl};
+    const long long run = ((long long)kl + 64LL * a.k_splits - 1) / (64LL * a.k_splits) * 64, first = min(run * split, (long long)kl);
+    return {(int)first, (int)min(run, kl - first)};
+}
+ds_status diff_join(const DiffAttnArgs& a, hipStream_t st);
 
 size_t diff_scratch_bytes(int n_heads, int q_total_rows, int k_total_rows, int n_seq);
 ds_status diff_fwd_general(const DiffAttnArgs& a, hipStream_t st);

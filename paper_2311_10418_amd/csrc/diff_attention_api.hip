@@ -1,12 +1,34 @@
 // C-ABI entry points and dispatch of differential attention.
 #include "diff_attention.hpp"
+#include <algorithm>
 #include <cmath>
 
+// Work-groups that share the keys of a head, for sequences of at most 64 rows of queries each: as many as make one for every compute unit with 128
+// keys or more each (from 257 keys on: two shares of 128 and their joining cost 9.7 us, 256 keys at once 8.1); two, which head sizes up to 64 have
+// the LDS for, with 1024 or more each; at most one for a lane of the wavefront that joins them.  One query of 16 heads of 64, us without -> with:
+//     1 sequence of 512, 1024, 4096, 32768 keys:  15 -> 10, 24 -> 10, 77 -> 12, 575 -> 38 (3.6 TB/s)
+//     16 sequences of 2048, 16384 keys:  44 -> 33, 296 -> 193 (one work-group for a compute unit: 37, 322); 33 queries over 1019 keys: 28 -> 23 (two: 29)
+static constexpr int kSplitQueries = 64, kSplitUnits = 256, kSplitMost = 64, kSplitFrom = 257, kSplitKeys = 128, kSplitKeysOfTwo = 1024;
+static int most_splits(int n_heads, int head_dim, int q_total_rows, int max_k_len, int n_seq) {
+    const long long items = (long long)n_seq * n_heads;
+    if (q_total_rows > (long long)kSplitQueries * n_seq || max_k_len < kSplitFrom) return 1;
+    auto with = [&](long long groups, int keys) {
+        return std::min({groups / items, (long long)kSplitMost, ((long long)max_k_len + keys - 1) / keys});
+    };
+    const long long one = with(kSplitUnits, kSplitKeys), two = head_dim <= 64 ? with(2 * kSplitUnits, kSplitKeysOfTwo) : 1;
+    return (int)std::max<long long>(std::max(one, two), 1);
+}
+
 // Scratch: the work lists of the matrix-core kernels, then what the dQ kernels hand to the dK/dV kernels, 16 bytes for each query of a head
-// (the general ones use 8 of them, as two arrays of floats), then the parts of dlambda, one float each.
+// (the general ones use 8 of them, as two arrays of floats), then the parts of dlambda, one float each.  In their place, where a forward call may split the keys: what the splits found.
 static size_t lists_size(int q_total_rows, int k_total_rows, int n_seq) { return attn_scratch_bytes(0, 0, q_total_rows, k_total_rows, n_seq); }
 size_t diff_scratch_bytes(int n_heads, int q_total_rows, int k_total_rows, int n_seq) {
-    return lists_size(q_total_rows, k_total_rows, n_seq) + (size_t)n_heads * q_total_rows * (16 + 4);
+    size_t of_row = 16 + 4;
+    for (const int head_dim : {64, 128}) {
+        const int splits = most_splits(n_heads, head_dim, q_total_rows, k_total_rows, n_seq);
+        if (splits > 1) of_row = std::max(of_row, (size_t)splits * (2 * head_dim + 4) * 4);
+    }
+    return lists_size(q_total_rows, k_total_rows, n_seq) + (size_t)n_heads * q_total_rows * of_row;
 }
 
 static bool four_at_once(const void* p, size_t size) { return !p || (uintptr_t)p % (4 * size) == 0; }
@@ -33,6 +55,9 @@ static ds_status check(DiffAttnArgs& a) {
     a.aug = after_lists;
     a.d1 = (float*)after_lists;
     a.d2 = a.d1 + entries;
+    a.split_part = (float*)after_lists;
+    const int k_rows = a.max_k_len < a.k_total_rows ? a.max_k_len : a.k_total_rows;
+    a.k_splits = !a.d_o && !a.mask && a.max_q_len <= kSplitQueries ? most_splits(a.n_heads, a.head_dim, a.q_total_rows, k_rows, a.n_seq) : 1;
     a.lam_part = (float*)(after_lists + entries * 16);
     return DS_OK;
 }

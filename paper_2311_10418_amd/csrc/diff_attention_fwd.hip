@@ -30,15 +30,28 @@ __global__ __launch_bounds__(256, HD == 64 && KS == 1 ? 3 : 2) void diff_fwd_mfm
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 31, g = lane >> 5;
-    const int item = blockIdx.x / a.n_heads, h = blockIdx.x - item * a.n_heads;
-    const int2 it = a.items_q[item];
-    if (item >= a.n_items[0]) return;
-    const int s = it.x, q0 = it.y * 128;
-    const int ql = a.q_len[s], kl = a.k_len[s];
+    int s, h, q0 = 0, split = 0;
+    if constexpr (KS == 1) {
+        const int item = blockIdx.x / a.n_heads;
+        const int2 it = a.items_q[item];
+        if (item >= a.n_items[0]) return;
+        s = it.x;
+        q0 = it.y * 128;
+        h = blockIdx.x - item * a.n_heads;
+    } else {                                            // one block of queries in a sequence: no list
+        split = blockIdx.x;
+        h = blockIdx.y;
+        s = blockIdx.z;
+        if (a.q_len[s] == 0) return;
+    }
+    const int ql = a.q_len[s];
+    const KeyRange range = KS == 1 ? KeyRange{0, a.k_len[s]} : split_keys(a, a.k_len[s], split);
+    const int kl = range.count;
+    const long long krow0 = (long long)a.k_row[s] + range.first;
     const long long qrow0 = a.q_row[s];
     const bf16_t* Q = (const bf16_t*)a.q + qrow0 * a.ldq + h * HD;
-    const bf16_t* K = (const bf16_t*)a.k + (long long)a.k_row[s] * a.ldk + h * HD;
-    const bf16_t* V = (const bf16_t*)a.v + (long long)a.k_row[s] * a.ldv + h * HD;
+    const bf16_t* K = (const bf16_t*)a.k + krow0 * a.ldk + h * HD;
+    const bf16_t* V = (const bf16_t*)a.v + krow0 * a.ldv + h * HD;
     KeySplit<KS> ks;
     ks.init(wave);
     const int qw0 = q0 + ks.group * 32;
@@ -182,6 +195,20 @@ __global__ __launch_bounds__(256, HD == 64 && KS == 1 ? 3 : 2) void diff_fwd_mfm
     for (int m = 0; m < 2; ++m) l[m] += __shfl_xor(l[m], 32, 64);
     if (qw0 >= ql) return;
     const long long row = qrow0 + qi;
+    if (KS > 1 && a.k_splits > 1) {
+        if (qi >= ql) return;
+        const SplitPart to = split_part(a, h, row, split);
+        if (g == 0) *reinterpret_cast<float4*>(to.stat) = make_float4(top[0], l[0], top[1], l[1]);
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int i = 0; i < ND * 4; ++i) {
+                const f32x16_t& f = o[m][i / 4];
+                const int e = 4 * (i % 4);
+                *reinterpret_cast<float4*>(to.o[m] + 8 * i + 4 * g) = make_float4(f[e], f[e + 1], f[e + 2], f[e + 3]);
+            }
+        return;
+    }
     const float r1 = l[0] > 0.f ? 1.0f / l[0] : 0.f, r2 = l[1] > 0.f ? 1.0f / l[1] : 0.f, lam = a.lambda[h];
 #pragma unroll
     for (int dt = 0; dt < ND; ++dt)
@@ -205,9 +232,10 @@ ds_status fwd_launch(const DiffAttnArgs& a, hipStream_t st) {
     const int smem = KeySplit<KS>::RING * 2 * (64 * HD * 2);
     const ds_status r = set_smem(kern, smem, attr);
     if (r != DS_OK) return r;
-    hipLaunchKernelGGL(kern, dim3((unsigned)a.max_items_q * a.n_heads), dim3(256), smem, st, a);
+    const dim3 grid = KS == 1 ? dim3((unsigned)a.max_items_q * a.n_heads) : dim3(a.k_splits, a.n_heads, a.n_seq);
+    hipLaunchKernelGGL(kern, grid, dim3(256), smem, st, a);
     DS_LAUNCH_CHECK();
-    return DS_OK;
+    return KS > 1 && a.k_splits > 1 ? diff_join(a, st) : DS_OK;
 }
 
 }  // namespace
@@ -225,8 +253,9 @@ bool diff_mfma_supported(const DiffAttnArgs& a) {
 }
 
 ds_status diff_fwd_mfma(const DiffAttnArgs& a0, hipStream_t st) {
-    DiffAttnArgs a = a0;
-    const ds_status r = attn_prepare_lists(a, false, st);
-    if (r != DS_OK) return r;
-    return diff_by_kind(a, [&](auto hd, auto causal, auto split) { return fwd_launch<decltype(hd)::value, decltype(causal)::value, decltype(split)::value>(a, st); });
+    return diff_by_kind(a0, [&](auto hd, auto causal, auto split) {
+        DiffAttnArgs a = a0;
+        const ds_status r = split == 1 ? attn_prepare_lists(a, false, st) : DS_OK;
+        return r != DS_OK ? r : fwd_launch<decltype(hd)::value, decltype(causal)::value, decltype(split)::value>(a, st);
+    });
 }

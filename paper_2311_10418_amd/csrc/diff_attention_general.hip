@@ -130,11 +130,15 @@ __global__ __launch_bounds__(256) void diff_fwd_kernel(DiffAttnArgs a) {
     __shared__ __attribute__((aligned(16))) float sK[Tl::FLOATS];
     __shared__ __attribute__((aligned(16))) float sV[Tl::FLOATS];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4;
-    const ColumnBlock cb = column_block(a, a.q_len, a.mask != 0);
+    ColumnBlock cb = column_block(a, a.q_len, a.mask != 0);
+    const int split = a.k_splits > 1 ? blockIdx.x : 0;                 // (one block of queries then)
+    if (a.k_splits > 1) cb.first = a.q_len[cb.s] > 0 ? 0 : -1;
     if (cb.first < 0) return;
-    const int s = cb.s, h = cb.h, q0 = cb.first, ql = a.q_len[s], kl = a.k_len[s], hd = a.head_dim, half = hd / 2;
+    const int s = cb.s, h = cb.h, q0 = cb.first, ql = a.q_len[s], hd = a.head_dim, half = hd / 2;
+    const KeyRange range = split_keys(a, a.k_len[s], split);
+    const int kl = range.count;
     const bool vec = a.vec;
-    const long long qrow0 = a.q_row[s], krow0 = a.k_row[s];
+    const long long qrow0 = a.q_row[s], krow0 = (long long)a.k_row[s] + range.first;
     const T* K = (const T*)a.k + krow0 * a.ldk + (long long)h * hd;
     const T* V = (const T*)a.v + krow0 * a.ldv + (long long)h * hd;
     const int qw0 = q0 + wave * 16, qi = qw0 + (lane & 15), qi_c = qi < ql ? qi : ql - 1;
@@ -200,8 +204,15 @@ __global__ __launch_bounds__(256) void diff_fwd_kernel(DiffAttnArgs a) {
     if (qi >= ql) return;
     l1 = groups_sum(l1);
     l2 = groups_sum(l2);
-    const float lam = a.lambda[h], r1 = kl > 0 ? 1.0f / l1 : 0.f, r2 = kl > 0 ? 1.0f / l2 : 0.f;      // (no keys: zeros)
     const long long row = qrow0 + qi;
+    if (a.k_splits > 1) {
+        const SplitPart to = split_part(a, h, row, split);
+        if (g == 0) *reinterpret_cast<float4*>(to.stat) = make_float4(m1, l1, m2, l2);
+        store_column<float, HH>(o1, 1.0f, to.o[0], half, g, true);
+        store_column<float, HH>(o2, 1.0f, to.o[1], half, g, true);
+        return;
+    }
+    const float lam = a.lambda[h], r1 = kl > 0 ? 1.0f / l1 : 0.f, r2 = kl > 0 ? 1.0f / l2 : 0.f;      // (no keys: zeros)
 #pragma unroll
     for (int i = 0; i < NS; ++i) {
         o2[i] *= r2;
@@ -213,6 +224,61 @@ __global__ __launch_bounds__(256) void diff_fwd_kernel(DiffAttnArgs a) {
         a.lse[(size_t)(2 * h) * a.lse_stride + row] = (m1 + __builtin_amdgcn_logf(l1)) * kLn2G;
         a.lse[(size_t)(2 * h + 1) * a.lse_stride + row] = (m2 + __builtin_amdgcn_logf(l2)) * kLn2G;
     }
+}
+
+// What the work-groups that shared a head's keys found, put together: a wavefront per query, lane i with the statistics of work-group i, then four
+// columns of one of the outputs per lane.  A work-group without keys has sum 0, and its maximum does not count.  A chain of two trips to memory and no
+// more for up to kAtOnce work-groups, whose outputs are on their way before the statistics are there.
+template <class T> __global__ __launch_bounds__(256) void diff_join_kernel(DiffAttnArgs a) {
+    constexpr int kAtOnce = 16;
+    const int lane = threadIdx.x & 63, q = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = blockIdx.y, s = blockIdx.z;
+    if (q >= a.q_len[s]) return;
+    const long long row = (long long)a.q_row[s] + q;
+    const int hd = a.head_dim, n = a.k_splits, quarter = hd / 4;
+    const size_t step = 2 * hd + 4;
+    const SplitPart p = split_part(a, h, row, 0);
+    const int m = lane >= quarter, col = 4 * (lane - m * quarter);     // this lane's output and columns
+    const bool on = lane < 2 * quarter;
+    const float* from = p.o[0] + 4 * (on ? lane : 0);
+    auto load = [&](int i) { return *reinterpret_cast<const f32x4_t*>(from + min(i, n - 1) * step); };
+    f32x4_t v[kAtOnce];
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) v[i] = load(i);
+    const f32x4_t st = lane < n ? *reinterpret_cast<const f32x4_t*>(p.stat + lane * step) : zero4();
+    float w[2], r[2], lse[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const float l = st[2 * i + 1], top = l == 0.f ? -INFINITY : st[2 * i];
+        float up = top;
+#pragma unroll
+        for (int j = 1; j < 64; j *= 2) up = fmaxf(up, __shfl_xor(up, j, 64));
+        w[i] = l == 0.f ? 0.f : __builtin_amdgcn_exp2f(top - up);
+        float sum = w[i] * l;
+#pragma unroll
+        for (int j = 1; j < 64; j *= 2) sum += __shfl_xor(sum, j, 64);
+        r[i] = sum == 0.f ? 0.f : 1.0f / sum;
+        lse[i] = (up + __builtin_amdgcn_logf(sum)) * kLn2G;
+    }
+    auto weight = [&](int i) {                          // (lanes n and above hold 0)
+        const float w1 = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w[0]), i));
+        const float w2 = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w[1]), i));
+        return m ? w2 : w1;
+    };
+    f32x4_t o = zero4();
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i)
+        if (i < n) o += v[i] * weight(i);
+#pragma unroll 8
+    for (int i = kAtOnce; i < n; ++i) o += load(i) * weight(i);
+    o *= r[m];
+    const float lam = a.lambda[h];
+    f32x4_t other;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) other[j] = __shfl(o[j], lane + quarter, 64);
+    if (m == 0) o -= other * lam;
+    T* to = (T*)(m ? a.o2 : a.o);
+    if (on && to) store4(to + row * a.ldo + (long long)h * hd + col, o, a.vec);
+    if (lane < 2) a.lse[(size_t)(2 * h + lane) * a.lse_stride + row] = lane ? lse[1] : lse[0];
 }
 
 // ---------------------------------------------------------------- backward: dQ, D_1, D_2, the parts of dlambda
@@ -399,7 +465,8 @@ __global__ __launch_bounds__(1024) void diff_dlambda_kernel(DiffAttnArgs a, int 
 }
 
 template <class T, int HH> void fwd_launch(const DiffAttnArgs& a, hipStream_t st) {
-    hipLaunchKernelGGL((diff_fwd_kernel<T, HH>), column_grid(a, a.max_q_len), dim3(256), 0, st, a);
+    const dim3 grid = a.k_splits > 1 ? dim3(a.k_splits, a.n_heads, a.n_seq) : column_grid(a, a.max_q_len);
+    hipLaunchKernelGGL((diff_fwd_kernel<T, HH>), grid, dim3(256), 0, st, a);
 }
 template <class T, int HH> void dq_launch(const DiffAttnArgs& a, hipStream_t st) {
     hipLaunchKernelGGL((diff_bwd_dq_kernel<T, HH>), column_grid(a, a.max_q_len), dim3(256), 0, st, a);
@@ -421,6 +488,14 @@ template <class T, int HH> void dkv_launch(const DiffAttnArgs& a, hipStream_t st
 
 ds_status diff_fwd_general(const DiffAttnArgs& a, hipStream_t st) {
     DS_DIFF_DISPATCH(fwd_launch);
+    DS_LAUNCH_CHECK();
+    return a.k_splits > 1 ? diff_join(a, st) : DS_OK;
+}
+
+ds_status diff_join(const DiffAttnArgs& a, hipStream_t st) {
+    const dim3 grid((a.max_q_len + 3) / 4, a.n_heads, a.n_seq);
+    if (a.dtype == DS_DTYPE_BF16) hipLaunchKernelGGL((diff_join_kernel<bf16_t>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((diff_join_kernel<float>), grid, dim3(256), 0, st, a);
     DS_LAUNCH_CHECK();
     return DS_OK;
 }

@@ -114,7 +114,7 @@ __device__ __forceinline__ void store_cols16(const f32x16_t (&acc)[HD / 32], flo
 // f(head size, causal, wavefronts that share a block of queries) with the template arguments of a call
 //
 // Sharing (KeySplit) pays where there is about one work-group for a compute unit or less, and costs where others would hide the transfers anyway:
-// its ring takes twice the LDS.  One wavefront to a block of queries -> sharing, forward, 16 heads of 64 / of 128, us a call:
+// its ring takes twice the LDS.  One wavefront to a block of queries -> sharing, forward, 16 heads of 64 / of 128, us a call (keys not split):
 //     1 sequence,   1 query,   4096 keys:  79 ->  55 / 108 ->  83      16 sequences, 33 queries, 1019 keys:  28 -> 26 / 37 -> 37
 //     4 sequences,  1 query,   2048 keys:  44 ->  36 /  59 ->  50      16 sequences, 20 queries, 1019 keys:  26 -> 26 / 35 -> 38
 //    64 sequences, 33 queries,  500 keys:  36 ->  38 /  61 ->  82     200 sequences, 20 queries,  300 keys:  52 -> 78 / 122 -> 208

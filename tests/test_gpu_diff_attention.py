@@ -158,6 +158,36 @@ def test_short_queries(dt, generic, causal, hd):
 
 
 @pytest.mark.parametrize("dt,generic", KINDS)
+@pytest.mark.parametrize("hd", [16, 64, 96, 128])
+def test_few_queries_over_long_keys(dt, generic, hd):
+    """Single tokens and short runs over keys that several work-groups share: shares that end inside a tile, sequences with fewer keys than shares or none."""
+    Case(hd, dt, 4, hd, [1], [5000], False).run(generic)
+    Case(hd + 1, dt, 2, hd, [1, 1, 0, 1, 1, 1], [2049, 1, 700, 0, 64, 1300], False).run(generic)
+    Case(hd + 2, dt, 3, hd, [64, 33, 2], [900, 513, 3], False, pad_cols=8).run(generic)
+    Case(hd + 3, dt, 1, hd, [17], [1900], False, scale=6.0).run(generic)
+
+
+@pytest.mark.parametrize("dt,generic", KINDS)
+def test_single_tokens_in_a_graph(dt, generic):
+    c = Case(8, dt, 4, 128, [1, 1, 1], [1500, 33, 700], False)
+    c.tensors()
+    c.forward(generic, keep=False)
+    torch.cuda.synchronize()
+    want = [c.o.clone(), c.lse.clone()]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c.forward(generic, keep=False)
+    for _ in range(3):
+        c.o[:] = 9.0
+        c.lse.fill_(9.0)
+        c.scratch.fill_(200)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(c.o, want[0]) and torch.equal(c.lse, want[1])
+
+
+@pytest.mark.parametrize("dt,generic", KINDS)
 @pytest.mark.parametrize("hd,pad", [(64, 8), (64, 4), (64, 1), (128, 3), (128, 64), (16, 2)])
 def test_columns_of_wider_tensors(dt, generic, hd, pad):
     """Row strides and first columns that allow accesses of 16, 8, or only 2 or 4 bytes."""
