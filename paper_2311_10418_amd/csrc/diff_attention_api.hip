@@ -3,29 +3,33 @@
 #include <algorithm>
 #include <cmath>
 
-// Work-groups that share the keys of a head, for sequences of at most 64 rows of queries each: as many as make one for every compute unit with 128
-// keys or more each (from 257 keys on: two shares of 128 and their joining cost 9.7 us, 256 keys at once 8.1); two, which head sizes up to 64 have
-// the LDS for, with 1024 or more each; at most one for a lane of the wavefront that joins them.  One query of 16 heads of 64, us without -> with:
-//     1 sequence of 512, 1024, 4096, 32768 keys:  15 -> 10, 24 -> 10, 77 -> 12, 575 -> 38 (3.6 TB/s)
-//     16 sequences of 2048, 16384 keys:  44 -> 33, 296 -> 193 (one work-group for a compute unit: 37, 322); 33 queries over 1019 keys: 28 -> 23 (two: 29)
-static constexpr int kSplitQueries = 64, kSplitUnits = 256, kSplitMost = 64, kSplitFrom = 257, kSplitKeys = 128, kSplitKeysOfTwo = 1024;
-static int most_splits(int n_heads, int head_dim, int q_total_rows, int max_k_len, int n_seq) {
+// Work-groups that share the keys of a head, for sequences of at most 64 rows of queries each: as many as make one for every compute unit, with a least
+// number of keys each; two, which head sizes up to 64 have the LDS for, with more keys each; at most one for a lane of the wavefront that joins them.
+// Matrix-core kernels: 128 keys, from 257 on (256 keys at once take 8.1 us, two shares of 128 and their joining 9.7); two from 1024 each on.
+// General kernels: 64 keys, for two as well.  One query of 16 heads of 64, us without -> with, bf16 / fp32:
+//     1 sequence of 512, 1024, 4096 keys:  15 -> 10, 24 -> 10, 77 -> 12 / 39 -> 11, 74 -> 11, 287 -> 22; of 32768 keys: 575 -> 37 (3.6 TB/s)
+//     16 sequences of 2048, 16384 keys:  44 -> 33, 295 -> 195 (5.5 TB/s; one work-group for a compute unit: 37, 322)
+//     16 sequences of 33 queries and 1019 keys:  28 -> 23 (two work-groups with half of them each: 29)
+static constexpr int kSplitQueries = 64, kSplitUnits = 256, kSplitMost = 64;
+static int most_splits(bool general, int n_heads, int head_dim, int q_total_rows, int max_k_len, int n_seq) {
+    const int from = general ? 129 : 257, keys_one = general ? 64 : 128, keys_two = general ? 64 : 1024;
     const long long items = (long long)n_seq * n_heads;
-    if (q_total_rows > (long long)kSplitQueries * n_seq || max_k_len < kSplitFrom) return 1;
+    if (q_total_rows > (long long)kSplitQueries * n_seq || max_k_len < from) return 1;
     auto with = [&](long long groups, int keys) {
         return std::min({groups / items, (long long)kSplitMost, ((long long)max_k_len + keys - 1) / keys});
     };
-    const long long one = with(kSplitUnits, kSplitKeys), two = head_dim <= 64 ? with(2 * kSplitUnits, kSplitKeysOfTwo) : 1;
+    const long long one = with(kSplitUnits, keys_one), two = head_dim <= 64 ? with(2 * kSplitUnits, keys_two) : 1;
     return (int)std::max<long long>(std::max(one, two), 1);
 }
 
 // Scratch: the work lists of the matrix-core kernels, then what the dQ kernels hand to the dK/dV kernels, 16 bytes for each query of a head
-// (the general ones use 8 of them, as two arrays of floats), then the parts of dlambda, one float each.  In their place, where a forward call may split the keys: what the splits found.
+// (the general ones use 8 of them, as two arrays of floats), then the parts of dlambda, one float each.  A forward call has the parts of split keys in
+// the place of both.
 static size_t lists_size(int q_total_rows, int k_total_rows, int n_seq) { return attn_scratch_bytes(0, 0, q_total_rows, k_total_rows, n_seq); }
 size_t diff_scratch_bytes(int n_heads, int q_total_rows, int k_total_rows, int n_seq) {
     size_t of_row = 16 + 4;
     for (const int head_dim : {64, 128}) {
-        const int splits = most_splits(n_heads, head_dim, q_total_rows, k_total_rows, n_seq);
+        const int splits = most_splits(true, n_heads, head_dim, q_total_rows, k_total_rows, n_seq);      // (never fewer than the others)
         if (splits > 1) of_row = std::max(of_row, (size_t)splits * (2 * head_dim + 4) * 4);
     }
     return lists_size(q_total_rows, k_total_rows, n_seq) + (size_t)n_heads * q_total_rows * of_row;
@@ -55,9 +59,8 @@ static ds_status check(DiffAttnArgs& a) {
     a.aug = after_lists;
     a.d1 = (float*)after_lists;
     a.d2 = a.d1 + entries;
+    a.k_splits = 1;
     a.split_part = (float*)after_lists;
-    const int k_rows = a.max_k_len < a.k_total_rows ? a.max_k_len : a.k_total_rows;
-    a.k_splits = !a.d_o && !a.mask && a.max_q_len <= kSplitQueries ? most_splits(a.n_heads, a.head_dim, a.q_total_rows, k_rows, a.n_seq) : 1;
     a.lam_part = (float*)(after_lists + entries * 16);
     return DS_OK;
 }
@@ -83,7 +86,10 @@ extern "C" ds_status ds_diff_attention_fwd(int32_t dtype, int32_t n_seq, int32_t
     a.scratch = scratch; a.scratch_bytes = scratch_bytes < 0 ? 0 : (size_t)scratch_bytes;
     const ds_status r = check(a);
     if (r != DS_OK) return r;
-    if (!force_generic && diff_mfma_supported(a)) return diff_fwd_mfma(a, (hipStream_t)hip_stream);
+    const bool general = force_generic || !diff_mfma_supported(a);
+    if (!mask && max_q_len <= kSplitQueries)
+        a.k_splits = most_splits(general, n_heads, head_dim, q_total_rows, std::min(max_k_len, k_total_rows), n_seq);
+    if (!general) return diff_fwd_mfma(a, (hipStream_t)hip_stream);
     return diff_fwd_general(a, (hipStream_t)hip_stream);
 }
 
