@@ -7,6 +7,8 @@
 // Tiles of the other side are kept in LDS row by row, every half head padded with zeros to HH columns (a multiple of 16), V and dO too:
 // the contraction over features does not see the order of the columns, and outputs go back through the same mapping.
 #include "diff_attention.hpp"
+#include "gemm.hpp"
+#include <type_traits>
 
 namespace {
 
@@ -42,14 +44,14 @@ __device__ __forceinline__ void store4(bf16_t* p, const f32x4_t& v, bool vec) {
         for (int j = 0; j < 4; ++j) p[j] = (bf16_t)v[j];
 }
 
-template <class T, int HH> struct Tile {
-    static constexpr int ROWS = HH <= 48 ? 64 : 32, HD = 2 * HH, LD = HD + 4, NV = ROWS * HD / 4 / 256;
+template <class T, int HH, int THREADS> struct Tile {
+    static constexpr int ROWS = HH <= 48 ? 64 : 32, HD = 2 * HH, LD = HD + 4, NV = ROWS * HD / 4 / THREADS;
     static constexpr int FLOATS = ROWS * LD;
     float4 v[NV];
     __device__ __forceinline__ void load(const T* src, long long ld, int r0, int n_rows, int half, bool vec) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int u = threadIdx.x + 256 * i, r = r0 + u / (HD / 4), d = (u % (HD / 4)) * 4, m = d >= HH;
+            const int u = threadIdx.x + THREADS * i, r = r0 + u / (HD / 4), d = (u % (HD / 4)) * 4, m = d >= HH;
             v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
             if (r < n_rows && d - m * HH < half) v[i] = load4<T>(src + (long long)r * ld + m * half + (d - m * HH), vec);
         }
@@ -57,7 +59,7 @@ template <class T, int HH> struct Tile {
     __device__ __forceinline__ void store(float* tile) const {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int u = threadIdx.x + 256 * i;
+            const int u = threadIdx.x + THREADS * i;
             *reinterpret_cast<float4*>(tile + (u / (HD / 4)) * LD + (u % (HD / 4)) * 4) = v[i];
         }
     }
@@ -110,22 +112,22 @@ __device__ __forceinline__ void second_product(const float* tile, int rb, int la
 __device__ __forceinline__ float groups_max(float v) { v = fmaxf(v, __shfl_xor(v, 16, 64)); return fmaxf(v, __shfl_xor(v, 32, 64)); }
 __device__ __forceinline__ float groups_sum(float v) { v += __shfl_xor(v, 16, 64); return v + __shfl_xor(v, 32, 64); }
 
-// A work-group's 64 columns: sequence, head, first column (negative: nothing to do).  Sequences last to first: a plan lists them by
+// A work-group's COLS columns: sequence, head, first column (negative: nothing to do).  Sequences last to first: a plan lists them by
 // ascending length, and the longest chains of tiles should start first.
 struct ColumnBlock { int s, h, first; };
-__device__ __forceinline__ ColumnBlock column_block(const AttnArgs& a, const int32_t* len, bool last_first) {
+template <int COLS = 64> __device__ __forceinline__ ColumnBlock column_block(const AttnArgs& a, const int32_t* len, bool last_first) {
     ColumnBlock c = {a.n_seq - 1 - (int)blockIdx.z, (int)blockIdx.y, -1};
-    const int n = (len[c.s] + 63) / 64, b = blockIdx.x;
-    if (b < n) c.first = 64 * (last_first ? n - 1 - b : b);
+    const int n = (len[c.s] + COLS - 1) / COLS, b = blockIdx.x;
+    if (b < n) c.first = COLS * (last_first ? n - 1 - b : b);
     return c;
 }
 // an odd number of blocks per grid row: work-groups go to the eight XCDs in turn, and the longest of every sequence should not meet on one
-dim3 column_grid(const AttnArgs& a, int max_len) { return dim3(((max_len + 63) / 64) | 1, a.n_heads, a.n_seq); }
+dim3 column_grid(const AttnArgs& a, int max_len, int cols = 64) { return dim3((max_len / cols + (max_len % cols != 0)) | 1, a.n_heads, a.n_seq); }
 
 // ---------------------------------------------------------------- forward
 template <class T, int HH>
-__global__ __launch_bounds__(256) void diff_fwd_kernel(DiffAttnArgs a) {
-    typedef Tile<T, HH> Tl;
+__global__ __launch_bounds__(256, HH <= 32 ? 3 : 2) void diff_fwd_kernel(DiffAttnArgs a) {
+    typedef Tile<T, HH, 256> Tl;
     constexpr int KT = Tl::ROWS, NB = KT / 16, NS = HH / 8;
     __shared__ __attribute__((aligned(16))) float sK[Tl::FLOATS];
     __shared__ __attribute__((aligned(16))) float sV[Tl::FLOATS];
@@ -166,21 +168,25 @@ __global__ __launch_bounds__(256) void diff_fwd_kernel(DiffAttnArgs a) {
             tv.load(V, a.ldv, k0 + KT, kl, half, vec);
         }
         if (k0 > wave_last || qw0 >= ql) continue;
-        f32x4_t p1[NB], p2[NB];
-        float x1 = -INFINITY, x2 = -INFINITY;
+        // one map after the other, strictly so above head size 32, where the scores of both would take the registers of the second or third wavefront
+        // of a SIMD (16 heads of 64, 31 sequences of about 445 in fp32: 473 -> 430 us; 16 heads of 128, 8 of about 1 820, causal: 3 184 -> 1 940)
+        auto map = [&](auto first, float& m, float& l, f32x4_t (&o)[NS]) {
+            constexpr int S0 = decltype(first)::value, S1 = S0 + NS / 2;
+            f32x4_t p[NB];
+            float x = -INFINITY;
 #pragma unroll
-        for (int kt = 0; kt < NB; ++kt) {
-            p1[kt] = first_product<HH, 0, NS / 2>(sK, 16 * kt, lane, qf);
-            p2[kt] = first_product<HH, NS / 2, NS>(sK, 16 * kt, lane, qf);
+            for (int kt = 0; kt < NB; ++kt) {
+                p[kt] = first_product<HH, S0, S1>(sK, 16 * kt, lane, qf);
+                const int kb = k0 + 16 * kt;
+                if (kb + 16 > kl || (a.mask && kb + 15 > qw0))         // (a branch: most blocks need no mask)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int key = k0 + 16 * kt + 4 * g + e;
-                if (key >= kl || (a.mask && key > qi)) p1[kt][e] = p2[kt][e] = -INFINITY;
-                x1 = fmaxf(x1, p1[kt][e]);
-                x2 = fmaxf(x2, p2[kt][e]);
+                    for (int e = 0; e < 4; ++e) {
+                        const int key = kb + 4 * g + e;
+                        if (key >= kl || (a.mask && key > qi)) p[kt][e] = -INFINITY;
+                    }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x = fmaxf(x, p[kt][e]);
             }
-        }
-        auto soften = [&](f32x4_t (&p)[NB], float x, float& m, float& l, f32x4_t (&o)[NS]) {
             const float m_new = fmaxf(m, groups_max(x) * c), m_use = m_new == -INFINITY ? 0.f : m_new;
             const float alpha = __builtin_amdgcn_exp2f(m - m_use);
             float rs = 0.f;
@@ -198,8 +204,9 @@ __global__ __launch_bounds__(256) void diff_fwd_kernel(DiffAttnArgs a) {
 #pragma unroll
             for (int kt = 0; kt < NB; ++kt) second_product<HH, 0, NS>(sV, 16 * kt, lane, p[kt], o);
         };
-        soften(p1, x1, m1, l1, o1);
-        soften(p2, x2, m2, l2, o2);
+        map(std::integral_constant<int, 0>{}, m1, l1, o1);
+        if constexpr (HH >= 32) __builtin_amdgcn_sched_barrier(0);
+        map(std::integral_constant<int, NS / 2>{}, m2, l2, o2);
     }
     if (qi >= ql) return;
     l1 = groups_sum(l1);
@@ -282,14 +289,36 @@ template <class T> __global__ __launch_bounds__(256) void diff_join_kernel(DiffA
 }
 
 // ---------------------------------------------------------------- backward: dQ, D_1, D_2, the parts of dlambda
-template <class T, int HH>
-__global__ __launch_bounds__(256) void diff_bwd_dq_kernel(DiffAttnArgs a) {
-    typedef Tile<T, HH> Tl;
+// Eight wavefronts, SPLITS = 2 or 4 for each 16 columns: they take every SPLITS-th 16 rows of a tile, and what they have is added up in the end, by
+// halves.  A work-group has 64 columns, or 32 where that makes too few of them for the compute units (see narrow()).
+template <int COLS> struct Share {
+    static constexpr int GROUPS = COLS / 16, SPLITS = 8 / GROUPS;
+};
+template <int COLS, int N> __device__ __forceinline__ void join_shares(float* lds, int split, int t, f32x4_t (&acc)[N]) {
+#pragma unroll
+    for (int half = Share<COLS>::SPLITS / 2; half >= 1; half /= 2) {
+        f32x4_t* p = reinterpret_cast<f32x4_t*>(lds) + (t - (split >= half ? half : 0) * (4 * COLS));
+        __syncthreads();                                // what the memory held before has been read
+        if (split >= half && split < 2 * half)
+#pragma unroll
+            for (int i = 0; i < N; ++i) p[256 * i] = acc[i];
+        __syncthreads();
+        if (split < half)
+#pragma unroll
+            for (int i = 0; i < N; ++i) acc[i] += p[256 * i];
+    }
+}
+
+template <class T, int HH, int COLS>
+__global__ __launch_bounds__(512, HH <= 32 ? 4 : 2) void diff_bwd_dq_kernel(DiffAttnArgs a) {
+    typedef Tile<T, HH, 512> Tl;
     constexpr int KT = Tl::ROWS, NS = HH / 8;
-    __shared__ __attribute__((aligned(16))) float sK[Tl::FLOATS];
-    __shared__ __attribute__((aligned(16))) float sV[Tl::FLOATS];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4;
-    const ColumnBlock cb = column_block(a, a.q_len, a.mask != 0);
+    __shared__ __attribute__((aligned(16))) float lds[2 * Tl::FLOATS];
+    static_assert(2 * Tl::FLOATS >= 256 * 4 * NS, "the sums of four wavefronts");
+    float *const sK = lds, *const sV = lds + Tl::FLOATS;
+    const int t = threadIdx.x, lane = t & 63, wave8 = __builtin_amdgcn_readfirstlane(t >> 6), g = lane >> 4;
+    const int wave = wave8 % Share<COLS>::GROUPS, split = wave8 / Share<COLS>::GROUPS;
+    const ColumnBlock cb = column_block<COLS>(a, a.q_len, a.mask != 0);
     if (cb.first < 0) return;
     const int s = cb.s, h = cb.h, q0 = cb.first, ql = a.q_len[s], kl = a.k_len[s], hd = a.head_dim, half = hd / 2;
     const bool vec = a.vec;
@@ -313,7 +342,7 @@ __global__ __launch_bounds__(256) void diff_bwd_dq_kernel(DiffAttnArgs a) {
         for (int i = 0; i < NS; ++i) d2 += (f[i].x * dof[i].x + f[i].y * dof[i].y) + (f[i].z * dof[i].z + f[i].w * dof[i].w);
         d2 = groups_sum(d2);
         d1 = groups_sum(d1) + lam * d2;
-        if (g == 0 && qi < ql) {
+        if (g == 0 && qi < ql && split == 0) {
             a.d1[(size_t)h * a.q_total_rows + row] = d1;
             a.d2[(size_t)h * a.q_total_rows + row] = d2;
         }
@@ -324,7 +353,7 @@ __global__ __launch_bounds__(256) void diff_bwd_dq_kernel(DiffAttnArgs a) {
 #pragma unroll
     for (int i = 0; i < NS; ++i) gacc[i] = zero4();
     float lam_sum = 0.f;
-    const int kv_end = a.mask ? min(kl, q0 + 64) : kl;
+    const int kv_end = a.mask ? min(kl, q0 + COLS) : kl;
     const int wave_last = a.mask ? min(kl - 1, qw0 + 15) : kl - 1;
     Tl tk, tv;
     if (kv_end > 0) {
@@ -342,39 +371,51 @@ __global__ __launch_bounds__(256) void diff_bwd_dq_kernel(DiffAttnArgs a) {
         }
         if (qw0 >= ql) continue;
 #pragma unroll
-        for (int kt = 0; kt < KT / 16; ++kt) {
+        for (int i = 0; i < KT / 16 / Share<COLS>::SPLITS; ++i) {
+            const int kt = Share<COLS>::SPLITS * i + split;
             if (k0 + 16 * kt > wave_last) break;
             f32x4_t p1 = first_product<HH, 0, NS / 2>(sK, 16 * kt, lane, qf);
             f32x4_t p2 = first_product<HH, NS / 2, NS>(sK, 16 * kt, lane, qf);
             const f32x4_t gr = first_product<HH, 0, NS>(sV, 16 * kt, lane, dof);
+            const int kb = k0 + 16 * kt;
+            if (kb + 16 > kl || (a.mask && kb + 15 > qw0))
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int key = kb + 4 * g + e;
+                    if (key >= kl || (a.mask && key > qi)) p1[e] = p2[e] = -INFINITY;
+                }
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const int key = k0 + 16 * kt + 4 * g + e;
-                const bool hidden = key >= kl || (a.mask && key > qi);
                 const float u1 = __builtin_amdgcn_exp2f(__builtin_fmaf(p1[e], c, -e1)), u2 = __builtin_amdgcn_exp2f(__builtin_fmaf(p2[e], c, -e2));
-                p1[e] = hidden ? 0.f : u1 * (gr[e] - d1);
-                p2[e] = hidden ? 0.f : -lam * u2 * (gr[e] - d2);
-                lam_sum += hidden ? 0.f : u2 * gr[e];
+                lam_sum = __builtin_fmaf(u2, gr[e], lam_sum);
+                p1[e] = u1 * (gr[e] - d1);
+                p2[e] = u2 * (d2 - gr[e]) * lam;
             }
             second_product<HH, 0, NS / 2>(sK, 16 * kt, lane, p1, gacc);
             second_product<HH, NS / 2, NS>(sK, 16 * kt, lane, p2, gacc);
         }
     }
-    lam_sum = wave_sum(qi < ql ? lam_sum : 0.f);
+    join_shares<COLS>(lds, split, t, gacc);
+    f32x4_t lam_join[1] = {{lam_sum, 0.f, 0.f, 0.f}};
+    join_shares<COLS>(lds, split, t, lam_join);
+    if (split != 0) return;
+    lam_sum = wave_sum(qi < ql ? lam_join[0][0] : 0.f);
     if (lane == 0 && qw0 < ql) a.lam_part[(size_t)h * a.q_total_rows + qrow0 + qw0] = lam_sum;
     if (qi < ql) store_column<T, HH>(gacc, a.scale, (T*)a.dq + (qrow0 + qi) * a.ldq + (long long)h * hd, half, g, vec);
 }
 
 // ---------------------------------------------------------------- backward: dK, dV
-template <class T, int HH>
-__global__ __launch_bounds__(256) void diff_bwd_dkv_kernel(DiffAttnArgs a) {
-    typedef Tile<T, HH> Tl;
+template <class T, int HH, int COLS>
+__global__ __launch_bounds__(512, HH <= 32 && COLS == 64 ? 4 : 2) void diff_bwd_dkv_kernel(DiffAttnArgs a) {
+    typedef Tile<T, HH, 512> Tl;
     constexpr int QT = Tl::ROWS, NS = HH / 8;
-    __shared__ __attribute__((aligned(16))) float sQ[Tl::FLOATS];
-    __shared__ __attribute__((aligned(16))) float sO[Tl::FLOATS];
+    __shared__ __attribute__((aligned(16))) float lds[2 * Tl::FLOATS];
+    static_assert(2 * Tl::FLOATS >= 256 * 4 * NS, "the sums of four wavefronts");
+    float *const sQ = lds, *const sO = lds + Tl::FLOATS;
     __shared__ __attribute__((aligned(16))) float stat[4][QT];         // log-sum-exps (exp2 domain), D_1, D_2 of the tile's queries
-    const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), g = lane >> 4;
-    const ColumnBlock cb = column_block(a, a.k_len, false);
+    const int t = threadIdx.x, lane = t & 63, wave8 = __builtin_amdgcn_readfirstlane(t >> 6), g = lane >> 4;
+    const int wave = wave8 % Share<COLS>::GROUPS, split = wave8 / Share<COLS>::GROUPS;
+    const ColumnBlock cb = column_block<COLS>(a, a.k_len, false);
     if (cb.first < 0) return;
     const int s = cb.s, h = cb.h, k0 = cb.first, ql = a.q_len[s], kl = a.k_len[s], hd = a.head_dim, half = hd / 2;
     const bool vec = a.vec;
@@ -414,7 +455,8 @@ __global__ __launch_bounds__(256) void diff_bwd_dkv_kernel(DiffAttnArgs a) {
         if (q0 + QT < ql) fetch(q0 + QT);
         if (kw0 >= kl) continue;
 #pragma unroll
-        for (int qt = 0; qt < QT / 16; ++qt) {
+        for (int i = 0; i < QT / 16 / Share<COLS>::SPLITS; ++i) {
+            const int qt = Share<COLS>::SPLITS * i + split;
             const int qb = q0 + 16 * qt;
             if (qb >= ql || (a.mask && qb + 15 < kw0)) continue;       // no visible query
             f32x4_t p1 = first_product<HH, 0, NS / 2>(sQ, 16 * qt, lane, kf);
@@ -423,22 +465,26 @@ __global__ __launch_bounds__(256) void diff_bwd_dkv_kernel(DiffAttnArgs a) {
             f32x4_t p;
             const f32x4_t e1 = *reinterpret_cast<const f32x4_t*>(&stat[0][16 * qt + 4 * g]), e2 = *reinterpret_cast<const f32x4_t*>(&stat[1][16 * qt + 4 * g]);
             const f32x4_t d1 = *reinterpret_cast<const f32x4_t*>(&stat[2][16 * qt + 4 * g]), d2 = *reinterpret_cast<const f32x4_t*>(&stat[3][16 * qt + 4 * g]);
+            // queries past the last one need no mask: they are zeros, their statistics too, so that a probability of 1 multiplies nothing
+            if (a.mask && qb < kw0 + 15)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (qb + 4 * g + e < ki) p1[e] = p2[e] = -INFINITY;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const int q = qb + 4 * g + e;
-                const bool hidden = q >= ql || (a.mask && q < ki);
-                const float u1 = hidden ? 0.f : __builtin_amdgcn_exp2f(__builtin_fmaf(p1[e], c, -e1[e]));
-                const float u2 = hidden ? 0.f : lam * __builtin_amdgcn_exp2f(__builtin_fmaf(p2[e], c, -e2[e]));
+                const float u1 = __builtin_amdgcn_exp2f(__builtin_fmaf(p1[e], c, -e1[e])), u2 = lam * __builtin_amdgcn_exp2f(__builtin_fmaf(p2[e], c, -e2[e]));
                 p[e] = u1 - u2;
-                p1[e] = hidden ? 0.f : u1 * (gr[e] - d1[e]);
-                p2[e] = hidden ? 0.f : -u2 * (gr[e] - d2[e]);
+                p1[e] = u1 * (gr[e] - d1[e]);
+                p2[e] = u2 * (d2[e] - gr[e]);
             }
             second_product<HH, 0, NS>(sO, 16 * qt, lane, p, dv);
             second_product<HH, 0, NS / 2>(sQ, 16 * qt, lane, p1, dk);
             second_product<HH, NS / 2, NS>(sQ, 16 * qt, lane, p2, dk);
         }
     }
-    if (ki >= kl) return;
+    join_shares<COLS>(lds, split, t, dk);
+    join_shares<COLS>(lds, split, t, dv);
+    if (split != 0 || ki >= kl) return;
     store_column<T, HH>(dk, a.scale, (T*)a.dk + (krow0 + ki) * a.ldk + (long long)h * hd, half, g, vec);
     store_column<T, HH>(dv, 1.0f, (T*)a.dv + (krow0 + ki) * a.ldv + (long long)h * hd, half, g, vec);
 }
@@ -468,11 +514,24 @@ template <class T, int HH> void fwd_launch(const DiffAttnArgs& a, hipStream_t st
     const dim3 grid = a.k_splits > 1 ? dim3(a.k_splits, a.n_heads, a.n_seq) : column_grid(a, a.max_q_len);
     hipLaunchKernelGGL((diff_fwd_kernel<T, HH>), grid, dim3(256), 0, st, a);
 }
+// Fewer work-groups of 64 columns than two for a compute unit: 32 columns each.  64 -> 32, dQ and dK/dV together, fp32, heads of 64: 23 sequences of 88
+// to 177, 4 heads, causal (276 work-groups) 59 -> 52 us; 3 of 100 to 200, 2 heads 50 -> 35; but 31 of 366 to 523, 16 heads (4 464) 1 114 -> 1 226.
+bool narrow(const AttnArgs& a, int max_len) { return (long long)a.n_seq * a.n_heads * (max_len / 64 + 1) <= 2LL * gemm_cu_count(); }
 template <class T, int HH> void dq_launch(const DiffAttnArgs& a, hipStream_t st) {
-    hipLaunchKernelGGL((diff_bwd_dq_kernel<T, HH>), column_grid(a, a.max_q_len), dim3(256), 0, st, a);
+    if constexpr (HH <= 48)                             // (above, a tile has no 16 rows for each of four wavefronts)
+        if (narrow(a, a.max_q_len)) {
+            hipLaunchKernelGGL((diff_bwd_dq_kernel<T, HH, 32>), column_grid(a, a.max_q_len, 32), dim3(512), 0, st, a);
+            return;
+        }
+    hipLaunchKernelGGL((diff_bwd_dq_kernel<T, HH, 64>), column_grid(a, a.max_q_len), dim3(512), 0, st, a);
 }
 template <class T, int HH> void dkv_launch(const DiffAttnArgs& a, hipStream_t st) {
-    hipLaunchKernelGGL((diff_bwd_dkv_kernel<T, HH>), column_grid(a, a.max_k_len), dim3(256), 0, st, a);
+    if constexpr (HH <= 48)
+        if (narrow(a, a.max_k_len)) {
+            hipLaunchKernelGGL((diff_bwd_dkv_kernel<T, HH, 32>), column_grid(a, a.max_k_len, 32), dim3(512), 0, st, a);
+            return;
+        }
+    hipLaunchKernelGGL((diff_bwd_dkv_kernel<T, HH, 64>), column_grid(a, a.max_k_len), dim3(512), 0, st, a);
 }
 
 }  // namespace
