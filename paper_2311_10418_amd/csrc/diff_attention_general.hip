@@ -6,6 +6,10 @@
 // are per-lane scalars, and register e of a block is, as it stands, the B operand of the second product for the rows {4 g + e}.
 // Tiles of the other side are kept in LDS row by row, every half head padded with zeros to HH columns (a multiple of 16), V and dO too:
 // the contraction over features does not see the order of the columns, and outputs go back through the same mapping.
+//
+// Bound by issue: the matrix pipe is busy 60 % of the SIMD cycles and vector instructions, more than two for each matrix instruction, take the rest.
+// Measured in fp32: 16 heads of 64, 31 sequences of 366 to 523, unmasked, forward 421 us, backward 1 011 (90 and 87 TFLOP/s
+// of the products they form, where a large product of matrices reaches 154); 4 heads of 64, 23 sequences of 88 to 177, causal, backward 45.
 #include "diff_attention.hpp"
 #include "gemm.hpp"
 #include <type_traits>

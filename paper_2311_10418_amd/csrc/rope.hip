@@ -3,7 +3,9 @@
 // amplitude, which is also the gradient.  Pairs are (2p, 2p + 1), interleaved, or (p, p + rot / 2), halves.
 //
 // Bound by memory: every value is read and written once.  An angle is the same for all heads of a row, so a thread keeps the
-// cosines and sines of its pairs in registers and walks over heads.
+// cosines and sines of its pairs in registers and walks over heads (about four: more of them would leave too few threads for the transfers).
+// Measured: bf16, 65 582 rows of 64 heads of 64, 205 us (5.2 TB/s; a large copy 5.0); fp32, interleaved, half of every head of 128, 7 685 rows of 8,
+// 13.3 us (4.8 TB/s); 64 rows of 64 heads of 64 4 us, a launch.
 #include "common.hpp"
 
 #include <cmath>
