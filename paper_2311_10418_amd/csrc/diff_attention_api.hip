@@ -1,5 +1,6 @@
 // C-ABI entry points and dispatch of differential attention.
 #include "diff_attention.hpp"
+#include "gemm.hpp"
 #include <algorithm>
 #include <cmath>
 
@@ -93,6 +94,13 @@ extern "C" ds_status ds_diff_attention_fwd(int32_t dtype, int32_t n_seq, int32_t
     return diff_fwd_general(a, (hipStream_t)hip_stream);
 }
 
+// Backward, few sequences of at most 16 tokens: launches are all that counts, and the general kernels round nothing but the results, which shows where a
+// gradient is the difference of few terms.  Matrix-core / general kernels, 16 heads of 64 (128), us: 16 sequences of 8 16.6 / 16.5 (22.5 / 22.3), of 16
+// 17.1 / 17.0 (23.1 / 23.2), of 32 18.6 / 19.4 (23.9 / 27.6); 32 of 16 18.4 / 25.7 (31.5 / 40.5).
+static bool fp32_costs_nothing(const DiffAttnArgs& a) {
+    return a.max_q_len <= 16 && a.max_k_len <= 16 && (long long)a.n_seq * a.n_heads <= gemm_cu_count();
+}
+
 extern "C" ds_status ds_diff_attention_bwd(int32_t dtype, int32_t n_seq, int32_t n_heads, int32_t head_dim, int32_t mask, const int32_t* q_row,
                                            const int32_t* q_len, const int32_t* k_row, const int32_t* k_len, int32_t max_q_len, int32_t max_k_len,
                                            const void* q, int32_t ldq, const void* k, int32_t ldk, const void* v, int32_t ldv, const float* lambda,
@@ -113,6 +121,6 @@ extern "C" ds_status ds_diff_attention_bwd(int32_t dtype, int32_t n_seq, int32_t
     const ds_status r = check(a);
     if (r != DS_OK) return r;
     if (!o2 || !d_o || !dq || !dk || !dv || !dlambda || (accumulate != 0 && accumulate != 1)) return DS_EINVAL;
-    if (!force_generic && diff_mfma_supported(a)) return diff_bwd_mfma(a, (hipStream_t)hip_stream);
+    if (!force_generic && !fp32_costs_nothing(a) && diff_mfma_supported(a)) return diff_bwd_mfma(a, (hipStream_t)hip_stream);
     return diff_bwd_general(a, (hipStream_t)hip_stream);
 }

@@ -157,6 +157,14 @@ def test_short_queries(dt, generic, causal, hd):
         Case(hd + q[0], dt, 8, hd, q[:1], [33], causal).run(generic)
 
 
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("hd", [64, 128])
+def test_very_short_sequences(causal, hd):
+    """At most 16 tokens: bf16 calls that need not round what they multiply, few or many of them."""
+    Case(hd, BF, 2, hd, [16, 1, 9, 0, 12], [16, 3, 9, 5, 0], causal).run(False)
+    Case(hd + 1, BF, 16, hd, [16, 7] * 9, [16, 7] * 9, causal).run(False, accumulate=True)
+
+
 @pytest.mark.parametrize("dt,generic", KINDS)
 @pytest.mark.parametrize("hd", [16, 64, 96, 128])
 def test_few_queries_over_long_keys(dt, generic, hd):
