@@ -271,3 +271,99 @@ def test_token_by_token(dt, heads, hd):
         torch.cuda.synchronize()
         for name, got, which in (("y", y, 0), ("u", u, 1)):
             check(to_np(got), torch.stack([e[which][t] for e, t in zip(exact, at)]).numpy(), TOL[dt], "%s step %d" % (name, step))
+
+
+@pytest.mark.parametrize("dt", [F32, BF])
+def test_two_blocks_at_once(dt):
+    """Two blocks with workspaces of their own, forward and backward on two streams, neither waiting for the other: the bits of each alone."""
+    blocks = [Block(*_problem(20 + i, lens, cuts, 4, 64, dt), 4, dt) for i, (lens, cuts) in enumerate([([200, 130, 5], [0, 3]), ([64, 300], [0, 1, 2])])]
+    want = []
+    for b in blocks:
+        b.forward()
+        b.backward()
+        torch.cuda.synchronize()
+        want.append(b.results())
+    streams = [torch.cuda.Stream() for _ in blocks]
+    for b in blocks:
+        for t in (b.y, b.u, b.dx):                     # (what a run writes whole; padding rows of o and dqkv have to stay zeros)
+            t.fill_(3.0)
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for b, st in zip(blocks, streams):
+            b.forward(st.cuda_stream)
+        for b, st in zip(blocks, streams):
+            b.backward(st.cuda_stream)
+    torch.cuda.synchronize()
+    for b, ref in zip(blocks, want):
+        assert all(torch.equal(x, y) for x, y in zip(b.results(), ref))
+
+
+FAR = 1 << 31                                           # elements of a tensor in front of the rows looked at
+
+
+def test_rows_behind_two_to_the_31_elements():
+    """The joint and the rotation on tensors of more than 2^31 elements: what the last row gets is what it gets alone."""
+    d = 4096
+    rows = FAR // d + 3
+    rng = np.random.default_rng(2)
+    rnd = lambda *s: torch.from_numpy(rng.standard_normal(s).astype(np.float32)).to(DEV).to(BF)  # noqa: E731
+    g = [rnd(d) for _ in range(5)]                      # gains, biases, gate
+    last = [rnd(1, d) for _ in range(4)]                # x, h, dy, du
+
+    def run(n):
+        x, h, dy, du = (torch.zeros((n, d), dtype=BF, device=DEV) for _ in range(4))
+        for t, v in zip((x, h, dy, du), last):
+            t[n - 1:] = v
+        st = torch.zeros((4, n), device=DEV)
+        u, dx = torch.zeros_like(h), torch.zeros_like(h)
+        ds.ds_resid_norm_fwd(x, h, x, st, g[0], g[1], g[4], g[2], g[3], u, 0.5, 2.0)
+        sums = [torch.zeros(d, device=DEV) for _ in range(5)]
+        part = torch.zeros(int(ds.ds_resid_norm_bwd_scratch_floats(n, d)), device=DEV)
+        ds.ds_resid_norm_bwd(dy, x, h, st, dx, h, part, du, g[0], g[1], g[4], g[2], sums[0], *sums[1:], 0.5, 2.0)
+        torch.cuda.synchronize()
+        return [t[n - 1:].clone() for t in (x, u, dx, h)] + [st[:, n - 1:].clone()]
+
+    for a, b in zip(run(rows), run(1)):
+        assert torch.equal(a, b)
+    heads, hd = 32, 128
+    x = torch.zeros((rows, d), dtype=BF, device=DEV)
+    x[rows - 1:] = last[0]
+    pos, freq = torch.full((rows,), 77, dtype=torch.int32, device=DEV), torch.from_numpy(ds.ds_rope_freqs(hd)).to(DEV)
+    one = last[0].clone()
+    ds.ds_rope(x, x, pos, freq, heads, hd, hd)
+    ds.ds_rope(one, one, pos[:1], freq, heads, hd, hd)
+    torch.cuda.synchronize()
+    assert torch.equal(x[rows - 1:], one) and not x[:rows - 1:4096].any()
+
+
+@pytest.mark.parametrize("generic", [False, True])
+@pytest.mark.parametrize("ql,kl,causal", [(200, 200, True), (1, 1300, False), (12, 12, True)])
+def test_attention_behind_two_to_the_31_elements(generic, ql, kl, causal):
+    """Queries and keys in rows far down a wide tensor (a long cache), short and long: the bits of the same sequence in a compact one."""
+    heads, hd, ld = 2, 64, 1 << 16
+    w = heads * hd
+    rng = np.random.default_rng(3)
+    rnd = lambda n: torch.from_numpy(rng.standard_normal((n, w)).astype(np.float32)).to(DEV).to(BF)  # noqa: E731
+    q, k, v, d_o = rnd(ql), rnd(kl), rnd(kl), rnd(ql)
+    lam = torch.tensor([0.3, 0.7], device=DEV)
+    i32 = lambda a: torch.tensor([a], dtype=torch.int32, device=DEV)  # noqa: E731
+
+    def run(front, ld):
+        qf = front if ql > 1 else 0                     # (a single token has a tensor of its own)
+
+        def place(t, n):
+            big = torch.zeros((n + t.shape[0], ld), dtype=BF, device=DEV)
+            big[n:, :w] = t
+            return big[:, :w]
+        tq, tk, tv, to = place(q, qf), place(k, front), place(v, front), place(d_o, qf)
+        o, o2, dq, dk, dv = (place(torch.zeros_like(t), n) for t, n in ((q, qf), (q, qf), (q, qf), (k, front), (v, front)))
+        lse, dlam = torch.zeros((2 * heads, qf + ql), device=DEV), torch.zeros(heads, device=DEV)
+        scratch = torch.zeros(int(ds.ds_diff_attention_scratch_bytes(heads, qf + ql, front + kl, 1)), dtype=torch.uint8, device=DEV)
+        rest = (i32(qf), i32(ql), i32(front), i32(kl), heads, hd, causal, ql, kl, scratch)
+        ds.ds_diff_attention_fwd(tq, tk, tv, lam, o, lse, *rest, o2=o2, force_generic=generic)
+        ds.ds_diff_attention_bwd(tq, tk, tv, lam, o, o2, to, lse, dq, dk, dv, dlam, *rest, force_generic=generic)
+        torch.cuda.synchronize()
+        return [t[qf:].clone() for t in (o, o2, dq)] + [dk[front:].clone(), dv[front:].clone(), lse[:, qf:].clone(), dlam]
+
+    for a, b in zip(run(FAR // ld + 5, ld), run(0, w)):
+        assert torch.equal(a, b)
