@@ -8,6 +8,7 @@
 // (dlambda is summed from the probabilities themselves, in fp32, and not from O_2, which is rounded to the tensors' type.)
 #pragma once
 #include "attention.hpp"
+#include "common.hpp"
 
 struct DiffAttnArgs : AttnArgs {                        // scale: 1 / sqrt(head_dim / 2); lse: [2 n_heads][lse_stride], map m of head h at row 2h + m
     const float* lambda;                                // [n_heads]
@@ -47,5 +48,24 @@ ds_status diff_bwd_general(const DiffAttnArgs& a, hipStream_t st);
 bool diff_mfma_supported(const DiffAttnArgs& a);
 ds_status diff_fwd_mfma(const DiffAttnArgs& a, hipStream_t st);
 ds_status diff_bwd_mfma(const DiffAttnArgs& a, hipStream_t st);
-// dlambda[h] = (accumulate ? dlambda[h] : 0) - the sums in lam_part, which stand `queries` rows apart within a sequence
-ds_status diff_dlambda(const DiffAttnArgs& a, int queries, hipStream_t st);
+// dlambda[h] = (accumulate ? dlambda[h] : 0) - the sums in lam_part, which stand QUERIES rows apart within a sequence: a work-group of the dK/dV launch
+// for each head, 16 threads for a sequence, in a fixed order.  (A launch of its own took 4 us.)
+template <int QUERIES, int THREADS> __device__ __forceinline__ void sum_dlambda(const DiffAttnArgs& a, int h, float* lds) {
+    const int lane = threadIdx.x & 15;
+    const float* p = a.lam_part + (size_t)h * a.q_total_rows;
+    float sum = 0.f;
+#pragma unroll 4
+    for (int s = threadIdx.x >> 4; s < a.n_seq; s += THREADS / 16) {
+        const int n = (a.q_len[s] + QUERIES - 1) / QUERIES;
+        const float* q = p + a.q_row[s];
+        for (int i = lane; i < n; i += 16) sum += q[(size_t)i * QUERIES];
+    }
+    sum = wave_sum(sum);
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = sum;
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+    sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; ++w) sum += lds[w];
+    a.dlambda[h] = (a.accumulate ? a.dlambda[h] : 0.f) - sum;
+}

@@ -44,7 +44,7 @@ static ds_status check(DiffAttnArgs& a) {
     if (a.mask != 0 && a.mask != 1) return DS_EINVAL;
     if (!a.q_row || !a.q_len || !a.k_row || !a.k_len || !a.q || !a.k || !a.v || !a.lambda || !a.o || !a.lse) return DS_EINVAL;
     if (a.max_q_len <= 0 || a.max_k_len <= 0 || a.q_total_rows <= 0 || a.k_total_rows <= 0) return DS_EINVAL;
-    if (a.n_seq > 65535 || a.n_heads > 65535) return DS_EINVAL;
+    if (a.n_seq > 65534 || a.n_heads > 65535) return DS_EINVAL;
     const long long wide = (long long)a.n_heads * a.head_dim;
     if (a.ldq < wide || a.ldk < wide || a.ldv < wide || a.ldo < wide) return DS_EINVAL;
     if (!a.scratch || (uintptr_t)a.scratch % 16 || a.scratch_bytes < diff_scratch_bytes(a.n_heads, a.q_total_rows, a.k_total_rows, a.n_seq)) return DS_EINVAL;
@@ -94,10 +94,11 @@ extern "C" ds_status ds_diff_attention_fwd(int32_t dtype, int32_t n_seq, int32_t
     return diff_fwd_general(a, (hipStream_t)hip_stream);
 }
 
-// Backward, few sequences of at most 16 tokens: launches are all that counts, and the general kernels round nothing but the results, which shows where a
-// gradient is the difference of few terms.  Matrix-core / general kernels, 16 heads of 64 (128), us: 16 sequences of 8 16.6 / 16.5 (22.5 / 22.3), of 16
-// 17.1 / 17.0 (23.1 / 23.2), of 32 18.6 / 19.4 (23.9 / 27.6); 32 of 16 18.4 / 25.7 (31.5 / 40.5).
-static bool fp32_costs_nothing(const DiffAttnArgs& a) {
+// Backward, few sequences of at most 16 tokens: launches are nearly all that counts, and the general kernels round nothing but the results, which shows
+// where a gradient is the difference of few terms (relative error of dQ and dK, 18 sequences of up to 12: 0.0031 -> 0.0017).  Matrix-core / general
+// kernels, 16 heads of 64 (128), us: 16 sequences of 8 14.4 / 14.8 (20.2 / 20.9), of 16 14.8 / 15.4 (20.7 / 21.7), of 32 15.9 / 17.8 (21.4 / 26.2); 32 of 16
+// 16.8 / 23.8 (28.4 / 38.6).
+static bool short_in_fp32(const DiffAttnArgs& a) {
     return a.max_q_len <= 16 && a.max_k_len <= 16 && (long long)a.n_seq * a.n_heads <= gemm_cu_count();
 }
 
@@ -121,6 +122,6 @@ extern "C" ds_status ds_diff_attention_bwd(int32_t dtype, int32_t n_seq, int32_t
     const ds_status r = check(a);
     if (r != DS_OK) return r;
     if (!o2 || !d_o || !dq || !dk || !dv || !dlambda || (accumulate != 0 && accumulate != 1)) return DS_EINVAL;
-    if (!force_generic && !fp32_costs_nothing(a) && diff_mfma_supported(a)) return diff_bwd_mfma(a, (hipStream_t)hip_stream);
+    if (!force_generic && !short_in_fp32(a) && diff_mfma_supported(a)) return diff_bwd_mfma(a, (hipStream_t)hip_stream);
     return diff_bwd_general(a, (hipStream_t)hip_stream);
 }

@@ -187,7 +187,12 @@ __global__ __launch_bounds__(256, HD == 64 ? 2 : 1) void diff_bwd_dkv_mfma_kerne
     PieceLoader<HD> ldQ, ldO;
     ldQ.setup(nullptr, a.ldq, 0, wave, lane);
     ldO.setup(nullptr, a.ldo, 0, wave, lane);
-    WorkDraw draw(a, 1);
+    const int first = (a.n_heads + 7) / 8 * 8;          // the first work-groups sum up dlambda
+    if ((int)blockIdx.x < first) {
+        if ((int)blockIdx.x < a.n_heads) sum_dlambda<32, 256>(a, blockIdx.x, reinterpret_cast<float*>(smem));
+        return;
+    }
+    LateDraw draw(a, 1, first);
     int kw0, ki, kl, ql, h, q_begin, nb;
     long long krow0;
     const char* aug_src;
@@ -401,10 +406,10 @@ ds_status bwd_launch(const DiffAttnArgs& a, hipStream_t st) {
     if (r != DS_OK) return r;
     hipLaunchKernelGGL(kq, dim3((unsigned)a.max_items_q * a.n_heads), dim3(256), smem_q, st, a);
     DS_LAUNCH_CHECK();
-    const unsigned items_kv = (unsigned)a.max_items_k * a.n_heads;
-    hipLaunchKernelGGL(kkv, dim3(HD == 128 ? persistent_grid(items_kv) : items_kv), dim3(256), smem_kv, st, a);
+    const unsigned items_kv = (unsigned)a.max_items_k * a.n_heads, for_dlambda = (a.n_heads + 7) / 8 * 8;
+    hipLaunchKernelGGL(kkv, dim3((HD == 128 ? persistent_grid(items_kv) : items_kv) + for_dlambda), dim3(256), smem_kv, st, a);
     DS_LAUNCH_CHECK();
-    return diff_dlambda(a, 32, st);
+    return DS_OK;
 }
 
 }  // namespace

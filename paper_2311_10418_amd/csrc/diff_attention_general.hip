@@ -119,8 +119,8 @@ __device__ __forceinline__ float groups_sum(float v) { v += __shfl_xor(v, 16, 64
 // A work-group's COLS columns: sequence, head, first column (negative: nothing to do).  Sequences last to first: a plan lists them by
 // ascending length, and the longest chains of tiles should start first.
 struct ColumnBlock { int s, h, first; };
-template <int COLS = 64> __device__ __forceinline__ ColumnBlock column_block(const AttnArgs& a, const int32_t* len, bool last_first) {
-    ColumnBlock c = {a.n_seq - 1 - (int)blockIdx.z, (int)blockIdx.y, -1};
+template <int COLS = 64> __device__ __forceinline__ ColumnBlock column_block(const AttnArgs& a, const int32_t* len, bool last_first, int z) {
+    ColumnBlock c = {a.n_seq - 1 - z, (int)blockIdx.y, -1};
     const int n = (len[c.s] + COLS - 1) / COLS, b = blockIdx.x;
     if (b < n) c.first = COLS * (last_first ? n - 1 - b : b);
     return c;
@@ -136,7 +136,7 @@ __global__ __launch_bounds__(256, HH <= 32 ? 3 : 2) void diff_fwd_kernel(DiffAtt
     __shared__ __attribute__((aligned(16))) float sK[Tl::FLOATS];
     __shared__ __attribute__((aligned(16))) float sV[Tl::FLOATS];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4;
-    ColumnBlock cb = column_block(a, a.q_len, a.mask != 0);
+    ColumnBlock cb = column_block(a, a.q_len, a.mask != 0, blockIdx.z);
     const int split = a.k_splits > 1 ? blockIdx.x : 0;                 // (one block of queries then)
     if (a.k_splits > 1) cb.first = a.q_len[cb.s] > 0 ? 0 : -1;
     if (cb.first < 0) return;
@@ -322,7 +322,7 @@ __global__ __launch_bounds__(512, HH <= 32 ? 4 : 2) void diff_bwd_dq_kernel(Diff
     float *const sK = lds, *const sV = lds + Tl::FLOATS;
     const int t = threadIdx.x, lane = t & 63, wave8 = __builtin_amdgcn_readfirstlane(t >> 6), g = lane >> 4;
     const int wave = wave8 % Share<COLS>::GROUPS, split = wave8 / Share<COLS>::GROUPS;
-    const ColumnBlock cb = column_block<COLS>(a, a.q_len, a.mask != 0);
+    const ColumnBlock cb = column_block<COLS>(a, a.q_len, a.mask != 0, blockIdx.z);
     if (cb.first < 0) return;
     const int s = cb.s, h = cb.h, q0 = cb.first, ql = a.q_len[s], kl = a.k_len[s], hd = a.head_dim, half = hd / 2;
     const bool vec = a.vec;
@@ -419,7 +419,11 @@ __global__ __launch_bounds__(512, HH <= 32 && COLS == 64 ? 4 : 2) void diff_bwd_
     __shared__ __attribute__((aligned(16))) float stat[4][QT];         // log-sum-exps (exp2 domain), D_1, D_2 of the tile's queries
     const int t = threadIdx.x, lane = t & 63, wave8 = __builtin_amdgcn_readfirstlane(t >> 6), g = lane >> 4;
     const int wave = wave8 % Share<COLS>::GROUPS, split = wave8 / Share<COLS>::GROUPS;
-    const ColumnBlock cb = column_block<COLS>(a, a.k_len, false);
+    if (blockIdx.z == 0) {                              // a layer of work-groups more, which start first: one for each head sums up dlambda
+        if (blockIdx.x == 0) sum_dlambda<16, 512>(a, blockIdx.y, lds);
+        return;
+    }
+    const ColumnBlock cb = column_block<COLS>(a, a.k_len, false, blockIdx.z - 1);
     if (cb.first < 0) return;
     const int s = cb.s, h = cb.h, k0 = cb.first, ql = a.q_len[s], kl = a.k_len[s], hd = a.head_dim, half = hd / 2;
     const bool vec = a.vec;
@@ -493,27 +497,6 @@ __global__ __launch_bounds__(512, HH <= 32 && COLS == 64 ? 4 : 2) void diff_bwd_
     store_column<T, HH>(dv, 1.0f, (T*)a.dv + (krow0 + ki) * a.ldv + (long long)h * hd, half, g, vec);
 }
 
-// ---------------------------------------------------------------- dlambda: one work-group per head, a wavefront per sequence, fixed order
-__global__ __launch_bounds__(1024) void diff_dlambda_kernel(DiffAttnArgs a, int queries) {
-    __shared__ float part[16];
-    const int h = blockIdx.x, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const float* p = a.lam_part + (size_t)h * a.q_total_rows;
-    float sum = 0.f;
-    for (int s = wave; s < a.n_seq; s += 16) {
-        const int n = (a.q_len[s] + queries - 1) / queries;
-        const float* q = p + a.q_row[s];
-        for (int i = lane; i < n; i += 64) sum += q[(size_t)i * queries];
-    }
-    sum = wave_sum(sum);
-    if (lane == 0) part[wave] = sum;
-    __syncthreads();
-    if (threadIdx.x != 0) return;
-    sum = 0.f;
-#pragma unroll
-    for (int w = 0; w < 16; ++w) sum += part[w];
-    a.dlambda[h] = (a.accumulate ? a.dlambda[h] : 0.f) - sum;
-}
-
 template <class T, int HH> void fwd_launch(const DiffAttnArgs& a, hipStream_t st) {
     const dim3 grid = a.k_splits > 1 ? dim3(a.k_splits, a.n_heads, a.n_seq) : column_grid(a, a.max_q_len);
     hipLaunchKernelGGL((diff_fwd_kernel<T, HH>), grid, dim3(256), 0, st, a);
@@ -529,13 +512,14 @@ template <class T, int HH> void dq_launch(const DiffAttnArgs& a, hipStream_t st)
         }
     hipLaunchKernelGGL((diff_bwd_dq_kernel<T, HH, 64>), column_grid(a, a.max_q_len), dim3(512), 0, st, a);
 }
+dim3 and_dlambda(dim3 g) { return dim3(g.x, g.y, g.z + 1); }
 template <class T, int HH> void dkv_launch(const DiffAttnArgs& a, hipStream_t st) {
     if constexpr (HH <= 48)
         if (narrow(a, a.max_k_len)) {
-            hipLaunchKernelGGL((diff_bwd_dkv_kernel<T, HH, 32>), column_grid(a, a.max_k_len, 32), dim3(512), 0, st, a);
+            hipLaunchKernelGGL((diff_bwd_dkv_kernel<T, HH, 32>), and_dlambda(column_grid(a, a.max_k_len, 32)), dim3(512), 0, st, a);
             return;
         }
-    hipLaunchKernelGGL((diff_bwd_dkv_kernel<T, HH, 64>), column_grid(a, a.max_k_len), dim3(512), 0, st, a);
+    hipLaunchKernelGGL((diff_bwd_dkv_kernel<T, HH, 64>), and_dlambda(column_grid(a, a.max_k_len)), dim3(512), 0, st, a);
 }
 
 }  // namespace
@@ -567,12 +551,6 @@ ds_status diff_bwd_general(const DiffAttnArgs& a, hipStream_t st) {
     DS_DIFF_DISPATCH(dq_launch);
     DS_LAUNCH_CHECK();
     DS_DIFF_DISPATCH(dkv_launch);
-    DS_LAUNCH_CHECK();
-    return diff_dlambda(a, 16, st);
-}
-
-ds_status diff_dlambda(const DiffAttnArgs& a, int queries, hipStream_t st) {
-    hipLaunchKernelGGL(diff_dlambda_kernel, dim3(a.n_heads), dim3(1024), 0, st, a, queries);
     DS_LAUNCH_CHECK();
     return DS_OK;
 }

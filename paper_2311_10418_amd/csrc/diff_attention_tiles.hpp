@@ -55,6 +55,24 @@ template <int HD> struct FragOffsets {
     }
 };
 
+// WorkDraw for a launch whose first work-groups (a multiple of 8) do something else.
+struct LateDraw : WorkDraw {
+    int groups;
+    __device__ __forceinline__ LateDraw(const AttnArgs& a, int list, int first) : WorkDraw(a, list), groups((int)gridDim.x - first) { k = ((int)blockIdx.x - first) >> 3; }
+    __device__ __forceinline__ int take() const {
+        int next = 0;
+        if (threadIdx.x == 0) next = (groups >> 3) + __hip_atomic_fetch_add(ctr + xcd, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        return next;
+    }
+    __device__ __forceinline__ void finish() const {
+        if (threadIdx.x != 0) return;
+        if (__hip_atomic_fetch_add(ctr + 8, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == groups - 1) {
+#pragma unroll
+            for (int i = 0; i < 9; ++i) ctr[i] = 0;
+        }
+    }
+};
+
 // Short queries (at most 64 or 32 in every sequence) of few sequences and heads: a work-group's four wavefronts hold two or one blocks of 32
 // queries, and KS = 2 or 4 of them share one, each taking every KS-th step of 32 keys; what they have is joined through LDS in the end.  Tiles then
 // come in a ring of four, three blocks of keys in flight: with few queries nothing else hides the transfers.  diff_by_kind has the rule.
