@@ -8,8 +8,8 @@
 // the contraction over features does not see the order of the columns, and outputs go back through the same mapping.
 //
 // Bound by issue: the matrix pipe is busy 60 % of the SIMD cycles and vector instructions, more than two for each matrix instruction, take the rest.
-// Measured in fp32: 16 heads of 64, 31 sequences of 366 to 523, unmasked, forward 421 us, backward 1 011 (90 and 87 TFLOP/s
-// of the products they form, where a large product of matrices reaches 154); 4 heads of 64, 23 sequences of 88 to 177, causal, backward 45.
+// Measured in fp32: 16 heads of 64, 31 sequences of 366 to 523, unmasked, forward 421 us, backward 997 (90 and 88 TFLOP/s
+// of the products they form, where a large product of matrices reaches 154); 4 heads of 64, 23 sequences of 88 to 177, causal, backward 41.5.
 #include "diff_attention.hpp"
 #include "gemm.hpp"
 #include <type_traits>
