@@ -20,6 +20,7 @@ struct DiffAttnArgs : AttnArgs {                        // scale: 1 / sqrt(head_
     int32_t vec;                                        // general kernels: rows of four elements may be accessed at once
     char* aug;                                          // matrix-core kernels: see diff_attention_bwd.hip
     int32_t k_splits;                                   // forward: work-groups that share the keys of a head (1: one has them all)
+    int32_t direct;                                     // matrix-core kernels: sequences have one block of 128 rows, and work-groups go by sequence and head without a list
     float* split_part;                                  // what each of them found: see SplitPart
 };
 

@@ -6,14 +6,14 @@
 
 // Work-groups that share the keys of a head, for sequences of at most 64 rows of queries each: as many as make one for every compute unit, with a least
 // number of keys each; two, which head sizes up to 64 have the LDS for, with more keys each; at most one for a lane of the wavefront that joins them.
-// Matrix-core kernels: 128 keys, from 257 on (256 keys at once take 8.1 us, two shares of 128 and their joining 9.7); two from 1024 each on.
+// Matrix-core kernels: 128 keys, from 321 on (300 keys at once take 9.3 us, three shares of them and their joining 9.7); two from 1024 each on.
 // General kernels: 64 keys, for two as well.  One query of 16 heads of 64, us without -> with, bf16 / fp32:
 //     1 sequence of 512, 1024, 4096 keys:  15 -> 10, 24 -> 10, 77 -> 12 / 39 -> 11, 74 -> 11, 287 -> 22; of 32768 keys: 575 -> 37 (3.6 TB/s)
 //     16 sequences of 2048, 16384 keys:  44 -> 33, 295 -> 195 (5.5 TB/s; one work-group for a compute unit: 37, 322)
 //     16 sequences of 33 queries and 1019 keys:  28 -> 23 (two work-groups with half of them each: 29)
 static constexpr int kSplitQueries = 64, kSplitUnits = 256, kSplitMost = 64;
 static int most_splits(bool general, int n_heads, int head_dim, int q_total_rows, int max_k_len, int n_seq) {
-    const int from = general ? 129 : 257, keys_one = general ? 64 : 128, keys_two = general ? 64 : 1024;
+    const int from = general ? 129 : 321, keys_one = general ? 64 : 128, keys_two = general ? 64 : 1024;
     const long long items = (long long)n_seq * n_heads;
     if (q_total_rows > (long long)kSplitQueries * n_seq || max_k_len < from) return 1;
     auto with = [&](long long groups, int keys) {
@@ -61,6 +61,7 @@ static ds_status check(DiffAttnArgs& a) {
     a.d1 = (float*)after_lists;
     a.d2 = a.d1 + entries;
     a.k_splits = 1;
+    a.n_items = (const int32_t*)a.scratch;              // (valid memory also where no list is made)
     a.split_part = (float*)after_lists;
     a.lam_part = (float*)(after_lists + entries * 16);
     return DS_OK;
@@ -94,10 +95,10 @@ extern "C" ds_status ds_diff_attention_fwd(int32_t dtype, int32_t n_seq, int32_t
     return diff_fwd_general(a, (hipStream_t)hip_stream);
 }
 
-// Backward, few sequences of at most 16 tokens: launches are nearly all that counts, and the general kernels round nothing but the results, which shows
-// where a gradient is the difference of few terms (relative error of dQ and dK, 18 sequences of up to 12: 0.0031 -> 0.0017).  Matrix-core / general
-// kernels, 16 heads of 64 (128), us: 16 sequences of 8 14.4 / 14.8 (20.2 / 20.9), of 16 14.8 / 15.4 (20.7 / 21.7), of 32 15.9 / 17.8 (21.4 / 26.2); 32 of 16
-// 16.8 / 23.8 (28.4 / 38.6).
+// Backward, few sequences of at most 16 tokens: launches are most of the time, and the general kernels round nothing but the results, which shows where a
+// gradient is the difference of few terms: relative error of dQ and dK, 18 sequences of up to 12, 0.0031 -> 0.0017.  Matrix-core / general kernels, 16
+// heads of 64 (128), us: 16 sequences of 16 10.4 / 15.4 (15.2 / 21.5); beyond, the difference grows: of 32 10.9 / 18.0 (15.9 / 26.1), 256 of 8 68 / 135
+// (154 / 316).
 static bool short_in_fp32(const DiffAttnArgs& a) {
     return a.max_q_len <= 16 && a.max_k_len <= 16 && (long long)a.n_seq * a.n_heads <= gemm_cu_count();
 }

@@ -17,10 +17,11 @@ __global__ __launch_bounds__(256, 2) void diff_bwd_dq_mfma_kernel(DiffAttnArgs a
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 31, g = lane >> 5;
     const int item = blockIdx.x / a.n_heads, h = blockIdx.x - item * a.n_heads;
-    if (item >= a.n_items[0]) return;
-    const int2 it = a.items_q[item];
+    if (item >= block_count(a, 0)) return;
+    const int2 it = block_of(a, a.items_q, item);
     const int s = it.x, q0 = it.y * 128;
     const int ql = a.q_len[s], kl = a.k_len[s];
+    if (ql == 0) return;                                // (in no list)
     const long long qrow0 = a.q_row[s];
     const bf16_t* Q = (const bf16_t*)a.q + qrow0 * a.ldq + h * HD;
     const bf16_t* dO = (const bf16_t*)a.d_o + qrow0 * a.ldo + h * HD;
@@ -210,7 +211,7 @@ __global__ __launch_bounds__(256, HD == 64 ? 2 : 1) void diff_bwd_dkv_mfma_kerne
     auto begin_item = [&] {
         const int item = draw.index() / a.n_heads;
         h = draw.index() - item * a.n_heads;
-        const int2 it = a.items_k[item];
+        const int2 it = block_of(a, a.items_k, item);
         const int s = __builtin_amdgcn_readfirstlane(it.x), k0 = __builtin_amdgcn_readfirstlane(it.y) * 128;
         ql = __builtin_amdgcn_readfirstlane(a.q_len[s]);
         kl = __builtin_amdgcn_readfirstlane(a.k_len[s]);
@@ -243,6 +244,7 @@ __global__ __launch_bounds__(256, HD == 64 ? 2 : 1) void diff_bwd_dkv_mfma_kerne
         if (PS) draw.finish();
         return;
     }
+    if (a.direct && a.k_len[a.n_seq - 1 - draw.index() / a.n_heads] == 0) return;        // (in no list)
     begin_item();
     for (int i = tid; i < 64 * HD / 16; i += 256) reinterpret_cast<uint4*>(s_zero)[i] = make_uint4(0u, 0u, 0u, 0u);
     bf16x8_t minus;                                     // -1 in the contraction slots 0 and 1 (lane half 0), where a statistic's hi and lo are put
@@ -404,10 +406,10 @@ ds_status bwd_launch(const DiffAttnArgs& a, hipStream_t st) {
     if (r != DS_OK) return r;
     r = set_smem(kkv, smem_kv, attr_kv);
     if (r != DS_OK) return r;
-    hipLaunchKernelGGL(kq, dim3((unsigned)a.max_items_q * a.n_heads), dim3(256), smem_q, st, a);
+    hipLaunchKernelGGL(kq, dim3((unsigned)(a.direct ? a.n_seq : a.max_items_q) * a.n_heads), dim3(256), smem_q, st, a);
     DS_LAUNCH_CHECK();
-    const unsigned items_kv = (unsigned)a.max_items_k * a.n_heads, for_dlambda = (a.n_heads + 7) / 8 * 8;
-    hipLaunchKernelGGL(kkv, dim3((HD == 128 ? persistent_grid(items_kv) : items_kv) + for_dlambda), dim3(256), smem_kv, st, a);
+    const unsigned items_kv = (unsigned)(a.direct ? a.n_seq : a.max_items_k) * a.n_heads, for_dlambda = (a.n_heads + 7) / 8 * 8;
+    hipLaunchKernelGGL(kkv, dim3((HD == 128 && !a.direct ? persistent_grid(items_kv) : items_kv) + for_dlambda), dim3(256), smem_kv, st, a);
     DS_LAUNCH_CHECK();
     return DS_OK;
 }
@@ -416,7 +418,8 @@ ds_status bwd_launch(const DiffAttnArgs& a, hipStream_t st) {
 
 ds_status diff_bwd_mfma(const DiffAttnArgs& a0, hipStream_t st) {
     DiffAttnArgs a = a0;
-    const ds_status r = attn_prepare_lists(a, true, st);
+    a.direct = one_block_each(a, a.max_q_len, a.max_k_len) && one_block_each(a, a.max_k_len, a.max_q_len);
+    const ds_status r = a.direct ? DS_OK : attn_prepare_lists(a, true, st);
     if (r != DS_OK) return r;
     return diff_by_kind(a, [&](auto hd, auto causal, auto split) { return bwd_launch<decltype(hd)::value, decltype(causal)::value, decltype(split)::value>(a, st); });
 }

@@ -39,8 +39,9 @@ __global__ __launch_bounds__(256, HD == 64 && KS == 1 ? 3 : 2) void diff_fwd_mfm
     int s, h, q0 = 0, split = 0;
     if constexpr (KS == 1) {
         const int item = blockIdx.x / a.n_heads;
-        const int2 it = a.items_q[item];
-        if (item >= a.n_items[0]) return;
+        const int2 it = block_of(a, a.items_q, item);
+        if (item >= block_count(a, 0)) return;
+        if (a.direct && a.q_len[it.x] == 0) return;     // (in no list)
         s = it.x;
         q0 = it.y * 128;
         h = blockIdx.x - item * a.n_heads;
@@ -238,7 +239,7 @@ ds_status fwd_launch(const DiffAttnArgs& a, hipStream_t st) {
     const int smem = KeySplit<KS>::RING * 2 * (64 * HD * 2);
     const ds_status r = set_smem(kern, smem, attr);
     if (r != DS_OK) return r;
-    const dim3 grid = KS == 1 ? dim3((unsigned)a.max_items_q * a.n_heads) : dim3(a.k_splits, a.n_heads, a.n_seq);
+    const dim3 grid = KS == 1 ? dim3((unsigned)(a.direct ? a.n_seq : a.max_items_q) * a.n_heads) : dim3(a.k_splits, a.n_heads, a.n_seq);
     hipLaunchKernelGGL(kern, grid, dim3(256), smem, st, a);
     DS_LAUNCH_CHECK();
     return KS > 1 && a.k_splits > 1 ? diff_join(a, st) : DS_OK;
@@ -261,7 +262,8 @@ bool diff_mfma_supported(const DiffAttnArgs& a) {
 ds_status diff_fwd_mfma(const DiffAttnArgs& a0, hipStream_t st) {
     return diff_by_kind(a0, [&](auto hd, auto causal, auto split) {
         DiffAttnArgs a = a0;
-        const ds_status r = split == 1 ? attn_prepare_lists(a, false, st) : DS_OK;
+        a.direct = one_block_each(a, a.max_q_len, a.max_k_len);
+        const ds_status r = split == 1 && !a.direct ? attn_prepare_lists(a, false, st) : DS_OK;
         return r != DS_OK ? r : fwd_launch<decltype(hd)::value, decltype(causal)::value, decltype(split)::value>(a, st);
     });
 }

@@ -55,17 +55,34 @@ template <int HD> struct FragOffsets {
     }
 };
 
-// WorkDraw for a launch whose first work-groups (a multiple of 8) do something else.
+// The block of 128 rows that belongs to a place in a launch, longest sequences first (a plan lists them by ascending length), and their number.
+__device__ __forceinline__ int2 block_of(const DiffAttnArgs& a, const int2* list, int item) { return a.direct ? make_int2(a.n_seq - 1 - item, 0) : list[item]; }
+__device__ __forceinline__ int block_count(const DiffAttnArgs& a, int list) { return a.direct ? a.n_seq : a.n_items[list]; }
+// No list where every sequence has one block and the order does not matter much: one work-group for a compute unit at most, or (head size 64, whose dK/dV
+// kernel is not persistent) all of them short and not too many.  Launch and kernel of the list take 3 to 4 us.  With -> without, forward / backward, us, 16
+// heads of 64: 16 sequences of 96 tokens 10.1 -> 7.0 / 20.0 -> 16.8, 64 of 128 23.1 -> 19.7 / 61.2 -> 58.7, 256 of 32 25.5 -> 21.6 / 86.9 -> 83.1; but 256 of
+// 128 85 -> 90 / 238 -> 242.
+inline bool one_block_each(const DiffAttnArgs& a, int max_len, int other_len) {
+    const long long items = (long long)a.n_seq * a.n_heads, units = gemm_cu_count();
+    return max_len <= 128 && (items <= units || (a.head_dim == 64 && other_len <= 128 && items * max_len <= 1024 * units));
+}
+
+// WorkDraw for a launch whose first work-groups (a multiple of 8) do something else.  Without a list every work-group has one item and draws no other.
 struct LateDraw : WorkDraw {
     int groups;
-    __device__ __forceinline__ LateDraw(const AttnArgs& a, int list, int first) : WorkDraw(a, list), groups((int)gridDim.x - first) { k = ((int)blockIdx.x - first) >> 3; }
+    bool once;
+    __device__ __forceinline__ LateDraw(const DiffAttnArgs& a, int list, int first) : WorkDraw(a, list), groups((int)gridDim.x - first), once(a.direct) {
+        k = ((int)blockIdx.x - first) >> 3;
+        total = block_count(a, list) * a.n_heads;
+    }
     __device__ __forceinline__ int take() const {
+        if (once) return 0x7fffff00 >> 3;               // past every item
         int next = 0;
         if (threadIdx.x == 0) next = (groups >> 3) + __hip_atomic_fetch_add(ctr + xcd, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         return next;
     }
     __device__ __forceinline__ void finish() const {
-        if (threadIdx.x != 0) return;
+        if (threadIdx.x != 0 || once) return;
         if (__hip_atomic_fetch_add(ctr + 8, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == groups - 1) {
 #pragma unroll
             for (int i = 0; i < 9; ++i) ctr[i] = 0;
@@ -132,19 +149,21 @@ __device__ __forceinline__ void store_cols16(const f32x16_t (&acc)[HD / 32], flo
 // f(head size, causal, wavefronts that share a block of queries) with the template arguments of a call
 //
 // Sharing (KeySplit) pays where there is about one work-group for a compute unit or less, and costs where others would hide the transfers anyway:
-// its ring takes twice the LDS.  One wavefront to a block of queries -> sharing, forward, 16 heads of 64 / of 128, us a call (keys not split):
+// its ring takes twice the LDS.  It pays from about 320 keys on, which a causal sequence of 64 does not have.  One wavefront to a block of queries ->
+// sharing, forward, 16 heads of 64 / of 128, us a call (keys not split, with a list on both sides):
 //     1 sequence,   1 query,   4096 keys:  79 ->  55 / 108 ->  83      16 sequences, 33 queries, 1019 keys:  28 -> 26 / 37 -> 37
 //     4 sequences,  1 query,   2048 keys:  44 ->  36 /  59 ->  50      16 sequences, 20 queries, 1019 keys:  26 -> 26 / 35 -> 38
 //    64 sequences, 33 queries,  500 keys:  36 ->  38 /  61 ->  82     200 sequences, 20 queries,  300 keys:  52 -> 78 / 122 -> 208
+// and without a list on either, keys split where there are enough: 1 sequence, 1 query, 256 keys 7.8 -> 8.0 / 10.2 -> 11.5, 300 keys 9.3 -> 9.7 / 12.0 -> 12.4,
+// 512 keys 12 -> 9.5 / 16 -> 12.2
 template <class F> ds_status diff_by_kind(const DiffAttnArgs& a, F f) {
     const bool few = (long long)a.n_seq * a.n_heads * a.head_dim <= 64LL * gemm_cu_count();
-    auto by_split = [&](auto hd, auto causal) {
-        if (!few) return f(hd, causal, std::integral_constant<int, 1>{});
-        if (a.max_q_len <= 32) return f(hd, causal, std::integral_constant<int, 4>{});
-        if (a.max_q_len <= 64) return f(hd, causal, std::integral_constant<int, 2>{});
-        return f(hd, causal, std::integral_constant<int, 1>{});
+    auto by_mask = [&](auto hd) {
+        if (a.mask) return f(hd, std::true_type{}, std::integral_constant<int, 1>{});
+        if (!few || a.max_k_len <= 320 || a.max_q_len > 64) return f(hd, std::false_type{}, std::integral_constant<int, 1>{});
+        if (a.max_q_len <= 32) return f(hd, std::false_type{}, std::integral_constant<int, 4>{});
+        return f(hd, std::false_type{}, std::integral_constant<int, 2>{});
     };
-    auto by_mask = [&](auto hd) { return a.mask ? by_split(hd, std::true_type{}) : by_split(hd, std::false_type{}); };
     return a.head_dim == 128 ? by_mask(std::integral_constant<int, 128>{}) : by_mask(std::integral_constant<int, 64>{});
 }
 
