@@ -123,9 +123,9 @@ __device__ __forceinline__ void join_splits(char* lds, const KeySplit<KS>& ks, i
     }
 }
 
-// Stores a transposed [HD x 32] accumulator block times mul (first half of the features) or mul2 (second half): lane column = row `row` of the output.  A lane holds 4 of every 8 features, the lane 32
-// further on the other 4: they swap, so that each has 8 of every 16 and the stores are 16 bytes wide.  Every lane of the wavefront takes part;
-// `on` says whether this lane's row is stored.
+// Stores a transposed [HD x 32] accumulator block times mul (first half of the features) or mul2 (second half): lane column = row `row` of the output.
+// A lane holds 4 of every 8 features, the lane 32 further on the other 4: they swap, so that each has 8 of every 16 and the stores are 16 bytes wide.
+// Every lane of the wavefront takes part; `on` says whether this lane's row is stored.
 template <int HD>
 __device__ __forceinline__ void store_cols16(const f32x16_t (&acc)[HD / 32], float mul, float mul2, bf16_t* __restrict__ row, int g, bool on) {
 #pragma unroll

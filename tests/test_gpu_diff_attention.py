@@ -165,6 +165,15 @@ def test_very_short_sequences(causal, hd):
     Case(hd + 1, BF, 16, hd, [16, 7] * 9, [16, 7] * 9, causal).run(False, accumulate=True)
 
 
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("hd", [64, 128])
+def test_sequences_of_one_block(causal, hd):
+    """At most 128 tokens on either side, which need no work list: without queries, without keys, of different lengths; few and many of them."""
+    Case(hd, BF, 2, hd, [100, 1, 0, 64, 128, 20], [120, 0, 33, 1, 128, 90], causal).run(False)
+    Case(hd + 1, BF, 1, hd, [0, 33, 0], [40, 0, 7], causal).run(False)
+    Case(hd + 2, BF, 8, hd, [40, 0, 17, 128] * 10, [33, 5, 0, 100] * 10, causal).run(False, accumulate=True)
+
+
 @pytest.mark.parametrize("dt,generic", KINDS)
 @pytest.mark.parametrize("hd", [16, 64, 96, 128])
 def test_few_queries_over_long_keys(dt, generic, hd):
