@@ -75,10 +75,11 @@ __device__ __forceinline__ float lanes_sum(float v) {
     return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
 }
 
-// 1 / sqrt(v), v >= 1e-6: the hardware's estimate (one unit in the last place) and one step of Newton's method
+// 1 / sqrt(v), v >= 1e-6: the hardware's estimate (one unit in the last place) and one step of Newton's method; 0 for the infinity that the sum of
+// squares of a row of large values becomes, where the step would make inf x 0 (ds_norm_fwd has 0 there, too: the row is its bias)
 __device__ __forceinline__ float inv_sqrt(float v) {
     const float r = __builtin_amdgcn_rsqf(v);
-    return r * __builtin_fmaf(-0.5f * v * r, r, 1.5f);
+    return r == 0.f ? 0.f : r * __builtin_fmaf(-0.5f * v * r, r, 1.5f);
 }
 
 // The columns of a wavefront's row: `n` of them here, of d in all

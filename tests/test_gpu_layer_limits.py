@@ -1,0 +1,47 @@
+"""The layer parts at the ends of their ranges: sums that overflow, scores far below zero, statistics of many digits, values that are not finite."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2311_10418_amd import binding as ds
+from helpers import DEV
+
+pytestmark = pytest.mark.gpu
+
+BF, F32 = torch.bfloat16, torch.float32
+i32 = lambda a: torch.tensor(a, dtype=torch.int32, device=DEV)  # noqa: E731
+
+
+# ------------------------------------------------------------------------------------ the joint of two blocks
+@pytest.mark.parametrize("dt", [F32, BF])
+@pytest.mark.parametrize("rms", [False, True])
+@pytest.mark.parametrize("d", [64, 1024, 2048, 4096])
+def test_rows_whose_sum_of_squares_overflows(dt, rms, d):
+    """A norm of such a row is its bias, as in ds_norm_fwd: the reciprocal deviation is 0.  Exactly so: with post_g . 0 + post_b for z, y = 0 x + 1 z is the bias."""
+    rows = 5
+    g = torch.Generator(device=DEV).manual_seed(d)
+    rnd = lambda *s: torch.randn(s, generator=g, device=DEV).to(dt)  # noqa: E731
+    large, plain = rnd(rows, d), rnd(rows, d)
+    large[1] *= 1e25
+    large[3] *= 3e18 if d == 4096 else 1e30
+    gain, bias = rnd(d), None if rms else rnd(d)
+    ref, st = torch.empty_like(large), torch.zeros((2, rows), device=DEV)
+    ds.ds_norm_fwd(large, gain, bias, ref, st, rms=rms)
+    new = lambda: torch.full((rows, d), 7.0, dtype=dt, device=DEV)  # noqa: E731
+    y, u, y2, stats, stats2 = new(), new(), new(), torch.zeros((4, rows), device=DEV), torch.zeros((4, rows), device=DEV)
+    ds.ds_resid_norm_fwd(large, plain, y, stats, pre_g=gain, pre_b=bias, u=u, resid_scale=1.0, branch_scale=0.0, rms=rms)       # the norm before the next block
+    ds.ds_resid_norm_fwd(plain, large, y2, stats2, post_g=gain, post_b=bias, resid_scale=0.0, branch_scale=1.0, rms=rms)        # the norm behind a block
+    f32 = lambda: torch.zeros(d, device=DEV)  # noqa: E731
+    dx, dh, dgate, sums = new(), new(), None, [f32() for _ in range(4)]
+    partial = torch.zeros(int(ds.ds_resid_norm_bwd_scratch_floats(rows, d)), device=DEV)
+    ds.ds_resid_norm_bwd(plain, y, plain, stats, dx, dh, partial, du=plain, pre_g=gain, dpre_g=sums[0], dpre_b=None if rms else sums[1], rms=rms)
+    dx2, dh2 = new(), new()
+    ds.ds_resid_norm_bwd(plain, y2, large, stats2, dx2, dh2, partial, post_g=gain, post_b=bias, dpost_g=sums[2], dpost_b=None if rms else sums[3], rms=rms)
+    torch.cuda.synchronize()
+    none = torch.zeros(d, device=DEV, dtype=dt) if rms else bias
+    for r in (1, 3):
+        assert torch.equal(ref[r], none) and torch.equal(u[r], none) and torch.equal(y2[r], none)
+        assert stats[3, r] == 0 and stats2[1, r] == 0
+        assert torch.equal(dx[r], plain[r]) and not dh2[r].any()                     # nothing goes through the norm
+    for t in (y, u, y2, dx, dh, dx2, dh2, *sums):
+        assert torch.isfinite(t).all()
