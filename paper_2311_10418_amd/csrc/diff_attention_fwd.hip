@@ -17,12 +17,13 @@
 // causal: forward 200 us (536 TFLOP/s, counting four head sizes of operations a pair), dQ 250, dK/dV 368; 16 heads of 64, 31 sequences of 366 to 523,
 // unmasked: dQ 76, dK/dV 89.  One map of the whole head (attention_mfma.hip) takes 152 to 179 us forward and 504 to 538 backward on the first of them.
 #include "diff_attention_tiles.hpp"
+#include <cfloat>
 #include <type_traits>
 
 namespace {
 
 constexpr float kSlack = 8.0f;                          // see diff_fwd_mfma_kernel
-constexpr float kLowest = -1e30f;                       // a maximum of nothing: finite, so that a step in which a query sees no key adds nothing
+constexpr float kLowest = -FLT_MAX;                     // a maximum of nothing: finite, so that a step in which a query sees no key adds nothing, and below no score
 
 // ------------------------------------------------------------------------------------ forward
 // A tile of 64 keys goes in two steps of 32, so that both maps' scores (32 registers) and both accumulators (128 at head size 128) leave room

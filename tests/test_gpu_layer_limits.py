@@ -45,3 +45,41 @@ def test_rows_whose_sum_of_squares_overflows(dt, rms, d):
         assert torch.equal(dx[r], plain[r]) and not dh2[r].any()                     # nothing goes through the norm
     for t in (y, u, y2, dx, dh, dx2, dh2, *sums):
         assert torch.isfinite(t).all()
+
+
+# ------------------------------------------------------------------------------------ differential attention
+def _run(q, k, v, d_o, lam, ql, kl, heads, hd, causal, generic=False, q_row=None, k_row=None, back=True):
+    """Sequences one behind the other (or at the rows given) -> o, o2, lse, dq, dk, dv, dlam."""
+    q_row = np.cumsum([0] + list(ql[:-1])).tolist() if q_row is None else q_row
+    k_row = np.cumsum([0] + list(kl[:-1])).tolist() if k_row is None else k_row
+    o, o2, dq, dk, dv = (torch.zeros_like(t) for t in (q, q, q, k, v))
+    lse, dlam = torch.zeros((2 * heads, q.shape[0]), device=DEV), torch.zeros(heads, device=DEV)
+    scratch = torch.zeros(int(ds.ds_diff_attention_scratch_bytes(heads, q.shape[0], k.shape[0], len(ql))), dtype=torch.uint8, device=DEV)
+    rest = (i32(q_row), i32(ql), i32(k_row), i32(kl), heads, hd, causal, max(ql), max(kl), scratch)
+    ds.ds_diff_attention_fwd(q, k, v, lam, o, lse, *rest, o2=o2, force_generic=generic)
+    if back:
+        ds.ds_diff_attention_bwd(q, k, v, lam, o, o2, d_o, lse, dq, dk, dv, dlam, *rest, force_generic=generic)
+    torch.cuda.synchronize()
+    return o, o2, lse, dq, dk, dv, dlam
+
+
+@pytest.mark.parametrize("dt,generic", [(F32, False), (BF, True), (BF, False)])
+@pytest.mark.parametrize("ql,kl,causal", [(5, 64, False), (1, 512, False), (33, 1024, False), (40, 1024, False), (200, 128, False), (150, 150, True)])
+@pytest.mark.parametrize("hd", [64, 128])
+def test_scores_far_below_zero(dt, generic, ql, kl, causal, hd):
+    """Every score -2^108 (before the scale, a power of two, so that products with it round nothing): all visible probabilities alike, and their sums and values,
+    small whole numbers, exact up to the rounding of results (half a step, and one of O2's in O) and of the reciprocal of the number of keys (2^-23)."""
+    g = torch.Generator(device=DEV).manual_seed(ql)
+    heads = 2
+    exp = 5 if hd == 64 else 6                          # a map has 2^exp features
+    q, k = torch.full((ql, heads * hd), 2.0 ** (54 - exp), dtype=dt, device=DEV), torch.full((kl, heads * hd), -2.0 ** 54, dtype=dt, device=DEV)
+    v = torch.randint(-8, 9, (kl, heads * hd), generator=g, device=DEV).to(dt)
+    lam = torch.tensor([0.5, 0.25], device=DEV)
+    o, o2, lse = _run(q, k, v, None, lam, [ql], [kl], heads, hd, causal, generic, back=False)[:3]
+    seen = torch.arange(1, ql + 1, device=DEV).clamp(max=kl) if causal else torch.full((ql,), kl, device=DEV)
+    mean = v.double().cumsum(0)[seen - 1] / seen[:, None]
+    half = 2.0 ** -8 if dt == BF else 2.0 ** -24
+    most = (half + 2.0 ** -21) * mean.abs()
+    assert ((o2.double() - mean).abs() <= most).all()
+    assert ((o.double() - mean * (1 - lam.double().repeat_interleave(hd))).abs() <= most).all()
+    assert torch.isfinite(lse).all()
