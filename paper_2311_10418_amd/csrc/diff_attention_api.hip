@@ -23,12 +23,12 @@ static int most_splits(bool general, int n_heads, int head_dim, int q_total_rows
     return (int)std::max<long long>(std::max(one, two), 1);
 }
 
-// Scratch: the work lists of the matrix-core kernels, then what the dQ kernels hand to the dK/dV kernels, 16 bytes for each query of a head
+// Scratch: the work lists of the matrix-core kernels, then what the dQ kernels hand to the dK/dV kernels, 32 bytes for each query of a head
 // (the general ones use 8 of them, as two arrays of floats), then the parts of dlambda, one float each.  A forward call has the parts of split keys in
 // the place of both.
 static size_t lists_size(int q_total_rows, int k_total_rows, int n_seq) { return attn_scratch_bytes(0, 0, q_total_rows, k_total_rows, n_seq); }
 size_t diff_scratch_bytes(int n_heads, int q_total_rows, int k_total_rows, int n_seq) {
-    size_t of_row = 16 + 4;
+    size_t of_row = 32 + 4;
     for (const int head_dim : {64, 128}) {
         const int splits = most_splits(true, n_heads, head_dim, q_total_rows, k_total_rows, n_seq);      // (never fewer than the others)
         if (splits > 1) of_row = std::max(of_row, (size_t)splits * (2 * head_dim + 4) * 4);
@@ -63,7 +63,7 @@ static ds_status check(DiffAttnArgs& a) {
     a.k_splits = 1;
     a.n_items = (const int32_t*)a.scratch;              // (valid memory also where no list is made)
     a.split_part = (float*)after_lists;
-    a.lam_part = (float*)(after_lists + entries * 16);
+    a.lam_part = (float*)(after_lists + entries * 32);
     return DS_OK;
 }
 

@@ -6,8 +6,24 @@
 
 namespace {
 
+// A float as the sum of three bf16 values, exactly: the difference from the first has at most 16 bits, that from the second at most 8.
+struct BfParts {
+    bf16_t p[3];
+    __device__ __forceinline__ explicit BfParts(float v) {
+#pragma unroll
+        for (int i = 0; i < 3; ++i) {
+            p[i] = (bf16_t)v;
+            v -= (float)p[i];
+        }
+    }
+    __device__ __forceinline__ static uint32_t bits(bf16_t b) { return __builtin_bit_cast(unsigned short, b); }
+    __device__ __forceinline__ uint32_t half(int g) const { return g ? bits(p[2]) : bits(p[0]) | bits(p[1]) << 16; }
+};
+constexpr int kStatTile = 64 * 32;                      // bytes
+
 // ------------------------------------------------------------------------------------ backward: dQ (and the statistics, the parts of dlambda)
-// For the dK/dV kernel a query leaves one entry of eight bf16 values, the {hi, lo} splits of lse_1 / scale, lse_2 / scale, D_1 and D_2 - D_1.
+// For the dK/dV kernel a query leaves one entry of sixteen bf16 values: lse_1 / scale, lse_2 / scale, D_1 and D_2 - D_1, each as the sum of three, which
+// together have all 24 bits of it: {first, second} of the four in the first half, {third, 0} of the four in the second (see BfParts).
 template <int HD, bool CAUSAL, int KS>
 __global__ __launch_bounds__(256, 2) void diff_bwd_dq_mfma_kernel(DiffAttnArgs a) {
     extern __shared__ __attribute__((aligned(16))) char smem[];
@@ -70,9 +86,9 @@ __global__ __launch_bounds__(256, 2) void diff_bwd_dq_mfma_kernel(DiffAttnArgs a
     d1 += __shfl_xor(d1, 32, 64);
     d1 += lam * d2;
     const float lse1 = a.lse[(size_t)(2 * h) * a.lse_stride + qrow0 + qi_c], lse2 = a.lse[(size_t)(2 * h + 1) * a.lse_stride + qrow0 + qi_c];
-    if (g == 0 && qi < ql && ks.split == 0)
-        reinterpret_cast<uint4*>(a.aug)[(size_t)h * a.q_total_rows + qrow0 + qi] =
-            make_uint4(split_hi_lo(lse1 * (1.0f / a.scale)), split_hi_lo(lse2 * (1.0f / a.scale)), split_hi_lo(d1), split_hi_lo(d2 - d1));
+    if (qi < ql && ks.split == 0)                       // lane half g writes half g
+        reinterpret_cast<uint4*>(a.aug)[2 * ((size_t)h * a.q_total_rows + qrow0 + qi) + g] =
+            make_uint4(BfParts(lse1 * (1.0f / a.scale)).half(g), BfParts(lse2 * (1.0f / a.scale)).half(g), BfParts(d1).half(g), BfParts(d2 - d1).half(g));
     const float e1 = lse1 * kLog2e, e2 = lse2 * kLog2e;
     const float c = a.scale * kLog2e;
 
@@ -168,14 +184,14 @@ __global__ __launch_bounds__(256, 2) void diff_bwd_dq_mfma_kernel(DiffAttnArgs a
 }
 
 // ------------------------------------------------------------------------------------ backward: dK, dV
-// A ring of four stages of Q tile, dO tile ([64][HD]) and statistics tile ([64 queries][8] bf16, see above), three blocks in flight.  One matrix
-// instruction with the statistics as its A operand and -1 in the two slots of a value subtracts it: score_i - lse_i / scale and, from the one dP,
-// dP - D_1 and dP - D_2.  At head size 128 work-groups are persistent, one to a compute unit (see attention_mfma.hip).
+// A ring of four stages of Q tile, dO tile ([64][HD]) and statistics tile ([64 queries][16] bf16, see above), three blocks in flight.  One matrix
+// instruction with the statistics as its A operand and -1 in the slots of a value subtracts it, with all its bits: score_i - lse_i / scale and, from the
+// one dP, dP - D_1 and dP - D_2.  At head size 128 work-groups are persistent, one to a compute unit (see attention_mfma.hip).
 template <int HD, bool CAUSAL>
 __global__ __launch_bounds__(256, HD == 64 ? 2 : 1) void diff_bwd_dkv_mfma_kernel(DiffAttnArgs a) {
     extern __shared__ __attribute__((aligned(16))) char smem[];
     constexpr int TILE = 64 * HD * 2;
-    constexpr int STAGE = 2 * TILE + 1024;
+    constexpr int STAGE = 2 * TILE + kStatTile;
     constexpr int NS = 4;
     constexpr bool PS = HD == 128;
     const int tid = threadIdx.x, lane = tid & 63;
@@ -199,14 +215,14 @@ __global__ __launch_bounds__(256, HD == 64 ? 2 : 1) void diff_bwd_dkv_mfma_kerne
     const char* aug_src;
     float lam;
     bf16x8_t kf[HD / 16], vf[HD / 16];
-    // block blk -> stage blk % 4 by direct transfers (the statistics by wavefront 0).  Queries past the last one are zeros in
+    // block blk -> stage blk % 4 by direct transfers (the statistics by wavefronts 0 and 1).  Queries past the last one are zeros in
     // all three: P is 1 there, and multiplies zeros (dV), and dS is 1 (0 - 0): no mask
     auto issue_block = [&](int blk) {
         const uint32_t n = lds0 + (blk & (NS - 1)) * STAGE;
         const int q0 = q_begin + blk * 64;
         ldQ.issue(n, q0);
         ldO.issue(n + TILE, q0);
-        if (wave == 0) lds_dma16_buffer(make_raw_buffer(aug_src + (long long)q0 * 16, (uint32_t)max(0, min(64, ql - q0)) * 16), (uint32_t)lane * 16, n + 2 * TILE);
+        if (wave < 2) lds_dma16_buffer(make_raw_buffer(aug_src + (long long)q0 * 32, (uint32_t)max(0, min(64, ql - q0)) * 32), (uint32_t)(wave * 64 + lane) * 16, n + 2 * TILE + wave * 1024);
     };
     auto begin_item = [&] {
         const int item = draw.index() / a.n_heads;
@@ -225,7 +241,7 @@ __global__ __launch_bounds__(256, HD == 64 ? 2 : 1) void diff_bwd_dkv_mfma_kerne
         ldQ.base = reinterpret_cast<const char*>((const bf16_t*)a.q + qrow0 * a.ldq + h * HD);
         ldO.base = reinterpret_cast<const char*>((const bf16_t*)a.d_o + qrow0 * a.ldo + h * HD);
         ldQ.n_valid = ldO.n_valid = ql;
-        aug_src = a.aug + ((size_t)h * a.q_total_rows + qrow0) * 16;
+        aug_src = a.aug + ((size_t)h * a.q_total_rows + qrow0) * 32;
         if (nb > 0) {
             issue_block(0);
             issue_block(1);
@@ -247,9 +263,9 @@ __global__ __launch_bounds__(256, HD == 64 ? 2 : 1) void diff_bwd_dkv_mfma_kerne
     if (a.direct && a.k_len[a.n_seq - 1 - draw.index() / a.n_heads] == 0) return;        // (in no list)
     begin_item();
     for (int i = tid; i < 64 * HD / 16; i += 256) reinterpret_cast<uint4*>(s_zero)[i] = make_uint4(0u, 0u, 0u, 0u);
-    bf16x8_t minus;                                     // -1 in the contraction slots 0 and 1 (lane half 0), where a statistic's hi and lo are put
+    bf16x8_t minus;                                     // -1 in the contraction slots 0, 1 (lane half 0) and 8, 9 (lane half 1), where a statistic's parts are put
 #pragma unroll
-    for (int j = 0; j < 8; ++j) minus[j] = (bf16_t)((g == 0 && j < 2) ? -1.0f : 0.0f);
+    for (int j = 0; j < 8; ++j) minus[j] = (bf16_t)(j < 2 ? -1.0f : 0.0f);
     const float c = a.scale * kLog2e;
 
     FragOffsets<HD> at;
@@ -275,7 +291,7 @@ __global__ __launch_bounds__(256, HD == 64 ? 2 : 1) void diff_bwd_dkv_mfma_kerne
         const char* sdO = sQ + TILE;
         const char* s_stat = sdO + TILE;
         // block b has landed for this wavefront (the two newest may still be in flight), then for everybody; the stage read before is free
-        if (wave == 0) __builtin_amdgcn_s_waitcnt(vmcnt_imm(2 * (2 * (HD / 32) + 1)));
+        if (wave < 2) __builtin_amdgcn_s_waitcnt(vmcnt_imm(2 * (2 * (HD / 32) + 1)));
         else __builtin_amdgcn_s_waitcnt(vmcnt_imm(2 * (2 * (HD / 32))));
         __builtin_amdgcn_s_barrier();
         issue_block(b + 3);
@@ -290,8 +306,8 @@ __global__ __launch_bounds__(256, HD == 64 ? 2 : 1) void diff_bwd_dkv_mfma_kerne
         f32x16_t sa[2], sb[2], ga[2];
         u32x4_t fs[2];
         bf16x8_t fq[NA], fo[NA], td[ND], tq[ND], pf[2][2], f1[2][2], f2[2][2];
-        auto less = [&](f32x16_t x, uint32_t hi_lo) {   // x minus a statistic of its rows
-            const u32x4_t f = {hi_lo, 0u, 0u, 0u};
+        auto less = [&](f32x16_t x, uint32_t parts) {   // x minus a statistic of its rows
+            const u32x4_t f = {parts, 0u, 0u, 0u};
             return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, f), minus, x, 0, 0, 0);
         };
         auto read_a = [&](int qt, int i) {
@@ -316,7 +332,7 @@ __global__ __launch_bounds__(256, HD == 64 ? 2 : 1) void diff_bwd_dkv_mfma_kerne
         auto phase_a = [&](int qt, bool with_prev) {
 #pragma unroll
             for (int e = 0; e < 16; ++e) { sa[qt][e] = 0.f; sb[qt][e] = 0.f; ga[qt][e] = 0.f; }
-            fs[qt] = *reinterpret_cast<const u32x4_t*>(s_stat + (qt * 32 + col) * 16);
+            fs[qt] = *reinterpret_cast<const u32x4_t*>(s_stat + (qt * 32 + col) * 32 + g * 16);
 #pragma unroll
             for (int i = 0; i < AHEAD; ++i) read_a(qt, i);
 #pragma unroll
@@ -401,7 +417,7 @@ ds_status bwd_launch(const DiffAttnArgs& a, hipStream_t st) {
     auto kq = diff_bwd_dq_mfma_kernel<HD, CAUSAL, KS>;
     auto kkv = diff_bwd_dkv_mfma_kernel<HD, CAUSAL>;
     const int smem_q = KeySplit<KS>::RING * 2 * (64 * HD * 2);
-    const int smem_kv = 4 * (2 * (64 * HD * 2) + 1024) + 64 + 64 * HD;      // stages, draws, zeros
+    const int smem_kv = 4 * (2 * (64 * HD * 2) + kStatTile) + 64 + 64 * HD; // stages, draws, zeros
     ds_status r = set_smem(kq, smem_q, attr_q);
     if (r != DS_OK) return r;
     r = set_smem(kkv, smem_kv, attr_kv);

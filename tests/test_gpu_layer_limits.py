@@ -83,3 +83,33 @@ def test_scores_far_below_zero(dt, generic, ql, kl, causal, hd):
     assert ((o2.double() - mean).abs() <= most).all()
     assert ((o.double() - mean * (1 - lam.double().repeat_interleave(hd))).abs() <= most).all()
     assert torch.isfinite(lse).all()
+
+
+@pytest.mark.parametrize("generic", [False, True])
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("ql,kl", [(48, 64), (33, 256)])
+def test_statistics_keep_all_their_digits(generic, hd, ql, kl):
+    """Keys and values all alike, lambda = -1: every probability is 1 / kl, a power of two, their sum twice that, and dP - D is 0.  The log-sum-exps (up to 2^11, the
+    second map's negative) and D (whole numbers of up to 21 bits) are what backward subtracts.  Eight roundings of 2^-24 in a log-sum-exp on its way are 2^-10 of a
+    probability, below half a step of bf16 (2^-9 downwards), so that rounding takes them away: dV is exact (within 2^-10 in the kernels that do not
+    round probabilities) and dK zero.  With 2^-17 of a log-sum-exp a probability would be up to 2^-6 off."""
+    rng = np.random.default_rng(hd + ql)
+    m = hd // 2
+    at = lambda a: torch.from_numpy(np.asarray(a, dtype=np.float32)).to(DEV).to(BF)  # noqa: E731
+    q = rng.integers(1, 128, (ql, hd)).astype(np.float64)
+    k = rng.integers(1, 128, (1, hd)) * 2.0 ** 10 / (q[:, :m].sum(1).max() * 64 / np.sqrt(m))
+    k = np.repeat(2.0 ** np.round(np.log2(k)) * np.where(np.arange(hd) < m, 1.0, -1.0), kl, 0)      # scores: whole numbers times powers of two, exact in fp32
+    top = np.abs(np.stack([q[:, :m] @ k[0, :m], q[:, m:] @ k[0, m:]])).max() / np.sqrt(m)
+    assert 2 ** 9 < top < 2 ** 11
+    v = np.repeat(rng.integers(65, 128, (1, hd)), kl, 0)
+    lam = torch.tensor([-1.0], device=DEV)
+    for d_o in (64.0 * np.eye(ql, hd), rng.integers(65, 128, (ql, hd)) * rng.choice([-1, 1], (ql, hd))):     # one probability in every value of dV; D of many digits
+        o, o2, lse, dq, dk, dv, dlam = _run(at(q), at(k), at(v), at(d_o), lam, [ql], [kl], 1, hd, False, generic)
+        assert torch.equal(o2, at(v[:1]).expand(ql, hd)) and torch.equal(o, at(2 * v[:1]).expand(ql, hd))
+        assert not dq.any() and not dk.any()
+        want = at(d_o.sum(0, keepdims=True) * 2 / kl).expand(kl, hd)
+        if generic:
+            size = torch.from_numpy(np.abs(d_o).sum(0) * 2 / kl).to(DEV)
+            assert ((dv.double() - want.double()).abs() <= 2.0 ** -7 * want.double().abs() + 2.0 ** -9 * size).all()
+        else:
+            assert torch.equal(dv, want)
