@@ -95,14 +95,6 @@ extern "C" ds_status ds_diff_attention_fwd(int32_t dtype, int32_t n_seq, int32_t
     return diff_fwd_general(a, (hipStream_t)hip_stream);
 }
 
-// Backward, few sequences of at most 16 tokens: launches are most of the time, and the general kernels round nothing but the results, which shows where a
-// gradient is the difference of few terms: relative error of dQ and dK, 18 sequences of up to 12, 0.0031 -> 0.0017.  Matrix-core / general kernels, 16
-// heads of 64 (128), us: 16 sequences of 16 10.4 / 15.4 (15.2 / 21.5); beyond, the difference grows: of 32 10.9 / 18.0 (15.9 / 26.1), 256 of 8 68 / 135
-// (154 / 316).
-static bool short_in_fp32(const DiffAttnArgs& a) {
-    return a.max_q_len <= 16 && a.max_k_len <= 16 && (long long)a.n_seq * a.n_heads <= gemm_cu_count();
-}
-
 extern "C" ds_status ds_diff_attention_bwd(int32_t dtype, int32_t n_seq, int32_t n_heads, int32_t head_dim, int32_t mask, const int32_t* q_row,
                                            const int32_t* q_len, const int32_t* k_row, const int32_t* k_len, int32_t max_q_len, int32_t max_k_len,
                                            const void* q, int32_t ldq, const void* k, int32_t ldk, const void* v, int32_t ldv, const float* lambda,
@@ -123,6 +115,6 @@ extern "C" ds_status ds_diff_attention_bwd(int32_t dtype, int32_t n_seq, int32_t
     const ds_status r = check(a);
     if (r != DS_OK) return r;
     if (!o2 || !d_o || !dq || !dk || !dv || !dlambda || (accumulate != 0 && accumulate != 1)) return DS_EINVAL;
-    if (!force_generic && !short_in_fp32(a) && diff_mfma_supported(a)) return diff_bwd_mfma(a, (hipStream_t)hip_stream);
+    if (!force_generic && diff_mfma_supported(a)) return diff_bwd_mfma(a, (hipStream_t)hip_stream);
     return diff_bwd_general(a, (hipStream_t)hip_stream);
 }

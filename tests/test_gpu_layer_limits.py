@@ -113,3 +113,23 @@ def test_statistics_keep_all_their_digits(generic, hd, ql, kl):
             assert ((dv.double() - want.double()).abs() <= 2.0 ** -7 * want.double().abs() + 2.0 ** -9 * size).all()
         else:
             assert torch.equal(dv, want)
+
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("hd", [64, 128])
+def test_gradients_of_a_sequence_do_not_depend_on_the_others(causal, hd):
+    """Short bf16 sequences alone, as the first of many, and beside longer ones: the same bits."""
+    heads = 8
+    short = [16, 1, 9, 12]
+    rng = np.random.default_rng(hd)
+    lens = {"alone": short, "many": short + [5, 16] * 40, "beside one more token": short + [17], "beside long ones": short + [200, 130]}
+    n = sum(max(lens.values(), key=sum))
+    t = [torch.from_numpy(rng.standard_normal((n, heads * hd)).astype(np.float32)).to(DEV).to(BF) for _ in range(4)]
+    lam = torch.linspace(0.1, 0.8, heads, device=DEV)
+    out = {name: _run(*[x[:sum(l)].clone() for x in t], lam, l, l, heads, hd, causal) for name, l in lens.items()}
+    m = sum(short)
+    for name, r in out.items():
+        for a, b in zip(out["alone"], r):
+            if a.shape[0] == m:
+                assert torch.equal(a, b[:m]), name
+        assert torch.equal(out["alone"][2], r[2][:, :m]), name
