@@ -540,8 +540,9 @@ int64_t ds_diff_attention_scratch_bytes(int32_t n_heads, int32_t q_total_rows, i
  * Rows not covered by any sequence are not touched; the sequences must not overlap; one with k_len[s] = 0 gets zero outputs.
  * Strides and alignments of the element type are taken as they are.  scratch: DEVICE, 16-byte aligned, at least
  * ds_diff_attention_scratch_bytes.  force_generic != 0 selects the kernels that compute in fp32 whatever the type.
- * Values that are not finite: a row is affected by the rows it sees, and by rows that mask = 1 hides up to 127 tokens behind it, since
- * whole blocks are multiplied by probabilities that are 0 there. */
+ * Values that are not finite: a row is affected by the rows it sees.  The bf16 matrix-core kernels multiply whole blocks by probabilities
+ * that are 0 where mask = 1 hides a token, so that an infinity or NaN may also reach rows up to 31 tokens in front of it in o, o2
+ * and dq (31 behind it in dk and dv). */
 ds_status ds_diff_attention_fwd(int32_t dtype, int32_t n_seq, int32_t n_heads, int32_t head_dim, int32_t mask,
                                 const int32_t* q_row, const int32_t* q_len, const int32_t* k_row, const int32_t* k_len,
                                 int32_t max_q_len, int32_t max_k_len,

@@ -7,10 +7,17 @@
 // Tiles of the other side are kept in LDS row by row, every half head padded with zeros to HH columns (a multiple of 16), V and dO too:
 // the contraction over features does not see the order of the columns, and outputs go back through the same mapping.
 //
+// Causal masks and values that are not finite.  A score that a column does not see is replaced whatever it is; but the second products run over whole
+// blocks of rows, probability 0 where a column does not see one, and 0 x Inf is NaN.  A wavefront whose sums are not finite in the end therefore looks
+// over the rows at its own places (rows further on it does not visit), and where those are not finite either it takes its columns one by one
+// (diff_attention_rows.hpp), so that a row is affected by the rows it sees and by no others.  (Looking the rows over as their tiles go to LDS took 2 to 7 % of
+// the kernels' time; this takes 1 % at most.)
+//
 // Bound by issue: the matrix pipe is busy 60 % of the SIMD cycles and vector instructions, more than two for each matrix instruction, take the rest.
 // Measured in fp32: 16 heads of 64, 31 sequences of 366 to 523, unmasked, forward 421 us, backward 997 (90 and 88 TFLOP/s
 // of the products they form, where a large product of matrices reaches 154); 4 heads of 64, 23 sequences of 88 to 177, causal, backward 41.5.
 #include "diff_attention.hpp"
+#include "diff_attention_rows.hpp"
 #include "gemm.hpp"
 #include <type_traits>
 
@@ -113,6 +120,15 @@ __device__ __forceinline__ void second_product(const float* tile, int rb, int la
         for (int s = S0; s < S1; ++s) out[s] = mfma4(p[e * (2 * HH + 4) + 16 * s], w[e], out[s]);
 }
 
+template <int N> __device__ __forceinline__ bool any_not_finite(const f32x4_t (&acc)[N]) {       // of the wavefront's sums
+    float nothing = 0.f;                                // 0, or NaN
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) nothing = __builtin_fmaf(acc[i][j], 0.f, nothing);
+    return __builtin_amdgcn_ballot_w64(nothing != 0.f) != 0;
+}
+
 __device__ __forceinline__ float groups_max(float v) { v = fmaxf(v, __shfl_xor(v, 16, 64)); return fmaxf(v, __shfl_xor(v, 32, 64)); }
 __device__ __forceinline__ float groups_sum(float v) { v += __shfl_xor(v, 16, 64); return v + __shfl_xor(v, 32, 64); }
 
@@ -212,9 +228,18 @@ __global__ __launch_bounds__(256, HH <= 32 ? 3 : 2) void diff_fwd_kernel(DiffAtt
         if constexpr (HH >= 32) __builtin_amdgcn_sched_barrier(0);
         map(std::integral_constant<int, NS / 2>{}, m2, l2, o2);
     }
-    if (qi >= ql) return;
     l1 = groups_sum(l1);
     l2 = groups_sum(l2);
+    if (a.mask && (any_not_finite(o1) || any_not_finite(o2)) && !rows_finite<T>(a.v, krow0, a.ldv, h, hd, qw0, min(kl, qw0 + KT), lane)) {
+        const float e1 = m1 + __builtin_amdgcn_logf(l1), e2 = m2 + __builtin_amdgcn_logf(l2);
+        for (int i = 0; i < min(16, ql - qw0); ++i) diff_fwd_row<T>(a, s, h, qw0 + i, __shfl(e1, i, 64), __shfl(e2, i, 64), lane);
+        if (g == 0 && qi < ql) {
+            a.lse[(size_t)(2 * h) * a.lse_stride + qrow0 + qi] = e1 * kLn2G;
+            a.lse[(size_t)(2 * h + 1) * a.lse_stride + qrow0 + qi] = e2 * kLn2G;
+        }
+        return;
+    }
+    if (qi >= ql) return;
     const long long row = qrow0 + qi;
     if (a.k_splits > 1) {
         const SplitPart to = split_part(a, h, row, split);
@@ -403,9 +428,17 @@ __global__ __launch_bounds__(512, HH <= 32 ? 4 : 2) void diff_bwd_dq_kernel(Diff
     f32x4_t lam_join[1] = {{lam_sum, 0.f, 0.f, 0.f}};
     join_shares<COLS>(lds, split, t, lam_join);
     if (split != 0) return;
-    lam_sum = wave_sum(qi < ql ? lam_join[0][0] : 0.f);
+    const bool by_rows = a.mask && (any_not_finite(gacc) || any_not_finite(lam_join)) &&
+                         !(rows_finite<T>(a.k, krow0, a.ldk, h, hd, qw0, min(kl, qw0 + 16), lane) && rows_finite<T>(a.v, krow0, a.ldv, h, hd, qw0, min(kl, qw0 + 16), lane));
+    if (by_rows) {
+        lam_sum = 0.f;
+        for (int i = 0; i < min(16, ql - qw0); ++i)
+            lam_sum += diff_dq_row<T>(a, s, h, qw0 + i, __shfl(e1, i, 64), __shfl(e2, i, 64), __shfl(d1, i, 64), __shfl(d2, i, 64), lane);
+    } else {
+        lam_sum = wave_sum(qi < ql ? lam_join[0][0] : 0.f);
+    }
     if (lane == 0 && qw0 < ql) a.lam_part[(size_t)h * a.q_total_rows + qrow0 + qw0] = lam_sum;
-    if (qi < ql) store_column<T, HH>(gacc, a.scale, (T*)a.dq + (qrow0 + qi) * a.ldq + (long long)h * hd, half, g, vec);
+    if (qi < ql && !by_rows) store_column<T, HH>(gacc, a.scale, (T*)a.dq + (qrow0 + qi) * a.ldq + (long long)h * hd, half, g, vec);
 }
 
 // ---------------------------------------------------------------- backward: dK, dV
@@ -492,7 +525,14 @@ __global__ __launch_bounds__(512, HH <= 32 && COLS == 64 ? 4 : 2) void diff_bwd_
     }
     join_shares<COLS>(lds, split, t, dk);
     join_shares<COLS>(lds, split, t, dv);
-    if (split != 0 || ki >= kl) return;
+    if (split != 0) return;
+    if (a.mask && (any_not_finite(dk) || any_not_finite(dv)) &&
+        !(rows_finite<T>(a.q, qrow0, a.ldq, h, hd, kw0, min(ql, kw0 + 16), lane) && rows_finite<T>(a.d_o, qrow0, a.ldo, h, hd, kw0, min(ql, kw0 + 16), lane) &&
+          stats_finite(a, h, qrow0, kw0, min(ql, kw0 + 16), lane))) {
+        for (int i = 0; i < min(16, kl - kw0); ++i) diff_dkv_row<T>(a, s, h, kw0 + i, lane);
+        return;
+    }
+    if (ki >= kl) return;
     store_column<T, HH>(dk, a.scale, (T*)a.dk + (krow0 + ki) * a.ldk + (long long)h * hd, half, g, vec);
     store_column<T, HH>(dv, 1.0f, (T*)a.dv + (krow0 + ki) * a.ldv + (long long)h * hd, half, g, vec);
 }

@@ -133,3 +133,44 @@ def test_gradients_of_a_sequence_do_not_depend_on_the_others(causal, hd):
             if a.shape[0] == m:
                 assert torch.equal(a, b[:m]), name
         assert torch.equal(out["alone"][2], r[2][:, :m]), name
+
+
+def _alike(a, b, exact, tag):
+    """The rows of `exact` to the bit.  The others may have been summed in another order: half a step of the type on either side, and what fp32 sums of these sizes
+    (scores of up to 2^3 of terms, 2^7 terms in dP - D, 16 times as large as their sum) are off by at most, 2^-9 of the largest value."""
+    half = 2.0 ** -8 if a.dtype == BF else 2.0 ** -24
+    assert torch.equal(a[exact], b[exact]), tag
+    if a.numel():
+        assert ((a.double() - b.double()).abs() <= 2 * half * a.double().abs() + 2.0 ** -9 * a.double().abs().max()).all(), tag
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("dt,generic", [(F32, False), (BF, True), (BF, False)])
+@pytest.mark.parametrize("heads,n,at", [(2, 300, 140), (2, 90, 67), (16, 700, 0), (16, 700, 700 - 1), (2, 40, 17)])
+@pytest.mark.parametrize("hd", [16, 48, 64, 80, 128])
+def test_values_that_are_not_finite_stay_where_they_are_seen(bad, dt, generic, heads, n, at, hd):
+    """Causal: a key or value row does not touch earlier queries (in the bf16 matrix-core kernels: earlier ones than those within 31 tokens), a query's row
+    not the gradients of later keys."""
+    reach = 31 if dt == BF and not generic and hd in (64, 128) else 0
+    rng = np.random.default_rng(n + hd)
+    t = [torch.from_numpy(rng.standard_normal((n, heads * hd)).astype(np.float32)).to(DEV).to(dt) for _ in range(4)]
+    lam = torch.linspace(0.1, 0.8, heads, device=DEV)
+    clean = _run(*t, lam, [n], [n], heads, hd, True, generic)
+    for i in (1, 2):                                    # a key, a value
+        s = [x.clone() for x in t]
+        s[i][at] = bad
+        r = _run(*s, lam, [n], [n], heads, hd, True, generic)
+        upto = max(0, at - reach)
+        for name, a, b in (("o", clean[0], r[0]), ("o2", clean[1], r[1]), ("dq", clean[3], r[3])):
+            _alike(a[:upto], b[:upto], slice(0, upto if reach else at // 64 * 64), (name, i))
+        assert torch.equal(clean[2][:, :at], r[2][:, :at]), i
+        if i == 2:
+            assert not torch.isfinite(r[0][at:]).any()
+    for i in (0, 3):                                    # a query, a gradient
+        s = [x.clone() for x in t]
+        s[i][at] = bad
+        r = _run(*s, lam, [n], [n], heads, hd, True, generic)
+        first = at + 1 + reach
+        for name, a, b in (("dk", clean[4], r[4]), ("dv", clean[5], r[5])):
+            _alike(a[first:], b[first:], slice(0 if reach else (at // 64 + 1) * 64 - first, None), (name, i))
+        assert not torch.isfinite(r[4 if i == 0 else 5][:at + 1]).all(dim=1).any(), i
