@@ -42,6 +42,13 @@ __device__ __forceinline__ KeyRange split_keys(const DiffAttnArgs& a, int kl, in
 }
 ds_status diff_join(const DiffAttnArgs& a, hipStream_t st);
 
+// Compute units that the rules of choice count on: an MI355X's, and not those of the current device, since the scratch is sized by one of them.
+constexpr int kDiffUnits = 256;
+// What a call takes (see DiffChoice in diff_attention_api.hip): wavefronts that share a block of queries, whether there is no work list; columns of a work-group
+int diff_mfma_sharing(const DiffAttnArgs& a);
+bool diff_mfma_direct(const DiffAttnArgs& a, bool backward);
+int diff_general_columns(const DiffAttnArgs& a, int max_len);
+
 size_t diff_scratch_bytes(int n_heads, int q_total_rows, int k_total_rows, int n_seq);
 ds_status diff_fwd_general(const DiffAttnArgs& a, hipStream_t st);
 ds_status diff_bwd_general(const DiffAttnArgs& a, hipStream_t st);

@@ -11,7 +11,7 @@
 //     1 sequence of 512, 1024, 4096 keys:  15 -> 10, 24 -> 10, 77 -> 12 / 39 -> 11, 74 -> 11, 287 -> 22; of 32768 keys: 575 -> 37 (3.6 TB/s)
 //     16 sequences of 2048, 16384 keys:  44 -> 33, 295 -> 195 (5.5 TB/s; one work-group for a compute unit: 37, 322)
 //     16 sequences of 33 queries and 1019 keys:  28 -> 23 (two work-groups with half of them each: 29)
-static constexpr int kSplitQueries = 64, kSplitUnits = 256, kSplitMost = 64;
+static constexpr int kSplitQueries = 64, kSplitMost = 64;
 static int most_splits(bool general, int n_heads, int head_dim, int q_total_rows, int max_k_len, int n_seq) {
     const int from = general ? 129 : 321, keys_one = general ? 64 : 128, keys_two = general ? 64 : 1024;
     const long long items = (long long)n_seq * n_heads;
@@ -19,7 +19,7 @@ static int most_splits(bool general, int n_heads, int head_dim, int q_total_rows
     auto with = [&](long long groups, int keys) {
         return std::min({groups / items, (long long)kSplitMost, ((long long)max_k_len + keys - 1) / keys});
     };
-    const long long one = with(kSplitUnits, keys_one), two = head_dim <= 64 ? with(2 * kSplitUnits, keys_two) : 1;
+    const long long one = with(kDiffUnits, keys_one), two = head_dim <= 64 ? with(2 * kDiffUnits, keys_two) : 1;
     return (int)std::max<long long>(std::max(one, two), 1);
 }
 
@@ -48,6 +48,8 @@ static ds_status check(DiffAttnArgs& a) {
     const long long wide = (long long)a.n_heads * a.head_dim;
     if (a.ldq < wide || a.ldk < wide || a.ldv < wide || a.ldo < wide) return DS_EINVAL;
     if (!a.scratch || (uintptr_t)a.scratch % 16 || a.scratch_bytes < diff_scratch_bytes(a.n_heads, a.q_total_rows, a.k_total_rows, a.n_seq)) return DS_EINVAL;
+    a.max_q_len = std::min(a.max_q_len, a.q_total_rows);
+    a.max_k_len = std::min(a.max_k_len, a.k_total_rows);
     const size_t size = dtype_size(a.dtype);
     for (const void* p : {a.q, a.k, a.v, (const void*)a.o, (const void*)a.o2, a.d_o, (const void*)a.dq, (const void*)a.dk, (const void*)a.dv})
         if ((uintptr_t)p % size) return DS_EINVAL;
@@ -65,6 +67,35 @@ static ds_status check(DiffAttnArgs& a) {
     a.split_part = (float*)after_lists;
     a.lam_part = (float*)(after_lists + entries * 32);
     return DS_OK;
+}
+
+// How a call goes to the kernels: fp32 arithmetic or bf16 matrix cores; bf16: whether there is no work list, wavefronts that share a block of queries; both:
+// work-groups that share a head's keys (forward); fp32 backward: columns of a work-group of the dQ and of the dK/dV kernel.
+struct DiffChoice { int32_t general, direct, sharing, k_splits, dq_columns, dkv_columns; };
+static DiffChoice choose(const DiffAttnArgs& a, bool backward, bool force_generic) {
+    DiffChoice c = {force_generic || !diff_mfma_supported(a), 0, 1, 1, 64, 64};
+    if (!c.general) {
+        c.direct = diff_mfma_direct(a, backward);
+        c.sharing = diff_mfma_sharing(a);
+    }
+    if (backward) {
+        c.dq_columns = diff_general_columns(a, a.max_q_len);
+        c.dkv_columns = diff_general_columns(a, a.max_k_len);
+    } else if (!a.mask && a.max_q_len <= kSplitQueries && (c.general || c.sharing > 1)) {
+        c.k_splits = most_splits(c.general, a.n_heads, a.head_dim, a.q_total_rows, a.max_k_len, a.n_seq);
+    }
+    return c;
+}
+// For tests: what `choose` says of a call whose tensors have the least strides and are aligned, in the order of DiffChoice.  Not part of the C ABI's header.
+extern "C" void ds_diff_attention_choice(int32_t dtype, int32_t n_seq, int32_t n_heads, int32_t head_dim, int32_t mask, int32_t max_q_len, int32_t max_k_len,
+                                         int32_t q_total_rows, int32_t k_total_rows, int32_t backward, int32_t force_generic, int32_t* out) {
+    DiffAttnArgs a = {};
+    a.dtype = dtype; a.n_seq = n_seq; a.n_heads = n_heads; a.head_dim = head_dim; a.mask = mask;
+    a.max_q_len = std::min(max_q_len, q_total_rows); a.max_k_len = std::min(max_k_len, k_total_rows);
+    a.q_total_rows = q_total_rows; a.k_total_rows = k_total_rows;
+    a.ldq = a.ldk = a.ldv = a.ldo = (long long)n_heads * head_dim;
+    const DiffChoice c = choose(a, backward != 0, force_generic != 0);
+    for (const int32_t v : {c.general, c.direct, c.sharing, c.k_splits, c.dq_columns, c.dkv_columns}) *out++ = v;
 }
 
 extern "C" int64_t ds_diff_attention_scratch_bytes(int32_t n_heads, int32_t q_total_rows, int32_t k_total_rows, int32_t n_seq) {
@@ -88,10 +119,9 @@ extern "C" ds_status ds_diff_attention_fwd(int32_t dtype, int32_t n_seq, int32_t
     a.scratch = scratch; a.scratch_bytes = scratch_bytes < 0 ? 0 : (size_t)scratch_bytes;
     const ds_status r = check(a);
     if (r != DS_OK) return r;
-    const bool general = force_generic || !diff_mfma_supported(a);
-    if (!mask && max_q_len <= kSplitQueries)
-        a.k_splits = most_splits(general, n_heads, head_dim, q_total_rows, std::min(max_k_len, k_total_rows), n_seq);
-    if (!general) return diff_fwd_mfma(a, (hipStream_t)hip_stream);
+    const DiffChoice c = choose(a, false, force_generic != 0);
+    a.k_splits = c.k_splits;
+    if (!c.general) return diff_fwd_mfma(a, (hipStream_t)hip_stream);
     return diff_fwd_general(a, (hipStream_t)hip_stream);
 }
 
@@ -115,6 +145,6 @@ extern "C" ds_status ds_diff_attention_bwd(int32_t dtype, int32_t n_seq, int32_t
     const ds_status r = check(a);
     if (r != DS_OK) return r;
     if (!o2 || !d_o || !dq || !dk || !dv || !dlambda || (accumulate != 0 && accumulate != 1)) return DS_EINVAL;
-    if (!force_generic && diff_mfma_supported(a)) return diff_bwd_mfma(a, (hipStream_t)hip_stream);
+    if (!choose(a, true, force_generic != 0).general) return diff_bwd_mfma(a, (hipStream_t)hip_stream);
     return diff_bwd_general(a, (hipStream_t)hip_stream);
 }

@@ -434,7 +434,7 @@ ds_status bwd_launch(const DiffAttnArgs& a, hipStream_t st) {
 
 ds_status diff_bwd_mfma(const DiffAttnArgs& a0, hipStream_t st) {
     DiffAttnArgs a = a0;
-    a.direct = one_block_each(a, a.max_q_len, a.max_k_len) && one_block_each(a, a.max_k_len, a.max_q_len);
+    a.direct = diff_mfma_direct(a, true);
     const ds_status r = a.direct ? DS_OK : attn_prepare_lists(a, true, st);
     if (r != DS_OK) return r;
     return diff_by_kind(a, [&](auto hd, auto causal, auto split) { return bwd_launch<decltype(hd)::value, decltype(causal)::value, decltype(split)::value>(a, st); });

@@ -260,10 +260,15 @@ bool diff_mfma_supported(const DiffAttnArgs& a) {
     return ((long long)a.q_total_rows / 128 + a.n_seq + 8) * a.n_heads <= 0x7fffffffLL && ((long long)a.k_total_rows / 128 + a.n_seq + 8) * a.n_heads <= 0x7fffffffLL;
 }
 
+int diff_mfma_sharing(const DiffAttnArgs& a) { return sharing(a); }
+bool diff_mfma_direct(const DiffAttnArgs& a, bool backward) {
+    return one_block_each(a, a.max_q_len, a.max_k_len) && (!backward || one_block_each(a, a.max_k_len, a.max_q_len));
+}
+
 ds_status diff_fwd_mfma(const DiffAttnArgs& a0, hipStream_t st) {
     return diff_by_kind(a0, [&](auto hd, auto causal, auto split) {
         DiffAttnArgs a = a0;
-        a.direct = one_block_each(a, a.max_q_len, a.max_k_len);
+        a.direct = diff_mfma_direct(a, false);
         const ds_status r = split == 1 && !a.direct ? attn_prepare_lists(a, false, st) : DS_OK;
         return r != DS_OK ? r : fwd_launch<decltype(hd)::value, decltype(causal)::value, decltype(split)::value>(a, st);
     });

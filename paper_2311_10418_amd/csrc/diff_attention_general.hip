@@ -541,11 +541,11 @@ template <class T, int HH> void fwd_launch(const DiffAttnArgs& a, hipStream_t st
     const dim3 grid = a.k_splits > 1 ? dim3(a.k_splits, a.n_heads, a.n_seq) : column_grid(a, a.max_q_len);
     hipLaunchKernelGGL((diff_fwd_kernel<T, HH>), grid, dim3(256), 0, st, a);
 }
-// Fewer work-groups of 64 columns than two for a compute unit: 32 columns each.  64 -> 32, dQ and dK/dV together, fp32, heads of 64: 23 sequences of 88
+// Fewer work-groups of 64 columns than two for a compute unit: 32 columns each (up to head size 96: above, a tile has no 16 rows for each of four wavefronts).  64 -> 32, dQ and dK/dV together, fp32, heads of 64: 23 sequences of 88
 // to 177, 4 heads, causal (276 work-groups) 59 -> 52 us; 3 of 100 to 200, 2 heads 50 -> 35; but 31 of 366 to 523, 16 heads (4 464) 1 114 -> 1 226.
-bool narrow(const AttnArgs& a, int max_len) { return (long long)a.n_seq * a.n_heads * (max_len / 64 + 1) <= 2LL * gemm_cu_count(); }
+bool narrow(const DiffAttnArgs& a, int max_len) { return diff_general_columns(a, max_len) == 32; }
 template <class T, int HH> void dq_launch(const DiffAttnArgs& a, hipStream_t st) {
-    if constexpr (HH <= 48)                             // (above, a tile has no 16 rows for each of four wavefronts)
+    if constexpr (HH <= 48)
         if (narrow(a, a.max_q_len)) {
             hipLaunchKernelGGL((diff_bwd_dq_kernel<T, HH, 32>), column_grid(a, a.max_q_len, 32), dim3(512), 0, st, a);
             return;
@@ -563,6 +563,10 @@ template <class T, int HH> void dkv_launch(const DiffAttnArgs& a, hipStream_t st
 }
 
 }  // namespace
+
+int diff_general_columns(const DiffAttnArgs& a, int max_len) {
+    return a.head_dim <= 96 && (long long)a.n_seq * a.n_heads * (max_len / 64 + 1) <= 2LL * kDiffUnits ? 32 : 64;
+}
 
 #define DS_DIFF_DISPATCH(launch)                                              \
     do {                                                                      \

@@ -63,7 +63,7 @@ __device__ __forceinline__ int block_count(const DiffAttnArgs& a, int list) { re
 // heads of 64: 16 sequences of 96 tokens 10.1 -> 7.0 / 20.0 -> 16.8, 64 of 128 23.1 -> 19.7 / 61.2 -> 58.7, 256 of 32 25.5 -> 21.6 / 86.9 -> 83.1; but 256 of
 // 128 85 -> 90 / 238 -> 242.
 inline bool one_block_each(const DiffAttnArgs& a, int max_len, int other_len) {
-    const long long items = (long long)a.n_seq * a.n_heads, units = gemm_cu_count();
+    const long long items = (long long)a.n_seq * a.n_heads, units = kDiffUnits;
     return max_len <= 128 && (items <= units || (a.head_dim == 64 && other_len <= 128 && items * max_len <= 1024 * units));
 }
 
@@ -156,12 +156,17 @@ __device__ __forceinline__ void store_cols16(const f32x16_t (&acc)[HD / 32], flo
 //    64 sequences, 33 queries,  500 keys:  36 ->  38 /  61 ->  82     200 sequences, 20 queries,  300 keys:  52 -> 78 / 122 -> 208
 // and without a list on either, keys split where there are enough: 1 sequence, 1 query, 256 keys 7.8 -> 8.0 / 10.2 -> 11.5, 300 keys 9.3 -> 9.7 / 12.0 -> 12.4,
 // 512 keys 12 -> 9.5 / 16 -> 12.2
+inline int sharing(const DiffAttnArgs& a) {
+    const bool few = (long long)a.n_seq * a.n_heads * a.head_dim <= 64LL * kDiffUnits;
+    if (a.mask || !few || a.max_k_len <= 320 || a.max_q_len > 64) return 1;
+    return a.max_q_len <= 32 ? 4 : 2;
+}
 template <class F> ds_status diff_by_kind(const DiffAttnArgs& a, F f) {
-    const bool few = (long long)a.n_seq * a.n_heads * a.head_dim <= 64LL * gemm_cu_count();
     auto by_mask = [&](auto hd) {
         if (a.mask) return f(hd, std::true_type{}, std::integral_constant<int, 1>{});
-        if (!few || a.max_k_len <= 320 || a.max_q_len > 64) return f(hd, std::false_type{}, std::integral_constant<int, 1>{});
-        if (a.max_q_len <= 32) return f(hd, std::false_type{}, std::integral_constant<int, 4>{});
+        const int ks = sharing(a);
+        if (ks == 1) return f(hd, std::false_type{}, std::integral_constant<int, 1>{});
+        if (ks == 4) return f(hd, std::false_type{}, std::integral_constant<int, 4>{});
         return f(hd, std::false_type{}, std::integral_constant<int, 2>{});
     };
     return a.head_dim == 128 ? by_mask(std::integral_constant<int, 128>{}) : by_mask(std::integral_constant<int, 64>{});

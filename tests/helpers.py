@@ -179,3 +179,13 @@ def gemm_launches(M, N, K, trans_a=False, epilogue=ds.DS_EPI_NONE, ws_floats=0, 
     n = ds.lib().ds_gemm_launches(int(trans_a), int(not trans_a), M, N, K, epilogue, ctypes.c_int64(ws_floats), int(colsum), int(accumulate), out)
     tiles = {-1: "256", 100: "192", 101: "128", 0: "128x128", 1: "128x64", 2: "64x64", 3: "128x128/2"}
     return [dict(rows=o[0], tile=tiles[o[1]], splits=o[2], whole=o[3], pieces=o[4], persistent=bool(o[5])) for o in list(out)[:n]]
+
+
+DIFF_CHOICE = ("general", "direct", "sharing", "splits", "dq_columns", "dkv_columns")
+
+
+def diff_choice(bf16, n_seq, heads, hd, causal, max_q, max_k, q_rows=None, k_rows=None, backward=False, generic=False):
+    """Which kernels a call of differential attention on aligned tensors takes (host): see DiffChoice in csrc/diff_attention_api.hip."""
+    out = (ctypes.c_int32 * len(DIFF_CHOICE))()
+    ds.lib().ds_diff_attention_choice(int(bf16), n_seq, heads, hd, int(causal), max_q, max_k, q_rows or n_seq * max_q, k_rows or n_seq * max_k, int(backward), int(generic), out)
+    return dict(zip(DIFF_CHOICE, out))
