@@ -67,3 +67,16 @@ def test_columns_of_the_fp32_backward_kernels(hd, n, length, cols):
     rng = np.random.default_rng(n + length)
     lens = [length] + [int(x) for x in rng.integers(1, 40, n - 1)]
     _run(F32, 4, hd, lens, lens, True, dict(general=1), dict(general=1, dq_columns=cols, dkv_columns=cols))
+
+
+@pytest.mark.parametrize("causal", [False, True])
+def test_many_items_for_each_persistent_work_group(causal):
+    """Heads of 128: work-groups of the dK/dV kernel draw three blocks of keys and more (over 4 x 256 pairs of block and head): blocks of many steps, whose ring of
+    four stages wraps, of one, and without any (no queries; keys beyond the last query of a causal sequence) in one order and another."""
+    rng = np.random.default_rng(12)
+    ql, kl = [], []
+    for i in range(52):
+        ql.append([0, 1, int(rng.integers(300, 420)), int(rng.integers(2, 70)), int(rng.integers(130, 300))][i % 5])
+        kl.append([int(rng.integers(1, 300)), int(rng.integers(130, 400)), int(rng.integers(1, 200)), int(rng.integers(150, 300)), 0 if i % 3 else 130][i % 5])
+    assert 16 * sum((k + 127) // 128 for k in kl) > 4 * 256
+    _run(BF, 16, 128, ql, kl, causal, dict(general=0, direct=0), dict(general=0, direct=0))
