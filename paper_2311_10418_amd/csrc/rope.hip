@@ -117,11 +117,19 @@ ds_status rope_launch(RopeArgs a, bool interleaved, hipStream_t st) {
     const bool copies = a.x != a.y && a.rot < a.head_dim;
     a.lanes = a.rot / 2 / V + (copies ? (a.head_dim - a.rot) / V : 0);
     a.per_row = a.lanes * ((a.n_heads + 3) / 4);        // about four heads per thread
-    const long long threads = (long long)a.rows * a.per_row, groups = (threads + 255) / 256;
-    if (groups > 0x7fffffffLL) return DS_EINVAL;
-    if (interleaved) hipLaunchKernelGGL((rope_kernel<T, true, V>), dim3((unsigned)groups), dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((rope_kernel<T, false, V>), dim3((unsigned)groups), dim3(256), 0, st, a);
-    DS_LAUNCH_CHECK();
+    // a launch has fewer than 2^32 threads, and per_row is below 2^30: a range of rows each
+    const long long rows = a.rows, most = (0xffffffffLL / 256) * 256 / a.per_row;
+    for (long long r0 = 0; r0 < rows; r0 += most) {
+        RopeArgs part = a;
+        part.rows = (int32_t)(rows - r0 < most ? rows - r0 : most);
+        part.pos = a.pos + r0;
+        part.x = (const T*)a.x + r0 * a.ldx;
+        part.y = (T*)a.y + r0 * a.ldy;
+        const dim3 grid((unsigned)(((long long)part.rows * a.per_row + 255) / 256));
+        if (interleaved) hipLaunchKernelGGL((rope_kernel<T, true, V>), grid, dim3(256), 0, st, part);
+        else hipLaunchKernelGGL((rope_kernel<T, false, V>), grid, dim3(256), 0, st, part);
+        DS_LAUNCH_CHECK();
+    }
     return DS_OK;
 }
 

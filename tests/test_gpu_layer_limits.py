@@ -174,3 +174,25 @@ def test_values_that_are_not_finite_stay_where_they_are_seen(bad, dt, generic, h
         for name, a, b in (("dk", clean[4], r[4]), ("dv", clean[5], r[5])):
             _alike(a[first:], b[first:], slice(0 if reach else (at // 64 + 1) * 64 - first, None), (name, i))
         assert not torch.isfinite(r[4 if i == 0 else 5][:at + 1]).all(dim=1).any(), i
+
+
+# ------------------------------------------------------------------------------------ rotary positions
+def test_rows_of_more_threads_than_a_launch_has():
+    """Single pairs of more rows than fit into 2^32 threads: the rows around the border and the last ones get what they get alone, all others are left alone."""
+    rows, hd = (1 << 32) // 3 + 1000, 6
+    freq = torch.from_numpy(ds.ds_rope_freqs(hd)).to(DEV)
+    x = torch.zeros((rows, hd), dtype=BF, device=DEV)
+    pos = torch.full((rows,), -1, dtype=torch.int32, device=DEV)
+    border = ((1 << 32) - 256) // 3
+    at = torch.tensor([0, 1, border - 1, border, border + 1, rows - 2, rows - 1], device=DEV)
+    g = torch.Generator(device=DEV).manual_seed(1)
+    x[at] = torch.randn((len(at), hd), generator=g, device=DEV).to(BF)
+    x[border + 2] = 5.0
+    pos[at] = torch.arange(3, 3 + len(at), dtype=torch.int32, device=DEV)
+    one = x[at].contiguous()
+    before = one.clone()
+    ds.ds_rope(x, x, pos, freq, 1, hd, hd)
+    ds.ds_rope(one, one, pos[at].contiguous(), freq, 1, hd, hd)
+    torch.cuda.synchronize()
+    assert torch.equal(x[at], one) and not torch.equal(one, before)
+    assert (x[border + 2] == 5.0).all() and not x[2:border - 1:9973].any() and not x[border + 3:rows - 2:9973].any()
