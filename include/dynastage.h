@@ -536,8 +536,8 @@ int64_t ds_diff_attention_scratch_bytes(int32_t n_heads, int32_t q_total_rows, i
  *     P_i = softmax(Q_i K_i^T / sqrt(head_dim / 2)),   O2 = P_2 V,   O = P_1 V - lambda[h] O2.
  * head_dim: a multiple of 16, at most 128.  lambda: DEVICE float32[n_heads].  o, o2: [q_total_rows, ...] with row stride ldo; o2 is
  * what the backward pass needs beside o and may be NULL.  lse: float32 [2 * n_heads, q_total_rows], map m of head h at 2h + m.
- * q_total_rows / k_total_rows: rows of the tensors holding the queries / the keys; max_q_len / max_k_len: upper bounds of the lengths.
- * Rows not covered by any sequence are not touched; the sequences must not overlap; one with k_len[s] = 0 gets zero outputs.
+ * q_total_rows / k_total_rows: rows of the tensors holding the queries / the keys; max_q_len / max_k_len: upper bounds of the lengths
+ * (of which the rows of the tensors are one too), in the kernels that compute in fp32 at most 2^28.  Rows not covered by any sequence are not touched; the sequences must not overlap; one with k_len[s] = 0 gets zero outputs.
  * Strides and alignments of the element type are taken as they are.  scratch: DEVICE, 16-byte aligned, at least
  * ds_diff_attention_scratch_bytes.  force_generic != 0 selects the kernels that compute in fp32 whatever the type.
  * Values that are not finite: a row is affected by the rows it sees.  The bf16 matrix-core kernels multiply whole blocks by probabilities

@@ -86,6 +86,8 @@ static DiffChoice choose(const DiffAttnArgs& a, bool backward, bool force_generi
     }
     return c;
 }
+// the general kernels: 64 tokens to a work-group of 512 threads, fewer than 2^32 of them along a sequence
+static bool too_long(const DiffAttnArgs& a) { return std::max(a.max_q_len, a.max_k_len) > 1 << 28; }
 // For tests: what `choose` says of a call whose tensors have the least strides and are aligned, in the order of DiffChoice.  Not part of the C ABI's header.
 extern "C" void ds_diff_attention_choice(int32_t dtype, int32_t n_seq, int32_t n_heads, int32_t head_dim, int32_t mask, int32_t max_q_len, int32_t max_k_len,
                                          int32_t q_total_rows, int32_t k_total_rows, int32_t backward, int32_t force_generic, int32_t* out) {
@@ -120,6 +122,7 @@ extern "C" ds_status ds_diff_attention_fwd(int32_t dtype, int32_t n_seq, int32_t
     const ds_status r = check(a);
     if (r != DS_OK) return r;
     const DiffChoice c = choose(a, false, force_generic != 0);
+    if (c.general && too_long(a)) return DS_EINVAL;
     a.k_splits = c.k_splits;
     if (!c.general) return diff_fwd_mfma(a, (hipStream_t)hip_stream);
     return diff_fwd_general(a, (hipStream_t)hip_stream);
@@ -146,5 +149,6 @@ extern "C" ds_status ds_diff_attention_bwd(int32_t dtype, int32_t n_seq, int32_t
     if (r != DS_OK) return r;
     if (!o2 || !d_o || !dq || !dk || !dv || !dlambda || (accumulate != 0 && accumulate != 1)) return DS_EINVAL;
     if (!choose(a, true, force_generic != 0).general) return diff_bwd_mfma(a, (hipStream_t)hip_stream);
+    if (too_long(a)) return DS_EINVAL;
     return diff_bwd_general(a, (hipStream_t)hip_stream);
 }

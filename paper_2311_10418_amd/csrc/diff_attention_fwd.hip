@@ -256,8 +256,9 @@ bool diff_mfma_supported(const DiffAttnArgs& a) {
         if (ld % 8 || ld >= ld_max) return false;
     for (const void* p : {a.q, a.k, a.v, (const void*)a.o, (const void*)a.o2, a.d_o, (const void*)a.dq, (const void*)a.dk, (const void*)a.dv})
         if ((uintptr_t)p & 15) return false;
-    // the grids: one work-group per (block of 128 rows, head), and at most eight for a head beside them
-    return ((long long)a.q_total_rows / 128 + a.n_seq + 8) * a.n_heads <= 0x7fffffffLL && ((long long)a.k_total_rows / 128 + a.n_seq + 8) * a.n_heads <= 0x7fffffffLL;
+    // the grids: one work-group per (block of 128 rows, head), and at most eight for a head beside them; fewer than 2^32 threads
+    const long long most = 0xffffffffLL / 256;
+    return ((long long)a.q_total_rows / 128 + a.n_seq + 8) * a.n_heads <= most && ((long long)a.k_total_rows / 128 + a.n_seq + 8) * a.n_heads <= most;
 }
 
 int diff_mfma_sharing(const DiffAttnArgs& a) { return sharing(a); }

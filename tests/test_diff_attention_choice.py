@@ -82,3 +82,12 @@ def test_columns_of_the_fp32_backward_kernels(which, length):
     for hd in (16, 64, 96):
         _sides(which, 32, 64, at={length: 255}, **{k: v for k, v in dict(a, hd=hd).items() if k != length})      # 128 pairs of 4 blocks: two for a compute unit
     assert diff_choice(**dict(a, hd=112))[which] == 64
+
+
+def test_grids_stay_below_two_to_the_32_threads():
+    """16 777 215 work-groups of 256 threads: beyond, bf16 calls take the general kernels, whose grids have heads and sequences on axes of their own."""
+    a = dict(bf16=True, n_seq=64000, hd=64, causal=True, max_q=1, max_k=1)
+    for backward in (False, True):
+        _sides("general", 0, 1, at=dict(heads=260), **a, backward=backward)          # (500 + 64 000 + 8) x 260
+        assert diff_choice(True, 1, 16, 64, False, 1, (1 << 31) - 1, 1, (1 << 31) - 1, backward)["general"] == 1
+        assert diff_choice(True, 1, 16, 64, False, 1, 1 << 26, 1, 1 << 26, backward)["general"] == 0

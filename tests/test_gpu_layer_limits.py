@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from paper_2311_10418_amd import binding as ds
-from helpers import DEV
+from helpers import DEV, diff_choice
 
 pytestmark = pytest.mark.gpu
 
@@ -174,6 +174,20 @@ def test_values_that_are_not_finite_stay_where_they_are_seen(bad, dt, generic, h
         for name, a, b in (("dk", clean[4], r[4]), ("dv", clean[5], r[5])):
             _alike(a[first:], b[first:], slice(0 if reach else (at // 64 + 1) * 64 - first, None), (name, i))
         assert not torch.isfinite(r[4 if i == 0 else 5][:at + 1]).all(dim=1).any(), i
+
+
+def test_more_work_groups_than_a_launch_of_the_matrix_core_kernels_has():
+    """64 000 single tokens, 261 heads: one key, so that O2 = V, O = (1 - lambda) V = V / 2 and dV = dO / 2, exactly; dP - D and with it dQ and dK are what two sums of 64
+    products in different orders differ by, 128 x 2^-24 of at most 2^10."""
+    n, heads, hd = 64000, 261, 64
+    assert diff_choice(True, n, heads, hd, True, 1, 1)["general"] and not diff_choice(True, n, heads - 1, hd, True, 1, 1)["general"]
+    g = torch.Generator(device=DEV).manual_seed(2)
+    q, k, v, d_o = (torch.randn((n, heads * hd), generator=g, device=DEV, dtype=BF) for _ in range(4))
+    lam = torch.full((heads,), 0.5, device=DEV)
+    o, o2, lse, dq, dk, dv, dlam = _run(q, k, v, d_o, lam, [1] * n, [1] * n, heads, hd, True)
+    assert torch.equal(o2, v) and torch.equal(o, v / 2) and torch.equal(dv, d_o / 2)
+    assert float(dq.abs().max()) <= 2.0 ** -7 and float(dk.abs().max()) <= 2.0 ** -7
+    assert torch.isfinite(dlam).all()
 
 
 # ------------------------------------------------------------------------------------ rotary positions

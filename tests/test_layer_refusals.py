@@ -134,3 +134,12 @@ def test_differential_attention(back):
         bad += [dict(o2=None), dict(d_o=None), dict(dq=None), dict(dk=None), dict(dv=None), dict(dlam=None), dict(accumulate=2), dict(dq=P + 1), dict(d_o=P + 1)]
     for kw in bad:
         assert _diff(back, **dict(dict(scratch_bytes=1 << 40), **kw)) == BAD, kw
+
+
+@pytest.mark.parametrize("back", [False, True])
+def test_differential_attention_of_too_long_sequences(back):
+    """The fp32 kernels, in bf16 too: more than 2^28 tokens of a sequence, queries or keys."""
+    n = (1 << 28) + 1
+    small = dict(scratch_bytes=1 << 60, n_seq=1, n_heads=1, head_dim=16, ldq=16, ldk=16, ldv=16, ldo=16)
+    for kw in (dict(max_q_len=n, q_total_rows=n), dict(max_k_len=n, k_total_rows=n), dict(max_q_len=0x7fffffff, q_total_rows=0x7fffffff, dtype=0)):
+        assert _diff(back, **dict(small, **kw)) == BAD, kw
