@@ -210,3 +210,33 @@ def test_rows_of_more_threads_than_a_launch_has():
     torch.cuda.synchronize()
     assert torch.equal(x[at], one) and not torch.equal(one, before)
     assert (x[border + 2] == 5.0).all() and not x[2:border - 1:9973].any() and not x[border + 3:rows - 2:9973].any()
+
+
+# ------------------------------------------------------------------------------------ numbers of more than 32 bits
+def test_strides_rows_and_lengths_beyond_32_bits_are_refused():
+    """(Taken modulo 2^32 each of these would be a call on other rows.)"""
+    heads, hd, ld = 2, 64, (1 << 32) + 256
+    w = heads * hd
+    far = torch.empty(ld + w, dtype=BF, device=DEV).as_strided((2, w), (ld, 1))      # two rows 2^32 + 256 elements apart
+    near = [torch.zeros((2, w), dtype=BF, device=DEV) for _ in range(5)]
+    lam, lse = torch.zeros(heads, device=DEV), torch.zeros((2 * heads, 2), device=DEV)
+    scratch = torch.zeros(int(ds.ds_diff_attention_scratch_bytes(heads, 2, 2, 1)), dtype=torch.uint8, device=DEV)
+    rest = (i32([0]), i32([2]), i32([0]), i32([2]), heads, hd, True)
+
+    def forward(q=near[0], k=near[1], v=near[2], o=near[3], longest=2):
+        ds.ds_diff_attention_fwd(q, k, v, lam, o, lse, *rest, longest, longest, scratch)
+
+    forward()
+    for kw in (dict(q=far), dict(k=far), dict(v=far), dict(o=far), dict(longest=(1 << 32) + 2)):
+        with pytest.raises(ValueError):
+            forward(**kw)
+    with pytest.raises(ValueError):
+        ds.ds_diff_attention_bwd(*near[:3], lam, far, far, far, lse, *near[:3], lam, *rest, 2, 2, scratch)
+    x = torch.empty(((1 << 32) + 2, 8), dtype=BF, device=DEV)
+    with pytest.raises(ValueError):
+        ds.ds_resid_norm_fwd(x, x, x, torch.empty(1, device=DEV).expand(4, (1 << 32) + 2))
+    with pytest.raises(ValueError):
+        ds.ds_resid_norm_bwd(x, x, x, lse, x, x, lam)
+    with pytest.raises(ValueError):
+        ds.ds_rope(x, x, torch.empty(1, dtype=torch.int32, device=DEV).expand((1 << 32) + 2), torch.zeros(4, dtype=torch.float64, device=DEV), 1, 8, 8)
+    torch.cuda.synchronize()
