@@ -80,3 +80,46 @@ def test_many_items_for_each_persistent_work_group(causal):
         kl.append([int(rng.integers(1, 300)), int(rng.integers(130, 400)), int(rng.integers(1, 200)), int(rng.integers(150, 300)), 0 if i % 3 else 130][i % 5])
     assert 16 * sum((k + 127) // 128 for k in kl) > 4 * 256
     _run(BF, 16, 128, ql, kl, causal, dict(general=0, direct=0), dict(general=0, direct=0))
+
+
+@pytest.mark.parametrize("dt,hd,direct", [(BF, 64, 0), (BF, 128, 0), (BF, 64, 1), (BF, 128, 1), (F32, 64, 0)])
+@pytest.mark.parametrize("causal", [False, True])
+def test_lists_and_draws_in_a_graph(dt, hd, direct, causal):
+    """Both directions captured with a scratch that holds anything before each replay: lists, counters of the persistent kernel and statistics are the call's own."""
+    lens = [40, 0, 128, 33] * 4 if direct else [150, 0, 129, 300, 64, 17] * 5
+    heads = 8
+    c = Case(3, dt, heads, hd, lens, lens[::-1], causal)
+    got = diff_choice(dt == BF, len(lens), heads, hd, causal, max(lens), max(lens), c.Tq, c.Tk, True)
+    assert (got["general"], got["direct"]) == (int(dt == F32), direct)
+    c.run(False)
+    outs = (c.o, c.o2, c.lse, c.dq, c.dk, c.dv, c.dlam)
+    want = [t.clone() for t in outs]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c.forward()
+        c.backward()
+    for i in range(4):
+        for t in outs:
+            t[:] = 9.0
+        c.scratch.fill_(50 * i)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(want, outs):
+            assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dt,generic", [(F32, False), (BF, True), (BF, False)])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("bound", [0, 50, 200, 5000])
+def test_no_tokens_at_all_and_bounds_that_are_too_large(dt, generic, causal, hd, bound):
+    """Sequences without queries, without keys, without either; upper bounds of the lengths above the lengths and above the rows."""
+    for ql, kl in (([0, 0, 0], [5, 0, 70]), ([5, 70, 0], [0, 0, 0]), ([0], [0]), ([3, 40, 130, 0], [200, 7, 1, 9])):
+        c = Case(hd + bound, dt, 2, hd, ql, kl, causal)
+        tables = c.args()
+        c.args = lambda: (*tables[:-3], max(tables[-3], bound), max(tables[-2], bound), tables[-1])
+        c.run(generic, accumulate=True)
+        lse = c.lse.cpu()
+        for r, n, k in zip(c.q_row, ql, kl):
+            assert k or bool((lse[:, r:r + n] == -float("inf")).all())
