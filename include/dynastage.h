@@ -539,7 +539,13 @@ int64_t ds_diff_attention_scratch_bytes(int32_t n_heads, int32_t q_total_rows, i
  * q_total_rows / k_total_rows: rows of the tensors holding the queries / the keys; max_q_len / max_k_len: upper bounds of the lengths
  * (of which the rows of the tensors are one too), in the kernels that compute in fp32 at most 2^28.  Rows not covered by any sequence are not touched; the sequences must not overlap; one with k_len[s] = 0 gets zero outputs.
  * Strides and alignments of the element type are taken as they are.  scratch: DEVICE, 16-byte aligned, at least
- * ds_diff_attention_scratch_bytes.  force_generic != 0 selects the kernels that compute in fp32 whatever the type.
+ * ds_diff_attention_scratch_bytes.
+ * Precision: bf16 heads of 64 and 128 with 16-byte aligned rows go to the matrix cores, where probabilities, their difference and their
+ * gradients are rounded to bf16 as they are multiplied (at most 2^-8 of each); every other call, and with force_generic != 0 all of them,
+ * to kernels that compute in fp32.  Backward takes the row sums of dO o and dO o2 from o and o2 as stored, and probabilities from lse: they
+ * are off by up to 2^-22 of a score's size (after scaling), which is a quarter of them at scores of 2^20.
+ * Speed: at most 64 queries over long keys (tokens on a cache; mask = 0) are shared out over work-groups if the q tensor has at
+ * most 64 rows for each sequence.
  * Values that are not finite: a row is affected by the rows it sees.  The bf16 matrix-core kernels multiply whole blocks by probabilities
  * that are 0 where mask = 1 hides a token, so that an infinity or NaN may also reach rows up to 31 tokens in front of it in o, o2
  * and dq (31 behind it in dk and dv). */

@@ -4,7 +4,8 @@
 #include <algorithm>
 #include <cmath>
 
-// Work-groups that share the keys of a head, for sequences of at most 64 rows of queries each: as many as make one for every compute unit, with a least
+// Work-groups that share the keys of a head, for sequences of at most 64 queries in a tensor of at most 64 rows for each of them (the shares go to
+// scratch by row of that tensor, whose lengths the scratch's size does not know): as many as make one for every compute unit, with a least
 // number of keys each; two, which head sizes up to 64 have the LDS for, with more keys each; at most one for a lane of the wavefront that joins them.
 // Matrix-core kernels: 128 keys, from 321 on (300 keys at once take 9.3 us, three shares of them and their joining 9.7); two from 1024 each on.
 // General kernels: 64 keys, for two as well.  One query of 16 heads of 64, us without -> with, bf16 / fp32:

@@ -9,13 +9,14 @@
 // P_1 - lambda P_2 before both sums are known, so it keeps two accumulators and multiplies every fragment of V^T by both maps'
 // probabilities (6 instead of 4 products of a head's width; a first pass over the scores for the sums would cost the same).
 //
-// Probabilities, their difference and dS are rounded to bf16 as they become operands (the matrix instructions take nothing wider at this rate; half a
-// step is 2^-9 of a probability); scores, statistics, sums, dP and dlambda are fp32.
+// Probabilities, their difference and dS are rounded to bf16 as they become operands (the matrix instructions take nothing wider at this rate), which is at
+// most 2^-8 of one, as for the results themselves; scores, statistics (in the dK/dV kernel as exact sums of bf16 values), sums, dP, D and dlambda are fp32.
+// D_1 and D_2 come from O and O_2 as stored.  Against 64 bits a result is 0.0024 to 0.0031 of its size off, where rounding it alone is 0.0017.
 //
 // Bound by issue: at two wavefronts per SIMD the matrix pipe (37 % of the cycles forward) and the vector instructions (43 %) add up, as an MFMA hides
 // about four vector instructions and a softmax of two maps has ten beside each.  Measured with 16 heads of 128, 8 sequences of 1 639 to 2 048 tokens,
-// causal: forward 200 us (536 TFLOP/s, counting four head sizes of operations a pair), dQ 250, dK/dV 368; 16 heads of 64, 31 sequences of 366 to 523,
-// unmasked: dQ 76, dK/dV 89.  One map of the whole head (attention_mfma.hip) takes 152 to 179 us forward and 504 to 538 backward on the first of them.
+// causal: forward 204 us (525 TFLOP/s, counting four head sizes of operations a pair), dQ 240, dK/dV 332; 16 heads of 64, 31 sequences of 366 to 523,
+// unmasked: dQ 77, dK/dV 91.  One map of the whole head (attention_mfma.hip) takes 152 to 179 us forward and 504 to 538 backward on the first of them.
 #include "diff_attention_tiles.hpp"
 #include <cfloat>
 #include <type_traits>

@@ -14,8 +14,9 @@
 // the kernels' time; this takes 1 % at most.)
 //
 // Bound by issue: the matrix pipe is busy 60 % of the SIMD cycles and vector instructions, more than two for each matrix instruction, take the rest.
-// Measured in fp32: 16 heads of 64, 31 sequences of 366 to 523, unmasked, forward 421 us, backward 997 (90 and 88 TFLOP/s
-// of the products they form, where a large product of matrices reaches 154); 4 heads of 64, 23 sequences of 88 to 177, causal, backward 41.5.
+// Measured in fp32: 16 heads of 64, 31 sequences of 366 to 523, unmasked, forward 398 us, backward 967 (93 and 90 TFLOP/s
+// of the products they form, where a large product of matrices reaches 154); 16 heads of 128, 8 of 1 639 to 2 048, causal, 1 791 and 6 036 (92 and 63: 32-row
+// tiles backward); 4 heads of 64, 23 sequences of 88 to 177, causal, backward 42.
 #include "diff_attention.hpp"
 #include "diff_attention_rows.hpp"
 #include "gemm.hpp"

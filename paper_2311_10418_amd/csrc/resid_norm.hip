@@ -458,7 +458,8 @@ int resident_groups(Kern kern, int threads, int& cached) {
     return gemm_cu_count() * per_cu;
 }
 
-// most work-groups of the backward kernel = rows of partial sums: eight rows and more each, and at most 2^24 floats of partial sums
+// most work-groups of the backward kernel = rows of partial sums: at most eight rows for each slot of a work-group until there are 1 024 of them (or what
+// the GPU holds), and so at most 2^24 floats of partial sums
 int bwd_most_groups(int rows, int d) {
     const int at_once = rows_per_group(d);
     const long long n = ((long long)rows + 8 * at_once - 1) / (8 * at_once), most = 1024;
