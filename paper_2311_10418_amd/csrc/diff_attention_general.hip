@@ -8,10 +8,9 @@
 // the contraction over features does not see the order of the columns, and outputs go back through the same mapping.
 //
 // Causal masks and values that are not finite.  A score that a column does not see is replaced whatever it is; but the second products run over whole
-// blocks of rows, probability 0 where a column does not see one, and 0 x Inf is NaN.  A wavefront whose sums are not finite in the end therefore looks
-// over the rows at its own places (rows further on it does not visit), and where those are not finite either it takes its columns one by one
-// (diff_attention_rows.hpp), so that a row is affected by the rows it sees and by no others.  (Looking the rows over as their tiles go to LDS took 2 to 7 % of
-// the kernels' time; this takes 1 % at most.)
+// blocks of rows, probability 0 where a column does not see one, and 0 x Inf is NaN (dP of a hidden row may overflow, too).  A wavefront whose sums are not
+// finite in the end therefore takes its columns one by one (diff_attention_rows.hpp), so that a row is affected by the rows it sees and by no others.
+// (Looking the rows over as their tiles go to LDS took 2 to 7 % of the kernels' time; this takes 1 % at most.)
 //
 // Bound by issue: the matrix pipe is busy 60 % of the SIMD cycles and vector instructions, more than two for each matrix instruction, take the rest.
 // Measured in fp32: 16 heads of 64, 31 sequences of 366 to 523, unmasked, forward 398 us, backward 967 (93 and 90 TFLOP/s
@@ -231,7 +230,7 @@ __global__ __launch_bounds__(256, HH <= 32 ? 3 : 2) void diff_fwd_kernel(DiffAtt
     }
     l1 = groups_sum(l1);
     l2 = groups_sum(l2);
-    if (a.mask && (any_not_finite(o1) || any_not_finite(o2)) && !rows_finite<T>(a.v, krow0, a.ldv, h, hd, qw0, min(kl, qw0 + KT), lane)) {
+    if (a.mask && (any_not_finite(o1) || any_not_finite(o2))) {
         const float e1 = m1 + __builtin_amdgcn_logf(l1), e2 = m2 + __builtin_amdgcn_logf(l2);
         for (int i = 0; i < min(16, ql - qw0); ++i) diff_fwd_row<T>(a, s, h, qw0 + i, __shfl(e1, i, 64), __shfl(e2, i, 64), lane);
         if (g == 0 && qi < ql) {
@@ -429,8 +428,7 @@ __global__ __launch_bounds__(512, HH <= 32 ? 4 : 2) void diff_bwd_dq_kernel(Diff
     f32x4_t lam_join[1] = {{lam_sum, 0.f, 0.f, 0.f}};
     join_shares<COLS>(lds, split, t, lam_join);
     if (split != 0) return;
-    const bool by_rows = a.mask && (any_not_finite(gacc) || any_not_finite(lam_join)) &&
-                         !(rows_finite<T>(a.k, krow0, a.ldk, h, hd, qw0, min(kl, qw0 + 16), lane) && rows_finite<T>(a.v, krow0, a.ldv, h, hd, qw0, min(kl, qw0 + 16), lane));
+    const bool by_rows = a.mask && (any_not_finite(gacc) || any_not_finite(lam_join));
     if (by_rows) {
         lam_sum = 0.f;
         for (int i = 0; i < min(16, ql - qw0); ++i)
@@ -527,9 +525,7 @@ __global__ __launch_bounds__(512, HH <= 32 && COLS == 64 ? 4 : 2) void diff_bwd_
     join_shares<COLS>(lds, split, t, dk);
     join_shares<COLS>(lds, split, t, dv);
     if (split != 0) return;
-    if (a.mask && (any_not_finite(dk) || any_not_finite(dv)) &&
-        !(rows_finite<T>(a.q, qrow0, a.ldq, h, hd, kw0, min(ql, kw0 + 16), lane) && rows_finite<T>(a.d_o, qrow0, a.ldo, h, hd, kw0, min(ql, kw0 + 16), lane) &&
-          stats_finite(a, h, qrow0, kw0, min(ql, kw0 + 16), lane))) {
+    if (a.mask && (any_not_finite(dk) || any_not_finite(dv))) {
         for (int i = 0; i < min(16, kl - kw0); ++i) diff_dkv_row<T>(a, s, h, kw0 + i, lane);
         return;
     }

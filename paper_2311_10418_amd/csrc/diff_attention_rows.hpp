@@ -1,5 +1,5 @@
 // Differential attention under a causal mask one row at a time, reading exactly the rows of the other side that belong together: what the general
-// kernels fall back to where a row next to a work-group's own is not finite.  A wavefront per row, lane i with the features i and i + 64 (of at most 128).
+// kernels fall back to where sums are not finite.  A wavefront per row, lane i with the features i and i + 64 (of at most 128).
 #pragma once
 #include "diff_attention.hpp"
 
@@ -26,23 +26,9 @@ __device__ __forceinline__ Pair both_maps(const DiffAttnArgs& a, Pair q, Pair k,
             __builtin_amdgcn_exp2f(__builtin_fmaf(wave_sum(__builtin_fmaf(q.b, k.b, first ? 0.f : both)), c, -e2))};
 }
 
-// whether rows first .. end - 1 of a head are finite, or (dK/dV) the statistics of such queries, at most 64 of them
-template <class T> __device__ __forceinline__ bool rows_finite(const void* base, long long row0, long long ld, int h, int hd, int first, int end, int lane) {
-    float nothing = 0.f;                                // 0, or NaN
-    for (int r = first; r < end; ++r) {
-        const Pair v = pair_of<T>(base, row0 + r, ld, h, hd, lane);
-        nothing = __builtin_fmaf(v.a, 0.f, __builtin_fmaf(v.b, 0.f, nothing));
-    }
-    return __builtin_amdgcn_ballot_w64(nothing != 0.f) == 0;
-}
-__device__ __forceinline__ bool stats_finite(const DiffAttnArgs& a, int h, long long row0, int first, int end, int lane) {
-    float nothing = 0.f;
-    if (first + lane < end) {
-        const long long row = row0 + first + lane;
-        for (const float* p : {a.lse + (size_t)(2 * h) * a.lse_stride, a.lse + (size_t)(2 * h + 1) * a.lse_stride, a.d1 + (size_t)h * a.q_total_rows, a.d2 + (size_t)h * a.q_total_rows})
-            nothing = __builtin_fmaf(p[row], 0.f, nothing);
-    }
-    return __builtin_amdgcn_ballot_w64(nothing != 0.f) == 0;
+// Whether a row's sums are NaN throughout, which nothing changes any more: asked for every 16 rows, so that a sequence of NaN takes no longer than another.
+__device__ __forceinline__ bool all_nan(Pair v, int hd, int lane) {
+    return __builtin_amdgcn_ballot_w64((lane < hd && v.a == v.a) || (lane + 64 < hd && v.b == v.b)) == 0;
 }
 
 // outputs of query qi
@@ -55,6 +41,7 @@ template <class T> __device__ __forceinline__ void diff_fwd_row(const DiffAttnAr
         const Pair p = both_maps(a, q, pair_of<T>(a.k, kr0 + j, a.ldk, h, hd, lane), e1, e2, lane), v = pair_of<T>(a.v, kr0 + j, a.ldv, h, hd, lane);
         o1 = {__builtin_fmaf(p.a, v.a, o1.a), __builtin_fmaf(p.a, v.b, o1.b)};
         o2 = {__builtin_fmaf(p.b, v.a, o2.a), __builtin_fmaf(p.b, v.b, o2.b)};
+        if (j % 16 == 15 && all_nan(o1, hd, lane) && all_nan(o2, hd, lane)) break;
     }
     const float lam = a.lambda[h];
     put_pair<T>(a.o, qr, a.ldo, h, hd, lane, {o1.a - o2.a * lam, o1.b - o2.b * lam});
@@ -75,6 +62,7 @@ template <class T> __device__ __forceinline__ float diff_dq_row(const DiffAttnAr
         const float dp = dot_pairs(d_o, pair_of<T>(a.v, kr0 + j, a.ldv, h, hd, lane)), ds1 = p.a * (dp - d1), ds2 = p.b * (d2 - dp) * lam;
         g = {__builtin_fmaf(first ? ds1 : ds2, k.a, g.a), __builtin_fmaf(ds2, k.b, g.b)};
         lam_sum = __builtin_fmaf(p.b, dp, lam_sum);
+        if (j % 16 == 15 && lam_sum != lam_sum && all_nan(g, hd, lane)) break;
     }
     put_pair<T>(a.dq, qr, a.ldq, h, hd, lane, {g.a * a.scale, g.b * a.scale});
     return lam_sum;
@@ -96,6 +84,7 @@ template <class T> __device__ __forceinline__ void diff_dkv_row(const DiffAttnAr
         const float ds1 = p.a * (dp - d1), p2 = lam * p.b, ds2 = p2 * (d2 - dp), both = p.a - p2;
         gk = {__builtin_fmaf(first ? ds1 : ds2, q.a, gk.a), __builtin_fmaf(ds2, q.b, gk.b)};
         gv = {__builtin_fmaf(both, d_o.a, gv.a), __builtin_fmaf(both, d_o.b, gv.b)};
+        if ((i - kj) % 16 == 15 && all_nan(gk, hd, lane) && all_nan(gv, hd, lane)) break;
     }
     put_pair<T>(a.dk, kr, a.ldk, h, hd, lane, {gk.a * a.scale, gk.b * a.scale});
     put_pair<T>(a.dv, kr, a.ldv, h, hd, lane, gv);

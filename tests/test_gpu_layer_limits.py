@@ -176,6 +176,27 @@ def test_values_that_are_not_finite_stay_where_they_are_seen(bad, dt, generic, h
         assert not torch.isfinite(r[4 if i == 0 else 5][:at + 1]).all(dim=1).any(), i
 
 
+@pytest.mark.parametrize("dt,generic", [(F32, False), (BF, True), (BF, False)])
+@pytest.mark.parametrize("hd", [16, 64, 128])
+def test_products_with_hidden_rows_may_overflow(dt, generic, hd):
+    """Causal: a value row and a gradient row of 2^100 each, finite, whose product is not; the value row's query and those behind it have gradients of 0, so that
+    nothing sees both.  Earlier queries' gradients and later keys' are what they are without."""
+    heads, n, at = 2, 80, 37
+    rng = np.random.default_rng(hd)
+    t = [torch.from_numpy(rng.standard_normal((n, heads * hd)).astype(np.float32)).to(DEV).to(dt) for _ in range(4)]
+    t[3][at:] = 0
+    lam = torch.linspace(0.1, 0.8, heads, device=DEV)
+    t[3][at - 2] = 2.0 ** 100
+    clean = _run(*t, lam, [n], [n], heads, hd, True, generic)
+    assert all(torch.isfinite(x).all() for x in clean)
+    s = [x.clone() for x in t]
+    s[2][at] = 2.0 ** 100
+    r = _run(*s, lam, [n], [n], heads, hd, True, generic)
+    for name, a, b in (("o", clean[0][:at], r[0][:at]), ("dq", clean[3][:at], r[3][:at]), ("dk", clean[4][at + 1:], r[4][at + 1:]), ("dv", clean[5], r[5])):
+        _alike(a, b, slice(0, 0), name)
+    assert torch.isfinite(r[6]).all()
+
+
 def test_more_work_groups_than_a_launch_of_the_matrix_core_kernels_has():
     """64 000 single tokens, 261 heads: one key, so that O2 = V, O = (1 - lambda) V = V / 2 and dV = dO / 2, exactly; dP - D and with it dQ and dK are what two sums of 64
     products in different orders differ by, 128 x 2^-24 of at most 2^10."""
