@@ -536,8 +536,9 @@ int64_t ds_diff_attention_scratch_bytes(int32_t n_heads, int32_t q_total_rows, i
  *     P_i = softmax(Q_i K_i^T / sqrt(head_dim / 2)),   O2 = P_2 V,   O = P_1 V - lambda[h] O2.
  * head_dim: a multiple of 16, at most 128.  lambda: DEVICE float32[n_heads].  o, o2: [q_total_rows, ...] with row stride ldo; o2 is
  * what the backward pass needs beside o and may be NULL.  lse: float32 [2 * n_heads, q_total_rows], map m of head h at 2h + m.
- * q_total_rows / k_total_rows: rows of the tensors holding the queries / the keys; max_q_len / max_k_len: upper bounds of the lengths
- * (of which the rows of the tensors are one too), in the kernels that compute in fp32 at most 2^28.  Rows not covered by any sequence are not touched; the sequences must not overlap; one with k_len[s] = 0 gets zero outputs.
+ * q_total_rows / k_total_rows: rows of the tensors holding the queries / the keys; max_q_len / max_k_len: upper bounds of the lengths (so
+ * are the rows of the tensors), in the kernels that compute in fp32 at most 2^28.
+ * Rows not covered by any sequence are not touched; the sequences must not overlap; one with k_len[s] = 0 gets zero outputs.
  * Strides and alignments of the element type are taken as they are.  scratch: DEVICE, 16-byte aligned, at least
  * ds_diff_attention_scratch_bytes.
  * Precision: bf16 heads of 64 and 128 with 16-byte aligned rows go to the matrix cores, where probabilities, their difference and their
@@ -583,7 +584,7 @@ int64_t ds_norm_bwd_scratch_floats(int32_t rows, int32_t d);
  *     y = resid_scale * x + branch_scale * gate . z      (the stream; stored)
  *     u = N_pre(y)    (of y as stored; pre_g = NULL: not computed)
  * rms = 0: LayerNorm (gain and bias, eps 1e-5); 1: RMSNorm (gain only, eps 1e-6), for both norms.
- * x, h, y, u: [rows, d] row-major, contiguous, d a multiple of 8, at most 4096; all tensors 16-byte aligned.
+ * x, h, y, u: [rows, d] row-major, contiguous, d a multiple of 8, at most 4096, rows at most 2^31 - 2^16 - 1; all tensors 16-byte aligned.
  * gate_kind: DS_GATE_NONE (gate NULL), DS_GATE_COL ([d], one factor per column), DS_GATE_ROW ([rows, d]).
  * row_valid: NULL, or DEVICE int32[rows]: where it is negative the inputs are not looked at (they may be NaN), y and u are
  * written as zeros.  stats: float32 [4, rows], mean and rstd of the rows of h, then of y, for the backward pass.

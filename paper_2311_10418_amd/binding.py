@@ -582,10 +582,9 @@ def _columns(t, name, rows, cols, dtype, device):
     return t.data_ptr(), ld if have > 1 else max(ld, wide)
 
 
-def _in_32_bits(*numbers):
-    """Rows, strides and lengths are int32 in the C ABI, and ctypes would take them modulo 2^32."""
-    if max(numbers) > 0x7fffffff:
-        raise ValueError("rows, row strides and lengths must be below 2^31, got %s" % (numbers,))
+def _too_large(*numbers):
+    """Rows, strides and lengths are int32 in the C ABI, and ctypes would take larger ones modulo 2^32."""
+    raise ValueError("rows, row strides and lengths must be below 2^31, got %s" % (numbers,))
 
 
 def _current(t):
@@ -615,7 +614,8 @@ def ds_resid_norm_fwd(x, h, y, stats, post_g=None, post_b=None, gate=None, pre_g
     torch, code, dev = _current(x)
     dt, full = x.dtype, x.shape
     rows, d = full
-    _in_32_bits(rows)
+    if rows > 0x7fffffff:
+        _too_large(rows)
     kind, gate_shape = _gate(gate, rows, d)
     col = (d,)
     rc = lib().ds_resid_norm_fwd(code, int(rms), rows, d, _tensor(x, "x", full, dt, dev), _tensor(h, "h", full, dt, dev),
@@ -636,7 +636,8 @@ def ds_resid_norm_bwd(dy, y, h, stats, dx, dh, partial, du=None, post_g=None, po
     torch, code, dev = _current(h)
     dt, f32, full = h.dtype, torch.float32, h.shape
     rows, d = full
-    _in_32_bits(rows)
+    if rows > 0x7fffffff:
+        _too_large(rows)
     kind, gate_shape = _gate(gate, rows, d)
     col = (d,)
     rc = lib().ds_resid_norm_bwd(code, int(rms), rows, d, _tensor(dy, "dy", full, dt, dev), _tensor(du, "du", full, dt, dev), _tensor(y, "y", full, dt, dev),
@@ -664,7 +665,9 @@ def _diff_tensors(torch, dev, q, k, v, lam, lse, q_row, q_len, k_row, k_len, n_h
               _tensor(k_len, "k_len", (n,), i32, dev))
     qkv = (*_columns(q, "q", q_rows, wide, dt, dev), *_columns(k, "k", k_rows, wide, dt, dev), *_columns(v, "v", k_rows, wide, dt, dev),
            _tensor(lam, "lam", (n_heads,), torch.float32, dev))
-    _in_32_bits(n, q_rows, k_rows, qkv[1], qkv[3], qkv[5], max_q_len, max_k_len)
+    sizes = (q_rows, k_rows, qkv[1], qkv[3], qkv[5], max_q_len, max_k_len)
+    if max(sizes) > 0x7fffffff:
+        _too_large(*sizes)
     need = ds_diff_attention_scratch_bytes(n_heads, q_rows, k_rows, n)
     return n, tables, qkv, _tensor(lse, "lse", (2 * n_heads, q_rows), torch.float32, dev), \
         (q_rows, k_rows, _tensor(scratch, "scratch", need, torch.uint8, dev), scratch.numel())
@@ -678,7 +681,8 @@ def ds_diff_attention_fwd(q, k, v, lam, o, lse, q_row, q_len, k_row, k_len, n_he
     wide = n_heads * head_dim
     po, ldo = _columns(o, "o", q.shape[0], wide, q.dtype, dev)
     po2, ldo2 = _columns(o2, "o2", q.shape[0], wide, q.dtype, dev) if o2 is not None else (None, ldo)
-    _in_32_bits(ldo)
+    if ldo > 0x7fffffff:
+        _too_large(ldo)
     if ldo2 != ldo:
         raise ValueError("o and o2 must have the same row stride, got %d and %d" % (ldo, ldo2))
     rc = lib().ds_diff_attention_fwd(code, n, n_heads, head_dim, int(causal), *tables, max_q_len, max_k_len, *qkv, po, po2, ldo, plse, *rest,
@@ -693,7 +697,8 @@ def ds_diff_attention_bwd(q, k, v, lam, o, o2, d_o, lse, dq, dk, dv, dlam, q_row
     n, tables, qkv, plse, rest = _diff_tensors(torch, dev, q, k, v, lam, lse, q_row, q_len, k_row, k_len, n_heads, head_dim, max_q_len, max_k_len, scratch)
     wide, dt, rows = n_heads * head_dim, q.dtype, q.shape[0]
     (po, ldo), (po2, ldo2), (pdo, lddo) = _columns(o, "o", rows, wide, dt, dev), _columns(o2, "o2", rows, wide, dt, dev), _columns(d_o, "d_o", rows, wide, dt, dev)
-    _in_32_bits(ldo)
+    if ldo > 0x7fffffff:
+        _too_large(ldo)
     if not ldo == ldo2 == lddo:
         raise ValueError("o, o2 and d_o must have the same row stride, got %d, %d and %d" % (ldo, ldo2, lddo))
     grads = []
@@ -711,7 +716,8 @@ def ds_rope(x, y, pos, freq, n_heads, head_dim, rot_dim, interleaved=False, inve
     """x, y: 2-D, one row per token, heads first; y may be x."""
     torch, code, dev = _current(x)
     rows = pos.shape[0]
-    _in_32_bits(rows)
+    if rows > 0x7fffffff:
+        _too_large(rows)
     px, ldx = _columns(x, "x", rows, n_heads * head_dim, x.dtype, dev)
     py, ldy = _columns(y, "y", rows, n_heads * head_dim, x.dtype, dev)
     rc = lib().ds_rope(code, rows, n_heads, head_dim, rot_dim, int(interleaved), int(inverse), _tensor(pos, "pos", (rows,), torch.int32, dev),
