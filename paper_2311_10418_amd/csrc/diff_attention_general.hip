@@ -10,7 +10,7 @@
 // Causal masks and values that are not finite.  A score that a column does not see is replaced whatever it is; but the second products run over whole
 // blocks of rows, probability 0 where a column does not see one, and 0 x Inf is NaN (dP of a hidden row may overflow, too).  A wavefront whose sums are not
 // finite in the end therefore takes its columns one by one (diff_attention_rows.hpp), so that a row is affected by the rows it sees and by no others.
-// (Looking the rows over as their tiles go to LDS took 2 to 7 % of the kernels' time; this takes 1 % at most.)
+// (Looking the rows over as their tiles go to LDS took 2 to 7 % of the kernels' time; this takes about 1 %.)
 //
 // Bound by issue: the matrix pipe is busy 60 % of the SIMD cycles and vector instructions, more than two for each matrix instruction, take the rest.
 // Measured in fp32: 16 heads of 64, 31 sequences of 366 to 523, unmasked, forward 398 us, backward 967 (93 and 90 TFLOP/s
