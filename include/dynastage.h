@@ -568,6 +568,41 @@ ds_status ds_diff_attention_bwd(int32_t dtype, int32_t n_seq, int32_t n_heads, i
                                 int32_t q_total_rows, int32_t k_total_rows, void* scratch, int64_t scratch_bytes,
                                 int32_t force_generic, void* hip_stream);
 
+/* Bytes of DEVICE scratch the calls below need.  Calls that share one scratch buffer must not overlap. */
+int64_t ds_rel_attention_scratch_bytes(int32_t n_heads, int32_t head_dim, int32_t reach, int32_t q_total_rows, int32_t k_total_rows, int32_t n_seq);
+
+/* Attention with a learned relative position bias: tables, tensors and mask as in ds_attention_fwd, with a bias for each head that depends on the distance of
+ * key and query alone, through buckets:
+ *     S_ij = scale * q_i . k_j + bias[bucket[clamp(j - p_i, -reach, reach) + reach]][h],   P = softmax(S),   O = P V,   p_i = q_pos[s] + i.
+ * Query i of sequence s stands at position p_i (q_pos: DEVICE int32[n_seq], or NULL: zeros; negative ones too), key j at position j.  mask = 1 hides keys with
+ * j > p_i.  With q_pos the queries may be the last tokens of a longer sequence whose keys lie in a cache, down to a single one.
+ * head_dim: a multiple of 8, at most 128.  scale: positive.  bias: [n_buckets, n_heads] of the tensors' type, contiguous; entries of -inf hide what has their
+ * bucket.  bucket: DEVICE int32[2 * reach + 1] (ds_rel_buckets makes the usual ones, reach = max_distance; any other table will do, entries outside of
+ * 0 .. n_buckets - 1 are clamped).  n_buckets and reach: at most 1024.
+ * lse: float32 [n_heads, q_total_rows].  A row that sees no key has zeros in o (and gradients) and -inf in lse.
+ * q_total_rows / k_total_rows: rows of the tensors holding the queries / the keys; max_q_len / max_k_len: upper bounds of the lengths (so are the rows of the
+ * tensors), at most 2^28.  Rows not covered by any sequence are not touched; the sequences must not overlap.
+ * Strides and alignments of the element type are taken as they are.  scratch: DEVICE, 16-byte aligned, at least ds_rel_attention_scratch_bytes. */
+ds_status ds_rel_attention_fwd(int32_t dtype, int32_t n_seq, int32_t n_heads, int32_t head_dim, int32_t mask, const int32_t* q_row,
+                               const int32_t* q_len, const int32_t* k_row, const int32_t* k_len, const int32_t* q_pos, int32_t max_q_len,
+                               int32_t max_k_len, const void* q, int32_t ldq, const void* k, int32_t ldk, const void* v, int32_t ldv, float scale,
+                               const void* bias, int32_t n_buckets, const int32_t* bucket, int32_t reach, void* o, int32_t ldo, float* lse,
+                               int32_t q_total_rows, int32_t k_total_rows, void* scratch, int64_t scratch_bytes, int32_t force_generic,
+                               void* hip_stream);
+/* Backward: given dO, O, lse produce dQ, dK, dV (same strides as q, k, v) and dbias, float32 [n_buckets, n_heads], overwritten or added to (accumulate).
+ * The row sums of dO O are taken from o as stored.  Sums have a fixed order: the same call gives the same bits. */
+ds_status ds_rel_attention_bwd(int32_t dtype, int32_t n_seq, int32_t n_heads, int32_t head_dim, int32_t mask, const int32_t* q_row,
+                               const int32_t* q_len, const int32_t* k_row, const int32_t* k_len, const int32_t* q_pos, int32_t max_q_len,
+                               int32_t max_k_len, const void* q, int32_t ldq, const void* k, int32_t ldk, const void* v, int32_t ldv, float scale,
+                               const void* bias, int32_t n_buckets, const int32_t* bucket, int32_t reach, const void* o, const void* d_o, int32_t ldo,
+                               const float* lse, void* dq, void* dk, void* dv, float* dbias, int32_t accumulate, int32_t q_total_rows,
+                               int32_t k_total_rows, void* scratch, int64_t scratch_bytes, int32_t force_generic, void* hip_stream);
+/* HOST: bucket[max_distance + d] of every distance d = key position - query position, -max_distance .. max_distance: of `half` buckets (all of them, or with
+ * bidirectional = 1 the first half for d <= 0 and the second for d > 0) the first half / 2 are single distances, the rest divide the distances up to
+ * max_distance evenly by their logarithm, and the last one has all beyond.  bidirectional = 0: d > 0 has bucket 0.
+ * Errors: DS_EINVAL (sizes beyond 1024, half < 2 or odd n_buckets with bidirectional, max_distance <= half / 2). */
+ds_status ds_rel_buckets(int32_t n_buckets, int32_t max_distance, int32_t bidirectional, int32_t* bucket);
+
 /* Row normalisation.  rms = 0: LayerNorm (gain g, bias b, eps 1e-5, stats = mean and rstd);
  * rms = 1: RMSNorm (gain only, eps 1e-6, stats = rstd).  stats: float32 [2, rows]. */
 ds_status ds_norm_fwd(int32_t dtype, int32_t rms, int32_t rows, int32_t d, const void* x,

@@ -147,3 +147,69 @@ def diff_attention_back(q, k, v, lam, o, o2, d_o, lse, n_heads, causal):
         out["dlam"].append(-(p[1] * g).sum())
         out["size_dlam"].append((p[1] * g_size).sum())
     return {n: np.array(t) if "dlam" in n else _flat(np.stack(t)) for n, t in out.items()}
+
+
+# ---------------------------------------------------------------- attention with a relative position bias
+def rel_buckets(n_buckets, max_distance, bidirectional):
+    """Bucket of each distance -max_distance .. max_distance; borders of the logarithmic ones compared in whole numbers."""
+    half = n_buckets // 2 if bidirectional else n_buckets
+    exact = half // 2
+    m = half - exact
+
+    def of(n):
+        if n < exact:
+            return n
+        return exact + max([t for t in range(m) if n ** m * exact ** t >= exact ** m * max_distance ** t])
+
+    side = [of(n) for n in range(max_distance + 1)]
+    return np.array(side[::-1] + [half + b if bidirectional else 0 for b in side[1:]])
+
+
+def _rel_scores(q, k, bias, bucket, n_heads, causal, pos, scale):
+    """Per head: scores, the sum of the sizes of their products, the table's place of each pair."""
+    lq, lk, reach = q.shape[0], k.shape[0], len(bucket) // 2
+    apart = np.arange(lk)[None, :] - (pos + np.arange(lq))[:, None]
+    of = np.clip(bucket, 0, bias.shape[0] - 1)[np.clip(apart, -reach, reach) + reach]
+    hd = q.shape[1] // n_heads
+    for h in range(n_heads):
+        c = slice(h * hd, (h + 1) * hd)
+        s = scale * (q[:, c] @ k[:, c].T) + bias[of, h]
+        if causal:
+            s = np.where(apart > 0, -np.inf, s)
+        yield h, c, s, scale * (np.abs(q[:, c]) @ np.abs(k[:, c]).T), of
+
+
+def _rel_probs(s):
+    """(softmax with rows of nothing as zeros, log-sum-exp)."""
+    with np.errstate(divide="ignore", invalid="ignore"):
+        top = np.where(np.isneginf(s.max(axis=1, initial=-np.inf)), 0.0, s.max(axis=1, initial=-np.inf))
+        e = np.exp(s - top[:, None])
+        total = e.sum(axis=1)
+        return np.where(total[:, None] > 0, e / np.where(total > 0, total, 1.0)[:, None], 0.0), top + np.log(total)
+
+
+def rel_attention(q, k, v, bias, bucket, n_heads, causal, pos=0, scale=1.0):
+    """-> o, lse [heads, lq], size of o, largest sum of sizes of a score's products [heads, lq]."""
+    o, size = np.zeros(q.shape), np.zeros(q.shape)
+    lse, terms = np.zeros((n_heads, q.shape[0])), np.zeros((n_heads, q.shape[0]))
+    for h, c, s, t, _ in _rel_scores(q, k, bias, bucket, n_heads, causal, pos, scale):
+        p, lse[h] = _rel_probs(s)
+        o[:, c], size[:, c] = p @ v[:, c], p @ np.abs(v[:, c])
+        terms[h] = np.where(np.isneginf(s), 0.0, t).max(axis=1, initial=0.0)
+    return o, lse, size, terms
+
+
+def rel_attention_back(q, k, v, bias, bucket, o, d_o, n_heads, causal, pos=0, scale=1.0):
+    """Gradients with D from o as given; "<name>_part": the same with everything that dS is a difference of counted by its absolute value."""
+    out = {n: np.zeros(t.shape) for n, t in (("dq", q), ("dk", k), ("dv", v), ("dbias", bias))}
+    out.update({n + "_part": np.zeros(t.shape) for n, t in list(out.items())})
+    for h, c, s, _, of in _rel_scores(q, k, bias, bucket, n_heads, causal, pos, scale):
+        p = _rel_probs(s)[0]
+        d = (d_o[:, c] * o[:, c]).sum(axis=1, keepdims=True)
+        ds = p * (d_o[:, c] @ v[:, c].T - d)
+        part = p * (np.abs(d_o[:, c]) @ np.abs(v[:, c]).T + (np.abs(d_o[:, c]) * np.abs(o[:, c])).sum(axis=1, keepdims=True))
+        for end, w, f in (("", ds, lambda t: t), ("_part", part, np.abs)):
+            out["dq" + end][:, c], out["dk" + end][:, c] = scale * w @ f(k[:, c]), scale * w.T @ f(q[:, c])
+            out["dbias" + end][:, h] = np.bincount(of.ravel(), w.ravel(), bias.shape[0])
+        out["dv"][:, c], out["dv_part"][:, c] = p.T @ d_o[:, c], p.T @ np.abs(d_o[:, c])
+    return out

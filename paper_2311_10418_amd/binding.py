@@ -32,6 +32,7 @@ EXPORTS = ["dp_plan", "dp_plan_sampled", "dp_plan_replicas", "ds_plan_recompute"
            "ds_stage_last_launch_count", "ds_stage_weights_unchanged", "ds_stage_profile_enable", "ds_stage_profile_read", "ds_pack", "ds_unpack", "ds_gemm", "ds_gemm_ws", "ds_attention_fwd",
            "ds_attention_bwd", "ds_attention_scratch_bytes", "ds_norm_fwd", "ds_norm_bwd", "ds_norm_bwd_scratch_floats", "ds_colsum", "ds_colsum_static",
            "ds_diff_attention_fwd", "ds_diff_attention_bwd", "ds_diff_attention_scratch_bytes",
+           "ds_rel_attention_fwd", "ds_rel_attention_bwd", "ds_rel_attention_scratch_bytes", "ds_rel_buckets",
            "ds_resid_norm_fwd", "ds_resid_norm_bwd", "ds_resid_norm_bwd_scratch_floats", "ds_rope", "ds_rope_freqs", "ds_layout_positions",
            "ds_mfma_probe", "ds_version"]
 
@@ -121,11 +122,15 @@ def lib():
         for name, args in (("ds_resid_norm_fwd", [i] * 4 + [p] * 5 + [i, p, f, f] + [p] * 6),
                            ("ds_resid_norm_bwd", [i] * 4 + [p] * 7 + [i, p, f, f] + [p] * 10 + [i, p]),
                            ("ds_rope", [i] * 7 + [p, p, f, p, l, p, l, p]), ("ds_rope_freqs", [i, d, i, d, d, d, d, p]), ("ds_layout_positions", [p, i, p]),
+                           ("ds_rel_attention_fwd", [i] * 5 + [p] * 5 + [i, i] + [p, i] * 3 + [f, p, i, p, i, p, i, p, i, i, p, l, i, p]),
+                           ("ds_rel_attention_bwd", [i] * 5 + [p] * 5 + [i, i] + [p, i] * 3 + [f, p, i, p, i, p, p, i] + [p] * 5 + [i, i, i, p, l, i, p]),
+                           ("ds_rel_buckets", [i, i, i, p]),
                            ("ds_diff_attention_fwd", [i] * 5 + [p] * 4 + [i, i] + [p, i] * 3 + [p, p, p, i, p, i, i, p, l, i, p]),
                            ("ds_diff_attention_bwd", [i] * 5 + [p] * 4 + [i, i] + [p, i] * 3 + [p, p, p, p, i] + [p] * 5 + [i, i, i, p, l, i, p])):
             getattr(_lib, name).argtypes = args
         _lib.ds_resid_norm_bwd_scratch_floats.argtypes, _lib.ds_resid_norm_bwd_scratch_floats.restype = [i, i], l
         _lib.ds_diff_attention_scratch_bytes.argtypes, _lib.ds_diff_attention_scratch_bytes.restype = [i] * 4, l
+        _lib.ds_rel_attention_scratch_bytes.argtypes, _lib.ds_rel_attention_scratch_bytes.restype = [i] * 6, l
         _lib.ds_layout_free.restype = None
         _lib.ds_stage_destroy.restype = None
     return _lib
@@ -710,6 +715,73 @@ def ds_diff_attention_bwd(q, k, v, lam, o, o2, d_o, lse, dq, dk, dv, dlam, q_row
                                      _tensor(dlam, "dlam", (n_heads,), torch.float32, dev), int(accumulate), *rest, int(force_generic),
                                      _raw_stream(torch, stream, dev))
     _check(rc, "ds_diff_attention_bwd")
+
+
+def ds_rel_attention_scratch_bytes(n_heads, head_dim, reach, q_total_rows, k_total_rows, n_seq):
+    return lib().ds_rel_attention_scratch_bytes(n_heads, head_dim, reach, q_total_rows, k_total_rows, n_seq)
+
+
+def _rel_tensors(torch, dev, q, k, v, bias, bucket, lse, q_row, q_len, k_row, k_len, q_pos, n_heads, head_dim, max_q_len, max_k_len, scale, scratch):
+    """The arguments both directions share, checked: (number of sequences, tables, lengths, tensors with strides, scale and bias, lse, row counts and scratch)."""
+    dt = q.dtype
+    n, wide, i32 = q_row.shape[0], n_heads * head_dim, torch.int32
+    q_rows, k_rows = q.shape[0], k.shape[0]
+    tables = (_tensor(q_row, "q_row", (n,), i32, dev), _tensor(q_len, "q_len", (n,), i32, dev), _tensor(k_row, "k_row", (n,), i32, dev),
+              _tensor(k_len, "k_len", (n,), i32, dev), _tensor(q_pos, "q_pos", (n,), i32, dev))
+    buckets, reach = bias.shape[0], bucket.shape[0] // 2
+    qkv = (*_columns(q, "q", q_rows, wide, dt, dev), *_columns(k, "k", k_rows, wide, dt, dev), *_columns(v, "v", k_rows, wide, dt, dev), scale,
+           _tensor(bias, "bias", (buckets, n_heads), dt, dev), buckets, _tensor(bucket, "bucket", (2 * reach + 1,), i32, dev), reach)
+    sizes = (q_rows, k_rows, qkv[1], qkv[3], qkv[5], max_q_len, max_k_len, buckets)
+    if max(sizes) > 0x7fffffff:
+        _too_large(*sizes)
+    need = ds_rel_attention_scratch_bytes(n_heads, head_dim, reach, q_rows, k_rows, n)
+    return n, tables, qkv, _tensor(lse, "lse", (n_heads, q_rows), torch.float32, dev), \
+        (q_rows, k_rows, _tensor(scratch, "scratch", need, torch.uint8, dev), scratch.numel())
+
+
+def ds_rel_attention_fwd(q, k, v, bias, bucket, o, lse, q_row, q_len, k_row, k_len, n_heads, head_dim, causal, max_q_len, max_k_len, scratch, scale=None,
+                         q_pos=None, force_generic=False, stream=None):
+    """q, k, v, o: 2-D, a row per token (column ranges of wider tensors are fine); bias [buckets, heads], bucket int32 [2 * reach + 1]; scratch: uint8.
+    scale: None is head_dim ** -0.5."""
+    torch, code, dev = _current(q)
+    scale = head_dim ** -0.5 if scale is None else scale
+    n, tables, qkv, plse, rest = _rel_tensors(torch, dev, q, k, v, bias, bucket, lse, q_row, q_len, k_row, k_len, q_pos, n_heads, head_dim, max_q_len, max_k_len, scale, scratch)
+    po, ldo = _columns(o, "o", q.shape[0], n_heads * head_dim, q.dtype, dev)
+    if ldo > 0x7fffffff:
+        _too_large(ldo)
+    rc = lib().ds_rel_attention_fwd(code, n, n_heads, head_dim, int(causal), *tables, max_q_len, max_k_len, *qkv, po, ldo, plse, *rest,
+                                    int(force_generic), _raw_stream(torch, stream, dev))
+    _check(rc, "ds_rel_attention_fwd")
+
+
+def ds_rel_attention_bwd(q, k, v, bias, bucket, o, d_o, lse, dq, dk, dv, dbias, q_row, q_len, k_row, k_len, n_heads, head_dim, causal, max_q_len, max_k_len,
+                         scratch, scale=None, q_pos=None, accumulate=False, force_generic=False, stream=None):
+    """dq, dk, dv have the strides of q, k, v; o and d_o the same row stride."""
+    torch, code, dev = _current(q)
+    scale = head_dim ** -0.5 if scale is None else scale
+    n, tables, qkv, plse, rest = _rel_tensors(torch, dev, q, k, v, bias, bucket, lse, q_row, q_len, k_row, k_len, q_pos, n_heads, head_dim, max_q_len, max_k_len, scale, scratch)
+    wide, dt, rows = n_heads * head_dim, q.dtype, q.shape[0]
+    (po, ldo), (pdo, lddo) = _columns(o, "o", rows, wide, dt, dev), _columns(d_o, "d_o", rows, wide, dt, dev)
+    if ldo > 0x7fffffff:
+        _too_large(ldo)
+    if ldo != lddo:
+        raise ValueError("o and d_o must have the same row stride, got %d and %d" % (ldo, lddo))
+    grads = []
+    for t, name, like in ((dq, "dq", q), (dk, "dk", k), (dv, "dv", v)):
+        grads.append(_columns(t, name, like.shape[0], wide, dt, dev)[0])
+        if t.stride(0) != like.stride(0) and like.shape[0] > 1:
+            raise ValueError("%s must have the row stride of %s, got %d and %d" % (name, name[1:], t.stride(0), like.stride(0)))
+    rc = lib().ds_rel_attention_bwd(code, n, n_heads, head_dim, int(causal), *tables, max_q_len, max_k_len, *qkv, po, pdo, ldo, plse, *grads,
+                                    _tensor(dbias, "dbias", bias.shape, torch.float32, dev), int(accumulate), *rest, int(force_generic),
+                                    _raw_stream(torch, stream, dev))
+    _check(rc, "ds_rel_attention_bwd")
+
+
+def ds_rel_buckets(n_buckets, max_distance, bidirectional=True):
+    """int32 [2 * max_distance + 1]: the bucket of each distance key - query, -max_distance .. max_distance (host)."""
+    out = np.zeros(2 * max(int(max_distance), 0) + 1, dtype=np.int32)
+    _check(lib().ds_rel_buckets(n_buckets, max_distance, int(bidirectional), _vp(out)), "ds_rel_buckets")
+    return out
 
 
 def ds_rope(x, y, pos, freq, n_heads, head_dim, rot_dim, interleaved=False, inverse=False, amplitude=1.0, stream=None):

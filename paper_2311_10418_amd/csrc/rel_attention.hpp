@@ -1,0 +1,108 @@
+// Arguments shared by the kernels of attention with a learned relative position bias.
+//
+// Query i of a sequence stands at position p_i = q_pos + i, key j at position j.  With b(d) = bias[bucket[clamp(d, -reach, reach) + reach]][h], the bias of
+// head h at distance d = j - p_i:
+//     S = s Q K^T + b(j - p_i)   (mask 1: -inf where j > p_i),   P = softmax(S),   O = P V,   lse = log sum exp S.
+// Backward, D = rowsum(dO O) with O as it is stored:
+//     dS = P (dO V^T - D),  dQ = s dS K,  dK = s dS^T Q,  dV = P^T dO,  dbias[c][h] = sum of dS over the pairs whose distance has bucket c.
+// A row that sees no key (none there, all hidden by the mask, or by biases of -inf) has O = 0, lse = -inf, and no gradient.
+//
+// Beyond `reach` the bias is one number on each side, so that only blocks of pairs near the diagonal look anything up: by distance, in a table in LDS that
+// holds the bias of one head in the exp2 domain.  What dbias sums goes by distance too, first in LDS, then to one slot in the scratch for each block of queries
+// (sum_dbias puts the slots together, in a fixed order): no atomics whose order could change a result.
+#pragma once
+#include "attention.hpp"
+#include "common.hpp"
+
+struct RelAttnArgs : AttnArgs {
+    const void* bias;                                   // [n_buckets][n_heads], of the tensors' type
+    const int32_t* bucket;                              // [2 reach + 1]
+    int32_t n_buckets, reach;
+    const int32_t* q_pos;                               // [n_seq] or NULL: zeros
+    float* dbias;                                       // [n_buckets][n_heads]
+    int32_t accumulate;
+    int32_t vec;                                        // general kernels: rows of four elements may be accessed at once
+    int32_t k_splits;                                   // forward: work-groups that share the keys of a head (1: one has them all)
+    float* d;                                           // general kernels: D, [n_heads][q_total_rows]
+    float* slots;                                       // sums of dS by distance, [block of queries][n_heads][2 reach + 1]
+    float* split_part;                                  // see RelPart
+    char* aug;                                          // matrix-core kernels: see rel_attention_mfma.hip
+};
+
+// Work-groups that share the keys of a sequence and head leave, for each query, its maximum (exp2 domain), sum and unscaled output.
+struct RelPart { float *stat, *o; };
+__device__ __forceinline__ RelPart rel_part(const RelAttnArgs& a, int h, long long row, int split) {
+    float* p = a.split_part + ((size_t)(h * (long long)a.q_total_rows + row) * a.k_splits + split) * (a.head_dim + 4);
+    return {p, p + 4};
+}
+ds_status rel_join(const RelAttnArgs& a, hipStream_t st);
+
+// Position of a sequence's first query.  Lengths stay below 2^28 and reach below 2^11, so that what lies beyond 2^30 may as well lie there.
+__device__ __forceinline__ int rel_position(const RelAttnArgs& a, int s) { return a.q_pos ? min(max(a.q_pos[s], -(1 << 30)), 1 << 30) : 0; }
+// keys of a sequence that its last query sees
+__device__ __forceinline__ int rel_keys(const RelAttnArgs& a, int kl, int ql, int pos) { return a.mask ? min(kl, max(0, pos + ql)) : kl; }
+// bias of head h at table entry i = distance + reach, clamped, in the exp2 domain
+__device__ __forceinline__ float rel_bias(const RelAttnArgs& a, int h, int i) {
+    const int b = min(max(a.bucket[min(max(i, 0), 2 * a.reach)], 0), a.n_buckets - 1);
+    const size_t at = (size_t)b * a.n_heads + h;
+    return 1.4426950408889634f * (a.dtype == DS_DTYPE_BF16 ? (float)((const bf16_t*)a.bias)[at] : ((const float*)a.bias)[at]);
+}
+// log-sum-exp as the backward kernels subtract it (exp2 domain): rows that see nothing get probabilities of 0
+__device__ __forceinline__ float rel_lse2(float lse) { return lse == -INFINITY ? INFINITY : lse * 1.4426950408889634f; }
+
+// lds[i] += v without a return, by the lanes of one wavefront and with no two of them at one address: LDS operations of a wavefront take effect in order, so
+// that the sum does not depend on timing as long as other wavefronts keep off it
+__device__ __forceinline__ void lds_add(float* lds, float v) {
+    __builtin_amdgcn_ds_faddf((__attribute__((address_space(3))) float*)lds, v, 0, 0, false);
+}
+
+// blocks of `cols` queries of all sequences before s: slots are numbered by sequence
+template <int COLS, int THREADS> __device__ __forceinline__ int blocks_before(const RelAttnArgs& a, int s, int* lds) {
+    int n = 0;
+    for (int i = threadIdx.x; i < s; i += THREADS) n += max(a.q_len[i] + COLS - 1, 0) / COLS;
+#pragma unroll
+    for (int m = 32; m >= 1; m >>= 1) n += __shfl_xor(n, m, 64);
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = n;
+    __syncthreads();
+    n = 0;
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; ++w) n += lds[w];
+    __syncthreads();
+    return n;
+}
+// dbias[.][h] = (accumulate ? itself : 0) + the sums in n slots: a work-group of the dK/dV launch for each head.  lds: (2 reach + 1) floats for each of
+// `groups` wavefront groups and the bucket table
+template <int THREADS> __device__ __forceinline__ void sum_dbias(const RelAttnArgs& a, int h, int n, float* lds) {
+    const int t = threadIdx.x, w = 2 * a.reach + 1;
+    const size_t step = (size_t)a.n_heads * w;
+    const float* from = a.slots + (size_t)h * w;
+    int32_t* of = reinterpret_cast<int32_t*>(lds + w);
+    for (int i = t; i < w; i += THREADS) {
+        float sum = 0.f;
+        int k = 0;
+        for (; k + 8 <= n; k += 8) {
+            float v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = from[(size_t)(k + j) * step + i];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sum += v[j];
+        }
+        for (; k < n; ++k) sum += from[(size_t)k * step + i];
+        lds[i] = sum;
+        of[i] = min(max(a.bucket[i], 0), a.n_buckets - 1);
+    }
+    __syncthreads();
+    for (int b = t; b < a.n_buckets; b += THREADS) {
+        float sum = 0.f;
+        for (int i = 0; i < w; ++i) sum += of[i] == b ? lds[i] : 0.f;
+        float* to = a.dbias + (size_t)b * a.n_heads + h;
+        *to = (a.accumulate ? *to : 0.f) + sum;
+    }
+}
+
+// Compute units that the rules of choice count on: an MI355X's, and not those of the current device, since the scratch is sized by one of them.
+constexpr int kRelUnits = 256;
+int rel_general_columns(const RelAttnArgs& a, int max_len);
+
+ds_status rel_fwd_general(const RelAttnArgs& a, hipStream_t st);
+ds_status rel_bwd_general(const RelAttnArgs& a, hipStream_t st);

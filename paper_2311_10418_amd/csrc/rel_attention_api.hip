@@ -1,0 +1,141 @@
+// C-ABI entry points and dispatch of attention with a relative position bias.
+#include "rel_attention.hpp"
+#include <algorithm>
+#include <cmath>
+
+constexpr int kRelReach = 1024, kRelBuckets = 1024, kRelLongest = 1 << 28;
+
+// Work-groups that share the keys of a head, for sequences of at most 64 queries in a tensor of at most 64 rows for each of them (the shares go to scratch
+// by row of that tensor, whose lengths the scratch's size does not know): as many as make one for every compute unit, of 64 keys at least, from 129 keys on; two
+// up to head size 64; at most one for a lane of the wavefront that joins them.
+static constexpr int kSplitQueries = 64, kSplitMost = 64;
+static int most_splits(int n_heads, int head_dim, int q_total_rows, int max_k_len, int n_seq) {
+    const long long items = (long long)n_seq * n_heads;
+    if (q_total_rows > (long long)kSplitQueries * n_seq || max_k_len < 129) return 1;
+    const long long groups = (head_dim <= 64 ? 2 : 1) * kRelUnits;
+    return (int)std::max(1LL, std::min({groups / items, (long long)kSplitMost, ((long long)max_k_len + 63) / 64}));
+}
+
+// Scratch: the work lists of the matrix-core kernels; what the dQ kernels hand to the dK/dV kernels, 32 bytes for each query of a head (the general ones use 4 of
+// them); the slots of dbias, for each block of 64 queries (of 32 where the general kernels have at most 512 work-groups of 64).  A forward call has the parts of
+// split keys in the place of the last two.
+static size_t lists_size(int q_total_rows, int k_total_rows, int n_seq) { return attn_scratch_bytes(0, 0, q_total_rows, k_total_rows, n_seq); }
+static size_t rel_scratch_bytes(int n_heads, int head_dim, int reach, int q_total_rows, int k_total_rows, int n_seq) {
+    const size_t entries = (size_t)n_heads * q_total_rows;
+    const size_t blocks = std::max(((size_t)q_total_rows / 64 + n_seq) * n_heads, (size_t)4 * kRelUnits);
+    const size_t backward = entries * 32 + blocks * (2 * reach + 1) * 4;
+    const int splits = most_splits(n_heads, head_dim, q_total_rows, k_total_rows, n_seq);
+    const size_t forward = splits > 1 ? entries * splits * (head_dim + 4) * 4 : 0;
+    return lists_size(q_total_rows, k_total_rows, n_seq) + std::max(backward, forward);
+}
+
+static bool four_at_once(const void* p, size_t size) { return !p || (uintptr_t)p % (4 * size) == 0; }
+
+static ds_status check(RelAttnArgs& a) {
+    if (a.n_seq <= 0 || a.n_heads <= 0 || a.head_dim <= 0 || a.head_dim > 128 || a.head_dim % 8) return DS_EINVAL;
+    if (a.dtype != DS_DTYPE_F32 && a.dtype != DS_DTYPE_BF16) return DS_EINVAL;
+    if (a.mask != 0 && a.mask != 1) return DS_EINVAL;
+    if (!a.q_row || !a.q_len || !a.k_row || !a.k_len || !a.q || !a.k || !a.v || !a.bias || !a.bucket || !a.o || !a.lse) return DS_EINVAL;
+    if (a.reach < 1 || a.reach > kRelReach || a.n_buckets < 1 || a.n_buckets > kRelBuckets) return DS_EINVAL;
+    if (!(a.scale > 0.f) || std::isinf(a.scale)) return DS_EINVAL;
+    if (a.max_q_len <= 0 || a.max_k_len <= 0 || a.q_total_rows <= 0 || a.k_total_rows <= 0) return DS_EINVAL;
+    if (a.n_seq > 65534 || a.n_heads > 65535) return DS_EINVAL;
+    const long long wide = (long long)a.n_heads * a.head_dim;
+    if (a.ldq < wide || a.ldk < wide || a.ldv < wide || a.ldo < wide) return DS_EINVAL;
+    if (!a.scratch || (uintptr_t)a.scratch % 16 ||
+        a.scratch_bytes < rel_scratch_bytes(a.n_heads, a.head_dim, a.reach, a.q_total_rows, a.k_total_rows, a.n_seq)) return DS_EINVAL;
+    a.max_q_len = std::min(a.max_q_len, a.q_total_rows);
+    a.max_k_len = std::min(a.max_k_len, a.k_total_rows);
+    if (std::max(a.max_q_len, a.max_k_len) > kRelLongest) return DS_EINVAL;
+    const size_t size = dtype_size(a.dtype);
+    for (const void* p : {a.q, a.k, a.v, (const void*)a.o, a.d_o, (const void*)a.dq, (const void*)a.dk, (const void*)a.dv, a.bias})
+        if ((uintptr_t)p % size) return DS_EINVAL;
+    a.vec = four_at_once(a.q, size) && four_at_once(a.k, size) && four_at_once(a.v, size) && four_at_once(a.o, size) && four_at_once(a.d_o, size) &&
+            four_at_once(a.dq, size) && four_at_once(a.dk, size) && four_at_once(a.dv, size) && a.ldq % 4 == 0 && a.ldk % 4 == 0 && a.ldv % 4 == 0 && a.ldo % 4 == 0;
+    char* after_lists = (char*)a.scratch + lists_size(a.q_total_rows, a.k_total_rows, a.n_seq);
+    const size_t entries = (size_t)a.n_heads * a.q_total_rows;
+    a.k_splits = 1;
+    a.aug = after_lists;
+    a.d = (float*)after_lists;
+    a.slots = (float*)(after_lists + entries * 32);
+    a.split_part = (float*)after_lists;
+    a.n_items = (const int32_t*)a.scratch;              // (valid memory also where no list is made)
+    return DS_OK;
+}
+
+// How a call goes to the kernels: work-groups that share a head's keys (forward)
+struct RelChoice { int32_t general, k_splits; };
+static RelChoice choose(const RelAttnArgs& a, bool backward, bool force_generic) {
+    RelChoice c = {1, 1};
+    (void)force_generic;
+    if (!backward && a.max_q_len <= kSplitQueries) c.k_splits = most_splits(a.n_heads, a.head_dim, a.q_total_rows, a.max_k_len, a.n_seq);
+    return c;
+}
+
+extern "C" int64_t ds_rel_attention_scratch_bytes(int32_t n_heads, int32_t head_dim, int32_t reach, int32_t q_total_rows, int32_t k_total_rows, int32_t n_seq) {
+    if (n_heads <= 0 || head_dim <= 0 || head_dim > 128 || reach <= 0 || reach > kRelReach || q_total_rows <= 0 || k_total_rows <= 0 || n_seq <= 0) return 0;
+    return (int64_t)rel_scratch_bytes(n_heads, head_dim, reach, q_total_rows, k_total_rows, n_seq);
+}
+
+extern "C" ds_status ds_rel_attention_fwd(int32_t dtype, int32_t n_seq, int32_t n_heads, int32_t head_dim, int32_t mask, const int32_t* q_row,
+                                          const int32_t* q_len, const int32_t* k_row, const int32_t* k_len, const int32_t* q_pos, int32_t max_q_len,
+                                          int32_t max_k_len, const void* q, int32_t ldq, const void* k, int32_t ldk, const void* v, int32_t ldv, float scale,
+                                          const void* bias, int32_t n_buckets, const int32_t* bucket, int32_t reach, void* o, int32_t ldo, float* lse,
+                                          int32_t q_total_rows, int32_t k_total_rows, void* scratch, int64_t scratch_bytes, int32_t force_generic,
+                                          void* hip_stream) {
+    RelAttnArgs a = {};
+    a.dtype = dtype; a.n_seq = n_seq; a.n_heads = n_heads; a.head_dim = head_dim; a.mask = mask;
+    a.q_row = q_row; a.q_len = q_len; a.k_row = k_row; a.k_len = k_len; a.q_pos = q_pos;
+    a.max_q_len = max_q_len; a.max_k_len = max_k_len;
+    a.q = q; a.k = k; a.v = v; a.ldq = ldq; a.ldk = ldk; a.ldv = ldv;
+    a.scale = scale; a.bias = bias; a.n_buckets = n_buckets; a.bucket = bucket; a.reach = reach;
+    a.o = o; a.ldo = ldo; a.lse = lse; a.lse_stride = q_total_rows;
+    a.q_total_rows = q_total_rows; a.k_total_rows = k_total_rows;
+    a.scratch = scratch; a.scratch_bytes = scratch_bytes < 0 ? 0 : (size_t)scratch_bytes;
+    const ds_status r = check(a);
+    if (r != DS_OK) return r;
+    const RelChoice c = choose(a, false, force_generic != 0);
+    a.k_splits = c.k_splits;
+    return rel_fwd_general(a, (hipStream_t)hip_stream);
+}
+
+extern "C" ds_status ds_rel_attention_bwd(int32_t dtype, int32_t n_seq, int32_t n_heads, int32_t head_dim, int32_t mask, const int32_t* q_row,
+                                          const int32_t* q_len, const int32_t* k_row, const int32_t* k_len, const int32_t* q_pos, int32_t max_q_len,
+                                          int32_t max_k_len, const void* q, int32_t ldq, const void* k, int32_t ldk, const void* v, int32_t ldv, float scale,
+                                          const void* bias, int32_t n_buckets, const int32_t* bucket, int32_t reach, const void* o, const void* d_o,
+                                          int32_t ldo, const float* lse, void* dq, void* dk, void* dv, float* dbias, int32_t accumulate,
+                                          int32_t q_total_rows, int32_t k_total_rows, void* scratch, int64_t scratch_bytes, int32_t force_generic,
+                                          void* hip_stream) {
+    RelAttnArgs a = {};
+    a.dtype = dtype; a.n_seq = n_seq; a.n_heads = n_heads; a.head_dim = head_dim; a.mask = mask;
+    a.q_row = q_row; a.q_len = q_len; a.k_row = k_row; a.k_len = k_len; a.q_pos = q_pos;
+    a.max_q_len = max_q_len; a.max_k_len = max_k_len;
+    a.q = q; a.k = k; a.v = v; a.ldq = ldq; a.ldk = ldk; a.ldv = ldv;
+    a.scale = scale; a.bias = bias; a.n_buckets = n_buckets; a.bucket = bucket; a.reach = reach;
+    a.o = const_cast<void*>(o); a.d_o = d_o; a.ldo = ldo; a.lse = const_cast<float*>(lse); a.lse_stride = q_total_rows;
+    a.dq = dq; a.dk = dk; a.dv = dv; a.dbias = dbias; a.accumulate = accumulate;
+    a.q_total_rows = q_total_rows; a.k_total_rows = k_total_rows;
+    a.scratch = scratch; a.scratch_bytes = scratch_bytes < 0 ? 0 : (size_t)scratch_bytes;
+    const ds_status r = check(a);
+    if (r != DS_OK) return r;
+    if (!d_o || !dq || !dk || !dv || !dbias || (accumulate != 0 && accumulate != 1)) return DS_EINVAL;
+    return rel_bwd_general(a, (hipStream_t)hip_stream);
+}
+
+// The bucket of distance n >= 0 among `half`: itself up to half of them, then by logarithm.  log(n / exact) / log(far / exact) is rarely a whole number of
+// steps but by design (n = far, and powers between): what lies within 2^-40 of one is taken to be one.
+static int bucket_of(int n, int half, int far) {
+    const int exact = half / 2;
+    if (n < exact) return n;
+    if (n >= far || exact < 1) return half - 1;
+    const long double steps = logl((long double)n / exact) / logl((long double)far / exact) * (half - exact);
+    return std::min(half - 1, exact + (int)floorl(steps + 0x1p-40L));
+}
+extern "C" ds_status ds_rel_buckets(int32_t n_buckets, int32_t max_distance, int32_t bidirectional, int32_t* bucket) {
+    if (!bucket || (bidirectional != 0 && bidirectional != 1) || n_buckets > kRelBuckets || max_distance > kRelReach) return DS_EINVAL;
+    const int half = bidirectional ? n_buckets / 2 : n_buckets;
+    if (half < 2 || (bidirectional && n_buckets % 2) || max_distance <= half / 2) return DS_EINVAL;
+    for (int d = -max_distance; d <= max_distance; ++d)
+        bucket[max_distance + d] = d <= 0 ? bucket_of(-d, half, max_distance) : bidirectional ? half + bucket_of(d, half, max_distance) : 0;
+    return DS_OK;
+}

@@ -91,3 +91,41 @@ def test_differential_attention_closed_forms():
     same = np.concatenate([np.concatenate([t[:, :hd // 2]] * 2, axis=1) for t in (q, k)], axis=0)      # both maps alike, lambda = 1: nothing is left
     o = layer.diff_attention(same[:l], same[l:], v[:, :hd], np.ones(1), 1, True)[0]
     assert np.allclose(o, 0)
+
+
+@pytest.mark.parametrize("causal,pos", [(False, 0), (True, 0), (True, 2), (False, -3)])
+def test_relative_bias_gradients_against_differences(causal, pos):
+    rng = np.random.default_rng(7)
+    H, hd, lq, lk, scale = 2, 4, 4, 5, 0.7
+    v = {"q": rng.standard_normal((lq, H * hd)), "k": rng.standard_normal((lk, H * hd)), "v": rng.standard_normal((lk, H * hd)), "bias": rng.standard_normal((6, H))}
+    bucket = np.array([0, 1, 1, 2, 3, 5, 4])
+    d_o = rng.standard_normal((lq, H * hd))
+
+    def forward(v):
+        return layer.rel_attention(v["q"], v["k"], v["v"], v["bias"], bucket, H, causal, pos, scale)[0]
+
+    g = layer.rel_attention_back(v["q"], v["k"], v["v"], v["bias"], bucket, forward(v), d_o, H, causal, pos, scale)
+    for key in v:
+        for at in np.ndindex(v[key].shape):
+            hi, lo = dict(v), dict(v)
+            hi[key], lo[key] = v[key].copy(), v[key].copy()
+            hi[key][at] += 1e-6
+            lo[key][at] -= 1e-6
+            slope = ((forward(hi) - forward(lo)) * d_o).sum() / 2e-6
+            assert abs(slope - g["d" + key][at]) <= 1e-6 * (1 + abs(slope)), key
+
+
+def test_relative_bias_closed_forms():
+    rng = np.random.default_rng(8)
+    k, v = rng.standard_normal((4, 8)), rng.standard_normal((4, 8))
+    bucket = layer.rel_buckets(4, 2, True)
+    assert list(bucket) == [1, 1, 0, 3, 3]
+    bias = np.log(np.array([[1.0], [2.0], [4.0], [8.0]]))           # zero queries: probabilities go by the buckets alone
+    o, lse = layer.rel_attention(np.zeros((2, 8)), k, v, bias, bucket, 1, False)[:2]
+    w = np.array([[1, 8, 8, 8], [2, 1, 8, 8.0]])
+    assert np.allclose(o, (w / w.sum(axis=1, keepdims=True)) @ v) and np.allclose(lse, np.log(w.sum(axis=1)))
+    o, lse = layer.rel_attention(np.zeros((2, 8)), k, v, bias, bucket, 1, True, pos=-1)[:2]      # the first row sees nothing, the second the first key
+    assert np.all(o[0] == 0) and lse[0, 0] == -np.inf and np.allclose(o[1], v[0])
+    half = 16                                                       # 32 buckets up to 128: 0..7 alone, 8..15 by the logarithm in steps of sqrt(sqrt(2))
+    b = layer.rel_buckets(32, 128, True)[:129][::-1]
+    assert list(b[:9]) == list(range(8)) + [8] and b[16] == 10 and b[32] == 12 and b[64] == 14 and b[128] == half - 1 and b[11] == 8 and b[12] == 9
