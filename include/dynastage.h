@@ -644,6 +644,33 @@ ds_status ds_resid_norm_bwd(int32_t dtype, int32_t rms, int32_t rows, int32_t d,
                             int32_t accumulate, void* hip_stream);
 int64_t ds_resid_norm_bwd_scratch_floats(int32_t rows, int32_t d);
 
+/* The gated feed-forward block, both projections, activation and product in one kernel:
+ *     G = x Wg^T + bg,   U = x Wu^T + bu,   H = act(G) . U
+ * x: [rows, d]; wg, wu: [d_ff, d], as forward products read them (one row per output); bg, bu: [d_ff] or NULL; h: [rows, d_ff].  All of the type dtype,
+ * row-major, contiguous, 16-byte aligned; d and d_ff multiples of 8, at most 65 536; rows at most 2^31 - 2^16 - 1.  The activation sees the sums before they
+ * are rounded.  act: DS_ACT_GELU (tanh form), DS_ACT_SILU, DS_ACT_RELU.
+ * g, u: [rows, d_ff], what the backward pass needs of G and U, or both NULL: nothing is kept.
+ * row_valid: NULL, or DEVICE int32[rows]: rows with a negative entry are zeros in every output, whatever the inputs hold there (NaN too).
+ * workspace: DEVICE float32, 16-byte aligned, or NULL: room for partial sums; ds_gated_mlp_workspace_floats is as much as any of the three calls uses, and a
+ * smaller one is used as far as it goes.  Calls that share a workspace must not overlap.
+ * force_generic != 0 takes every product in fp32.  Few rows (at most 64, bf16) go to a kernel that reads the weights once. */
+enum { DS_ACT_GELU = 0, DS_ACT_SILU = 1, DS_ACT_RELU = 2 };
+int64_t ds_gated_mlp_workspace_floats(int32_t rows, int32_t d, int32_t d_ff);
+ds_status ds_gated_mlp_fwd(int32_t dtype, int32_t act, int32_t rows, int32_t d, int32_t d_ff, const void* x, const void* wg, const void* wu, const void* bg,
+                           const void* bu, const int32_t* row_valid, void* h, void* g, void* u, float* workspace, int64_t workspace_floats,
+                           int32_t force_generic, void* hip_stream);
+/* Its gradient with respect to G, U and x, from dh and what the forward pass kept:
+ *     dG = dH . U . act'(G),   dU = dH . act(G),   dx = dG Wg^T + dU Wu^T  (of dG and dU as stored; one product over 2 d_ff)
+ * wg, wu: [d, d_ff] here (one row per input feature), so that both passes read their weights along the contraction.  dg may be g, du may be u. */
+ds_status ds_gated_mlp_bwd(int32_t dtype, int32_t act, int32_t rows, int32_t d, int32_t d_ff, const void* dh, const void* g, const void* u, const void* wg,
+                           const void* wu, const int32_t* row_valid, void* dg, void* du, void* dx, float* workspace, int64_t workspace_floats,
+                           int32_t force_generic, void* hip_stream);
+/* Gradients of the parameters, float32, overwritten or added to (accumulate): dwg = x^T dg and dwu = x^T du, [d, d_ff]; dbg, dbu: [d_ff], the column sums
+ * of dg and du, or both NULL.  rows >= 1.  Every row counts: where dg and du are zero (rows that row_valid left out) x has to be finite.
+ * The biases' gradients need a workspace of at least 128 * d_ff floats. */
+ds_status ds_gated_mlp_wgrad(int32_t dtype, int32_t rows, int32_t d, int32_t d_ff, const void* x, const void* dg, const void* du, float* dwg, float* dwu, float* dbg,
+                             float* dbu, int32_t accumulate, float* workspace, int64_t workspace_floats, int32_t force_generic, void* hip_stream);
+
 /* Rotary positions.  x: [rows, >= n_heads * head_dim] with row stride ldx (elements), heads consecutive column groups; of each
  * head the first rot_dim columns are turned in pairs, (2p, 2p + 1) with interleaved = 1, (p, p + rot_dim / 2) with 0: pair p of
  * row r by the angle pos[r] * freq[p],

@@ -213,3 +213,28 @@ def rel_attention_back(q, k, v, bias, bucket, o, d_o, n_heads, causal, pos=0, sc
             out["dbias" + end][:, h] = np.bincount(of.ravel(), w.ravel(), bias.shape[0])
         out["dv"][:, c], out["dv_part"][:, c] = p.T @ d_o[:, c], p.T @ np.abs(d_o[:, c])
     return out
+
+
+# ---------------------------------------------------------------- the gated feed-forward block
+def act(z, kind):
+    """Activation and its derivative: "gelu" (tanh form), "silu", "relu"."""
+    if kind == "relu":
+        return np.maximum(z, 0.0), (z > 0) * 1.0
+    if kind == "silu":
+        s = 0.5 * (1.0 + np.tanh(0.5 * z))
+        return z * s, s + z * s * (1.0 - s)
+    c, a = math.sqrt(2.0 / math.pi), 0.044715
+    t = np.tanh(c * (z + a * z ** 3))
+    return 0.5 * z * (1.0 + t), 0.5 * (1.0 + t) + 0.5 * z * (1.0 - t * t) * c * (1.0 + 3.0 * a * z * z)
+
+
+def gated_mlp(x, wg, wu, bg, bu, kind):
+    """Weights [in, out] -> h, g, u."""
+    g, u = x @ wg + bg, x @ wu + bu
+    return act(g, kind)[0] * u, g, u
+
+
+def gated_mlp_back(dh, g, u, kind):
+    """-> dg, du."""
+    f, df = act(g, kind)
+    return dh * u * df, dh * f

@@ -19,6 +19,7 @@ DS_MODEL_GPT, DS_MODEL_T5 = 0, 1
 DS_DTYPE_F32, DS_DTYPE_BF16 = 0, 1
 DS_EPI_NONE, DS_EPI_GELU, DS_EPI_RESID, DS_EPI_DGELU, DS_EPI_ACC32, DS_EPI_GATE, DS_EPI_DGATE, DS_EPI_GELU_D, DS_EPI_MULR = range(9)
 DS_GATE_NONE, DS_GATE_COL, DS_GATE_ROW = range(3)
+DS_ACT_GELU, DS_ACT_SILU, DS_ACT_RELU = range(3)
 DS_ROPE_PLAIN, DS_ROPE_LINEAR, DS_ROPE_BASE, DS_ROPE_BANDS = range(4)
 
 PROF_KINDS = ("gemm_fwd", "gemm_dgrad", "gemm_wgrad", "attn_fwd", "attn_bwd", "norm", "colsum", "other", "transpose")
@@ -33,6 +34,7 @@ EXPORTS = ["dp_plan", "dp_plan_sampled", "dp_plan_replicas", "ds_plan_recompute"
            "ds_attention_bwd", "ds_attention_scratch_bytes", "ds_norm_fwd", "ds_norm_bwd", "ds_norm_bwd_scratch_floats", "ds_colsum", "ds_colsum_static",
            "ds_diff_attention_fwd", "ds_diff_attention_bwd", "ds_diff_attention_scratch_bytes",
            "ds_rel_attention_fwd", "ds_rel_attention_bwd", "ds_rel_attention_scratch_bytes", "ds_rel_buckets",
+           "ds_gated_mlp_fwd", "ds_gated_mlp_bwd", "ds_gated_mlp_wgrad", "ds_gated_mlp_workspace_floats",
            "ds_resid_norm_fwd", "ds_resid_norm_bwd", "ds_resid_norm_bwd_scratch_floats", "ds_rope", "ds_rope_freqs", "ds_layout_positions",
            "ds_mfma_probe", "ds_version"]
 
@@ -125,12 +127,15 @@ def lib():
                            ("ds_rel_attention_fwd", [i] * 5 + [p] * 5 + [i, i] + [p, i] * 3 + [f, p, i, p, i, p, i, p, i, i, p, l, i, p]),
                            ("ds_rel_attention_bwd", [i] * 5 + [p] * 5 + [i, i] + [p, i] * 3 + [f, p, i, p, i, p, p, i] + [p] * 5 + [i, i, i, p, l, i, p]),
                            ("ds_rel_buckets", [i, i, i, p]),
+                           ("ds_gated_mlp_fwd", [i] * 5 + [p] * 10 + [l, i, p]), ("ds_gated_mlp_bwd", [i] * 5 + [p] * 10 + [l, i, p]),
+                           ("ds_gated_mlp_wgrad", [i] * 4 + [p] * 7 + [i, p, l, i, p]),
                            ("ds_diff_attention_fwd", [i] * 5 + [p] * 4 + [i, i] + [p, i] * 3 + [p, p, p, i, p, i, i, p, l, i, p]),
                            ("ds_diff_attention_bwd", [i] * 5 + [p] * 4 + [i, i] + [p, i] * 3 + [p, p, p, p, i] + [p] * 5 + [i, i, i, p, l, i, p])):
             getattr(_lib, name).argtypes = args
         _lib.ds_resid_norm_bwd_scratch_floats.argtypes, _lib.ds_resid_norm_bwd_scratch_floats.restype = [i, i], l
         _lib.ds_diff_attention_scratch_bytes.argtypes, _lib.ds_diff_attention_scratch_bytes.restype = [i] * 4, l
         _lib.ds_rel_attention_scratch_bytes.argtypes, _lib.ds_rel_attention_scratch_bytes.restype = [i] * 6, l
+        _lib.ds_gated_mlp_workspace_floats.argtypes, _lib.ds_gated_mlp_workspace_floats.restype = [i] * 3, l
         _lib.ds_layout_free.restype = None
         _lib.ds_stage_destroy.restype = None
     return _lib
@@ -782,6 +787,59 @@ def ds_rel_buckets(n_buckets, max_distance, bidirectional=True):
     out = np.zeros(2 * max(int(max_distance), 0) + 1, dtype=np.int32)
     _check(lib().ds_rel_buckets(n_buckets, max_distance, int(bidirectional), _vp(out)), "ds_rel_buckets")
     return out
+
+
+def ds_gated_mlp_workspace_floats(rows, d, d_ff):
+    return lib().ds_gated_mlp_workspace_floats(rows, d, d_ff)
+
+
+def _workspace(t, dev):
+    """(address, floats) of an optional float32 workspace."""
+    import torch
+    return (None, 0) if t is None else (_tensor(t, "workspace", 0, torch.float32, dev), t.numel())
+
+
+def ds_gated_mlp_fwd(x, wg, wu, h, bg=None, bu=None, g=None, u=None, act=DS_ACT_GELU, row_valid=None, workspace=None, force_generic=False, stream=None):
+    """x [rows, d], wg and wu [d_ff, d], h (and g, u) [rows, d_ff]."""
+    torch, code, dev = _current(x)
+    dt = x.dtype
+    (rows, d), ff = x.shape, wg.shape[0]
+    if max(rows, d, ff) > 0x7fffffff:
+        _too_large(rows, d, ff)
+    out, col, weight = (rows, ff), (ff,), (ff, d)
+    rc = lib().ds_gated_mlp_fwd(code, act, rows, d, ff, _tensor(x, "x", (rows, d), dt, dev), _tensor(wg, "wg", weight, dt, dev), _tensor(wu, "wu", weight, dt, dev),
+                                _tensor(bg, "bg", col, dt, dev), _tensor(bu, "bu", col, dt, dev), _tensor(row_valid, "row_valid", (rows,), torch.int32, dev),
+                                _tensor(h, "h", out, dt, dev), _tensor(g, "g", out, dt, dev), _tensor(u, "u", out, dt, dev), *_workspace(workspace, dev),
+                                int(force_generic), _raw_stream(torch, stream, dev))
+    _check(rc, "ds_gated_mlp_fwd")
+
+
+def ds_gated_mlp_bwd(dh, g, u, wg, wu, dg, du, dx, act=DS_ACT_GELU, row_valid=None, workspace=None, force_generic=False, stream=None):
+    """dh, g, u, dg, du [rows, d_ff], wg and wu [d, d_ff], dx [rows, d]; dg may be g, du may be u."""
+    torch, code, dev = _current(dh)
+    dt = dh.dtype
+    (rows, ff), d = dh.shape, wg.shape[0]
+    if max(rows, d, ff) > 0x7fffffff:
+        _too_large(rows, d, ff)
+    wide, weight = (rows, ff), (d, ff)
+    rc = lib().ds_gated_mlp_bwd(code, act, rows, d, ff, _tensor(dh, "dh", wide, dt, dev), _tensor(g, "g", wide, dt, dev), _tensor(u, "u", wide, dt, dev),
+                                _tensor(wg, "wg", weight, dt, dev), _tensor(wu, "wu", weight, dt, dev), _tensor(row_valid, "row_valid", (rows,), torch.int32, dev),
+                                _tensor(dg, "dg", wide, dt, dev), _tensor(du, "du", wide, dt, dev), _tensor(dx, "dx", (rows, d), dt, dev), *_workspace(workspace, dev),
+                                int(force_generic), _raw_stream(torch, stream, dev))
+    _check(rc, "ds_gated_mlp_bwd")
+
+
+def ds_gated_mlp_wgrad(x, dg, du, dwg, dwu, dbg=None, dbu=None, accumulate=False, workspace=None, force_generic=False, stream=None):
+    """x [rows, d], dg and du [rows, d_ff], dwg and dwu float32 [d, d_ff], dbg and dbu float32 [d_ff]."""
+    torch, code, dev = _current(x)
+    dt, f32 = x.dtype, torch.float32
+    (rows, d), ff = x.shape, dg.shape[1]
+    if max(rows, d, ff) > 0x7fffffff:
+        _too_large(rows, d, ff)
+    rc = lib().ds_gated_mlp_wgrad(code, rows, d, ff, _tensor(x, "x", (rows, d), dt, dev), _tensor(dg, "dg", (rows, ff), dt, dev), _tensor(du, "du", (rows, ff), dt, dev),
+                                  _tensor(dwg, "dwg", (d, ff), f32, dev), _tensor(dwu, "dwu", (d, ff), f32, dev), _tensor(dbg, "dbg", (ff,), f32, dev),
+                                  _tensor(dbu, "dbu", (ff,), f32, dev), int(accumulate), *_workspace(workspace, dev), int(force_generic), _raw_stream(torch, stream, dev))
+    _check(rc, "ds_gated_mlp_wgrad")
 
 
 def ds_rope(x, y, pos, freq, n_heads, head_dim, rot_dim, interleaved=False, inverse=False, amplitude=1.0, stream=None):

@@ -1,0 +1,140 @@
+// C-ABI entry points and dispatch of the gated feed-forward block.
+#include "gated_mlp.hpp"
+#include "gemm.hpp"
+#include <algorithm>
+#include <initializer_list>
+#include <type_traits>
+
+namespace {
+
+// dG and dU, 8 elements to a thread.  dg may be g, du may be u.  Bound by memory: three tensors read, two written.
+template <class T, int ACT>
+__global__ __launch_bounds__(256) void glu_grad_kernel(long long n8, int ff8, const T* __restrict__ dh, const T* g, const T* u, const int32_t* __restrict__ row_valid, T* dg, T* du) {
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n8; i += (long long)gridDim.x * 256) {
+        float zg[8], zu[8], z[8], a[8], b[8];
+        const bool valid = !row_valid || row_valid[(uint32_t)(i / ff8)] >= 0;
+        Vec8<T>::load(dh + i * 8, z);
+        Vec8<T>::load(g + i * 8, zg);
+        Vec8<T>::load(u + i * 8, zu);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            float f, df;
+            glu_act<ACT>(zg[j], f, df);
+            a[j] = valid ? z[j] * zu[j] * df : 0.f;
+            b[j] = valid ? z[j] * f : 0.f;
+        }
+        Vec8<T>::store(dg + i * 8, a);
+        Vec8<T>::store(du + i * 8, b);
+    }
+}
+
+template <class T> ds_status grad_launch(const GluArgs& a, const void* dh, const void* g, const void* u, void* dg, void* du, hipStream_t st) {
+    return glu_by_act(a.act, [&](auto act) -> ds_status {
+        const long long n8 = (long long)a.rows * a.ff / 8;
+        const unsigned blocks = (unsigned)std::min<long long>((n8 + 255) / 256, 1 << 16);
+        hipLaunchKernelGGL((glu_grad_kernel<T, decltype(act)::value>), dim3(blocks), dim3(256), 0, st, n8, a.ff / 8, (const T*)dh, (const T*)g, (const T*)u, a.row_valid, (T*)dg, (T*)du);
+        DS_LAUNCH_CHECK();
+        return DS_OK;
+    });
+}
+
+constexpr int64_t kSumFloats = 128;                    // for each column: room for the biases' gradients
+constexpr int kWide = 1 << 16, kRows = 0x7fffffff - (1 << 16);
+
+ds_status check(int32_t dtype, int32_t rows, int32_t d, int32_t ff, std::initializer_list<const void*> needed, std::initializer_list<const void*> others, const float* workspace,
+                int64_t workspace_floats) {
+    if (dtype != DS_DTYPE_F32 && dtype != DS_DTYPE_BF16) return DS_EINVAL;
+    if (rows < 0 || rows > kRows || d <= 0 || d % 8 || d > kWide || ff <= 0 || ff % 8 || ff > kWide) return DS_EINVAL;
+    if (((int64_t)rows + 63) / 64 * ((std::max(d, ff) + 63) / 64) > 0x7fffffff / 256) return DS_EINVAL;       // (work-items of a launch)
+    for (const void* p : needed)
+        if (!p || ((uintptr_t)p & 15)) return DS_EINVAL;
+    for (const void* p : others)
+        if ((uintptr_t)p & 15) return DS_EINVAL;
+    if (workspace_floats < 0 || (workspace_floats > 0 && (!workspace || ((uintptr_t)workspace & 15)))) return DS_EINVAL;
+    return DS_OK;
+}
+bool known_act(int32_t act) { return act == DS_ACT_GELU || act == DS_ACT_SILU || act == DS_ACT_RELU; }
+
+}  // namespace
+
+extern "C" int64_t ds_gated_mlp_workspace_floats(int32_t rows, int32_t d, int32_t d_ff) {
+    if (rows <= 0 || d <= 0 || d_ff <= 0) return 0;
+    return std::max((int64_t)1 << 24, kSumFloats * d_ff);
+}
+
+extern "C" ds_status ds_gated_mlp_fwd(int32_t dtype, int32_t act, int32_t rows, int32_t d, int32_t d_ff, const void* x, const void* wg, const void* wu, const void* bg,
+                                      const void* bu, const int32_t* row_valid, void* h, void* g, void* u, float* workspace, int64_t workspace_floats,
+                                      int32_t force_generic, void* hip_stream) {
+    const ds_status r = check(dtype, rows, d, d_ff, {x, wg, wu, h}, {bg, bu, g, u}, workspace, workspace_floats);
+    if (r != DS_OK) return r;
+    if (!known_act(act) || !g != !u) return DS_EINVAL;
+    if (rows == 0) return DS_OK;
+    GluArgs a = {};
+    a.dtype = dtype; a.act = act; a.rows = rows; a.d = d; a.ff = d_ff;
+    a.x = x; a.wg = wg; a.wu = wu; a.bg = bg; a.bu = bu; a.row_valid = row_valid; a.h = h; a.g = g; a.u = u;
+    if (dtype == DS_DTYPE_F32 || force_generic) return glu_fwd_general(a, (hipStream_t)hip_stream);
+    if (rows <= kGluFewRows) return glu_fwd_few(a, (hipStream_t)hip_stream);
+    return glu_fwd_tile(a, (hipStream_t)hip_stream);
+}
+
+extern "C" ds_status ds_gated_mlp_bwd(int32_t dtype, int32_t act, int32_t rows, int32_t d, int32_t d_ff, const void* dh, const void* g, const void* u, const void* wg,
+                                      const void* wu, const int32_t* row_valid, void* dg, void* du, void* dx, float* workspace, int64_t workspace_floats,
+                                      int32_t force_generic, void* hip_stream) {
+    ds_status r = check(dtype, rows, d, d_ff, {dh, g, u, wg, wu, dg, du, dx}, {}, workspace, workspace_floats);
+    if (r != DS_OK) return r;
+    if (!known_act(act)) return DS_EINVAL;
+    if (rows == 0) return DS_OK;
+    hipStream_t st = (hipStream_t)hip_stream;
+    GluArgs a = {};
+    a.dtype = dtype; a.act = act; a.rows = rows; a.d = d; a.ff = d_ff;
+    a.wg = wg; a.wu = wu; a.row_valid = row_valid; a.dg = dg; a.du = du; a.dx = dx;
+    r = dtype == DS_DTYPE_BF16 ? grad_launch<bf16_t>(a, dh, g, u, dg, du, st) : grad_launch<float>(a, dh, g, u, dg, du, st);
+    if (r != DS_OK) return r;
+    return dtype == DS_DTYPE_F32 || force_generic ? glu_dx_general(a, st) : glu_dx_tile(a, st);
+}
+
+extern "C" ds_status ds_gated_mlp_wgrad(int32_t dtype, int32_t rows, int32_t d, int32_t d_ff, const void* x, const void* dg, const void* du, float* dwg, float* dwu, float* dbg,
+                                        float* dbu, int32_t accumulate, float* workspace, int64_t workspace_floats, int32_t force_generic, void* hip_stream) {
+    ds_status r = check(dtype, rows, d, d_ff, {x, dg, du, dwg, dwu}, {dbg, dbu}, workspace, workspace_floats);
+    if (r != DS_OK) return r;
+    if (rows == 0 || (accumulate != 0 && accumulate != 1) || !dbg != !dbu) return DS_EINVAL;
+    if (dbg && workspace_floats < kSumFloats * d_ff) return DS_EINVAL;
+    hipStream_t st = (hipStream_t)hip_stream;
+    TnGroup group;
+    group.n = 2; group.K = rows; group.accumulate = accumulate; group.f32 = dtype == DS_DTYPE_F32;
+    group.p[0] = TnProblem{x, dg, dwg, d, d_ff};
+    group.p[1] = TnProblem{x, du, dwu, d, d_ff};
+    for (int i = 0; i < TnGroup::kSlabs; ++i) {
+        group.slab[i] = workspace;
+        group.slab_end[i] = (int32_t)std::min<int64_t>(workspace_floats >> group.block_log2(), INT32_MAX);
+    }
+    TnPick pick{-1, 1};
+    if (!force_generic && tn_group_takes(group.p[0], rows, group.f32)) pick = pick_tn_group(group);
+    if (pick.kind >= 0) {
+        r = launch_tn_group(pick, group, st);
+        if (r != DS_OK) return r;
+    } else if (dtype == DS_DTYPE_BF16 && !force_generic && !tn_group_takes(group.p[0], rows, false)) {
+        // sizes that the products' own kernels do not take: the rows are shared out until there are two work-groups for a compute unit
+        const int64_t tiles = (int64_t)((d + 127) / 128) * ((d_ff + 127) / 128) * 2, outputs = (int64_t)d * d_ff;
+        const int64_t most = outputs <= INT32_MAX ? workspace_floats / (2 * outputs) : 1;
+        GluWgrad w = {rows, d, d_ff, accumulate, 1, x, {dg, du}, {dwg, dwu}, workspace};
+        w.splits = (int32_t)std::max<int64_t>(1, std::min({2 * (int64_t)gemm_cu_count() / tiles, most, ((int64_t)rows + 255) / 256}));
+        r = glu_wgrad_tile(w, st);
+        if (r != DS_OK) return r;
+    } else {
+        for (int i = 0; i < 2; ++i) {
+            GemmEpi p{};
+            p.accumulate = accumulate;
+            r = launch_gemm(dtype, 1, 0, d, d_ff, rows, x, i ? du : dg, i ? dwu : dwg, DS_EPI_ACC32, p, force_generic != 0, workspace_floats > 0 ? workspace : nullptr,
+                            (size_t)workspace_floats, st);
+            if (r != DS_OK) return r;
+        }
+    }
+    if (!dbg) return DS_OK;
+    SumGroup sums;                                      // (behind the products in the stream: the workspace is free again)
+    sums.n = 2; sums.accumulate = accumulate;
+    sums.it[0] = SumItem{dg, dbg, rows, d_ff, d_ff, 1};
+    sums.it[1] = SumItem{du, dbu, rows, d_ff, d_ff, 1};
+    int launched = 0;
+    return launch_sum_group(dtype, sums, workspace, (size_t)workspace_floats, st, &launched);
+}

@@ -597,7 +597,6 @@ template <class T, int HD> ds_status bwd_launch(const RelAttnArgs& a, hipStream_
 
 template <class F> ds_status by_size(const RelAttnArgs& a, F&& f) {
     auto of = [&](auto zero) {
-        typedef decltype(zero) T;
         if (a.head_dim <= 32) return f(zero, std::integral_constant<int, 32>{});
         if (a.head_dim <= 64) return f(zero, std::integral_constant<int, 64>{});
         if (a.head_dim <= 96) return f(zero, std::integral_constant<int, 96>{});

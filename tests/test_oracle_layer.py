@@ -129,3 +129,31 @@ def test_relative_bias_closed_forms():
     half = 16                                                       # 32 buckets up to 128: 0..7 alone, 8..15 by the logarithm in steps of sqrt(sqrt(2))
     b = layer.rel_buckets(32, 128, True)[:129][::-1]
     assert list(b[:9]) == list(range(8)) + [8] and b[16] == 10 and b[32] == 12 and b[64] == 14 and b[128] == half - 1 and b[11] == 8 and b[12] == 9
+
+
+@pytest.mark.parametrize("kind", ["gelu", "silu", "relu"])
+def test_gated_mlp_gradients_against_differences(kind):
+    rng = np.random.default_rng(9)
+    v = {"x": rng.standard_normal((3, 4)), "wg": rng.standard_normal((4, 5)), "wu": rng.standard_normal((4, 5)), "bg": rng.standard_normal(5), "bu": rng.standard_normal(5)}
+    dh = rng.standard_normal((3, 5))
+
+    def forward(v):
+        return layer.gated_mlp(v["x"], v["wg"], v["wu"], v["bg"], v["bu"], kind)
+
+    _, g, u = forward(v)
+    dg, du = layer.gated_mlp_back(dh, g, u, kind)
+    grads = {"x": dg @ v["wg"].T + du @ v["wu"].T, "wg": v["x"].T @ dg, "wu": v["x"].T @ du, "bg": dg.sum(axis=0), "bu": du.sum(axis=0)}
+    for key in v:
+        for at in np.ndindex(v[key].shape):
+            hi, lo = dict(v), dict(v)
+            hi[key], lo[key] = v[key].copy(), v[key].copy()
+            hi[key][at] += 1e-6
+            lo[key][at] -= 1e-6
+            slope = ((forward(hi)[0] - forward(lo)[0]) * dh).sum() / 2e-6
+            assert abs(slope - grads[key][at]) <= 1e-6 * (1 + abs(slope)), key
+
+
+def test_activations():
+    z = np.array([-30.0, -1.0, 0.0, 1.0, 30.0])
+    assert np.allclose(layer.act(z, "silu")[0], z / (1 + np.exp(-z))) and np.allclose(layer.act(z, "relu")[0], [0, 0, 0, 1, 30])
+    assert np.allclose(layer.act(z, "gelu")[0], [0, -0.15880801, 0, 0.84119199, 30])
