@@ -26,7 +26,9 @@ struct RelAttnArgs : AttnArgs {
     float* d;                                           // general kernels: D, [n_heads][q_total_rows]
     float* slots;                                       // sums of dS by distance, [block of queries][n_heads][2 reach + 1]
     float* split_part;                                  // see RelPart
-    char* aug;                                          // matrix-core kernels: see rel_attention_mfma.hip
+    char* aug;                                          // matrix-core kernels: what the dQ kernel hands to the dK/dV kernel
+    int32_t direct;                                     // matrix-core kernels: sequences have one block of 128 rows, and work-groups go by sequence and head without a list
+    int32_t first_group, groups;                        // dK/dV grid: work-groups in front that sum up dbias, work-groups behind them
 };
 
 // Work-groups that share the keys of a sequence and head leave, for each query, its maximum (exp2 domain), sum and unscaled output.
@@ -106,3 +108,7 @@ int rel_general_columns(const RelAttnArgs& a, int max_len);
 
 ds_status rel_fwd_general(const RelAttnArgs& a, hipStream_t st);
 ds_status rel_bwd_general(const RelAttnArgs& a, hipStream_t st);
+// bf16 matrix-core kernels; what they do not take (see rel_mfma_supported) the general ones do
+bool rel_mfma_supported(const RelAttnArgs& a);
+ds_status rel_fwd_mfma(const RelAttnArgs& a, hipStream_t st);
+ds_status rel_bwd_mfma(const RelAttnArgs& a, hipStream_t st);

@@ -63,12 +63,15 @@ static ds_status check(RelAttnArgs& a) {
     return DS_OK;
 }
 
-// How a call goes to the kernels: work-groups that share a head's keys (forward)
-struct RelChoice { int32_t general, k_splits; };
-static RelChoice choose(const RelAttnArgs& a, bool backward, bool force_generic) {
-    RelChoice c = {1, 1};
-    (void)force_generic;
+// How a call goes to the kernels: fp32 arithmetic or bf16 matrix cores; work-groups that share a head's keys (forward); bf16: whether there is no work list
+struct RelChoice { int32_t general, k_splits, direct; };
+static RelChoice choose(RelAttnArgs& a, bool backward, bool force_generic) {
+    RelChoice c = {1, 1, 0};
     if (!backward && a.max_q_len <= kSplitQueries) c.k_splits = most_splits(a.n_heads, a.head_dim, a.q_total_rows, a.max_k_len, a.n_seq);
+    a.k_splits = c.k_splits;
+    c.general = force_generic || !rel_mfma_supported(a);
+    if (!c.general) c.direct = a.max_q_len <= 128 && (!backward || a.max_k_len <= 128);
+    a.direct = c.direct;
     return c;
 }
 
@@ -94,9 +97,7 @@ extern "C" ds_status ds_rel_attention_fwd(int32_t dtype, int32_t n_seq, int32_t 
     a.scratch = scratch; a.scratch_bytes = scratch_bytes < 0 ? 0 : (size_t)scratch_bytes;
     const ds_status r = check(a);
     if (r != DS_OK) return r;
-    const RelChoice c = choose(a, false, force_generic != 0);
-    a.k_splits = c.k_splits;
-    return rel_fwd_general(a, (hipStream_t)hip_stream);
+    return choose(a, false, force_generic != 0).general ? rel_fwd_general(a, (hipStream_t)hip_stream) : rel_fwd_mfma(a, (hipStream_t)hip_stream);
 }
 
 extern "C" ds_status ds_rel_attention_bwd(int32_t dtype, int32_t n_seq, int32_t n_heads, int32_t head_dim, int32_t mask, const int32_t* q_row,
@@ -119,7 +120,7 @@ extern "C" ds_status ds_rel_attention_bwd(int32_t dtype, int32_t n_seq, int32_t 
     const ds_status r = check(a);
     if (r != DS_OK) return r;
     if (!d_o || !dq || !dk || !dv || !dbias || (accumulate != 0 && accumulate != 1)) return DS_EINVAL;
-    return rel_bwd_general(a, (hipStream_t)hip_stream);
+    return choose(a, true, force_generic != 0).general ? rel_bwd_general(a, (hipStream_t)hip_stream) : rel_bwd_mfma(a, (hipStream_t)hip_stream);
 }
 
 // The bucket of distance n >= 0 among `half`: itself up to half of them, then by logarithm.  log(n / exact) / log(far / exact) is rarely a whole number of
