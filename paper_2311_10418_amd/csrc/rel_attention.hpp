@@ -58,6 +58,21 @@ __device__ __forceinline__ void lds_add(float* lds, float v) {
     __builtin_amdgcn_ds_faddf((__attribute__((address_space(3))) float*)lds, v, 0, 0, false);
 }
 
+// v of the lane N above (row_shl) or below (row_shr) within each 16 lanes, 0 where there is none: rides on the addition that uses it
+template <int N> __device__ __forceinline__ float lanes_above(float v) {
+    if constexpr (N == 0) return v;
+    else return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x100 + N, 0xf, 0xf, true));
+}
+template <int N> __device__ __forceinline__ float lanes_below(float v) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x110 + N, 0xf, 0xf, true));
+}
+// Sums along the diagonals of a block whose columns are 16 lanes: the value of row r (a constant) in lane c belongs to distance r - c, which is -d for the lane d
+// that it is shifted to where d = c - r is a lane, and 16 - d where it comes in again at the other end.
+template <int R> __device__ __forceinline__ void add_diagonals(float x, float& minus, float& around) {
+    minus += lanes_above<R>(x);
+    if constexpr (R != 0) around += lanes_below<16 - R>(x);
+}
+
 // blocks of `cols` queries of all sequences before s: slots are numbered by sequence
 template <int COLS, int THREADS> __device__ __forceinline__ int blocks_before(const RelAttnArgs& a, int s, int* lds) {
     int n = 0;

@@ -367,6 +367,7 @@ __global__ __launch_bounds__(512, HD <= 64 ? 4 : 2) void rel_bwd_dq_kernel(RelAt
     const int slot = blocks_before<COLS, 512>(a, s, reinterpret_cast<int*>(sK)) + cb.block;
     const int near = a.reach + kPad + 4 * g - pi;                      // [key tile row e]: entry near + kb + e
     const float side_bias[2] = {rel_bias(a, h, 0), rel_bias(a, h, 2 * a.reach)};
+    const float live = qi < ql ? 1.f : 0.f;             // (a lane past the last query repeats the last one: its sums do not count)
     float beyond[2] = {0.f, 0.f};
     f32x4_t gacc[NS];
 #pragma unroll
@@ -399,17 +400,23 @@ __global__ __launch_bounds__(512, HD <= 64 ? 4 : 2) void rel_bwd_dq_kernel(RelAt
                 }
 #pragma unroll
             for (int e = 0; e < 4; ++e) p[e] = __builtin_amdgcn_exp2f(p[e]) * (gr[e] - d);
-            // (a lane past the last query repeats the last one: its sums do not count)
             if (side) {
-                const float add = qi < ql ? (p[0] + p[1]) + (p[2] + p[3]) : 0.f;
+                const float add = live * ((p[0] + p[1]) + (p[2] + p[3]));
                 beyond[0] += side < 0 ? add : 0.f;
                 beyond[1] += side < 0 ? 0.f : add;
             } else {
+                // rows 4 g + e of 16 columns: two sums a lane, of distances 16 apart; the four groups of lanes overlap and add theirs one after the other
+                float minus = 0.f, around = 0.f;
+                add_diagonals<0>(live * p[0], minus, around);
+                add_diagonals<1>(live * p[1], minus, around);
+                add_diagonals<2>(live * p[2], minus, around);
+                add_diagonals<3>(live * p[3], minus, around);
+                float* to = &sums[kb - pw0 + 4 * g - (lane & 15) + a.reach + kPad];
 #pragma unroll
                 for (int part = 0; part < 4; ++part)
-                    if (g == part && qi < ql) {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) lds_add(&sums[near + kb + e], p[e]);
+                    if (g == part) {
+                        lds_add(to, minus);
+                        if ((lane & 15) > 12) lds_add(to + 16, around);
                     }
             }
             second_product<HD>(sK, 16 * kt, lane, p, gacc);
@@ -447,13 +454,19 @@ __global__ __launch_bounds__(512, HD <= 64 ? 4 : 2) void rel_bwd_dq_kernel(RelAt
     __syncthreads();
     // the block's slot: what the wavefronts have, distances beyond reach with those at it
     float* to = a.slots + ((size_t)slot * a.n_heads + h) * (2 * a.reach + 1);
-    for (int i = t; i <= 2 * a.reach; i += 512) {
+    for (int i = t; i <= 2 * (a.reach + kPad); i += 512) {
         float sum = 0.f;
-        const int from = i == 0 ? 0 : i + kPad, last = i == 2 * a.reach ? 2 * (a.reach + kPad) : i + kPad;
-        for (int j = from; j <= last; ++j)
 #pragma unroll
-            for (int w = 0; w < 8; ++w) sum += table[wide * (1 + w) + j];
-        to[i] = sum;
+        for (int w = 0; w < 8; ++w) sum += table[wide * (1 + w) + i];
+        const int at = i - kPad;
+        if (at > 0 && at < 2 * a.reach) to[at] = sum;
+        else table[i] = sum;
+    }
+    __syncthreads();
+    if (wave8 < 2) {
+        float sum = lane <= kPad ? table[wave8 * (2 * a.reach + kPad) + lane] : 0.f;
+        sum = wave_sum(sum);
+        if (lane == 0) to[wave8 * 2 * a.reach] = sum;
     }
 }
 

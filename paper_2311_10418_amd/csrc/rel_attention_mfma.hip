@@ -4,9 +4,10 @@
 // Forward and dQ: a wavefront's block of scores covers 95 (63) distances.  Where all lie beyond reach the bias is one number and rides in the FMA that scales the
 // scores: no instruction more.  Near blocks read the table of the head in LDS, whose entries stand by distance, so that the 16 rows of a lane are 16 constant
 // offsets from one address (ds_read2_b32 of neighbours), and scale their scores in that step instead of the later one.
-// dbias: dS is there in fp32, before it is rounded for the product, in the dQ kernel.  Blocks beyond reach add it up in a register, near ones with ds_add_f32 at
-// the same offsets of an array by distance; a lane's address differs from its neighbour's by one entry, so that no two lanes of a half meet, and the halves
-// (rows 4 apart) have an array each.  Work-groups leave their sums in a slot; work-groups in front of the dK/dV grid add the slots up.
+// dbias: dS is there in fp32, before it is rounded for the product, in the dQ kernel.  Blocks beyond reach add it up in a register, near ones along their
+// diagonals: two additions an element with a shift of lanes in them (row_shl, row_shr), two values a lane and block into an array by distance in LDS, private to
+// the lane half and the wavefront.  (16 ds_add_f32 a block instead: 160 cycles each, and the dQ kernel took 370 us instead of @DQ@ for 31 sequences of 366 to 523,
+// 16 heads of 64.)  Work-groups leave their sums in a slot; work-groups in front of the dK/dV grid add the slots up.
 // dK/dV: the loop over the blocks of queries is cut by distance, so that steps stay straight code: steps with the table and steps with one number.
 //
 // Few queries over long keys (k_splits > 1): the keys of a head are dealt out to work-groups, see RelPart.  Sequences of at most 128 queries and keys need no
@@ -358,10 +359,11 @@ __global__ __launch_bounds__(256, 2) void rel_bwd_dq_mfma_kernel(RelAttnArgs a) 
     fill_table(a, h, table);
     for (int i = tid; i < 8 * wide; i += 256) table[wide + i] = 0.f;
     __syncthreads();
-    // sums of dS by distance: two arrays for each wavefront, since its lane halves hold rows 4 apart and would meet in one
+    // sums of dS by distance: two arrays for each wavefront, since the distances of its lane halves, rows 4 apart, overlap
     float* const sums = table + wide * (1 + 2 * wave + g);
     const float flat_behind = rel_bias(a, h, 0), flat_front = rel_bias(a, h, 2 * a.reach);
-    float beyond_behind = 0.f, beyond_front = 0.f;
+    float beyond_behind = 0.f, beyond_front = 0.f, carry = 0.f;
+    float* to = sums;                                   // (where `carry` belongs: 32 on)
     const int wave_last = CAUSAL ? min(kl - 1, pw0 + 31) : kl - 1;
     const int nb = (kv_end + 63) / 64;
     for (int b = 0; b < nb; ++b) {
@@ -427,9 +429,32 @@ __global__ __launch_bounds__(256, 2) void rel_bwd_dq_mfma_kernel(RelAttnArgs a) 
 #pragma unroll
             for (int e = 0; e < 16; ++e) sacc[e] *= pacc[e] - delta;          // dS^T
             if (near) {
-                float* to = sums + at;
-#pragma unroll
-                for (int e = 0; e < 16; ++e) lds_add(to + 8 * (e >> 2) + (e & 3), sacc[e]);
+                // rows 8 (e / 4) + e % 4 (+ 4 g) of columns 16 (lane / 16 % 2) + lane % 16: three sums a lane, of distances 16 apart.  The third is the first of the
+                // half behind, 32 keys on, and goes there in a register.
+                float sum[3] = {carry, 0.f, 0.f};
+                add_diagonals<0>(sacc[0], sum[0], sum[1]);
+                add_diagonals<1>(sacc[1], sum[0], sum[1]);
+                add_diagonals<2>(sacc[2], sum[0], sum[1]);
+                add_diagonals<3>(sacc[3], sum[0], sum[1]);
+                add_diagonals<8>(sacc[4], sum[0], sum[1]);
+                add_diagonals<9>(sacc[5], sum[0], sum[1]);
+                add_diagonals<10>(sacc[6], sum[0], sum[1]);
+                add_diagonals<11>(sacc[7], sum[0], sum[1]);
+                add_diagonals<0>(sacc[8], sum[1], sum[2]);
+                add_diagonals<1>(sacc[9], sum[1], sum[2]);
+                add_diagonals<2>(sacc[10], sum[1], sum[2]);
+                add_diagonals<3>(sacc[11], sum[1], sum[2]);
+                add_diagonals<8>(sacc[12], sum[1], sum[2]);
+                add_diagonals<9>(sacc[13], sum[1], sum[2]);
+                add_diagonals<10>(sacc[14], sum[1], sum[2]);
+                add_diagonals<11>(sacc[15], sum[1], sum[2]);
+                to = sums + (kv0 + kt * 32 - pw0 + 4 * g - (lane & 31) + a.reach + kTablePad);
+                wave_lds_sync();                                            // (one lane's second place is another's first)
+                to[0] += sum[0];
+                wave_lds_sync();
+                to[16] += sum[1];
+                wave_lds_sync();
+                carry = sum[2];
             } else {
                 float x[8];
 #pragma unroll
@@ -450,6 +475,7 @@ __global__ __launch_bounds__(256, 2) void rel_bwd_dq_mfma_kernel(RelAttnArgs a) 
         }
     }
     if (qi < ql) store_cols<HD>(gacc, a.scale, (bf16_t*)a.dq + (qrow0 + qi) * a.ldq + h * HD, g);
+    to[32] += carry;
     beyond_behind = wave_sum(beyond_behind);
     beyond_front = wave_sum(beyond_front);
     if (lane == 0) {
