@@ -5,6 +5,7 @@
 // Weight gradients:             dWg = x^T dG,  dWu = x^T dU  ([d][d_ff]), dbg and dbu the column sums of dG and dU.
 #pragma once
 #include "common.hpp"
+#include <type_traits>
 
 struct GluArgs {
     int32_t dtype, act, rows, d, ff;
@@ -54,3 +55,8 @@ struct GluWgrad {
     float *dw[2], *workspace;
 };
 ds_status glu_wgrad_tile(const GluWgrad& a, hipStream_t st);
+// the same with 256 x 256 tiles (gemm.hip): d and d_ff multiples of 64, dx: d of 256; and the estimate of their time in microseconds, of `columns` (a multiple of 256)
+// weight rows and a contraction over K
+ds_status glu_fwd_big(const GluArgs& a, float* ws, size_t ws_floats, hipStream_t st);
+ds_status glu_dx_big(const GluArgs& a, float* ws, size_t ws_floats, hipStream_t st);
+double glu_big_cost(int M, int columns, int K, size_t ws_floats);

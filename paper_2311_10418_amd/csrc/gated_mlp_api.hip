@@ -53,6 +53,13 @@ ds_status check(int32_t dtype, int32_t rows, int32_t d, int32_t ff, std::initial
     if (workspace_floats < 0 || (workspace_floats > 0 && (!workspace || ((uintptr_t)workspace & 15)))) return DS_EINVAL;
     return DS_OK;
 }
+// Whether a product goes to the 256 x 256 tiles
+bool big_takes(const GluArgs& a, bool dx, size_t ws_floats) {
+    if (a.d % 64 || a.ff % 64 || (dx && a.d % 256) || (int64_t)a.rows * std::max(a.d, a.ff) > (int64_t)1 << 40) return false;
+    const int columns = dx ? a.d : (a.ff + 127) / 128 * 256, K = dx ? 2 * a.ff : a.d;
+    if (const char* e = getenv("GLU_BIG")) return e[0] == '1';
+    return (int64_t)((a.rows + 255) / 256) * (columns / 256) >= gemm_cu_count();
+}
 bool known_act(int32_t act) { return act == DS_ACT_GELU || act == DS_ACT_SILU || act == DS_ACT_RELU; }
 
 }  // namespace
@@ -74,6 +81,8 @@ extern "C" ds_status ds_gated_mlp_fwd(int32_t dtype, int32_t act, int32_t rows, 
     a.x = x; a.wg = wg; a.wu = wu; a.bg = bg; a.bu = bu; a.row_valid = row_valid; a.h = h; a.g = g; a.u = u;
     if (dtype == DS_DTYPE_F32 || force_generic) return glu_fwd_general(a, (hipStream_t)hip_stream);
     if (rows <= kGluFewRows) return glu_fwd_few(a, (hipStream_t)hip_stream);
+    const size_t floats = workspace_floats > 0 ? (size_t)workspace_floats : 0;
+    if (big_takes(a, false, floats)) return glu_fwd_big(a, workspace, floats, (hipStream_t)hip_stream);
     return glu_fwd_tile(a, (hipStream_t)hip_stream);
 }
 
@@ -90,7 +99,9 @@ extern "C" ds_status ds_gated_mlp_bwd(int32_t dtype, int32_t act, int32_t rows, 
     a.wg = wg; a.wu = wu; a.row_valid = row_valid; a.dg = dg; a.du = du; a.dx = dx;
     r = dtype == DS_DTYPE_BF16 ? grad_launch<bf16_t>(a, dh, g, u, dg, du, st) : grad_launch<float>(a, dh, g, u, dg, du, st);
     if (r != DS_OK) return r;
-    return dtype == DS_DTYPE_F32 || force_generic ? glu_dx_general(a, st) : glu_dx_tile(a, st);
+    if (dtype == DS_DTYPE_F32 || force_generic) return glu_dx_general(a, st);
+    const size_t floats = workspace_floats > 0 ? (size_t)workspace_floats : 0;
+    return big_takes(a, true, floats) ? glu_dx_big(a, workspace, floats, st) : glu_dx_tile(a, st);
 }
 
 extern "C" ds_status ds_gated_mlp_wgrad(int32_t dtype, int32_t rows, int32_t d, int32_t d_ff, const void* x, const void* dg, const void* du, float* dwg, float* dwu, float* dbg,

@@ -12,6 +12,7 @@
 // Epilogues go back through LDS so that global stores (and the residual / activation reads) are 16 bytes per lane
 // and row-contiguous.  Work-group ids are remapped so that each XCD (own L2) gets a contiguous run of tiles.
 #include "gemm_epilogue.hpp"
+#include "gated_mlp.hpp"
 
 #include <atomic>
 #include <cmath>
@@ -147,14 +148,27 @@ __host__ __device__ __forceinline__ void nt_tile_coords(int logical, int tiles_m
 // finish puts the counters back to zero (ps_ctr[8] counts the finished ones).
 //
 // GRP (TN form): the work-groups of several weight gradients over the same K rows (grp), problem after problem.
-template <int EPI, bool TNF, bool PS, bool GRP = false, int NUA = 8>
+//
+// GLU (NT form, grp holds its operands): the gated feed-forward block's products.
+//   1  forward, EPI kEpiGlu + activation: a tile is 256 rows x 128 columns of H.  Of the 128 weight rows that a wavefront multiplies the first 64 are Wg's, the
+//      others Wu's for the same 64 columns (each wavefront fetches 64 of one matrix), so that the two halves of its accumulators are G and U of the same
+//      outputs: one even and one odd pass of the epilogue.  N is the width of H, a multiple of 64: a wavefront has all its columns or none.
+//   2  dx: the K loop runs through (A, B) and then through (A2, B2); K is the length of one of them.
+struct GluOperands {
+    const bf16_t *second_a, *second_b;              // forward: B is Wg, second_b Wu
+    const bf16_t* bu;                               // forward: bias of U (that of G is p.bias)
+    bf16_t *g, *u;                                  // forward: NULL or where G and U go
+};
+constexpr int kEpiGlu = 32;
+template <int EPI, bool TNF, bool PS, bool GRP = false, int NUA = 8, int GLU = 0>
 __global__ __launch_bounds__(256, 1) void gemm_bf16_nt_kernel(int M, int N, int K, const bf16_t* __restrict__ A,
                                                               const bf16_t* __restrict__ B, bf16_t* __restrict__ C,
                                                               int tiles_m, int tiles_n, int splits,
                                                               int n_main, int tail_splits,
                                                               float* __restrict__ split_ws, GemmEpi p,
                                                               int ps_wgs, int* __restrict__ ps_ctr,
-                                                              std::conditional_t<GRP, TnGroup, NoGroup> grp) {
+                                                              std::conditional_t<GRP, TnGroup, std::conditional_t<GLU != 0, GluOperands, NoGroup>> grp) {
+    static_assert(GLU == 0 || !(TNF || GRP), "the gated block: NT");
     static_assert(!(PS && TNF), "the persistent form exists for the NT kernel only");
     static_assert(!GRP || (TNF && EPI == DS_EPI_ACC32), "groups are of weight gradients");
     static_assert(NUA == 8 || !(TNF || PS), "lower tiles: NT, one round");
@@ -221,7 +235,7 @@ __global__ __launch_bounds__(256, 1) void gemm_bf16_nt_kernel(int M, int N, int 
     // This work-group's part of the contraction: NT whole K tiles; TN whole 32-row steps (a product's depth), k_len rows from row k_first on,
     // counted in K tiles from there.  (Divisions go through vector registers: what steers the K loop comes back to scalar ones.)
     constexpr int DEPTH = TNF ? BK / 2 : BK;
-    const int steps = TNF ? (K + DEPTH - 1) / DEPTH : K / DEPTH, per_split = (steps + nsplit - 1) / nsplit;
+    const int steps = TNF ? (K + DEPTH - 1) / DEPTH : GLU == 2 ? 2 * (K / DEPTH) : K / DEPTH, per_split = (steps + nsplit - 1) / nsplit;
     const int s_begin = split * per_split, s_end = s_begin + per_split < steps ? s_begin + per_split : steps;
     const int k_first = __builtin_amdgcn_readfirstlane(s_begin * DEPTH);
     const int k_len = __builtin_amdgcn_readfirstlane((s_end * DEPTH < K ? s_end * DEPTH : K) - s_begin * DEPTH);
@@ -233,6 +247,7 @@ __global__ __launch_bounds__(256, 1) void gemm_bf16_nt_kernel(int M, int N, int 
     const char* pa = nullptr;
     const char* pb = nullptr;
     uint32_t len_a = 0;                             // NT: length of A's rows from m0 on
+    [[maybe_unused]] uint32_t len_b = 0;            // GLU = 1: of this wavefront's weight rows
     auto set_tile = [&](int lg) {
         nt_tile_coords(lg, tiles_m, tiles_n, tile_m, tile_n);
         tile_m = __builtin_amdgcn_readfirstlane(tile_m);
@@ -242,7 +257,15 @@ __global__ __launch_bounds__(256, 1) void gemm_bf16_nt_kernel(int M, int N, int 
         const uint64_t bytes = (uint64_t)(uint32_t)(M - m0 < TA ? M - m0 : TA) * (uint32_t)K * 2u;
         len_a = bytes > 0xFFFFFFFFu ? 0xFFFFFFFFu : (uint32_t)bytes;
         pa = reinterpret_cast<const char*>(A) + (TNF ? ((long long)k_first * M + m0) * 2 : (long long)m0 * K * 2);
-        pb = reinterpret_cast<const char*>(B) + (TNF ? ((long long)k_first * N + n0) * 2 : (long long)n0 * K * 2);
+        if constexpr (GLU == 1) {
+            // this wavefront's 64 rows of the tile's 256, as the lane offsets count them; those past the end arrive as zeros
+            n0 = tile_n * 128;
+            const int first = n0 + (wave >> 1) * 64, left = N - first < 0 ? 0 : N - first < 64 ? N - first : 64;
+            pb = reinterpret_cast<const char*>(wave & 1 ? grp.second_b : B) + (long long)(first - wave * 64) * K * 2;
+            len_b = left ? (uint32_t)(wave * 64 + left) * (uint32_t)K * 2u : 0u;
+        } else {
+            pb = reinterpret_cast<const char*>(B) + (TNF ? ((long long)k_first * N + n0) * 2 : (long long)n0 * K * 2);
+        }
     };
     set_tile(logical);
     uint32_t offA[NUA], offB[8];
@@ -268,7 +291,13 @@ __global__ __launch_bounds__(256, 1) void gemm_bf16_nt_kernel(int M, int N, int 
             const int left = k_len - tile * BK;
             return make_raw_buffer((which ? pb : pa) + (long long)tile * BK * ld2, ((uint32_t)((left < BK ? left : BK) - 1) * ld2 + 512u) & inside);
         } else {
-            return make_raw_buffer((which ? pb : pa) + (long long)tile * (BK * 2), (which ? 0xFFFFFFFFu : len_a) & inside);
+            if constexpr (GLU == 1) return make_raw_buffer((which ? pb : pa) + (long long)tile * (BK * 2), (which ? len_b : len_a) & inside);
+            else if constexpr (GLU == 2) {
+                const long long behind = (long long)((K / BK - 1 - tile) >> 31);        // all ones in the second half
+                const long long to = which ? reinterpret_cast<const char*>(grp.second_b) - reinterpret_cast<const char*>(B)
+                                           : reinterpret_cast<const char*>(grp.second_a) - reinterpret_cast<const char*>(A);
+                return make_raw_buffer((which ? pb : pa) + (long long)tile * (BK * 2) + ((to - (long long)K * 2) & behind), (which ? 0xFFFFFFFFu : len_a) & inside);
+            } else return make_raw_buffer((which ? pb : pa) + (long long)tile * (BK * 2), (which ? 0xFFFFFFFFu : len_a) & inside);
         }
     };
     const uint32_t lds_a = lds0 + (uint32_t)wave * (NUA * 1024), lds_b = lds0 + (uint32_t)wave * 8192;
@@ -329,9 +358,16 @@ __global__ __launch_bounds__(256, 1) void gemm_bf16_nt_kernel(int M, int N, int 
     const bool direct = !tail && splits == 1;      // this work-group applies the epilogue itself
     // The bias is the last term of every sum, as in the kernels with smaller tiles and for split contractions: a row does not depend on
     // the tile that takes it.  (It can't be the first: 1 + 2^24 - 2^24.)
-    constexpr bool BIAS = EPI == DS_EPI_NONE || EPI == DS_EPI_GELU || EPI == DS_EPI_RESID || EPI == DS_EPI_GELU_D;
+    constexpr bool BIAS = EPI == DS_EPI_NONE || EPI == DS_EPI_GELU || EPI == DS_EPI_RESID || EPI == DS_EPI_GELU_D || GLU == 1;
     bf16x8_t bias[2];                               // of the columns this lane finishes in the epilogue; none: zeros
     auto load_bias = [&]() {
+        if constexpr (GLU == 1) {
+            const int first = n0 + wn * 64;
+            const bool on = direct && first < N;
+            buffer_load16(make_buffer(reinterpret_cast<const bf16_t*>(p.bias) + first, on && p.bias ? 128u : 0u), (uint32_t)(lane & 7) * 16, bias[0]);
+            buffer_load16(make_buffer(grp.bu + first, on && grp.bu ? 128u : 0u), (uint32_t)(lane & 7) * 16, bias[1]);
+            return;
+        }
         const auto b = make_buffer(reinterpret_cast<const bf16_t*>(p.bias) + n0 + wn * 128, direct && p.bias ? 256u : 0u);
 #pragma unroll
         for (int h = 0; h < 2; ++h) buffer_load16(b, (uint32_t)(lane & 7) * 16 + h * 128, bias[h]);
@@ -353,7 +389,7 @@ __global__ __launch_bounds__(256, 1) void gemm_bf16_nt_kernel(int M, int N, int 
                 next_local = (ps_wgs >> 3) + __hip_atomic_fetch_add(ps_ctr + (blockIdx.x & 7), 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         }
         // the first K tile is there: behind its transfers came those of the second one and, persistent, at least the previous tile's stores
-        constexpr int BEHIND = 16 + 32 * (epilogue_second<EPI>() || EPI == DS_EPI_ACC32 ? 2 : 1);
+        constexpr int BEHIND = GLU == 1 ? 32 : 16 + 32 * (epilogue_second<EPI>() || EPI == DS_EPI_ACC32 ? 2 : 1);
         if (PS && primed) __builtin_amdgcn_s_waitcnt(vmcnt_imm(BEHIND < 63 ? BEHIND : 63));
         else __builtin_amdgcn_s_waitcnt(vmcnt_imm(NUA + 8));
         __builtin_amdgcn_s_barrier();
@@ -393,7 +429,7 @@ __global__ __launch_bounds__(256, 1) void gemm_bf16_nt_kernel(int M, int N, int 
         // floats, 16-byte chunk c of row r at c ^ r.  Pass s takes columns 64 (s % 2) .. of rows 16 (s / 2) ..; a lane finishes rows
         // lane / 8 and lane / 8 + 8 of it (g = 0, 1), 8 columns each.
         constexpr int NP = 2 * NUA;                     // passes
-        const int em0 = m0 + wm * WA, en0 = n0 + wn * 128, etile_m = tile_m, elogical = logical;
+        const int em0 = m0 + wm * WA, en0 = n0 + wn * (GLU == 1 ? 64 : 128), etile_m = tile_m, elogical = logical;
         int elane = lane;                              // (opaque, so that no address of the epilogue is kept in registers over the K loop)
         asm volatile("" : "+v"(elane));
         const int rd_row = elane >> 3, rd_col = (elane & 7) * 8, wr_row = elane & 15, wr_col = elane >> 4;
@@ -406,14 +442,14 @@ __global__ __launch_bounds__(256, 1) void gemm_bf16_nt_kernel(int M, int N, int 
             return make_buffer(reinterpret_cast<const char*>(tensor) + ((size_t)em0 * N + en0) * es, on ? (uint32_t)row_cnt * (uint32_t)N * es : 0u);
         };
         const uint32_t lane_off = (uint32_t)rd_row * (uint32_t)N + rd_col;       // elements
-        auto at = [&](int s, int g, int es) { return (lane_off + (uint32_t)((s >> 1) * 16 + g * 8) * (uint32_t)N + (s & 1) * 64) * es; };
+        auto at = [&](int s, int g, int es) { return (lane_off + (uint32_t)((s >> 1) * 16 + g * 8) * (uint32_t)N + (GLU == 1 ? 0 : (s & 1) * 64)) * es; };
         // What the epilogue reads from memory: PRE passes ahead, the first ones before the next tile's transfers
         constexpr bool READS = epilogue_reads<EPI>(), READS2 = EPI == DS_EPI_DGATE, OLD = EPI == DS_EPI_ACC32;
         constexpr int PRE = READS2 || OLD ? 4 : 8;
         EpiPre<bf16_t> pre[PRE][2];
         f32x4_t old[PRE][2][2];                       // accumulation: what is added to
         const buffer_t in_r = rows(READS ? p.R : C, 2, READS && direct), in_r2 = rows(READS2 ? p.R2 : C, 2, READS2 && direct);
-        const buffer_t in_valid = make_buffer(p.row_valid + em0, EPI == DS_EPI_RESID && direct && p.row_valid ? row_cnt * 4u : 0u);
+        const buffer_t in_valid = make_buffer(p.row_valid + em0, (EPI == DS_EPI_RESID || GLU == 1) && direct && p.row_valid ? row_cnt * 4u : 0u);
         const buffer_t in_old = rows(C, 4, OLD && direct && p.accumulate);
         auto prefetch_pass = [&](int s) {
 #pragma unroll
@@ -567,6 +603,29 @@ __global__ __launch_bounds__(256, 1) void gemm_bf16_nt_kernel(int M, int N, int 
                 const uint32_t o = off + ((s >> 1) * 16 + g * 8) * ld * 4 + (s & 1) * 256;
                 buffer_store16(f32x4_t{v[0], v[1], v[2], v[3]}, out, o);
                 buffer_store16(f32x4_t{v[4], v[5], v[6], v[7]}, out, o + 16);
+            }, [](int) {});
+        } else if constexpr (GLU == 1) {
+            // an even pass brings 64 columns of G, the odd one behind it those of U for the same rows
+            const bool on = en0 < N;
+            const buffer_t out = rows(C, 2, on), out_g = rows(grp.g, 2, on && grp.g), out_u = rows(grp.u, 2, on && grp.u);
+            float gate[2][8];
+            passes(no, [&](int s, int g, float (&v)[8]) {
+                const int valid = buffer_load4(in_valid, (uint32_t)((s >> 1) * 16 + g * 8 + rd_row) * 4);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = valid < 0 ? 0.f : v[j] + column[s & 1][j];
+                if (!(s & 1)) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) gate[g][j] = v[j];
+                    return;
+                }
+                float h[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) h[j] = glu_act<EPI - kEpiGlu>(gate[g][j]) * v[j];
+                buffer_store16_nt(pack8<bf16_t>(h), out, at(s, g, 2));
+                if (grp.g) {
+                    buffer_store16_nt(pack8<bf16_t>(gate[g]), out_g, at(s, g, 2));
+                    buffer_store16_nt(pack8<bf16_t>(v), out_u, at(s, g, 2));
+                }
             }, [](int) {});
         } else {
             constexpr bool LONG = EPI == DS_EPI_GELU || EPI == DS_EPI_GELU_D || EPI == DS_EPI_DGELU || EPI == DS_EPI_GATE || EPI == DS_EPI_DGATE;
@@ -876,6 +935,84 @@ ds_status launch_nt(int M, int N, int K, const void* A, const void* B, void* C, 
     return DS_OK;
 }
 
+// Forward of the gated block: sums the tail tiles' partial products and finishes them, 8 columns of H to a thread
+template <int EPI>
+__global__ __launch_bounds__(256) void glu_tail_finish_kernel(int M, int N, int tiles_m, int tiles_n, int n_main, int tail_splits, const float* __restrict__ ws, bf16_t* __restrict__ C,
+                                                              GemmEpi p, GluOperands o) {
+    const int tile = blockIdx.y;
+    int tile_m, tile_n;
+    nt_tile_coords(n_main + tile, tiles_m, tiles_n, tile_m, tile_n);
+    const float* base = ws + (size_t)tile * tail_splits * (BM * BN);
+    for (int i = blockIdx.x * blockDim.x + threadIdx.x; i < BM * 16; i += gridDim.x * blockDim.x) {
+        const int r = i >> 4, c = (i & 15) * 8, m = tile_m * BM + r, n = tile_n * 128 + c;
+        if (m >= M || n >= N) continue;
+        const float* from = base + (size_t)r * BN + (c >> 6) * 128 + (c & 63);
+        float g[8], u[8], b[8], h[8];
+        Vec8<float>::load(from, g);
+        Vec8<float>::load(from + 64, u);
+        for (int sp = 1; sp < tail_splits; ++sp) {
+            float w[8];
+            Vec8<float>::load(from + (size_t)sp * (BM * BN), w);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) g[j] += w[j];
+            Vec8<float>::load(from + (size_t)sp * (BM * BN) + 64, w);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) u[j] += w[j];
+        }
+        auto add = [&](const void* bias, float (&v)[8]) {
+            if (!bias) return;
+            Vec8<bf16_t>::load(reinterpret_cast<const bf16_t*>(bias) + n, b);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] += b[j];
+        };
+        add(p.bias, g);
+        add(o.bu, u);
+        if (p.row_valid && p.row_valid[m] < 0)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) g[j] = u[j] = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) h[j] = glu_act<EPI - kEpiGlu>(g[j]) * u[j];
+        const size_t to = (size_t)m * N + n;
+        Vec8<bf16_t>::store(C + to, h);
+        if (o.g) {
+            Vec8<bf16_t>::store(o.g + to, g);
+            Vec8<bf16_t>::store(o.u + to, u);
+        }
+    }
+}
+
+// The gated block's products with 256 x 256 tiles: launch_nt with a tile's columns counted as the kernel counts them
+template <int EPI, int GLU>
+ds_status launch_glu(int M, int N, int K, const void* A, const void* B, void* C, const GemmEpi& p, const GluOperands& o, float* split_ws, size_t split_ws_floats,
+                     hipStream_t st) {
+    static bool attr_set = false;
+    auto kern = gemm_bf16_nt_kernel<EPI, false, false, false, 8, GLU>;
+    auto kern_ps = gemm_bf16_nt_kernel<EPI, false, true, false, 8, GLU>;
+    if (!attr_set) {
+        DS_HIP_CHECK(hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, RING));
+        DS_HIP_CHECK(hipFuncSetAttribute(reinterpret_cast<const void*>(kern_ps), hipFuncAttributeMaxDynamicSharedMemorySize, RING));
+        attr_set = true;
+    }
+    const BigPlan plan = plan_big(false, EPI, M, GLU == 1 ? (N + 127) / 128 * BN : N, GLU == 2 ? 2 * K : K, split_ws ? split_ws_floats : 0);
+    const int tiles = plan.tiles_m * plan.tiles_n, n_cu = gemm_cu_count();
+    int* ctr = nt_persistent(plan) ? ps_counters() : nullptr;
+    if (ctr)
+        hipLaunchKernelGGL(kern_ps, dim3(n_cu + (tiles - plan.n_main) * plan.tail_splits), dim3(256), RING, st, M, N, K, (const bf16_t*)A, (const bf16_t*)B, (bf16_t*)C, plan.tiles_m,
+                           plan.tiles_n, 1, plan.n_main, plan.tail_splits, split_ws, p, n_cu, ctr, o);
+    else
+        hipLaunchKernelGGL(kern, dim3(plan.n_main + (tiles - plan.n_main) * plan.tail_splits), dim3(256), RING, st, M, N, K, (const bf16_t*)A, (const bf16_t*)B, (bf16_t*)C, plan.tiles_m,
+                           plan.tiles_n, 1, plan.n_main, plan.tail_splits, split_ws, p, 0, (int*)nullptr, o);
+    DS_LAUNCH_CHECK();
+    if (plan.tail_splits == 1) return DS_OK;
+    const dim3 finish(8, tiles - plan.n_main);
+    if constexpr (GLU == 1)
+        hipLaunchKernelGGL(glu_tail_finish_kernel<EPI>, finish, dim3(256), 0, st, M, N, plan.tiles_m, plan.tiles_n, plan.n_main, plan.tail_splits, split_ws, (bf16_t*)C, p, o);
+    else
+        hipLaunchKernelGGL(tail_finish_kernel<EPI>, finish, dim3(256), 0, st, M, N, plan.tiles_m, plan.tiles_n, plan.n_main, plan.tail_splits, split_ws, (bf16_t*)C, p);
+    DS_LAUNCH_CHECK();
+    return DS_OK;
+}
+
 // NT, every tile unsplit, tiles of 32 NUA rows
 template <int EPI, int NUA>
 ds_status launch_nt_lower(int M, int N, int K, const void* A, const void* B, void* C, const GemmEpi& p, hipStream_t st) {
@@ -1085,6 +1222,21 @@ ds_status launch_gemm(int32_t dtype, int32_t ta, int32_t tb, int32_t M, int32_t 
     }
     return DS_EINVAL;
 }
+
+ds_status glu_fwd_big(const GluArgs& a, float* ws, size_t ws_floats, hipStream_t st) {
+    return glu_by_act(a.act, [&](auto act) -> ds_status {
+        GemmEpi p{};
+        p.bias = a.bg;
+        p.row_valid = a.row_valid;
+        const GluOperands o = {nullptr, (const bf16_t*)a.wu, (const bf16_t*)a.bu, (bf16_t*)a.g, (bf16_t*)a.u};
+        return launch_glu<kEpiGlu + decltype(act)::value, 1>(a.rows, a.ff, a.d, a.x, a.wg, a.h, p, o, ws, ws_floats, st);
+    });
+}
+ds_status glu_dx_big(const GluArgs& a, float* ws, size_t ws_floats, hipStream_t st) {
+    const GluOperands o = {(const bf16_t*)a.du, (const bf16_t*)a.wu, nullptr, nullptr, nullptr};
+    return launch_glu<DS_EPI_NONE, 2>(a.rows, a.d, a.ff, a.dg, a.wg, a.dx, GemmEpi{}, o, ws, ws_floats, st);
+}
+double glu_big_cost(int M, int columns, int K, size_t ws_floats) { return big_cost(plan_big(false, DS_EPI_NONE, M, columns, K, ws_floats), false, M, columns); }
 
 // adds up the partial sums of a group's tiles; kFinishParts work-groups per tile, tiles counted over the whole group
 constexpr int kFinishParts = 8;
