@@ -14,6 +14,8 @@ struct GluArgs {
     void *h, *g, *u;                                    // g, u: both or neither
     const void *dg, *du;                                // backward: the operands of dx
     void* dx;
+    int32_t splits;                                     // dx: pieces of the contraction, and where their sums go
+    float* part;
 };
 
 // The activation of z and its derivative.  DS_ACT_RELU's at 0 is 0.
@@ -46,7 +48,7 @@ ds_status glu_fwd_general(const GluArgs& a, hipStream_t st);
 ds_status glu_dx_general(const GluArgs& a, hipStream_t st);
 // bf16 on the matrix cores (gated_mlp_mfma.hip), any size: 128 x 128 tiles; few rows; weight gradients with 2 splits [d][d_ff] floats of workspace if splits > 1
 ds_status glu_fwd_tile(const GluArgs& a, hipStream_t st);
-ds_status glu_dx_tile(const GluArgs& a, hipStream_t st);
+ds_status glu_dx_tile(const GluArgs& a, int splits, float* workspace, hipStream_t st);      // splits > 1: as many [rows][d] floats of workspace
 constexpr int kGluFewRows = 64;
 ds_status glu_fwd_few(const GluArgs& a, hipStream_t st);
 struct GluWgrad {

@@ -53,12 +53,30 @@ ds_status check(int32_t dtype, int32_t rows, int32_t d, int32_t ff, std::initial
     if (workspace_floats < 0 || (workspace_floats > 0 && (!workspace || ((uintptr_t)workspace & 15)))) return DS_EINVAL;
     return DS_OK;
 }
-// Whether a product goes to the 256 x 256 tiles
-bool big_takes(const GluArgs& a, bool dx, size_t ws_floats) {
-    if (a.d % 64 || a.ff % 64 || (dx && a.d % 256) || (int64_t)a.rows * std::max(a.d, a.ff) > (int64_t)1 << 40) return false;
+// Estimated microseconds of the 128 x 128 tiles: two work-groups to a compute unit, which share it; per K tile 0.93 for two, 0.55 for one alone.  Measured (warm, d x d_ff,
+// rows: estimate / measured), forward: 1024 x 2816, 512 14 / 14, 957 20 / 18, 1500 30 / 29, 4096 52 / 49, 8192 94 / 88; 2048 x 5504, 700 53 / 50, 8192 343 / 339; 256 x 1024,
+// 8192 14 / 16.
+double tile_cost(int64_t groups, int steps) {
+    const int64_t full = groups / 512, rest = groups % 512;
+    return 4 + full * (0.93 * steps + 1.2) + (rest == 0 ? 0 : rest <= 256 ? 0.55 * steps + 1.2 : 0.9 * steps + 1.2);
+}
+// How a product goes: 256 x 256 tiles, or 128 x 128 with the contraction of dx in `splits` pieces.  Both sides by their estimates (that of the large tiles: gemm.hip);
+// measured, large / small: forward 1024 x 2816, 957 rows 33 / 18 us, 4096 61 / 49, 16 384 180 / 187, 40 000 408 / 459; 2048 x 5504, 512 44 / 31, 957 47 / 51, 8192 288 / 339.
+struct GluChoice { bool big; int splits; };
+GluChoice choose(const GluArgs& a, bool dx, size_t ws_floats) {
+    GluChoice c = {false, 1};
+    const int64_t groups = (int64_t)((a.rows + 127) / 128) * (dx ? (a.d + 127) / 128 : (a.ff + 63) / 64);
+    const int steps = dx ? 2 * ((a.ff + 63) / 64) : (a.d + 63) / 64;
+    double cost = tile_cost(groups, steps);
+    if (dx)
+        for (int s = 2; s <= 16 && groups * s <= 512 && steps / s >= 4 && (size_t)s * a.rows * a.d <= ws_floats; ++s) {
+            const double split = tile_cost(groups * s, (steps + s - 1) / s) + 4 + 1e-6 * s * a.rows * a.d;
+            if (split < 0.95 * cost) cost = split, c.splits = s;
+        }
+    if (a.d % 64 || a.ff % 64 || (dx && a.d % 256)) return c;
     const int columns = dx ? a.d : (a.ff + 127) / 128 * 256, K = dx ? 2 * a.ff : a.d;
-    if (const char* e = getenv("GLU_BIG")) return e[0] == '1';
-    return (int64_t)((a.rows + 255) / 256) * (columns / 256) >= gemm_cu_count();
+    c.big = glu_big_cost(a.rows, columns, K, ws_floats) < cost;
+    return c;
 }
 bool known_act(int32_t act) { return act == DS_ACT_GELU || act == DS_ACT_SILU || act == DS_ACT_RELU; }
 
@@ -67,6 +85,15 @@ bool known_act(int32_t act) { return act == DS_ACT_GELU || act == DS_ACT_SILU ||
 extern "C" int64_t ds_gated_mlp_workspace_floats(int32_t rows, int32_t d, int32_t d_ff) {
     if (rows <= 0 || d <= 0 || d_ff <= 0) return 0;
     return std::max((int64_t)1 << 24, kSumFloats * d_ff);
+}
+
+// For tests: what `choose` says of a bf16 call with more than kGluFewRows rows: 256 x 256 tiles, pieces of the contraction.  Not part of the C ABI's header.
+extern "C" void ds_gated_mlp_choice(int32_t rows, int32_t d, int32_t d_ff, int32_t dx, int64_t workspace_floats, int32_t* out) {
+    GluArgs a = {};
+    a.rows = rows; a.d = d; a.ff = d_ff;
+    const GluChoice c = choose(a, dx != 0, (size_t)workspace_floats);
+    out[0] = c.big;
+    out[1] = c.splits;
 }
 
 extern "C" ds_status ds_gated_mlp_fwd(int32_t dtype, int32_t act, int32_t rows, int32_t d, int32_t d_ff, const void* x, const void* wg, const void* wu, const void* bg,
@@ -82,7 +109,7 @@ extern "C" ds_status ds_gated_mlp_fwd(int32_t dtype, int32_t act, int32_t rows, 
     if (dtype == DS_DTYPE_F32 || force_generic) return glu_fwd_general(a, (hipStream_t)hip_stream);
     if (rows <= kGluFewRows) return glu_fwd_few(a, (hipStream_t)hip_stream);
     const size_t floats = workspace_floats > 0 ? (size_t)workspace_floats : 0;
-    if (big_takes(a, false, floats)) return glu_fwd_big(a, workspace, floats, (hipStream_t)hip_stream);
+    if (choose(a, false, floats).big) return glu_fwd_big(a, workspace, floats, (hipStream_t)hip_stream);
     return glu_fwd_tile(a, (hipStream_t)hip_stream);
 }
 
@@ -101,7 +128,8 @@ extern "C" ds_status ds_gated_mlp_bwd(int32_t dtype, int32_t act, int32_t rows, 
     if (r != DS_OK) return r;
     if (dtype == DS_DTYPE_F32 || force_generic) return glu_dx_general(a, st);
     const size_t floats = workspace_floats > 0 ? (size_t)workspace_floats : 0;
-    return big_takes(a, true, floats) ? glu_dx_big(a, workspace, floats, st) : glu_dx_tile(a, st);
+    const GluChoice c = choose(a, true, floats);
+    return c.big ? glu_dx_big(a, workspace, floats, st) : glu_dx_tile(a, c.splits, workspace, st);
 }
 
 extern "C" ds_status ds_gated_mlp_wgrad(int32_t dtype, int32_t rows, int32_t d, int32_t d_ff, const void* x, const void* dg, const void* du, float* dwg, float* dwu, float* dbg,

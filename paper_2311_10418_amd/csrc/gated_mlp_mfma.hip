@@ -79,6 +79,8 @@ template <int ACT> __global__ __launch_bounds__(256, 2) void glu_tile_kernel(Glu
     const int logical = xcd_contiguous(blockIdx.x, gridDim.x), group = logical / (8 * tiles_n), in = logical - group * 8 * tiles_n, deep = min(8, tiles_m - 8 * group);
     const int m0 = __builtin_amdgcn_readfirstlane((8 * group + in % deep) * 128), n0 = __builtin_amdgcn_readfirstlane(in / deep * (FWD ? 64 : 128));
     const int K = FWD ? a.d : a.ff, N = FWD ? a.ff : a.d, steps = (K + TK - 1) / TK, all = FWD ? steps : 2 * steps;
+    // dx: this work-group's piece of the contraction
+    const int per = FWD ? all : (all + a.splits - 1) / a.splits, begin = FWD ? 0 : min((int)blockIdx.y * per, all), end = FWD ? all : min(begin + per, all);
     const uint32_t lds0 = lds_address(smem);
     RowLoader la[FWD ? 1 : 2], lb[FWD ? 1 : 2];
     if constexpr (FWD) {
@@ -107,10 +109,10 @@ template <int ACT> __global__ __launch_bounds__(256, 2) void glu_tile_kernel(Glu
 #pragma unroll
         for (int j = 0; j < 4; ++j) acc[i][j] = zero4();
     const int at[2] = {fr * 128 + ((fg ^ ((fr >> 1) & 7)) << 4), fr * 128 + (((4 + fg) ^ ((fr >> 1) & 7)) << 4)};
-    issue(0);
-    for (int step = 0; step < all; ++step) {
+    if (begin < end) issue(begin);
+    for (int step = begin; step < end; ++step) {
         wait_and_sync();
-        if (step + 1 < all) issue(step + 1);
+        if (step + 1 < end) issue(step + 1);
         const char *ta = smem + (step & 1) * STAGE + wm * 8192, *tb = smem + (step & 1) * STAGE + TILE + wn * 8192;
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
@@ -152,6 +154,8 @@ template <int ACT> __global__ __launch_bounds__(256, 2) void glu_tile_kernel(Glu
                     put4((bf16_t*)a.g + to, v);
                     put4((bf16_t*)a.u + to, u);
                 }
+            } else if (a.splits > 1) {
+                *reinterpret_cast<f32x4_t*>(a.part + (size_t)blockIdx.y * a.rows * a.d + to) = v;
             } else {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) v[e] = valid ? v[e] : 0.f;
@@ -319,7 +323,7 @@ template <int ACT> ds_status tile_launch(const GluArgs& a, hipStream_t st) {
     const ds_status r = allow_lds(kern, attr);
     if (r != DS_OK) return r;
     const int tiles_m = (a.rows + 127) / 128, tiles_n = ACT >= 0 ? (a.ff + 63) / 64 : (a.d + 127) / 128;
-    hipLaunchKernelGGL(kern, dim3((unsigned)tiles_m * tiles_n), dim3(256), 2 * STAGE, st, a, tiles_m, tiles_n);
+    hipLaunchKernelGGL(kern, dim3((unsigned)tiles_m * tiles_n, ACT >= 0 ? 1 : a.splits), dim3(256), 2 * STAGE, st, a, tiles_m, tiles_n);
     DS_LAUNCH_CHECK();
     return DS_OK;
 }
@@ -329,7 +333,15 @@ template <int ACT> ds_status tile_launch(const GluArgs& a, hipStream_t st) {
 ds_status glu_fwd_tile(const GluArgs& a, hipStream_t st) {
     return glu_by_act(a.act, [&](auto act) { return tile_launch<decltype(act)::value>(a, st); });
 }
-ds_status glu_dx_tile(const GluArgs& a, hipStream_t st) { return tile_launch<-1>(a, st); }
+ds_status glu_dx_tile(const GluArgs& a0, int splits, float* workspace, hipStream_t st) {
+    GluArgs a = a0;
+    a.splits = splits;
+    a.part = workspace;
+    const ds_status r = tile_launch<-1>(a, st);
+    if (r != DS_OK || splits == 1) return r;
+    GemmEpi p{};                                        // (rows that do not count are zeros in dG and dU, and so in dx)
+    return launch_splitk_finish<bf16_t, DS_EPI_NONE>(a.rows, a.d, splits, workspace, a.dx, p, st);
+}
 
 ds_status glu_fwd_few(const GluArgs& a, hipStream_t st) {
     return glu_by_act(a.act, [&](auto act) -> ds_status {
