@@ -23,9 +23,27 @@ namespace {
 constexpr int kTablePad = 94;                           // distances that a near block (64 x 32 pairs) may reach beyond `reach`
 constexpr int kAllLds = 160 * 1024;
 __host__ __device__ constexpr int table_floats(int reach) { return (2 * (reach + kTablePad) + 1 + 3) & ~3; }
-__device__ __forceinline__ void fill_table(const RelAttnArgs& a, int h, float* table) {
-    for (int i = threadIdx.x; i < 2 * (a.reach + kTablePad) + 1; i += 256) table[i] = rel_bias(a, h, i - kTablePad);
-}
+// The table of a head, in three parts, so that its two trips to memory (the buckets, then their biases) go beside those that a work-group begins with anyway (its
+// item, then its tables).  The last entries of a long reach are made in the end.
+struct TableFill {
+    int bucket[2];
+    float bias[2];
+    static __device__ __forceinline__ int entries(const RelAttnArgs& a) { return 2 * (a.reach + kTablePad) + 1; }
+    __device__ __forceinline__ void buckets(const RelAttnArgs& a) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) bucket[i] = a.bucket[min(max((int)threadIdx.x + 256 * i - kTablePad, 0), 2 * a.reach)];
+    }
+    __device__ __forceinline__ void biases(const RelAttnArgs& a, int h) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) bias[i] = kLog2e * (float)((const bf16_t*)a.bias)[(size_t)min(max(bucket[i], 0), a.n_buckets - 1) * a.n_heads + h];
+    }
+    __device__ __forceinline__ void store(const RelAttnArgs& a, int h, float* table) const {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            if ((int)threadIdx.x + 256 * i < entries(a)) table[threadIdx.x + 256 * i] = bias[i];
+        for (int i = threadIdx.x + 512; i < entries(a); i += 256) table[i] = rel_bias(a, h, i - kTablePad);
+    }
+};
 template <int HD> __device__ __forceinline__ void store_cols_f32(const f32x16_t (&acc)[HD / 32], float* __restrict__ out_row, int g) {
 #pragma unroll
     for (int dt = 0; dt < HD / 32; ++dt)
@@ -77,6 +95,8 @@ __global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void rel_fwd_mfma_kernel(Rel
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 31, g = lane >> 5;
+    TableFill fill;
+    fill.buckets(a);
     int item = blockIdx.x / a.n_heads;
     const int h = blockIdx.x - item * a.n_heads, split = a.k_splits > 1 ? item % a.k_splits : 0;
     int2 it;
@@ -89,6 +109,7 @@ __global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void rel_fwd_mfma_kernel(Rel
     const int s = __builtin_amdgcn_readfirstlane(it.x), q0 = __builtin_amdgcn_readfirstlane(it.y) * 128;
     const int ql = __builtin_amdgcn_readfirstlane(a.q_len[s]), pos0 = __builtin_amdgcn_readfirstlane(rel_position(a, s));
     if (q0 >= ql) return;
+    fill.biases(a, h);
     int kl = rel_keys(a, __builtin_amdgcn_readfirstlane(a.k_len[s]), ql, pos0), kfirst = 0;
     if (a.k_splits > 1) {                               // keys kfirst .. kfirst + kl - 1: whole tiles, as evenly as they go
         const long long run = ((long long)kl + 64LL * a.k_splits - 1) / (64LL * a.k_splits) * 64;
@@ -134,9 +155,9 @@ __global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void rel_fwd_mfma_kernel(Rel
         ldV.issue(lds0 + TILE, 0);
     }
     float* table = reinterpret_cast<float*>(smem + 4 * TILE);
-    fill_table(a, h, table);
+    fill.store(a, h, table);
     __syncthreads();
-    const float flat_behind = rel_bias(a, h, 0), flat_front = rel_bias(a, h, 2 * a.reach);
+    const float flat_behind = table[0], flat_front = table[2 * (a.reach + kTablePad)];
     for (int b = 0; b < nb; ++b) {
         const int kv0 = b * 64;
         char* sK = smem + (b & 1) * (2 * TILE);
@@ -284,6 +305,8 @@ __global__ __launch_bounds__(256, 2) void rel_bwd_dq_mfma_kernel(RelAttnArgs a) 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 31, g = lane >> 5;
+    TableFill fill;
+    fill.buckets(a);
     const int item = blockIdx.x / a.n_heads, h = blockIdx.x - item * a.n_heads;
     int2 it;
     if (a.direct) {
@@ -301,6 +324,7 @@ __global__ __launch_bounds__(256, 2) void rel_bwd_dq_mfma_kernel(RelAttnArgs a) 
         for (int i = tid; i <= 2 * a.reach; i += 256) slot[i] = 0.f;
         return;
     }
+    fill.biases(a, h);
     const int kl = rel_keys(a, __builtin_amdgcn_readfirstlane(a.k_len[s]), ql, pos);
     const long long qrow0 = a.q_row[s];
     const bf16_t* Q = (const bf16_t*)a.q + qrow0 * a.ldq + h * HD;
@@ -356,12 +380,12 @@ __global__ __launch_bounds__(256, 2) void rel_bwd_dq_mfma_kernel(RelAttnArgs a) 
 #pragma unroll
         for (int e = 0; e < 16; ++e) gacc[dt][e] = 0.f;
 
-    fill_table(a, h, table);
+    fill.store(a, h, table);
     for (int i = tid; i < 8 * wide; i += 256) table[wide + i] = 0.f;
     __syncthreads();
     // sums of dS by distance: two arrays for each wavefront, since the distances of its lane halves, rows 4 apart, overlap
     float* const sums = table + wide * (1 + 2 * wave + g);
-    const float flat_behind = rel_bias(a, h, 0), flat_front = rel_bias(a, h, 2 * a.reach);
+    const float flat_behind = table[0], flat_front = table[2 * (a.reach + kTablePad)];
     float beyond_behind = 0.f, beyond_front = 0.f, carry = 0.f;
     float* to = sums;                                   // (where `carry` belongs: 32 on)
     const int wave_last = CAUSAL ? min(kl - 1, pw0 + 31) : kl - 1;
@@ -559,8 +583,10 @@ __global__ __launch_bounds__(256, HD == 64 ? 2 : 1) void rel_bwd_dkv_mfma_kernel
             lds_dma16_at(aug_src + (size_t)r * 16, n + 2 * TILE + wave * 1024);
         }
     };
+    TableFill fill;
     // take up the item `draw` stands at: its tables, the first three blocks, the K / V fragments
     auto begin_item = [&] {
+        fill.buckets(a);
         const int item = draw.index() / a.n_heads;
         h = draw.index() - item * a.n_heads;
         const int2 it = a.direct ? make_int2(a.n_seq - 1 - item, 0) : a.items_k[item];
@@ -569,6 +595,7 @@ __global__ __launch_bounds__(256, HD == 64 ? 2 : 1) void rel_bwd_dkv_mfma_kernel
         pos = __builtin_amdgcn_readfirstlane(rel_position(a, s));
         ql = __builtin_amdgcn_readfirstlane(a.q_len[s]);
         kl = __builtin_amdgcn_readfirstlane(a.k_len[s]);
+        fill.biases(a, h);
         const long long qrow0 = __builtin_amdgcn_readfirstlane(a.q_row[s]);
         krow0 = __builtin_amdgcn_readfirstlane(a.k_row[s]);
         kw0 = k0 + wave * 32;
@@ -620,11 +647,11 @@ __global__ __launch_bounds__(256, HD == 64 ? 2 : 1) void rel_bwd_dkv_mfma_kernel
     int next = 0;
     if (PS) next = draw.take();                         // (needed after the loop)
     if (h != table_head) {                              // (nobody reads the old one: a barrier ended the item before)
-        fill_table(a, h, table);
+        fill.store(a, h, table);
         __syncthreads();
         table_head = h;
     }
-    const float flat_behind = rel_bias(a, h, 0), flat_front = rel_bias(a, h, 2 * a.reach);
+    const float flat_behind = table[0], flat_front = table[2 * (a.reach + kTablePad)];
     // the K / V fragments (ordinary loads) and the stores of the item before are complete before the loop: left to the
     // compiler, its waits for them would sit inside the loop as "nothing outstanding", which would also drain the
     // transfers in flight.  So are the zeros of s_zero, in front of the first step's barrier.
