@@ -739,9 +739,8 @@ def _rel_tensors(torch, dev, q, k, v, bias, bucket, lse, q_row, q_len, k_row, k_
     sizes = (q_rows, k_rows, qkv[1], qkv[3], qkv[5], max_q_len, max_k_len, buckets)
     if max(sizes) > 0x7fffffff:
         _too_large(*sizes)
-    need = ds_rel_attention_scratch_bytes(n_heads, head_dim, reach, q_rows, k_rows, n)
     return n, tables, qkv, _tensor(lse, "lse", (n_heads, q_rows), torch.float32, dev), \
-        (q_rows, k_rows, _tensor(scratch, "scratch", need, torch.uint8, dev), scratch.numel())
+        (q_rows, k_rows, _tensor(scratch, "scratch", 0, torch.uint8, dev), scratch.numel())          # (its size is checked behind the call)
 
 
 def ds_rel_attention_fwd(q, k, v, bias, bucket, o, lse, q_row, q_len, k_row, k_len, n_heads, head_dim, causal, max_q_len, max_k_len, scratch, scale=None,

@@ -27,7 +27,7 @@ struct RelAttnArgs : AttnArgs {
     float* slots;                                       // sums of dS by distance, [block of queries][n_heads][2 reach + 1]
     float* split_part;                                  // see RelPart
     char* aug;                                          // matrix-core kernels: what the dQ kernel hands to the dK/dV kernel
-    int32_t direct;                                     // matrix-core kernels: sequences have one block of 128 rows, and work-groups go by sequence and head without a list
+    int32_t direct, direct_k;                           // matrix-core kernels: blocks of 128 queries / keys that a sequence may have, and work-groups go by them; 0: by a list
     int32_t first_group, groups;                        // dK/dV grid: work-groups in front that sum up dbias, work-groups behind them
 };
 
@@ -73,10 +73,13 @@ template <int R> __device__ __forceinline__ void add_diagonals(float x, float& m
     if constexpr (R != 0) around += lanes_below<16 - R>(x);
 }
 
-// blocks of `cols` queries of all sequences before s: slots are numbered by sequence
-template <int COLS, int THREADS> __device__ __forceinline__ int blocks_before(const RelAttnArgs& a, int s, int* lds) {
+// blocks of `cols` queries of all sequences before s (slots are numbered by sequence): this thread's part, and the sum of all
+template <int COLS, int THREADS> __device__ __forceinline__ int blocks_part(const RelAttnArgs& a, int s) {
     int n = 0;
     for (int i = threadIdx.x; i < s; i += THREADS) n += max(a.q_len[i] + COLS - 1, 0) / COLS;
+    return n;
+}
+template <int THREADS> __device__ __forceinline__ int blocks_sum(int n, int* lds) {
 #pragma unroll
     for (int m = 32; m >= 1; m >>= 1) n += __shfl_xor(n, m, 64);
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = n;
@@ -127,3 +130,12 @@ ds_status rel_bwd_general(const RelAttnArgs& a, hipStream_t st);
 bool rel_mfma_supported(const RelAttnArgs& a);
 ds_status rel_fwd_mfma(const RelAttnArgs& a, hipStream_t st);
 ds_status rel_bwd_mfma(const RelAttnArgs& a, hipStream_t st);
+// one query to a sequence, rows of 16-byte pieces (rel_attention_few.hip); keys that a work-group takes at a time
+bool rel_few_supported(const RelAttnArgs& a);
+ds_status rel_fwd_few(const RelAttnArgs& a, hipStream_t st);
+constexpr int rel_few_lanes(int32_t dtype, int head_dim) {                  // lanes that hold a row: a power of two
+    int n = 4;
+    while (n * (dtype == DS_DTYPE_BF16 ? 8 : 4) < head_dim) n *= 2;
+    return n;
+}
+constexpr int rel_few_keys(int32_t dtype, int head_dim) { return 2048 / rel_few_lanes(dtype, head_dim); }

@@ -6,14 +6,23 @@
 constexpr int kRelReach = 1024, kRelBuckets = 1024, kRelLongest = 1 << 28;
 
 // Work-groups that share the keys of a head, for sequences of at most 64 queries in a tensor of at most 64 rows for each of them (the shares go to scratch
-// by row of that tensor, whose lengths the scratch's size does not know): as many as make one for every compute unit, of 64 keys at least, from 129 keys on; two
-// up to head size 64; at most one for a lane of the wavefront that joins them.
+// by row of that tensor, whose lengths the scratch's size does not know): from 129 keys on, 64 at least each, at most one for a lane of the wavefront that joins them;
+// matrix-core kernels as many as make two for every compute unit at head size 64, one at 128; general ones three.
+// Tokens on a cache, 16 heads, us, 1 / 2 / 3 / 4 to a compute unit: bf16, heads of 64, 16 sequences of 1 019 keys, one query  - / 19.0 / 17.6 / 20.9, of 16 384  - / 206 / 213 / 266,
+// one of 32 768  - / 32 / 36 / 43; heads of 128, 25.5 / 29.2 / 30.1 / 31.2, 431 / 390 / 435 / 387, 49 / 52 / 57 / 62; fp32, four queries, 1 019 keys: heads of 64  - / 41 / 36 / 44, of 128
+// 106 / 65 / 56 / 69.
 static constexpr int kSplitQueries = 64, kSplitMost = 64;
-static int most_splits(int n_heads, int head_dim, int q_total_rows, int max_k_len, int n_seq) {
+static int most_splits(bool general, int n_heads, int head_dim, int q_total_rows, int max_k_len, int n_seq) {
     const long long items = (long long)n_seq * n_heads;
     if (q_total_rows > (long long)kSplitQueries * n_seq || max_k_len < 129) return 1;
-    const long long groups = (head_dim <= 64 ? 2 : 1) * kRelUnits;
+    const long long groups = (general ? 3 : head_dim <= 64 ? 2 : 1) * kRelUnits;
     return (int)std::max(1LL, std::min({groups / items, (long long)kSplitMost, ((long long)max_k_len + 63) / 64}));
+}
+// The kernel for single queries: its work-groups take rel_few_keys keys at a time, and four of them to a compute unit wait for memory together.
+static int few_splits(int32_t dtype, int n_heads, int head_dim, int q_total_rows, int max_q_len, int max_k_len, int n_seq) {
+    if (q_total_rows > (long long)kSplitQueries * n_seq) return 1;
+    const long long items = (long long)n_seq * n_heads * max_q_len, keys = rel_few_keys(dtype, head_dim);
+    return (int)std::max(1LL, std::min({4LL * kRelUnits / items, (long long)kSplitMost, ((long long)max_k_len + keys - 1) / keys}));
 }
 
 // Scratch: the work lists of the matrix-core kernels; what the dQ kernels hand to the dK/dV kernels, 32 bytes for each query of a head (the general ones use 4 of
@@ -24,7 +33,8 @@ static size_t rel_scratch_bytes(int n_heads, int head_dim, int reach, int q_tota
     const size_t entries = (size_t)n_heads * q_total_rows;
     const size_t blocks = std::max(((size_t)q_total_rows / 64 + n_seq) * n_heads, (size_t)4 * kRelUnits);
     const size_t backward = entries * 32 + blocks * (2 * reach + 1) * 4;
-    const int splits = most_splits(n_heads, head_dim, q_total_rows, k_total_rows, n_seq);
+    const int splits = std::max(most_splits(true, n_heads, head_dim, q_total_rows, k_total_rows, n_seq),
+                                few_splits(DS_DTYPE_F32, n_heads, head_dim, q_total_rows, 1, k_total_rows, n_seq));      // (never fewer than the others)
     const size_t forward = splits > 1 ? entries * splits * (head_dim + 4) * 4 : 0;
     return lists_size(q_total_rows, k_total_rows, n_seq) + std::max(backward, forward);
 }
@@ -63,14 +73,31 @@ static ds_status check(RelAttnArgs& a) {
     return DS_OK;
 }
 
-// How a call goes to the kernels: fp32 arithmetic or bf16 matrix cores; work-groups that share a head's keys (forward); bf16: whether there is no work list
-struct RelChoice { int32_t general, k_splits, direct; };
+// Blocks of 128 rows that each of the sequences may have, if a grid of all of them is at most a quarter larger than one that goes by a list (and has no more than
+// there are slots for); otherwise 0.
+static int blocks_without_list(int max_len, int total_rows, int n_seq) {
+    const long long blocks = ((long long)max_len + 127) / 128, all = blocks * n_seq;
+    return all <= (long long)total_rows / 64 + n_seq && 4 * all <= 5 * ((long long)total_rows / 128 + n_seq) ? (int)blocks : 0;
+}
+
+// How a call goes to the kernels: fp32 arithmetic or bf16 matrix cores; work-groups that share a head's keys (forward); bf16: whether there is no work list; the
+// kernel for few queries instead (forward)
+struct RelChoice { int32_t general, k_splits, direct, few; };
 static RelChoice choose(RelAttnArgs& a, bool backward, bool force_generic) {
-    RelChoice c = {1, 1, 0};
-    if (!backward && a.max_q_len <= kSplitQueries) c.k_splits = most_splits(a.n_heads, a.head_dim, a.q_total_rows, a.max_k_len, a.n_seq);
-    a.k_splits = c.k_splits;
+    RelChoice c = {1, 1, 0, 0};
+    if (!backward && !force_generic && rel_few_supported(a) && !rel_mfma_supported(a)) {
+        c.few = 1;
+        c.k_splits = a.k_splits = few_splits(a.dtype, a.n_heads, a.head_dim, a.q_total_rows, a.max_q_len, a.max_k_len, a.n_seq);
+        return c;
+    }
     c.general = force_generic || !rel_mfma_supported(a);
-    if (!c.general) c.direct = a.max_q_len <= 128 && (!backward || a.max_k_len <= 128);
+    if (!backward && a.max_q_len <= kSplitQueries) c.k_splits = most_splits(c.general, a.n_heads, a.head_dim, a.q_total_rows, a.max_k_len, a.n_seq);
+    a.k_splits = c.k_splits;
+    if (!c.general) c.direct = blocks_without_list(a.max_q_len, a.q_total_rows, a.n_seq);
+    if (c.direct && backward) {
+        a.direct_k = blocks_without_list(a.max_k_len, a.k_total_rows, a.n_seq);
+        if (a.direct_k == 0) c.direct = 0;
+    }
     a.direct = c.direct;
     return c;
 }
@@ -97,7 +124,9 @@ extern "C" ds_status ds_rel_attention_fwd(int32_t dtype, int32_t n_seq, int32_t 
     a.scratch = scratch; a.scratch_bytes = scratch_bytes < 0 ? 0 : (size_t)scratch_bytes;
     const ds_status r = check(a);
     if (r != DS_OK) return r;
-    return choose(a, false, force_generic != 0).general ? rel_fwd_general(a, (hipStream_t)hip_stream) : rel_fwd_mfma(a, (hipStream_t)hip_stream);
+    const RelChoice c = choose(a, false, force_generic != 0);
+    if (c.few) return rel_fwd_few(a, (hipStream_t)hip_stream);
+    return c.general ? rel_fwd_general(a, (hipStream_t)hip_stream) : rel_fwd_mfma(a, (hipStream_t)hip_stream);
 }
 
 extern "C" ds_status ds_rel_attention_bwd(int32_t dtype, int32_t n_seq, int32_t n_heads, int32_t head_dim, int32_t mask, const int32_t* q_row,

@@ -132,10 +132,21 @@ template <int COLS> __device__ __forceinline__ ColumnBlock column_block(const Re
 // an odd number of blocks per grid row: work-groups go to the eight XCDs in turn, and the longest of every sequence should not meet on one
 dim3 column_grid(const RelAttnArgs& a, int max_len, int cols) { return dim3((max_len / cols + (max_len % cols != 0)) | 1, a.n_heads, a.n_seq); }
 
-// the table of a head: entry i = distance + reach + kPad
-template <int THREADS> __device__ __forceinline__ void fill_table(const RelAttnArgs& a, int h, float* table) {
-    for (int i = threadIdx.x; i < 2 * (a.reach + kPad) + 1; i += THREADS) table[i] = rel_bias(a, h, i - kPad);
-}
+// The table of a head, entry i = distance + reach + kPad, in three parts: its two trips to memory (the buckets, then their biases) go beside those that a work-group
+// begins with anyway.  The last entries of a long reach are made in the end.
+template <class T, int THREADS> struct TableFill {
+    int bucket;
+    float bias;
+    __device__ __forceinline__ void buckets(const RelAttnArgs& a) { bucket = a.bucket[min(max((int)threadIdx.x - kPad, 0), 2 * a.reach)]; }
+    __device__ __forceinline__ void biases(const RelAttnArgs& a, int h) {
+        bias = kLog2eG * to_f32(((const T*)a.bias)[(size_t)min(max(bucket, 0), a.n_buckets - 1) * a.n_heads + h]);
+    }
+    __device__ __forceinline__ void store(const RelAttnArgs& a, int h, float* table) const {
+        const int n = 2 * (a.reach + kPad) + 1;
+        if ((int)threadIdx.x < n) table[threadIdx.x] = bias;
+        for (int i = threadIdx.x + THREADS; i < n; i += THREADS) table[i] = rel_bias(a, h, i - kPad);
+    }
+};
 // Where a block of 16 rows and 16 columns lies whose distances are first .. first + 30: -1 / 1: beyond reach on one side, 0: near
 __device__ __forceinline__ int side_of(int first, int reach) { return first + 30 <= -reach ? -1 : first >= reach ? 1 : 0; }
 
@@ -149,10 +160,13 @@ __global__ __launch_bounds__(256, HD <= 64 ? 3 : 2) void rel_fwd_kernel(RelAttnA
     extern __shared__ __attribute__((aligned(16))) float lds[];
     float *const sK = lds, *const sV = lds + Tl::FLOATS, *const table = lds + 2 * Tl::FLOATS;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4;
+    TableFill<T, 256> fill;
+    fill.buckets(a);
     ColumnBlock cb = column_block<64>(a, a.q_len, a.mask != 0, blockIdx.z);
     const int split = a.k_splits > 1 ? blockIdx.x : 0;                 // (one block of queries then)
     if (a.k_splits > 1) cb.block = a.q_len[cb.s] > 0 ? 0 : -1;
     if (cb.block < 0) return;
+    fill.biases(a, cb.h);
     const int s = cb.s, h = cb.h, q0 = 64 * cb.block, ql = a.q_len[s], hd = a.head_dim, pos = rel_position(a, s);
     int kl = rel_keys(a, a.k_len[s], ql, pos), kfirst = 0;
     if (a.k_splits > 1) {                                              // keys kfirst .. kfirst + kl - 1: whole tiles of 64, as evenly as they go
@@ -180,9 +194,10 @@ __global__ __launch_bounds__(256, HD <= 64 ? 3 : 2) void rel_fwd_kernel(RelAttnA
         tk.load(K, a.ldk, 0, kl, hd, vec);
         tv.load(V, a.ldv, 0, kl, hd, vec);
     }
-    fill_table<256>(a, h, table);
+    fill.store(a, h, table);
+    __syncthreads();
     const float *const near = table + a.reach + kPad + 4 * g - pi;     // [key tile row e]: near[kb + e]
-    const float side_bias[2] = {rel_bias(a, h, 0), rel_bias(a, h, 2 * a.reach)};
+    const float side_bias[2] = {table[0], table[2 * (a.reach + kPad)]};
     for (int k0 = 0; k0 < kv_end; k0 += KT) {
         __syncthreads();                                               // the previous tile has been read by everybody
         tk.store(sK);
@@ -333,8 +348,12 @@ __global__ __launch_bounds__(512, HD <= 64 ? 4 : 2) void rel_bwd_dq_kernel(RelAt
     const int t = threadIdx.x, lane = t & 63, wave8 = __builtin_amdgcn_readfirstlane(t >> 6), g = lane >> 4;
     float *const sums = table + wide * (1 + wave8);                    // this wavefront's sums of dS by distance
     const int wave = wave8 % Share<COLS>::GROUPS, split = wave8 / Share<COLS>::GROUPS;
+    TableFill<T, 512> fill;
+    fill.buckets(a);
+    const int before = blocks_part<COLS, 512>(a, a.n_seq - 1 - blockIdx.z);
     const ColumnBlock cb = column_block<COLS>(a, a.q_len, a.mask != 0, blockIdx.z);
     if (cb.block < 0) return;
+    fill.biases(a, cb.h);
     const int s = cb.s, h = cb.h, q0 = COLS * cb.block, ql = a.q_len[s], pos = rel_position(a, s), kl = rel_keys(a, a.k_len[s], ql, pos), hd = a.head_dim;
     const bool vec = a.vec;
     const long long qrow0 = a.q_row[s], krow0 = a.k_row[s];
@@ -362,11 +381,11 @@ __global__ __launch_bounds__(512, HD <= 64 ? 4 : 2) void rel_bwd_dq_kernel(RelAt
         if (g == 0 && qi < ql && split == 0) a.d[(size_t)h * a.q_total_rows + row] = d;
     }
     const float e2 = rel_lse2(a.lse[(size_t)h * a.lse_stride + row]), c = a.scale * kLog2eG;
-    fill_table<512>(a, h, table);
+    fill.store(a, h, table);
     for (int i = t; i < 8 * wide; i += 512) table[wide + i] = 0.f;
-    const int slot = blocks_before<COLS, 512>(a, s, reinterpret_cast<int*>(sK)) + cb.block;
+    const int slot = blocks_sum<512>(before, reinterpret_cast<int*>(sK)) + cb.block;
     const int near = a.reach + kPad + 4 * g - pi;                      // [key tile row e]: entry near + kb + e
-    const float side_bias[2] = {rel_bias(a, h, 0), rel_bias(a, h, 2 * a.reach)};
+    const float side_bias[2] = {table[0], table[2 * (a.reach + kPad)]};
     const float live = qi < ql ? 1.f : 0.f;             // (a lane past the last query repeats the last one: its sums do not count)
     float beyond[2] = {0.f, 0.f};
     f32x4_t gacc[NS];
@@ -483,12 +502,15 @@ __global__ __launch_bounds__(512, HD <= 64 && COLS == 64 ? 4 : 2) void rel_bwd_d
     if (blockIdx.z == 0) {                              // a layer of work-groups more, which start first: one for each head sums up dbias
         if (blockIdx.x != 0) return;
         int* words = reinterpret_cast<int*>(lds);
-        const int n = slot_cols == 32 ? blocks_before<32, 512>(a, a.n_seq, words) : blocks_before<64, 512>(a, a.n_seq, words);
+        const int n = blocks_sum<512>(slot_cols == 32 ? blocks_part<32, 512>(a, a.n_seq) : blocks_part<64, 512>(a, a.n_seq), words);
         sum_dbias<512>(a, blockIdx.y, n, lds);
         return;
     }
+    TableFill<T, 512> fill;
+    fill.buckets(a);
     const ColumnBlock cb = column_block<COLS>(a, a.k_len, false, blockIdx.z - 1);
     if (cb.block < 0) return;
+    fill.biases(a, cb.h);
     const int s = cb.s, h = cb.h, k0 = COLS * cb.block, ql = a.q_len[s], kl = a.k_len[s], hd = a.head_dim, pos = rel_position(a, s);
     const bool vec = a.vec;
     const long long qrow0 = a.q_row[s], krow0 = a.k_row[s];
@@ -514,8 +536,9 @@ __global__ __launch_bounds__(512, HD <= 64 && COLS == 64 ? 4 : 2) void rel_bwd_d
     f32x4_t dk[NS], dv[NS];
 #pragma unroll
     for (int i = 0; i < NS; ++i) { dk[i] = zero4(); dv[i] = zero4(); }
-    fill_table<512>(a, h, table);
-    const float side_bias[2] = {rel_bias(a, h, 0), rel_bias(a, h, 2 * a.reach)};
+    fill.store(a, h, table);
+    __syncthreads();
+    const float side_bias[2] = {table[0], table[2 * (a.reach + kPad)]};
     const int near = a.reach + kPad + ki - pos - 4 * g;                // [query tile row e]: entry near - qb - e
     for (int q0 = q_begin; q0 < ql; q0 += QT) {
         __syncthreads();

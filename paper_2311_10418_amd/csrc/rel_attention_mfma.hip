@@ -10,8 +10,8 @@
 // 16 heads of 64.)  Work-groups leave their sums in a slot; work-groups in front of the dK/dV grid add the slots up.
 // dK/dV: the loop over the blocks of queries is cut by distance, so that steps stay straight code: steps with the table and steps with one number.
 //
-// Few queries over long keys (k_splits > 1): the keys of a head are dealt out to work-groups, see RelPart.  Sequences of at most 128 queries and keys need no
-// work list (direct): its launch would take longer than what it saves.
+// Few queries over long keys (k_splits > 1): the keys of a head are dealt out to work-groups, see RelPart.  Where the grid of all blocks that a sequence
+// may have is hardly larger than the list's (direct), there is none: its launch takes 5 us.
 #include "rel_attention.hpp"
 #include "attention_tiles.hpp"
 #include <algorithm>
@@ -23,6 +23,7 @@ namespace {
 constexpr int kTablePad = 94;                           // distances that a near block (64 x 32 pairs) may reach beyond `reach`
 constexpr int kAllLds = 160 * 1024;
 __host__ __device__ constexpr int table_floats(int reach) { return (2 * (reach + kTablePad) + 1 + 3) & ~3; }
+__device__ __forceinline__ float uniform(float v) { return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, v))); }
 // The table of a head, in three parts, so that its two trips to memory (the buckets, then their biases) go beside those that a work-group begins with anyway (its
 // item, then its tables).  The last entries of a long reach are made in the end.
 struct TableFill {
@@ -52,6 +53,13 @@ template <int HD> __device__ __forceinline__ void store_cols_f32(const f32x16_t 
             *reinterpret_cast<f32x4_t*>(out_row + dt * 32 + 8 * q4 + 4 * g) = f32x4_t{acc[dt][4 * q4], acc[dt][4 * q4 + 1], acc[dt][4 * q4 + 2], acc[dt][4 * q4 + 3]};
 }
 
+// Item of a grid without a list: `blocks` blocks of 128 rows to each sequence, whether it has them or not.  Sequences last to first (a plan lists them by ascending
+// length), and under a causal mask their last queries first.
+__device__ __forceinline__ int2 direct_item(const RelAttnArgs& a, int item, int blocks, bool last_first) {
+    const int n = item / blocks, b = item - n * blocks;
+    return make_int2(a.n_seq - 1 - n, last_first ? blocks - 1 - b : b);
+}
+
 // Items of the dK/dV kernel, as WorkDraw, in a grid whose first a.first_group work-groups do something else
 struct RelDraw {
     int32_t* ctr;
@@ -61,8 +69,8 @@ struct RelDraw {
         const int me = (int)blockIdx.x - a.first_group;
         ctr = const_cast<int32_t*>(a.n_items) + kCtrHeader;
         groups = a.groups;
-        fixed = a.direct;
-        total = (a.direct ? a.n_seq : a.n_items[1]) * a.n_heads;
+        fixed = a.direct != 0;
+        total = (a.direct ? a.n_seq * a.direct_k : a.n_items[1]) * a.n_heads;
         xcd = me & 7;
         k = me >> 3;
     }
@@ -100,8 +108,8 @@ __global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void rel_fwd_mfma_kernel(Rel
     int item = blockIdx.x / a.n_heads;
     const int h = blockIdx.x - item * a.n_heads, split = a.k_splits > 1 ? item % a.k_splits : 0;
     int2 it;
-    if (a.direct) {                                     // one block of queries to a sequence, and no list
-        it = make_int2(a.n_seq - 1 - item / a.k_splits, 0);
+    if (a.direct) {                                     // no list; work-groups that share keys: one block of queries to a sequence
+        it = direct_item(a, a.k_splits > 1 ? item / a.k_splits : item, a.direct, CAUSAL);
     } else {
         it = a.items_q[item];                           // (within the list's capacity; read beside its length, not behind it)
         if (item >= a.n_items[0]) return;
@@ -157,7 +165,7 @@ __global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void rel_fwd_mfma_kernel(Rel
     float* table = reinterpret_cast<float*>(smem + 4 * TILE);
     fill.store(a, h, table);
     __syncthreads();
-    const float flat_behind = table[0], flat_front = table[2 * (a.reach + kTablePad)];
+    const float flat_behind = uniform(table[0]), flat_front = uniform(table[2 * (a.reach + kTablePad)]);
     for (int b = 0; b < nb; ++b) {
         const int kv0 = b * 64;
         char* sK = smem + (b & 1) * (2 * TILE);
@@ -209,25 +217,19 @@ __global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void rel_fwd_mfma_kernel(Rel
                 }
             }
         }
-        // the first V^T fragments of the second product are fetched now and land during the softmax
-        constexpr int NV = 4 * (HD / 32);
-        bf16x8_t fv[NV];
-        auto read_v = [&](int i) { fv[i] = read_tr<HD>(sV, tro, i / (HD / 32), i % (HD / 32)); };
-#pragma unroll
-        for (int i = 0; i < AHEAD_V; ++i) read_v(i);
-        __builtin_amdgcn_sched_barrier(kFence);
         // the bias: near blocks get theirs from the table, and their scores are in the exp2 domain from here on; the rest has one number
         const int first = kv0 - pw0 - 31;               // the block's distances: first .. first + 94
         float cc = c, flat = first >= a.reach ? flat_front : flat_behind;
         if (first + 94 > -a.reach && first < a.reach) {
-            int at = kv0 - pi + 4 * g + a.reach + kTablePad;
-            asm volatile("" : "+v"(at));                // (a real branch, as the mask's below)
+            int lane_at = lane;                         // (opaque: a real branch, as the mask's below, and nothing of it kept in registers)
+            asm volatile("" : "+v"(lane_at));
+            const int at = kv0 - pw0 + a.reach + kTablePad - (lane_at & 31) + 4 * (lane_at >> 5);
             const float* near = table + at;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {               // (eight at a time: registers)
+            for (int i = 0; i < 8; ++i) {               // (four at a time: registers)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const int kt = i >> 1, e = (i & 1) * 8 + j;
+                for (int j = 0; j < 4; ++j) {
+                    const int kt = i >> 2, e = (i & 3) * 4 + j;
                     sacc[kt][e] = __builtin_fmaf(sacc[kt][e], c, near[kt * 32 + 8 * (e >> 2) + (e & 3)]);
                 }
                 if (HD == 64) __builtin_amdgcn_sched_barrier(0);
@@ -235,6 +237,13 @@ __global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void rel_fwd_mfma_kernel(Rel
             cc = 1.f;
             flat = 0.f;
         }
+        // the first V^T fragments of the second product are fetched now and land during the softmax
+        constexpr int NV = 4 * (HD / 32);
+        bf16x8_t fv[NV];
+        auto read_v = [&](int i) { fv[i] = read_tr<HD>(sV, tro, i / (HD / 32), i % (HD / 32)); };
+#pragma unroll
+        for (int i = 0; i < AHEAD_V; ++i) read_v(i);
+        __builtin_amdgcn_sched_barrier(kFence);
         const bool need_mask = (kv0 + 64 > kl) || (CAUSAL && kv0 + 63 > pw0);
         if (need_mask) {
             // the volatile statement keeps the whole mask computation inside a real branch: hoisted or if-converted,
@@ -310,7 +319,7 @@ __global__ __launch_bounds__(256, 2) void rel_bwd_dq_mfma_kernel(RelAttnArgs a) 
     const int item = blockIdx.x / a.n_heads, h = blockIdx.x - item * a.n_heads;
     int2 it;
     if (a.direct) {
-        it = make_int2(a.n_seq - 1 - item, 0);
+        it = direct_item(a, item, a.direct, CAUSAL);
     } else {
         if (item >= a.n_items[0]) return;
         it = a.items_q[item];
@@ -385,7 +394,7 @@ __global__ __launch_bounds__(256, 2) void rel_bwd_dq_mfma_kernel(RelAttnArgs a) 
     __syncthreads();
     // sums of dS by distance: two arrays for each wavefront, since the distances of its lane halves, rows 4 apart, overlap
     float* const sums = table + wide * (1 + 2 * wave + g);
-    const float flat_behind = table[0], flat_front = table[2 * (a.reach + kTablePad)];
+    const float flat_behind = uniform(table[0]), flat_front = uniform(table[2 * (a.reach + kTablePad)]);
     float beyond_behind = 0.f, beyond_front = 0.f, carry = 0.f;
     float* to = sums;                                   // (where `carry` belongs: 32 on)
     const int wave_last = CAUSAL ? min(kl - 1, pw0 + 31) : kl - 1;
@@ -560,7 +569,7 @@ __global__ __launch_bounds__(256, HD == 64 ? 2 : 1) void rel_bwd_dkv_mfma_kernel
     RelDraw draw(a);
     float* table = reinterpret_cast<float*>(smem + NS * STAGE + 64 + 64 * HD);
     if ((int)blockIdx.x < a.first_group) {              // work-groups in front: one for each head sums up dbias
-        if ((int)blockIdx.x < a.n_heads) sum_dbias<256>(a, blockIdx.x, a.direct ? a.n_seq : a.n_items[0], reinterpret_cast<float*>(smem));
+        if ((int)blockIdx.x < a.n_heads) sum_dbias<256>(a, blockIdx.x, a.direct ? a.n_seq * a.direct : a.n_items[0], reinterpret_cast<float*>(smem));
         return;
     }
     int kw0, ki, kl, ql, h, q_begin, nb, pos, table_head = -1;
@@ -589,7 +598,7 @@ __global__ __launch_bounds__(256, HD == 64 ? 2 : 1) void rel_bwd_dkv_mfma_kernel
         fill.buckets(a);
         const int item = draw.index() / a.n_heads;
         h = draw.index() - item * a.n_heads;
-        const int2 it = a.direct ? make_int2(a.n_seq - 1 - item, 0) : a.items_k[item];
+        const int2 it = a.direct ? direct_item(a, item, a.direct_k, false) : a.items_k[item];
         const int s = __builtin_amdgcn_readfirstlane(it.x);
         k0 = __builtin_amdgcn_readfirstlane(it.y) * 128;
         pos = __builtin_amdgcn_readfirstlane(rel_position(a, s));
@@ -651,7 +660,7 @@ __global__ __launch_bounds__(256, HD == 64 ? 2 : 1) void rel_bwd_dkv_mfma_kernel
         __syncthreads();
         table_head = h;
     }
-    const float flat_behind = table[0], flat_front = table[2 * (a.reach + kTablePad)];
+    const float flat_behind = uniform(table[0]), flat_front = uniform(table[2 * (a.reach + kTablePad)]);
     // the K / V fragments (ordinary loads) and the stores of the item before are complete before the loop: left to the
     // compiler, its waits for them would sit inside the loop as "nothing outstanding", which would also drain the
     // transfers in flight.  So are the zeros of s_zero, in front of the first step's barrier.
@@ -769,7 +778,7 @@ __global__ __launch_bounds__(256, HD == 64 ? 2 : 1) void rel_bwd_dkv_mfma_kernel
     // Blocks in order of their queries: (causal) those that not all keys of the work-group are seen by, then by the bias of this wavefront's pairs: beyond
     // reach in front (unmasked only), near, beyond reach behind; the ragged last one.  Every wavefront goes through as many steps.
     const int n_diag = CAUSAL ? min(nb, max(0, (k0 + 127 - pos - q_begin + 63) / 64)) : 0;
-    const int n_full = max(n_diag, (ql - q_begin) / 64);                     // blocks b < n_full have all their 64 rows
+    const int n_full = min(nb, max(n_diag, (ql - q_begin) / 64));            // blocks b < n_full have all their 64 rows (nb = 0: no keys here)
     const int before = kw0 - pos - q_begin;             // distance of this wavefront's first key and the first query: block b has before - 64 b - 63 .. before - 64 b + 31
     const int n_front = CAUSAL ? 0 : min(n_full, max(0, (before - 63 - a.reach + 64) >> 6));                        // blocks with before - 64 b - 63 >= reach
     const int n_near = min(n_full, max(0, (before + 31 + a.reach + 63) >> 6));                                      // ... and before - 64 b + 31 > -reach
@@ -814,7 +823,7 @@ ds_status fwd_launch(const RelAttnArgs& a, hipStream_t st) {
     const int smem = 4 * (64 * HD * 2) + table_floats(a.reach) * 4;
     ds_status r = set_smem(kern, kAllLds, attr);
     if (r != DS_OK) return r;
-    hipLaunchKernelGGL(kern, dim3((unsigned)(a.direct ? a.n_seq * a.k_splits : a.max_items_q) * a.n_heads), dim3(256), smem, st, a);
+    hipLaunchKernelGGL(kern, dim3((unsigned)(a.direct ? a.n_seq * a.direct * a.k_splits : a.max_items_q) * a.n_heads), dim3(256), smem, st, a);
     DS_LAUNCH_CHECK();
     return DS_OK;
 }
@@ -830,9 +839,9 @@ ds_status bwd_launch(const RelAttnArgs& a, hipStream_t st) {
     if (r != DS_OK) return r;
     r = set_smem(kkv, kAllLds, attr_kv);
     if (r != DS_OK) return r;
-    hipLaunchKernelGGL(kq, dim3((unsigned)(a.direct ? a.n_seq : a.max_items_q) * a.n_heads), dim3(256), smem_q, st, a);
+    hipLaunchKernelGGL(kq, dim3((unsigned)(a.direct ? a.n_seq * a.direct : a.max_items_q) * a.n_heads), dim3(256), smem_q, st, a);
     DS_LAUNCH_CHECK();
-    const unsigned items_kv = (unsigned)(a.direct ? a.n_seq : a.max_items_k) * a.n_heads;
+    const unsigned items_kv = (unsigned)(a.direct ? a.n_seq * a.direct_k : a.max_items_k) * a.n_heads;
     RelAttnArgs b = a;
     b.first_group = (a.n_heads + 7) / 8 * 8;            // (the rest keeps its XCDs)
     b.groups = dkv_persistent(HD) && !a.direct ? (int32_t)persistent_grid(items_kv) : (int32_t)items_kv;
@@ -851,8 +860,8 @@ bool rel_mfma_supported(const RelAttnArgs& a) {
         if ((uintptr_t)p & 15) return false;
     if (a.d_o && !(a.scale >= 0x1p-20f && a.scale <= 0x1p20f)) return false;        // (log-sum-exps reach the dK/dV kernel divided by it)
     // work-items of a launch: 32 bits
-    const long long items = (long long)std::max(a.q_total_rows, a.k_total_rows) / 128 + (long long)a.n_seq * std::max(1, a.k_splits);
-    return items * a.n_heads + a.n_heads + 8 < 1LL << 23;
+    const long long items = (long long)std::max(a.q_total_rows, a.k_total_rows) / 128 + (long long)a.n_seq * 2;
+    return items * a.n_heads + a.n_heads + 8 < 1LL << 23;       // (shares of keys: 512 work-groups at most)
 }
 
 static ds_status prepare(RelAttnArgs& a, bool backward, hipStream_t st) {
