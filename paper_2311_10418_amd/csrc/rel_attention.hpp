@@ -90,33 +90,55 @@ template <int THREADS> __device__ __forceinline__ int blocks_sum(int n, int* lds
     __syncthreads();
     return n;
 }
-// dbias[.][h] = (accumulate ? itself : 0) + the sums in n slots: a work-group of the dK/dV launch for each head.  lds: (2 reach + 1) floats for each of
-// `groups` wavefront groups and the bucket table
+// dbias[.][h] = (accumulate ? itself : 0) + the sums in n slots, in a fixed order: a work-group of the dK/dV launch for each head.  Up to 320 distances each wavefront
+// takes every so-manieth slot, five distances a lane; more go by thread.  Eight threads to a bucket then look for its distances.  (With a thread to a distance and to a
+// bucket this took 12 us of every backward call.)  lds: 2 reach + 1 pairs and, up to 320, as many floats for each wavefront.
 template <int THREADS> __device__ __forceinline__ void sum_dbias(const RelAttnArgs& a, int h, int n, float* lds) {
-    const int t = threadIdx.x, w = 2 * a.reach + 1;
+    constexpr int WAVES = THREADS / 64, MOST = 5;
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6, w = 2 * a.reach + 1;
     const size_t step = (size_t)a.n_heads * w;
     const float* from = a.slots + (size_t)h * w;
-    int32_t* of = reinterpret_cast<int32_t*>(lds + w);
+    const bool shared = w <= 64 * MOST;
+    float2* pair = reinterpret_cast<float2*>(lds + (shared ? WAVES * w : 0));
+    if (shared) {
+        float sum[MOST];
+#pragma unroll
+        for (int j = 0; j < MOST; ++j) sum[j] = 0.f;
+#pragma unroll 4
+        for (int k = wave; k < n; k += WAVES)
+#pragma unroll
+            for (int j = 0; j < MOST; ++j) sum[j] += from[(size_t)k * step + min(lane + 64 * j, w - 1)];
+#pragma unroll
+        for (int j = 0; j < MOST; ++j)
+            if (lane + 64 * j < w) lds[wave * w + lane + 64 * j] = sum[j];
+        __syncthreads();
+    }
     for (int i = t; i < w; i += THREADS) {
         float sum = 0.f;
-        int k = 0;
-        for (; k + 8 <= n; k += 8) {
-            float v[8];
+        if (shared) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = from[(size_t)(k + j) * step + i];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) sum += v[j];
+            for (int j = 0; j < WAVES; ++j) sum += lds[j * w + i];
+        } else {
+#pragma unroll 8
+            for (int k = 0; k < n; ++k) sum += from[(size_t)k * step + i];
         }
-        for (; k < n; ++k) sum += from[(size_t)k * step + i];
-        lds[i] = sum;
-        of[i] = min(max(a.bucket[i], 0), a.n_buckets - 1);
+        pair[i] = make_float2(sum, __builtin_bit_cast(float, min(max(a.bucket[i], 0), a.n_buckets - 1)));
     }
     __syncthreads();
-    for (int b = t; b < a.n_buckets; b += THREADS) {
+    for (int b0 = 0; b0 < a.n_buckets; b0 += THREADS / 8) {
+        const int b = b0 + (t >> 3);
         float sum = 0.f;
-        for (int i = 0; i < w; ++i) sum += of[i] == b ? lds[i] : 0.f;
-        float* to = a.dbias + (size_t)b * a.n_heads + h;
-        *to = (a.accumulate ? *to : 0.f) + sum;
+#pragma unroll 8
+        for (int i = t & 7; i < w; i += 8) {
+            const float2 x = pair[i];
+            sum += __builtin_bit_cast(int, x.y) == b ? x.x : 0.f;
+        }
+#pragma unroll
+        for (int m = 1; m < 8; m *= 2) sum += __shfl_xor(sum, m, 64);
+        if ((t & 7) == 0 && b < a.n_buckets) {
+            float* to = a.dbias + (size_t)b * a.n_heads + h;
+            *to = (a.accumulate ? *to : 0.f) + sum;
+        }
     }
 }
 
