@@ -576,13 +576,20 @@ int64_t ds_rel_attention_scratch_bytes(int32_t n_heads, int32_t head_dim, int32_
  *     S_ij = scale * q_i . k_j + bias[bucket[clamp(j - p_i, -reach, reach) + reach]][h],   P = softmax(S),   O = P V,   p_i = q_pos[s] + i.
  * Query i of sequence s stands at position p_i (q_pos: DEVICE int32[n_seq], or NULL: zeros; negative ones too), key j at position j.  mask = 1 hides keys with
  * j > p_i.  With q_pos the queries may be the last tokens of a longer sequence whose keys lie in a cache, down to a single one.
- * head_dim: a multiple of 8, at most 128.  scale: positive.  bias: [n_buckets, n_heads] of the tensors' type, contiguous; entries of -inf hide what has their
- * bucket.  bucket: DEVICE int32[2 * reach + 1] (ds_rel_buckets makes the usual ones, reach = max_distance; any other table will do, entries outside of
+ * head_dim: a multiple of 8, at most 128.  scale: positive.  bias: [n_buckets, n_heads] of the tensors' type, contiguous; entries of -inf, or below -2.3e38 (a
+ * type's lowest value), hide what has their bucket.  bucket: DEVICE int32[2 * reach + 1] (ds_rel_buckets makes the usual ones, reach = max_distance; any other table will do, entries outside of
  * 0 .. n_buckets - 1 are clamped).  n_buckets and reach: at most 1024.
  * lse: float32 [n_heads, q_total_rows].  A row that sees no key has zeros in o (and gradients) and -inf in lse.
  * q_total_rows / k_total_rows: rows of the tensors holding the queries / the keys; max_q_len / max_k_len: upper bounds of the lengths (so are the rows of the
  * tensors), at most 2^28.  Rows not covered by any sequence are not touched; the sequences must not overlap.
- * Strides and alignments of the element type are taken as they are.  scratch: DEVICE, 16-byte aligned, at least ds_rel_attention_scratch_bytes. */
+ * Strides and alignments of the element type are taken as they are.  scratch: DEVICE, 16-byte aligned, at least ds_rel_attention_scratch_bytes; what it holds
+ * before a call does not matter.  Outputs must not overlap inputs.
+ * Precision: bf16 heads of 64 and 128 with 16-byte aligned rows go to the matrix cores, where probabilities and their gradients are rounded to bf16 as they are
+ * multiplied (at most 2^-8 of each); every other call, and with force_generic != 0 all of them, to kernels that compute in fp32.  Backward takes probabilities from lse:
+ * they are off by up to 2^-22 of a score's size (after scaling, with its bias).
+ * Speed: at most 64 queries over long keys (tokens on a cache) are shared out over work-groups if the q tensor has at most 64 rows for each sequence.
+ * Values that are not finite: a row is affected by the rows it sees.  The bf16 matrix-core kernels multiply whole blocks by probabilities that are 0 where mask = 1
+ * hides a token, so that an infinity or NaN may also reach rows up to 63 tokens in front of it in o, up to 31 in dq (31 behind it in dk and dv). */
 ds_status ds_rel_attention_fwd(int32_t dtype, int32_t n_seq, int32_t n_heads, int32_t head_dim, int32_t mask, const int32_t* q_row,
                                const int32_t* q_len, const int32_t* k_row, const int32_t* k_len, const int32_t* q_pos, int32_t max_q_len,
                                int32_t max_k_len, const void* q, int32_t ldq, const void* k, int32_t ldk, const void* v, int32_t ldv, float scale,
@@ -647,7 +654,7 @@ int64_t ds_resid_norm_bwd_scratch_floats(int32_t rows, int32_t d);
 /* The gated feed-forward block, both projections, activation and product in one kernel:
  *     G = x Wg^T + bg,   U = x Wu^T + bu,   H = act(G) . U
  * x: [rows, d]; wg, wu: [d_ff, d], as forward products read them (one row per output); bg, bu: [d_ff] or NULL; h: [rows, d_ff].  All of the type dtype,
- * row-major, contiguous, 16-byte aligned; d and d_ff multiples of 8, at most 65 536; rows at most 2^31 - 2^16 - 1.  The activation sees the sums before they
+ * row-major, contiguous, 16-byte aligned; d and d_ff multiples of 8, at most 65 536; ceil(rows / 64) * ceil(max(d, d_ff) / 64) at most 2^23.  The activation sees the sums before they
  * are rounded.  act: DS_ACT_GELU (tanh form), DS_ACT_SILU, DS_ACT_RELU.
  * g, u: [rows, d_ff], what the backward pass needs of G and U, or both NULL: nothing is kept.
  * row_valid: NULL, or DEVICE int32[rows]: rows with a negative entry are zeros in every output, whatever the inputs hold there (NaN too).

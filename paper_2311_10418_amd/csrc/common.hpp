@@ -1,6 +1,7 @@
 // Shared device/host helpers for the HIP translation units.
 #pragma once
 #include <hip/hip_runtime.h>
+#include <atomic>
 #include <cstdint>
 #include "../../include/dynastage.h"
 
@@ -248,6 +249,17 @@ __device__ __forceinline__ void lds_dma16_buffer_group(i32x4_t buf, const uint32
                      "buffer_load_dwordx4 %1, %4, 0 offen offset:1024 lds\n\tbuffer_load_dwordx4 %2, %4, 0 offen offset:2048 lds\n\t"
                      "buffer_load_dwordx4 %3, %4, 0 offen offset:3072 lds"
                      : : "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(buf), "s"(m0v) : "memory", "m0");
+}
+
+// Allows a kernel dynamic LDS beyond 64 KB, once for each device (`done`: a bit for each, static beside the launch)
+template <class Kern> ds_status allow_dynamic_lds(Kern kern, int bytes, std::atomic<uint64_t>& done) {
+    int dev = 0;
+    if (hipGetDevice(&dev) != hipSuccess || dev < 0) return DS_EHIP;
+    const uint64_t bit = dev < 64 ? 1ull << dev : 0;
+    if (bit && (done.load(std::memory_order_relaxed) & bit)) return DS_OK;
+    DS_HIP_CHECK(hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, bytes));
+    done.fetch_or(bit, std::memory_order_relaxed);
+    return DS_OK;
 }
 
 static inline size_t dtype_size(int32_t dtype) { return dtype == DS_DTYPE_BF16 ? 2 : 4; }

@@ -310,17 +310,10 @@ template <int ACT, int RB> __global__ __launch_bounds__(256) void glu_few_kernel
     }
 }
 
-template <class Kern> ds_status allow_lds(Kern kern, bool& done) {
-    if (!done) {
-        DS_HIP_CHECK(hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, 2 * STAGE));
-        done = true;
-    }
-    return DS_OK;
-}
 template <int ACT> ds_status tile_launch(const GluArgs& a, hipStream_t st) {
-    static bool attr = false;
+    static std::atomic<uint64_t> allowed{0};
     auto kern = glu_tile_kernel<ACT>;
-    const ds_status r = allow_lds(kern, attr);
+    const ds_status r = allow_dynamic_lds(kern, 2 * STAGE, allowed);
     if (r != DS_OK) return r;
     const int tiles_m = (a.rows + 127) / 128, tiles_n = ACT >= 0 ? (a.ff + 63) / 64 : (a.d + 127) / 128;
     hipLaunchKernelGGL(kern, dim3((unsigned)tiles_m * tiles_n, ACT >= 0 ? 1 : a.splits), dim3(256), 2 * STAGE, st, a, tiles_m, tiles_n);
@@ -354,8 +347,8 @@ ds_status glu_fwd_few(const GluArgs& a, hipStream_t st) {
 }
 
 ds_status glu_wgrad_tile(const GluWgrad& a, hipStream_t st) {
-    static bool attr = false;
-    const ds_status r = allow_lds(glu_wgrad_kernel, attr);
+    static std::atomic<uint64_t> allowed{0};
+    const ds_status r = allow_dynamic_lds(glu_wgrad_kernel, 2 * STAGE, allowed);
     if (r != DS_OK) return r;
     const int tiles_m = (a.d + 127) / 128, tiles_n = (a.ff + 127) / 128;
     hipLaunchKernelGGL(glu_wgrad_kernel, dim3((unsigned)tiles_m * tiles_n, a.splits, 2), dim3(256), 2 * STAGE, st, a, tiles_m, tiles_n);

@@ -981,21 +981,29 @@ __global__ __launch_bounds__(256) void glu_tail_finish_kernel(int M, int N, int 
     }
 }
 
-// The gated block's products with 256 x 256 tiles: launch_nt with a tile's columns counted as the kernel counts them
+__global__ void glu_clear_kernel(int* ctr) {
+    if (threadIdx.x < 16) ctr[threadIdx.x] = 0;
+}
+// The gated block's products with 256 x 256 tiles: launch_nt with a tile's columns counted as the kernel counts them.  The tile counters of the persistent form lie at the
+// end of the caller's workspace, whose calls do not overlap, and are cleared here (2 us): two captured graphs never share any.
 template <int EPI, int GLU>
 ds_status launch_glu(int M, int N, int K, const void* A, const void* B, void* C, const GemmEpi& p, const GluOperands& o, float* split_ws, size_t split_ws_floats,
                      hipStream_t st) {
-    static bool attr_set = false;
+    static std::atomic<uint64_t> allowed{0}, allowed_ps{0};
     auto kern = gemm_bf16_nt_kernel<EPI, false, false, false, 8, GLU>;
     auto kern_ps = gemm_bf16_nt_kernel<EPI, false, true, false, 8, GLU>;
-    if (!attr_set) {
-        DS_HIP_CHECK(hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, RING));
-        DS_HIP_CHECK(hipFuncSetAttribute(reinterpret_cast<const void*>(kern_ps), hipFuncAttributeMaxDynamicSharedMemorySize, RING));
-        attr_set = true;
-    }
-    const BigPlan plan = plan_big(false, EPI, M, GLU == 1 ? (N + 127) / 128 * BN : N, GLU == 2 ? 2 * K : K, split_ws ? split_ws_floats : 0);
+    ds_status r = allow_dynamic_lds(kern, RING, allowed);
+    if (r != DS_OK) return r;
+    r = allow_dynamic_lds(kern_ps, RING, allowed_ps);
+    if (r != DS_OK) return r;
+    const size_t room = split_ws && split_ws_floats > 16 ? (split_ws_floats - 16) & ~(size_t)3 : 0;
+    const BigPlan plan = plan_big(false, EPI, M, GLU == 1 ? (N + 127) / 128 * BN : N, GLU == 2 ? 2 * K : K, room);
     const int tiles = plan.tiles_m * plan.tiles_n, n_cu = gemm_cu_count();
-    int* ctr = nt_persistent(plan) ? ps_counters() : nullptr;
+    int* ctr = room && nt_persistent(plan) ? reinterpret_cast<int*>(split_ws + room) : nullptr;
+    if (ctr) {
+        hipLaunchKernelGGL(glu_clear_kernel, dim3(1), dim3(64), 0, st, ctr);
+        DS_LAUNCH_CHECK();
+    }
     if (ctr)
         hipLaunchKernelGGL(kern_ps, dim3(n_cu + (tiles - plan.n_main) * plan.tail_splits), dim3(256), RING, st, M, N, K, (const bf16_t*)A, (const bf16_t*)B, (bf16_t*)C, plan.tiles_m,
                            plan.tiles_n, 1, plan.n_main, plan.tail_splits, split_ws, p, n_cu, ctr, o);

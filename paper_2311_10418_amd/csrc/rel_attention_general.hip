@@ -587,17 +587,11 @@ __global__ __launch_bounds__(512, HD <= 64 && COLS == 64 ? 4 : 2) void rel_bwd_d
     store_column<T, HD>(dv, 1.0f, (T*)a.dv + (krow0 + ki) * a.ldv + (long long)h * hd, hd, g, vec);
 }
 
-template <class Kern> ds_status allow_lds(Kern kern, bool& done) {     // (the most that a call of any reach asks for)
-    if (!done) {
-        DS_HIP_CHECK(hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024));
-        done = true;
-    }
-    return DS_OK;
-}
+constexpr int kAllLds = 160 * 1024;                     // (calls of a long reach ask for nearly as much)
 template <class T, int HD> ds_status fwd_launch(const RelAttnArgs& a, hipStream_t st) {
-    static bool attr = false;
+    static std::atomic<uint64_t> allowed{0};
     auto kern = rel_fwd_kernel<T, HD>;
-    const ds_status r = allow_lds(kern, attr);
+    const ds_status r = allow_dynamic_lds(kern, kAllLds, allowed);
     if (r != DS_OK) return r;
     const dim3 grid = a.k_splits > 1 ? dim3(a.k_splits, a.n_heads, a.n_seq) : column_grid(a, a.max_q_len, 64);
     hipLaunchKernelGGL(kern, grid, dim3(256), (2 * Tile<T, HD, 256>::FLOATS + table_floats(a.reach)) * 4, st, a);
@@ -605,18 +599,18 @@ template <class T, int HD> ds_status fwd_launch(const RelAttnArgs& a, hipStream_
     return DS_OK;
 }
 template <class T, int HD, int COLS> ds_status dq_launch(const RelAttnArgs& a, hipStream_t st) {
-    static bool attr = false;
+    static std::atomic<uint64_t> allowed{0};
     auto kern = rel_bwd_dq_kernel<T, HD, COLS>;
-    const ds_status r = allow_lds(kern, attr);
+    const ds_status r = allow_dynamic_lds(kern, kAllLds, allowed);
     if (r != DS_OK) return r;
     hipLaunchKernelGGL(kern, column_grid(a, a.max_q_len, COLS), dim3(512), (2 * Tile<T, HD, 512>::FLOATS + 9 * table_floats(a.reach)) * 4, st, a);
     DS_LAUNCH_CHECK();
     return DS_OK;
 }
 template <class T, int HD, int COLS> ds_status dkv_launch(const RelAttnArgs& a, int slot_cols, hipStream_t st) {
-    static bool attr = false;
+    static std::atomic<uint64_t> allowed{0};
     auto kern = rel_bwd_dkv_kernel<T, HD, COLS>;
-    const ds_status r = allow_lds(kern, attr);
+    const ds_status r = allow_dynamic_lds(kern, kAllLds, allowed);
     if (r != DS_OK) return r;
     dim3 grid = column_grid(a, a.max_k_len, COLS);
     grid.z += 1;

@@ -818,10 +818,10 @@ __global__ __launch_bounds__(256, HD == 64 ? 2 : 1) void rel_bwd_dkv_mfma_kernel
 
 template <int HD, bool CAUSAL>
 ds_status fwd_launch(const RelAttnArgs& a, hipStream_t st) {
-    static bool attr = false;
+    static std::atomic<uint64_t> allowed{0};
     auto kern = rel_fwd_mfma_kernel<HD, CAUSAL>;
     const int smem = 4 * (64 * HD * 2) + table_floats(a.reach) * 4;
-    ds_status r = set_smem(kern, kAllLds, attr);
+    ds_status r = allow_dynamic_lds(kern, kAllLds, allowed);
     if (r != DS_OK) return r;
     hipLaunchKernelGGL(kern, dim3((unsigned)(a.direct ? a.n_seq * a.direct * a.k_splits : a.max_items_q) * a.n_heads), dim3(256), smem, st, a);
     DS_LAUNCH_CHECK();
@@ -830,14 +830,14 @@ ds_status fwd_launch(const RelAttnArgs& a, hipStream_t st) {
 
 template <int HD, bool CAUSAL>
 ds_status bwd_launch(const RelAttnArgs& a, hipStream_t st) {
-    static bool attr_q = false, attr_kv = false;
+    static std::atomic<uint64_t> allowed_q{0}, allowed_kv{0};
     auto kq = rel_bwd_dq_mfma_kernel<HD, CAUSAL>;
     auto kkv = rel_bwd_dkv_mfma_kernel<HD, CAUSAL>;
     const int smem_q = 4 * (64 * HD * 2) + 9 * table_floats(a.reach) * 4;
     const int smem_kv = 4 * (2 * (64 * HD * 2) + 2048) + 64 + 64 * HD + table_floats(a.reach) * 4;      // stages, draws, zeros, table
-    ds_status r = set_smem(kq, kAllLds, attr_q);
+    ds_status r = allow_dynamic_lds(kq, kAllLds, allowed_q);
     if (r != DS_OK) return r;
-    r = set_smem(kkv, kAllLds, attr_kv);
+    r = allow_dynamic_lds(kkv, kAllLds, allowed_kv);
     if (r != DS_OK) return r;
     hipLaunchKernelGGL(kq, dim3((unsigned)(a.direct ? a.n_seq * a.direct : a.max_items_q) * a.n_heads), dim3(256), smem_q, st, a);
     DS_LAUNCH_CHECK();

@@ -212,6 +212,14 @@ def test_biases_that_hide(dt, generic):
     for causal in (False, True):
         c = Case(20, dt, 2, 64, [100, 70], [100, 160], causal, buckets=4, table=table, bias=bias)
         c.run(generic)
+    low = torch.finfo(dt).min                           # the type's lowest value hides as well
+    bias = _rnd(rng, (4, 2), dt)
+    bias[2] = low
+    c = Case(26, dt, 2, 64, [100], [130], False, buckets=4, table=table, bias=bias).tensors()
+    c.bias = np.where(bias == low, -np.inf, bias)
+    c.forward(generic)
+    c.backward(generic)
+    c.check(generic)
     bias = np.full((1, 1), -np.inf)
     c = Case(21, dt, 1, 64, [70], [90], False, buckets=1, table=[0, 0, 0], bias=np.where(np.isinf(bias), -np.inf, 0.0)).tensors()
     c.bias = bias
