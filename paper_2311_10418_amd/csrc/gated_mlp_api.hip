@@ -78,6 +78,10 @@ GluChoice choose(const GluArgs& a, bool dx, size_t ws_floats) {
     c.big = glu_big_cost(a.rows, columns, K, ws_floats) < cost;
     return c;
 }
+// fp32: bf16 parts where the contraction is long enough to pay for their prologue.  us, fp32 products / bf16 parts: forward d = 128, 4 096 rows 15 / 14, 957 rows 9 / 11; 192 x 768, 2 048 rows
+// 20 / 17; 256 x 1024, 7 684 rows 84 / 71, 128 rows 15 / 13; 1024 x 2816, 957 rows 118 / 94, 7 684 rows 778 / 628; backward 128 x 512, 957 rows 35 / 26; 256 x 1024, 957 rows 65 / 40;
+// 1024 x 2816, 128 rows 155 / 46, 7 684 rows 867 / 737.
+bool split_f32(const GluArgs& a, bool dx) { return (dx || a.d >= 192) && glu_f32_supported(a); }
 bool known_act(int32_t act) { return act == DS_ACT_GELU || act == DS_ACT_SILU || act == DS_ACT_RELU; }
 
 }  // namespace
@@ -106,8 +110,9 @@ extern "C" ds_status ds_gated_mlp_fwd(int32_t dtype, int32_t act, int32_t rows, 
     GluArgs a = {};
     a.dtype = dtype; a.act = act; a.rows = rows; a.d = d; a.ff = d_ff;
     a.x = x; a.wg = wg; a.wu = wu; a.bg = bg; a.bu = bu; a.row_valid = row_valid; a.h = h; a.g = g; a.u = u;
-    if (dtype == DS_DTYPE_F32 || force_generic) return glu_fwd_general(a, (hipStream_t)hip_stream);
+    if (force_generic) return glu_fwd_general(a, (hipStream_t)hip_stream);
     if (rows <= kGluFewRows) return glu_fwd_few(a, (hipStream_t)hip_stream);
+    if (dtype == DS_DTYPE_F32) return split_f32(a, false) ? glu_fwd_f32(a, (hipStream_t)hip_stream) : glu_fwd_general(a, (hipStream_t)hip_stream);
     const size_t floats = workspace_floats > 0 ? (size_t)workspace_floats : 0;
     if (choose(a, false, floats).big) return glu_fwd_big(a, workspace, floats, (hipStream_t)hip_stream);
     return glu_fwd_tile(a, (hipStream_t)hip_stream);
@@ -126,8 +131,9 @@ extern "C" ds_status ds_gated_mlp_bwd(int32_t dtype, int32_t act, int32_t rows, 
     a.wg = wg; a.wu = wu; a.row_valid = row_valid; a.dg = dg; a.du = du; a.dx = dx;
     r = dtype == DS_DTYPE_BF16 ? grad_launch<bf16_t>(a, dh, g, u, dg, du, st) : grad_launch<float>(a, dh, g, u, dg, du, st);
     if (r != DS_OK) return r;
-    if (dtype == DS_DTYPE_F32 || force_generic) return glu_dx_general(a, st);
     const size_t floats = workspace_floats > 0 ? (size_t)workspace_floats : 0;
+    if (force_generic || (dtype == DS_DTYPE_F32 && !split_f32(a, true))) return glu_dx_general(a, st);
+    if (dtype == DS_DTYPE_F32) return glu_dx_f32(a, floats ? workspace : nullptr, floats, st);
     const GluChoice c = choose(a, true, floats);
     return c.big ? glu_dx_big(a, workspace, floats, st) : glu_dx_tile(a, c.splits, workspace, st);
 }

@@ -262,33 +262,49 @@ __global__ __launch_bounds__(256, 2) void glu_wgrad_kernel(GluWgrad a, int tiles
 // ---------------------------------------------------------------- few rows
 // The weights are what is read, once: a work-group takes 8 columns of H, its four wavefronts a quarter of K each, operands straight from memory into fragments.
 // The 16 weight rows of a block are 8 of Wg and the same 8 of Wu; the wavefronts' sums and the two halves meet in LDS.  RB blocks of 16 rows of x.
-template <int ACT, int RB> __global__ __launch_bounds__(256) void glu_few_kernel(GluArgs a) {
-    constexpr int AHEAD = RB == 1 ? 8 : 4;
+// A lane's piece of a row is 16 bytes: bf16 one instruction of 16x16x32 for 4 lanes' pieces, fp32 four of 16x16x4.
+template <class T> struct FewPiece;
+template <> struct FewPiece<bf16_t> {
+    typedef bf16x8_t type;
+    static __device__ __forceinline__ f32x4_t product(const type& w, const type& x, const f32x4_t& c) { return mfma(w, x, c); }
+};
+template <> struct FewPiece<float> {
+    typedef f32x4_t type;
+    static __device__ __forceinline__ f32x4_t product(const type& w, const type& x, f32x4_t c) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(w[e], x[e], c, 0, 0, 0);
+        return c;
+    }
+};
+template <class T, int ACT, int RB> __global__ __launch_bounds__(256) void glu_few_kernel(GluArgs a) {
+    typedef FewPiece<T> P;
+    typedef typename P::type piece_t;
+    constexpr int AHEAD = RB == 1 ? 8 : 4, N = 16 / sizeof(T), DEPTH = 4 * N;
     __shared__ __attribute__((aligned(16))) float part[4][RB * 16][16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), fr = lane & 15, fg = lane >> 4, n0 = blockIdx.x * 8, K = a.d;
-    const int steps = (K + 31) / 32, per = (steps + 3) / 4, s_end = min(steps, (wave + 1) * per);
-    const bf16_t* w = (const bf16_t*)(fr < 8 ? a.wg : a.wu) + (size_t)(n0 + (fr & 7)) * K;
-    const bf16_t* x[RB];
+    const int steps = (K + DEPTH - 1) / DEPTH, per = (steps + 3) / 4, s_end = min(steps, (wave + 1) * per);
+    const T* w = (const T*)(fr < 8 ? a.wg : a.wu) + (size_t)(n0 + (fr & 7)) * K;
+    const T* x[RB];
 #pragma unroll
-    for (int b = 0; b < RB; ++b) x[b] = (const bf16_t*)a.x + (size_t)min(b * 16 + fr, a.rows - 1) * K;
-    const bf16x8_t none = {};
+    for (int b = 0; b < RB; ++b) x[b] = (const T*)a.x + (size_t)min(b * 16 + fr, a.rows - 1) * K;
+    const piece_t none = {};
     f32x4_t acc[RB];
 #pragma unroll
     for (int b = 0; b < RB; ++b) acc[b] = zero4();
     for (int s0 = wave * per; s0 < s_end; s0 += AHEAD) {
-        bf16x8_t fw[AHEAD], fx[AHEAD][RB];
+        piece_t fw[AHEAD], fx[AHEAD][RB];
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) {
-            const int k = (s0 + i) * 32 + fg * 8;
+            const int k = (s0 + i) * DEPTH + fg * N;
             const bool in = s0 + i < s_end && k < K;       // (K is a multiple of 8)
-            fw[i] = in ? *reinterpret_cast<const bf16x8_t*>(w + k) : none;
+            fw[i] = in ? *reinterpret_cast<const piece_t*>(w + k) : none;
 #pragma unroll
-            for (int b = 0; b < RB; ++b) fx[i][b] = in ? *reinterpret_cast<const bf16x8_t*>(x[b] + k) : none;
+            for (int b = 0; b < RB; ++b) fx[i][b] = in ? *reinterpret_cast<const piece_t*>(x[b] + k) : none;
         }
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i)
 #pragma unroll
-            for (int b = 0; b < RB; ++b) acc[b] = mfma(fw[i], fx[i][b], acc[b]);
+            for (int b = 0; b < RB; ++b) acc[b] = P::product(fw[i], fx[i][b], acc[b]);
     }
 #pragma unroll
     for (int b = 0; b < RB; ++b) *reinterpret_cast<f32x4_t*>(&part[wave][b * 16 + fr][4 * fg]) = acc[b];
@@ -298,14 +314,14 @@ template <int ACT, int RB> __global__ __launch_bounds__(256) void glu_few_kernel
         if (m >= a.rows) break;
         float g = (part[0][m][c] + part[1][m][c]) + (part[2][m][c] + part[3][m][c]);
         float u = (part[0][m][c + 8] + part[1][m][c + 8]) + (part[2][m][c + 8] + part[3][m][c + 8]);
-        if (a.bg) g += (float)((const bf16_t*)a.bg)[n];
-        if (a.bu) u += (float)((const bf16_t*)a.bu)[n];
+        if (a.bg) g += to_f32(((const T*)a.bg)[n]);
+        if (a.bu) u += to_f32(((const T*)a.bu)[n]);
         const bool valid = !a.row_valid || a.row_valid[m] >= 0;
         const size_t to = (size_t)m * a.ff + n;
-        ((bf16_t*)a.h)[to] = (bf16_t)(valid ? glu_act<ACT>(g) * u : 0.f);
+        ((T*)a.h)[to] = from_f32<T>(valid ? glu_act<ACT>(g) * u : 0.f);
         if (a.g) {
-            ((bf16_t*)a.g)[to] = (bf16_t)(valid ? g : 0.f);
-            ((bf16_t*)a.u)[to] = (bf16_t)(valid ? u : 0.f);
+            ((T*)a.g)[to] = from_f32<T>(valid ? g : 0.f);
+            ((T*)a.u)[to] = from_f32<T>(valid ? u : 0.f);
         }
     }
 }
@@ -336,15 +352,17 @@ ds_status glu_dx_tile(const GluArgs& a0, int splits, float* workspace, hipStream
     return launch_splitk_finish<bf16_t, DS_EPI_NONE>(a.rows, a.d, splits, workspace, a.dx, p, st);
 }
 
-ds_status glu_fwd_few(const GluArgs& a, hipStream_t st) {
+template <class T> static ds_status few_launch(const GluArgs& a, hipStream_t st) {
     return glu_by_act(a.act, [&](auto act) -> ds_status {
         constexpr int ACT = decltype(act)::value;
-        auto kern = a.rows <= 16 ? glu_few_kernel<ACT, 1> : a.rows <= 32 ? glu_few_kernel<ACT, 2> : glu_few_kernel<ACT, 4>;
+        auto kern = a.rows <= 16 ? glu_few_kernel<T, ACT, 1> : a.rows <= 32 ? glu_few_kernel<T, ACT, 2> : glu_few_kernel<T, ACT, 4>;
         hipLaunchKernelGGL(kern, dim3(a.ff / 8), dim3(256), 0, st, a);
         DS_LAUNCH_CHECK();
         return DS_OK;
     });
 }
+
+ds_status glu_fwd_few(const GluArgs& a, hipStream_t st) { return a.dtype == DS_DTYPE_BF16 ? few_launch<bf16_t>(a, st) : few_launch<float>(a, st); }
 
 ds_status glu_wgrad_tile(const GluWgrad& a, hipStream_t st) {
     static std::atomic<uint64_t> allowed{0};

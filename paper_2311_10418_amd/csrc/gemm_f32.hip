@@ -26,8 +26,10 @@
 // 4 apart land 16 banks apart).  B columns are stored in the order (n/32, (n/4)%2, (n/8)%4, n%4), so that the accumulator
 // blocks 2p, 2p+1 of a lane hold 8 CONSECUTIVE columns 32 p + 8 g .. + 7 of its row: the epilogue works on them in
 // registers, 128 contiguous bytes per row and group of 4 lanes, without going through LDS again.
+#include "gated_mlp.hpp"
 #include "gemm_epilogue.hpp"
 
+#include <algorithm>
 #include <type_traits>
 #include <utility>
 
@@ -260,6 +262,19 @@ template <int ROWS, bool KC, bool PERM> struct SplitTile {
             }
         }
     }
+    // The gated block's two weight matrices as one tile of 2 x (32 rows of Wg, the same 32 of Wu): the first two wavefronts fetch Wg's, the others Wu's (KC, 128 rows)
+    __device__ __forceinline__ void setup_pair(const float* wg, const float* wu, long long ld_, int r0, int rows_, int t) {
+        static_assert(!KC || ROWS == 128 || ROWS == 64, "");
+        ld = ld_;
+        base = (__builtin_amdgcn_readfirstlane(t >> 7) ? wu : wg) + (long long)r0 * ld_;
+        rows = rows_ - r0;
+#pragma unroll
+        for (int i = 0; i < NC; ++i) {
+            const int u = t + 256 * i, r = u >> 2, c = u & 3, at = place(r);
+            off[i] = (uint32_t)(((i * 32 + (r & 31)) * (int)ld_ + (c >> 1) * 16 + (c & 1) * 4) * 4);
+            lds[i] = at * 64 + ((c ^ ((at >> 2) & 3)) << 4);
+        }
+    }
     // The tile at k0, through a buffer that ends where the operand does: rows (KC) or k rows past the end read as zeros, without a
     // test per lane.  What else lies outside: k beyond k_end in the last tile of KC operands is replaced by zeros, columns
     // beyond the operand's (not KC) belong to outputs that are not stored.  The buffer's length stays below 2^31, beyond every offset
@@ -329,18 +344,26 @@ template <int ROWS, bool KC, bool PERM> struct SplitTile {
 
 // C[M,N] = A * B with the orders of gemm_f32_mfma_kernel.  Grid: (N tiles, M tiles) with k_per_split = K, or, GRP, the work-groups of
 // several weight gradients in a row.  4 wavefronts of (BM / 2) x (BN / 2).
-template <int EPI, bool AKC, bool BKC, int BM, int BN, bool GRP>
+//
+// GLU: the gated feed-forward block's products.  1: forward (EPI: the activation), B and second_b are Wg and Wu; a lane's two accumulator blocks are G and U of the same
+// 64 x 64 outputs.  2: dx, the K loop runs through (A, B) and then through (second_a, second_b) into the same accumulators.
+struct GluOperandsF32 {
+    const float *second_a, *second_b, *bu;
+    float *g, *u;
+};
+template <int EPI, bool AKC, bool BKC, int BM, int BN, bool GRP, int GLU = 0>
 __global__ __launch_bounds__(256, 2) void gemm_f32_split_kernel(int M, int N, int K, const float* __restrict__ A, long long lda,
                                                                 const float* __restrict__ B, long long ldb, float* __restrict__ C,
                                                                 int k_per_split, GemmEpi p,
-                                                                std::conditional_t<GRP, TnGroup, NoGroup> grp) {
+                                                                std::conditional_t<GRP, TnGroup, std::conditional_t<GLU != 0, GluOperandsF32, NoGroup>> grp) {
+    static_assert(GLU == 0 || (AKC && BKC && !GRP && (GLU == 2 || BN == 128)), "the gated block: NT");
     typedef SplitTile<BM, AKC, false> TA;
     typedef SplitTile<BN, BKC, true> TB;
     constexpr int STAGE = 3 * (TA::PLANE + TB::PLANE);
     constexpr int NA = BM / 64, NB = BN / 64;
     extern __shared__ __attribute__((aligned(16))) char smem[];
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6, wm = wave >> 1, wn = wave & 1;
-    int m0 = blockIdx.y * BM, n0 = blockIdx.x * BN, split = 0;
+    int m0 = blockIdx.y * BM, n0 = blockIdx.x * (GLU == 1 ? 64 : BN), split = 0;
     float* partial = nullptr;
     if constexpr (GRP) {
         int l = xcd_contiguous(blockIdx.x, gridDim.x);
@@ -374,7 +397,8 @@ __global__ __launch_bounds__(256, 2) void gemm_f32_split_kernel(int M, int N, in
     TA ta;
     TB tb;
     ta.setup(A, lda, m0, M, t);
-    tb.setup(B, ldb, n0, N, t);
+    if constexpr (GLU == 1) tb.setup_pair(B, grp.second_b, ldb, n0, N, t);
+    else tb.setup(B, ldb, n0, N, t);
     auto load = [&](int set, int k0) {
         ta.load(set, k0, k_end, t);
         tb.load(set, k0, k_end, t);
@@ -422,6 +446,19 @@ __global__ __launch_bounds__(256, 2) void gemm_f32_split_kernel(int M, int N, in
         step(set0, set1, k0);
         if (k0 + F_BK < k_end) step(set1, set0, k0 + F_BK);
     }
+    if constexpr (GLU == 2) {                                         // (nobody reads the stages any more)
+        ta.setup(grp.second_a, lda, m0, M, t);
+        tb.setup(grp.second_b, ldb, n0, N, t);
+        load(0, k_begin);
+        load(1, k_begin + F_BK);
+        unroll<STEPS>([&](auto k) { store_step(set0, k); });
+        __syncthreads();
+        for (int k0 = k_begin; k0 < k_end; k0 += 2 * F_BK) {
+            step(set0, set1, k0);
+            if (k0 + F_BK < k_end) step(set1, set0, k0 + F_BK);
+        }
+    }
+    auto column = [&](int j) { return GLU == 1 ? n0 + wn * 32 : n0 + wn * (BN / 2) + 32 * j; };      // first of a block of 32
     // Where an element has bits that its three parts do not hold, or a result is not finite (an operand that is not, a part that
     // is not, products next to the largest float): the tile again with fp32 products.
     bool again = (lost & 0xffff) != 0;
@@ -437,12 +474,20 @@ __global__ __launch_bounds__(256, 2) void gemm_f32_split_kernel(int M, int N, in
             const int m = m0 + wm * (BM / 2) + i * 32 + (lane & 31);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const int n = n0 + wn * (BN / 2) + 32 * j + 16 * h + 8 * (lane >> 5);
+                const int n = column(j) + 16 * h + 8 * (lane >> 5);
                 again |= m < M && n < N && !(largest[h] < __builtin_inff());
             }
         }
     again = __syncthreads_or(again);
     if (again) {
+        auto other_a = [&](const float* x, int pass) {                // GLU = 2: the second pair of operands
+            if constexpr (GLU == 2) return pass ? x + (grp.second_a - A) : x;
+            else return x;
+        };
+        auto other_b = [&](const float* x, int pass) {
+            if constexpr (GLU == 2) return pass ? x + (grp.second_b - B) : x;
+            else return x;
+        };
         const float* pa[NA];
         const float* pb[NB];
 #pragma unroll
@@ -456,18 +501,23 @@ __global__ __launch_bounds__(256, 2) void gemm_f32_split_kernel(int M, int N, in
         }
 #pragma unroll
         for (int j = 0; j < NB; ++j) {
-            const int n = min(n0 + wn * (BN / 2) + 32 * j + TB::place(lane & 31), N - 1);
+            const int n = min(column(j) + TB::place(lane & 31), N - 1);
             pb[j] = B + (BKC ? (long long)n * ldb : (long long)n);
+            if constexpr (GLU == 1) {
+                if (j == 1) pb[j] = grp.second_b + (long long)n * ldb;
+            }
         }
+#pragma unroll
+        for (int pass = 0; pass < (GLU == 2 ? 2 : 1); ++pass)
         for (int k0 = k_begin; k0 < k_end; k0 += 8) {                 // the operands of four steps in flight
             float fa[4][NA], fb[4][NB];
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
                 const int k = k0 + 2 * u + (lane >> 5);
 #pragma unroll
-                for (int i = 0; i < NA; ++i) fa[u][i] = k < k_end ? pa[i][AKC ? (long long)k : (long long)k * lda] : 0.f;
+                for (int i = 0; i < NA; ++i) fa[u][i] = k < k_end ? other_a(pa[i], pass)[AKC ? (long long)k : (long long)k * lda] : 0.f;
 #pragma unroll
-                for (int j = 0; j < NB; ++j) fb[u][j] = k < k_end ? pb[j][BKC ? (long long)k : (long long)k * ldb] : 0.f;
+                for (int j = 0; j < NB; ++j) fb[u][j] = k < k_end ? other_b(pb[j], pass)[BKC ? (long long)k : (long long)k * ldb] : 0.f;
             }
 #pragma unroll
             for (int u = 0; u < 4; ++u)
@@ -476,6 +526,45 @@ __global__ __launch_bounds__(256, 2) void gemm_f32_split_kernel(int M, int N, in
 #pragma unroll
                     for (int j = 0; j < NB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(fb[u][j], fa[u][i], acc[i][j], 0, 0, 0);
         }
+    }
+    if constexpr (GLU == 1) {
+        // G and U of an element are in one lane.  (Ordinary stores straight from the registers, 32 bytes of a row to a lane: streaming ones, which go to memory piece by piece, or rows put
+        // together in LDS first took as long within the noise, 83 to 92 us for 7 684 x 256 x 1024 with G and U kept.)
+        const int m = m0 + wm * (BM / 2) + (lane & 31);
+        static_assert(NA == 1 || GLU != 1, "64 rows to a tile");
+        if (m >= M) return;
+        const bool valid = !p.row_valid || p.row_valid[m] >= 0;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int n = n0 + wn * 32 + 16 * h + 8 * (lane >> 5);
+            if (n >= N) continue;                                     // (N is a multiple of 8)
+            float g[8], u[8], b[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) g[e] = acc[0][0][8 * h + e], u[e] = acc[0][NB - 1][8 * h + e];
+            if (p.bias) {
+                Vec8<float>::load(reinterpret_cast<const float*>(p.bias) + n, b);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) g[e] += b[e];
+            }
+            if (grp.bu) {
+                Vec8<float>::load(grp.bu + n, b);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) u[e] += b[e];
+            }
+            const size_t to = (size_t)m * N + n;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                g[e] = valid ? g[e] : 0.f;
+                u[e] = valid ? u[e] : 0.f;
+                b[e] = valid ? glu_act<EPI>(g[e]) * u[e] : 0.f;
+            }
+            store8(C + to, pack8<float>(b));
+            if (grp.g) {
+                store8(grp.g + to, pack8<float>(g));
+                store8(grp.u + to, pack8<float>(u));
+            }
+        }
+        return;
     }
 #pragma unroll
     for (int i = 0; i < NA; ++i) {
@@ -490,6 +579,11 @@ __global__ __launch_bounds__(256, 2) void gemm_f32_split_kernel(int M, int N, in
                 float v[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] = acc[i][j][8 * h + e];
+                if constexpr (GLU == 2) {
+                    if (p.row_valid && p.row_valid[m] < 0)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) v[e] = 0.f;
+                }
                 if (GRP && partial) Vec8<float>::store(partial + mt * BN + nt, v);
                 else epilogue8<float, EPI>(m, n, N, v, C, p);
             }
@@ -507,6 +601,18 @@ ds_status launch_split(dim3 grid, int M, int N, int K, const float* A, const flo
         attr_set = true;
     }
     hipLaunchKernelGGL(kern, grid, dim3(256), smem, st, M, N, K, A, (long long)(AKC ? K : M), B, (long long)(BKC ? K : N), C, k_per_split, p, grp);
+    DS_LAUNCH_CHECK();
+    return DS_OK;
+}
+
+template <int EPI, int BN, int GLU>
+ds_status launch_glu(int columns, int M, int N, int K, const float* A, const float* B, float* C, const GemmEpi& p, const GluOperandsF32& o, hipStream_t st) {
+    constexpr int smem = 2 * 3 * 64 * (G_BM + BN);
+    static std::atomic<uint64_t> allowed{0};
+    auto kern = gemm_f32_split_kernel<EPI, true, true, G_BM, BN, false, GLU>;
+    const ds_status r = allow_dynamic_lds(kern, smem, allowed);
+    if (r != DS_OK) return r;
+    hipLaunchKernelGGL(kern, dim3((N + columns - 1) / columns, (M + G_BM - 1) / G_BM), dim3(256), smem, st, M, N, K, A, (long long)K, B, (long long)K, C, K, p, o);
     DS_LAUNCH_CHECK();
     return DS_OK;
 }
@@ -618,6 +724,32 @@ ds_status launch_gemm_f32_mfma(int32_t ta, int32_t tb, int32_t M, int32_t N, int
     case DS_EPI_MULR: return launch_epi<DS_EPI_MULR>(ta, tb, M, N, K, a, b, c, p, split_ws, split_ws_floats, st);
     }
     return DS_EINVAL;
+}
+
+bool glu_f32_supported(const GluArgs& a) { return a.rows <= 65535 * G_BM && std::max(a.d, a.ff) <= (1 << 22); }
+ds_status glu_fwd_f32(const GluArgs& a, hipStream_t st) {
+    return glu_by_act(a.act, [&](auto act) -> ds_status {
+        GemmEpi p{};
+        p.bias = a.bg;
+        p.row_valid = a.row_valid;
+        const GluOperandsF32 o = {nullptr, (const float*)a.wu, (const float*)a.bu, (float*)a.g, (float*)a.u};
+        return launch_glu<decltype(act)::value, G_BN, 1>(64, a.rows, a.ff, a.d, (const float*)a.x, (const float*)a.wg, (float*)a.h, p, o, st);
+    });
+}
+ds_status glu_dx_f32(const GluArgs& a, float* ws, size_t ws_floats, hipStream_t st) {
+    GemmEpi p{};
+    p.row_valid = a.row_valid;
+    const GluOperandsF32 o = {(const float*)a.du, (const float*)a.wu, nullptr, nullptr, nullptr};
+    const float *dg = (const float*)a.dg, *wg = (const float*)a.wg;
+    const long long rows = (a.rows + 63) / 64, wide = (a.d + 127) / 128, narrow = (a.d + 63) / 64;
+    const int n_cu = gemm_cu_count();
+    if (rows * wide >= 2 * n_cu && 2 * wide - narrow <= narrow / 8) return launch_glu<DS_EPI_NONE, 128, 2>(128, a.rows, a.d, a.ff, dg, wg, (float*)a.dx, p, o, st);
+    if (rows * narrow >= n_cu * 7 / 8) return launch_glu<DS_EPI_NONE, 64, 2>(64, a.rows, a.d, a.ff, dg, wg, (float*)a.dx, p, o, st);
+    // few work-groups: two products, which cut their contractions
+    ds_status r = launch_gemm_f32_mfma(0, 1, a.rows, a.d, a.ff, a.dg, a.wg, a.dx, DS_EPI_NONE, GemmEpi{}, ws, ws_floats, st);
+    if (r != DS_OK) return r;
+    p.R = a.dx;
+    return launch_gemm_f32_mfma(0, 1, a.rows, a.d, a.ff, a.du, a.wu, a.dx, DS_EPI_RESID, p, ws, ws_floats, st);
 }
 
 // K loops per tile: as many as give the fewest K tiles, one after another, at two work-groups per CU (0.84 us per K tile of the
