@@ -102,6 +102,19 @@ static RelChoice choose(RelAttnArgs& a, bool backward, bool force_generic) {
     return c;
 }
 
+// For tests: what `choose` says of a call whose tensors have the least strides and are aligned: the members of RelChoice, then blocks of keys without a list (backward)
+// and columns of a work-group of the general dQ and dK/dV kernels.  Not part of the C ABI's header.
+extern "C" void ds_rel_attention_choice(int32_t dtype, int32_t n_seq, int32_t n_heads, int32_t head_dim, int32_t max_q_len, int32_t max_k_len, int32_t q_total_rows,
+                                        int32_t k_total_rows, int32_t backward, int32_t force_generic, int32_t* out) {
+    RelAttnArgs a = {};
+    a.dtype = dtype; a.n_seq = n_seq; a.n_heads = n_heads; a.head_dim = head_dim; a.scale = 1.0f;
+    a.max_q_len = std::min(max_q_len, q_total_rows); a.max_k_len = std::min(max_k_len, k_total_rows);
+    a.q_total_rows = q_total_rows; a.k_total_rows = k_total_rows;
+    a.ldq = a.ldk = a.ldv = a.ldo = (long long)n_heads * head_dim;
+    const RelChoice c = choose(a, backward != 0, force_generic != 0);
+    for (const int32_t v : {c.general, c.k_splits, c.direct, c.few, backward && c.direct ? a.direct_k : 0, rel_general_columns(a, a.max_q_len), rel_general_columns(a, a.max_k_len)}) *out++ = v;
+}
+
 extern "C" int64_t ds_rel_attention_scratch_bytes(int32_t n_heads, int32_t head_dim, int32_t reach, int32_t q_total_rows, int32_t k_total_rows, int32_t n_seq) {
     if (n_heads <= 0 || head_dim <= 0 || head_dim > 128 || reach <= 0 || reach > kRelReach || q_total_rows <= 0 || k_total_rows <= 0 || n_seq <= 0) return 0;
     return (int64_t)rel_scratch_bytes(n_heads, head_dim, reach, q_total_rows, k_total_rows, n_seq);
