@@ -657,10 +657,11 @@ int64_t ds_resid_norm_bwd_scratch_floats(int32_t rows, int32_t d);
  * row-major, contiguous, 16-byte aligned; d and d_ff multiples of 8, at most 65 536; ceil(rows / 64) * ceil(max(d, d_ff) / 64) at most 2^23.  The activation sees the sums before they
  * are rounded.  act: DS_ACT_GELU (tanh form), DS_ACT_SILU, DS_ACT_RELU.
  * g, u: [rows, d_ff], what the backward pass needs of G and U, or both NULL: nothing is kept.
- * row_valid: NULL, or DEVICE int32[rows]: rows with a negative entry are zeros in every output, whatever the inputs hold there (NaN too).
- * workspace: DEVICE float32, 16-byte aligned, or NULL: room for partial sums; ds_gated_mlp_workspace_floats is as much as any of the three calls uses, and a
+ * row_valid: NULL, or DEVICE int32[rows]: rows with a negative entry are zeros in every output, whatever the inputs hold there (NaN too; dx: where the weights are finite).
+ * workspace: DEVICE float32, 16-byte aligned, or NULL: room for partial sums and tile counters; ds_gated_mlp_workspace_floats is as much as any of the three calls uses, and a
  * smaller one is used as far as it goes.  Calls that share a workspace must not overlap.
- * force_generic != 0 takes every product in fp32.  Few rows (at most 64, bf16) go to a kernel that reads the weights once. */
+ * force_generic != 0 takes every product in fp32 matrix instructions; without it fp32 products may be made of bf16 parts of each value, as those of ds_gemm.  Forward, at most 64 rows go
+ * to a kernel that reads the weights once. */
 enum { DS_ACT_GELU = 0, DS_ACT_SILU = 1, DS_ACT_RELU = 2 };
 int64_t ds_gated_mlp_workspace_floats(int32_t rows, int32_t d, int32_t d_ff);
 ds_status ds_gated_mlp_fwd(int32_t dtype, int32_t act, int32_t rows, int32_t d, int32_t d_ff, const void* x, const void* wg, const void* wu, const void* bg,

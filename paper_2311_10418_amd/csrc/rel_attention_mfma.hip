@@ -6,9 +6,14 @@
 // offsets from one address (ds_read2_b32 of neighbours), and scale their scores in that step instead of the later one.
 // dbias: dS is there in fp32, before it is rounded for the product, in the dQ kernel.  Blocks beyond reach add it up in a register, near ones along their
 // diagonals: two additions an element with a shift of lanes in them (row_shl, row_shr), two values a lane and block into an array by distance in LDS, private to
-// the lane half and the wavefront.  (16 ds_add_f32 a block instead: 160 cycles each, and the dQ kernel took 370 us instead of @DQ@ for 31 sequences of 366 to 523,
+// the lane half and the wavefront.  (16 ds_add_f32 a block instead: 160 cycles each, and the dQ kernel took 370 us instead of 77 for 31 sequences of 366 to 523,
 // 16 heads of 64.)  Work-groups leave their sums in a slot; work-groups in front of the dK/dV grid add the slots up.
 // dK/dV: the loop over the blocks of queries is cut by distance, so that steps stay straight code: steps with the table and steps with one number.
+//
+// What bounds them: vector instructions beside the matrix pipe (exponential, FMA, maximum and packing of every score), which share a SIMD's issue.  Measured, us
+// (TFLOP/s of the products that they do; share of the cycles with the matrix pipe / with the vector ALU busy): 31 sequences of 366 to 523, 16 heads of 64, bidirectional, forward
+// 55 (450; 20 / 48 %), dQ 76 (490; 22 / 45), dK/dV 91 (545; 28 / 29); 8 of 1 638 to 2 048, 16 heads of 128, causal, 160 (685; 32 / 41), 226 (725; 35 / 33), 332 (660; 33 / 25).  Forward
+// and dK/dV take as long as ordinary attention within 4 %: what the bias adds is the table's reads at near blocks and, in dQ, the diagonal sums.
 //
 // Few queries over long keys (k_splits > 1): the keys of a head are dealt out to work-groups, see RelPart.  Where the grid of all blocks that a sequence
 // may have is hardly larger than the list's (direct), there is none: its launch takes 5 us.
@@ -45,6 +50,12 @@ struct TableFill {
         for (int i = threadIdx.x + 512; i < entries(a); i += 256) table[i] = rel_bias(a, h, i - kTablePad);
     }
 };
+// a float as the sum of three bf16 values, exactly (the difference from the first has at most 16 bits, that from the second at most 8), as a row of eight
+__device__ __forceinline__ uint4 three_parts(float v) {
+    const uint32_t two = split_hi_lo(v);
+    const float rest = (v - __builtin_bit_cast(float, two << 16)) - __builtin_bit_cast(float, two & 0xffff0000u);
+    return make_uint4(two, (uint32_t)__builtin_bit_cast(unsigned short, (bf16_t)rest), 0u, 0u);
+}
 template <int HD> __device__ __forceinline__ void store_cols_f32(const f32x16_t (&acc)[HD / 32], float* __restrict__ out_row, int g) {
 #pragma unroll
     for (int dt = 0; dt < HD / 32; ++dt)
@@ -369,11 +380,10 @@ __global__ __launch_bounds__(256, 2) void rel_bwd_dq_mfma_kernel(RelAttnArgs a) 
     delta += __shfl_xor(delta, 32, 64);
     const float lse_q = a.lse[(size_t)h * a.lse_stride + qrow0 + qi_c];
     if (g == 0 && qi < ql) {
-        // for the dK/dV kernel: the {hi, lo} bf16 splits of lse/scale and delta that it appends
-        // to its contractions (hi + lo reproduces the value to ~2^-17 relative)
+        // for the dK/dV kernel: lse/scale and delta as the sums of three bf16 values, which it appends to its contractions
         const size_t at = (size_t)h * a.lse_stride + qrow0 + qi;
-        reinterpret_cast<uint4*>(a.aug_lse)[at] = make_uint4(split_hi_lo(lse_q == -INFINITY ? 1e30f : lse_q * (1.0f / a.scale)), 0u, 0u, 0u);
-        reinterpret_cast<uint4*>(a.aug_delta)[at] = make_uint4(split_hi_lo(delta), 0u, 0u, 0u);
+        reinterpret_cast<uint4*>(a.aug_lse)[at] = three_parts(lse_q == -INFINITY ? 1e30f : lse_q * (1.0f / a.scale));
+        reinterpret_cast<uint4*>(a.aug_delta)[at] = three_parts(delta);
     }
     const float lse2 = qi < ql ? rel_lse2(lse_q) : INFINITY;         // (a lane past the last query repeats it, with probabilities of 0)
     const float c = a.scale * kLog2e;
@@ -537,15 +547,14 @@ __global__ __launch_bounds__(256, 2) void rel_bwd_dq_mfma_kernel(RelAttnArgs a) 
 
 // ------------------------------------------------------------------------------------ backward: dK, dV
 // LDS, a ring of four stages of: Q tile, dO tile ([64][HD]) and the two statistics tiles ([64 rows][8] bf16:
-// {hi, lo, 0 x 6} of lse/scale and of delta, as the dQ kernel left them).  Three blocks are in flight while one is
+// three parts and five zeros of lse/scale and of delta, as the dQ kernel left them).  Three blocks are in flight while one is
 // consumed: with one wavefront per SIMD (about 370 registers) nothing else hides the latency of the transfers.
 //
-// Persistent work-groups at head size 128 (PS): as many as fit on the chip, each drawing its next item (key block, head) while it works on the
-// current one, and requesting that item's first three query blocks and its K / V fragments BEFORE it stores the current
-// results.  With a work-group per item nothing hid what lies between two items (the end of one work-group, the start of
-// the next, three dependent table reads, the first tiles): about 10 of 27 us per item at 65 536 tokens of mean length 385,
-// where an item has 7.5 steps on average (1015 -> 962 us).  Not at head size 64, where two work-groups share a CU and
-// the dispatcher's replacement is quicker than a draw (one-step items 47 us, 59 with draws).
+// Persistent work-groups at head size 128 (PS) where work goes by a list: as many as fit on the chip, each drawing its next item (key block, head) while it works on
+// the current one, and requesting that item's first three query blocks and its K / V fragments BEFORE it stores the current results.  With a work-group per item
+// nothing hides what lies between two items (the end of one work-group, the start of the next, dependent table reads, the first tiles); measured with ordinary attention,
+// 65 536 tokens of mean length 385: 1015 -> 962 us.  Not at head size 64, where two work-groups share a CU and the dispatcher's replacement is quicker than a draw
+// (there, one-step items 47 us, 59 with draws).  Without a list lengths are much the same, and a work-group takes one item.
 template <int HD, bool CAUSAL>
 __global__ __launch_bounds__(256, HD == 64 ? 2 : 1) void rel_bwd_dkv_mfma_kernel(RelAttnArgs a) {
     extern __shared__ __attribute__((aligned(16))) char smem[];
@@ -636,9 +645,9 @@ __global__ __launch_bounds__(256, HD == 64 ? 2 : 1) void rel_bwd_dkv_mfma_kernel
     }
     begin_item();
     for (int i = tid; i < 64 * HD / 16; i += 256) reinterpret_cast<uint4*>(s_zero)[i] = make_uint4(0u, 0u, 0u, 0u);
-    bf16x8_t neg_ones;                                  // contraction slots 0, 1 (lane half 0) pick -hi - lo
+    bf16x8_t neg_ones;                                  // contraction slots 0 to 2 (lane half 0) pick the three parts
 #pragma unroll
-    for (int j = 0; j < 8; ++j) neg_ones[j] = (bf16_t)((g == 0 && j < 2) ? -1.0f : 0.0f);
+    for (int j = 0; j < 8; ++j) neg_ones[j] = (bf16_t)((g == 0 && j < 3) ? -1.0f : 0.0f);
     const float c = a.scale * kLog2e;
 
     TrOffsets<HD> tro;
@@ -666,9 +675,8 @@ __global__ __launch_bounds__(256, HD == 64 ? 2 : 1) void rel_bwd_dkv_mfma_kernel
     // transfers in flight.  So are the zeros of s_zero, in front of the first step's barrier.
     __builtin_amdgcn_s_waitcnt(0x0070);
     // One step = one 64-query block, straight code: any branch inside it, even one that is never taken, splits the live
-    // ranges of the 128 accumulator registers and costs hundreds of register copies per step.  The step exists in two
-    // versions, with the mask as selects and without, and the loop is cut into three: the (at most two) blocks on the
-    // diagonal, the blocks in the middle, the ragged last block.
+    // ranges of the 128 accumulator registers and costs hundreds of register copies per step.  The step exists with the
+    // mask as selects and without, with biases from the table and with one number, and the loop is cut where these change.
     const bool wave_has_keys = kw0 < kl;
     auto step = [&](int b, auto masked_t, auto near_t, float flat) {
         constexpr bool MASKED = decltype(masked_t)::value, NEAR = decltype(near_t)::value;

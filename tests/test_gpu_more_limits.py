@@ -38,6 +38,26 @@ def test_sequences_of_all_lengths_without_a_list(hd):
         c.run(False, accumulate=causal)
 
 
+@pytest.mark.parametrize("hd", [64, 128])
+def test_large_log_sum_exps(hd):
+    """Scores of about 3008 by their bias: an error of 2^-17 of that would be one of 2 % of every probability.  One query to a sequence, so that nothing averages it out; the only
+    roundings are those of P to bf16, of the results, and of fp32 scores of this size (E)."""
+    n, heads = 24, 2
+    c = Case(35, BF, heads, hd, [1] * n, [9 + i for i in range(n)], False, buckets=1, table=[0, 0, 0], bias=np.full((1, heads), 3008.0)).tensors()
+    c.d_o = np.abs(c.d_o)
+    c.tdo = c.place(c.d_o, c.q_on, np.nan)
+    c.forward()
+    c.backward()
+    torch.cuda.synchronize()
+    dv = to_np(c.dv)
+    for s in range(n):
+        qs, ks = slice(c.q_row[s], c.q_row[s] + 1), slice(c.k_row[s], c.k_row[s] + c.kl[s])
+        terms = layer.rel_attention(c.q[qs], c.k[ks], c.v[ks], c.bias, c.bucket, heads, False, 0, c.scale)[3]
+        ref = layer.rel_attention_back(c.q[qs], c.k[ks], c.v[ks], c.bias, c.bucket, to_np(c.o)[qs], c.d_o[qs], heads, False, 0, c.scale)
+        E = U * (128 * terms.max() + 8 * 2 * 3010.0 + 256)
+        assert np.all(np.abs(dv[ks] - ref["dv"]) <= 2.0 ** -8 * np.abs(ref["dv"]) + (2.0 ** -8 + 2 * E + 256 * U) * ref["dv_part"])
+
+
 @pytest.mark.parametrize("dt", [BF, F32])
 @pytest.mark.parametrize("hd", [64, 128])
 def test_no_tokens_at_all(hd, dt):
