@@ -83,6 +83,22 @@ GluChoice choose(const GluArgs& a, bool dx, size_t ws_floats) {
 // 20 / 17; 256 x 1024, 7 684 rows 84 / 71, 128 rows 15 / 13; 1024 x 2816, 957 rows 118 / 94, 7 684 rows 778 / 628; backward 128 x 512, 957 rows 35 / 26; 256 x 1024, 957 rows 65 / 40;
 // 1024 x 2816, 128 rows 155 / 46, 7 684 rows 867 / 737.
 bool split_f32(const GluArgs& a, bool dx) { return (dx || a.d >= 192) && glu_f32_supported(a); }
+// Shares of the rows of the weight gradients' 128 x 128 tiles, by an estimate: two work-groups to a compute unit 1.05 us per 64 rows, one alone 0.7, and the launch that adds shares up.
+// Measured, us, with 1 / 2 / 3 / 4 shares (chosen: *): d x d_ff x rows 1856 x 960 x 1418 *23 / 28 / 35 / 41; 832 x 384 x 784 *11 / 12 / 13 / 14; 1000 x 1000 x 2000 26 / *23 / 24 / 25, 20 000 215 / 125 / 113 /
+// *93; 512 x 4416 x 49 573 643 / 694 / *522, 5 000 *65 / 72 / 66; 128 x 192 x 65 536 591 / 301 / 204 / 152, with 32 / 64 /
+// 128 31 / *27 / 31.
+int wgrad_splits(int rows, int d, int ff, int64_t ws_floats) {
+    const int64_t tiles = (int64_t)((d + 127) / 128) * ((ff + 127) / 128) * 2, outputs = 2 * (int64_t)d * ff, steps = ((int64_t)rows + 63) / 64;
+    int best = 1;
+    double least = 0;
+    for (int s = 1; s <= 128 && s <= steps && (s == 1 || s * outputs <= ws_floats); ++s) {
+        const int64_t full = tiles * s / 512, rest = tiles * s % 512;
+        const double rounds = 1.05 * full + (rest == 0 ? 0 : rest <= 256 ? 0.7 : 0.7 + 0.35 * (rest - 256) / 256);
+        const double cost = rounds * ((steps + s - 1) / s) + (s > 1 ? 4 + 0.03 * s + 1e-6 * (s + 1) * outputs : 0);
+        if (s == 1 || cost < least) least = cost, best = s;
+    }
+    return best;
+}
 bool known_act(int32_t act) { return act == DS_ACT_GELU || act == DS_ACT_SILU || act == DS_ACT_RELU; }
 
 }  // namespace
@@ -92,11 +108,12 @@ extern "C" int64_t ds_gated_mlp_workspace_floats(int32_t rows, int32_t d, int32_
     return std::max((int64_t)1 << 24, kSumFloats * d_ff);
 }
 
-// For tests: what `choose` says of a bf16 call with more than kGluFewRows rows: 256 x 256 tiles, pieces of the contraction.  Not part of the C ABI's header.
+// For tests: what `choose` says of a bf16 call with more than kGluFewRows rows: 256 x 256 tiles, pieces of the contraction; dx = 2: shares of the weight gradients' tiles.  Not part of
+// the C ABI's header.
 extern "C" void ds_gated_mlp_choice(int32_t rows, int32_t d, int32_t d_ff, int32_t dx, int64_t workspace_floats, int32_t* out) {
     GluArgs a = {};
     a.rows = rows; a.d = d; a.ff = d_ff;
-    const GluChoice c = choose(a, dx != 0, (size_t)workspace_floats);
+    const GluChoice c = dx == 2 ? GluChoice{false, wgrad_splits(rows, d, d_ff, workspace_floats)} : choose(a, dx != 0, (size_t)workspace_floats);
     out[0] = c.big;
     out[1] = c.splits;
 }
@@ -160,11 +177,9 @@ extern "C" ds_status ds_gated_mlp_wgrad(int32_t dtype, int32_t rows, int32_t d, 
         r = launch_tn_group(pick, group, st);
         if (r != DS_OK) return r;
     } else if (dtype == DS_DTYPE_BF16 && !force_generic && !tn_group_takes(group.p[0], rows, false)) {
-        // sizes that the products' own kernels do not take: the rows are shared out until there are two work-groups for a compute unit
-        const int64_t tiles = (int64_t)((d + 127) / 128) * ((d_ff + 127) / 128) * 2, outputs = (int64_t)d * d_ff;
-        const int64_t most = outputs <= INT32_MAX ? workspace_floats / (2 * outputs) : 1;
+        // sizes that the products' own kernels do not take
         GluWgrad w = {rows, d, d_ff, accumulate, 1, x, {dg, du}, {dwg, dwu}, workspace};
-        w.splits = (int32_t)std::max<int64_t>(1, std::min({2 * (int64_t)gemm_cu_count() / tiles, most, ((int64_t)rows + 255) / 256}));
+        w.splits = wgrad_splits(rows, d, d_ff, workspace_floats);
         r = glu_wgrad_tile(w, st);
         if (r != DS_OK) return r;
     } else {

@@ -262,6 +262,25 @@ __global__ __launch_bounds__(256, 2) void glu_wgrad_kernel(GluWgrad a, int tiles
     }
 }
 
+// the shares' sums, in their order; four values to a thread, eight loads in flight
+__global__ __launch_bounds__(256) void glu_wgrad_finish_kernel(GluWgrad a, long long n4) {
+    const f32x4_t* from = reinterpret_cast<const f32x4_t*>(a.workspace) + (size_t)blockIdx.y * a.splits * n4;
+    f32x4_t* to = reinterpret_cast<f32x4_t*>(a.dw[blockIdx.y]);
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n4; i += (long long)gridDim.x * 256) {
+        f32x4_t sum = from[i];
+        int s = 1;
+        for (; s + 8 <= a.splits; s += 8) {
+            f32x4_t v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = from[(size_t)(s + j) * n4 + i];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sum += v[j];
+        }
+        for (; s < a.splits; ++s) sum += from[(size_t)s * n4 + i];
+        to[i] = a.accumulate ? to[i] + sum : sum;
+    }
+}
+
 // ---------------------------------------------------------------- few rows
 // The weights are what is read, once: a work-group takes 8 columns of H, its four wavefronts a quarter of K each, operands straight from memory into fragments.
 // The 16 weight rows of a block are 8 of Wg and the same 8 of Wu; the wavefronts' sums and the two halves meet in LDS.  RB blocks of 16 rows of x.
@@ -376,9 +395,8 @@ ds_status glu_wgrad_tile(const GluWgrad& a, hipStream_t st) {
     hipLaunchKernelGGL(glu_wgrad_kernel, dim3((unsigned)tiles_m * tiles_n, a.splits, 2), dim3(256), 2 * STAGE, st, a, tiles_m, tiles_n);
     DS_LAUNCH_CHECK();
     if (a.splits == 1) return DS_OK;
-    for (int i = 0; i < 2; ++i) {
-        const ds_status s = launch_reduce_partials(a.splits, a.d * a.ff, a.workspace + (size_t)i * a.splits * a.d * a.ff, a.dw[i], a.accumulate, st);
-        if (s != DS_OK) return s;
-    }
+    const long long n4 = (long long)a.d * a.ff / 4;
+    hipLaunchKernelGGL(glu_wgrad_finish_kernel, dim3((unsigned)std::min<long long>((n4 + 255) / 256, 2048), 2), dim3(256), 0, st, a, n4);
+    DS_LAUNCH_CHECK();
     return DS_OK;
 }

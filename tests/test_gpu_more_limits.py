@@ -8,8 +8,8 @@ import torch
 
 from oracle import layer
 from paper_2311_10418_amd import binding as ds
-from helpers import DEV, to_np
-from test_gpu_gated_mlp import Block
+from helpers import DEV, to_dev, to_np
+from test_gpu_gated_mlp import Block, _rnd
 from test_gpu_rel_attention import Case
 
 pytestmark = pytest.mark.gpu
@@ -142,6 +142,22 @@ def test_gated_block_with_any_workspace(floats):
     Block(BF, 3000, 256, 1024, "gelu", bias=True, pad=0.1, floats=floats).run()
     Block(BF, 20000, 256, 512, "relu", pad=0.1, floats=floats).run()
     Block(F32, 300, 200, 520, "silu", bias=True, floats=floats).run()
+
+
+@pytest.mark.parametrize("rows,d,ff,floats", [(64 * 70, 128, 192, 1 << 24), (64 * 70, 128, 192, 5 * 2 * 128 * 192 + 7), (3000, 1000, 72, 1 << 24), (1000, 72, 1000, 1 << 20), (65, 128, 192, 1 << 20),
+                                               (1, 200, 8, 1 << 20), (20000, 136, 328, 1 << 24)])
+def test_shares_of_weight_gradients(rows, d, ff, floats):
+    """Rows of the tiles' weight gradients shared out, from one share to dozens; rounding: rows additions in fp32, in any order, and one more where they are added to what is there."""
+    rng = np.random.default_rng([6, rows, d, ff])
+    x, dg, du = (_rnd(rng, (rows, c), BF) for c in (d, ff, ff))
+    out = [torch.full((d, ff), 3.0, device=DEV) for _ in range(2)]
+    ws = torch.full((floats,), float("nan"), device=DEV)
+    for accumulate in (False, True):
+        before = [to_np(t) for t in out]
+        ds.ds_gated_mlp_wgrad(to_dev(x, BF), to_dev(dg, BF), to_dev(du, BF), *out, accumulate=accumulate, workspace=ws)
+        for got, dy, was in zip(out, (dg, du), before):
+            ref = x.T @ dy + (was if accumulate else 0.0)
+            assert np.all(np.abs(to_np(got) - ref) <= U * (rows * (np.abs(x).T @ np.abs(dy)) + np.abs(ref)) + 2.0 ** -130)
 
 
 def test_persistent_tiles_of_two_calls_at_once():

@@ -84,3 +84,15 @@ def test_gated_block_tiles():
         for floats in (0, 1 << 18, 1 << 24):
             big, splits = glu(rows, 512, 1408, dx=True, floats=floats)
             assert splits == 1 or splits * rows * 512 <= floats
+
+
+def test_shares_of_weight_gradients():
+    def shares(rows, d, ff, floats=1 << 24):
+        return glu(rows, d, ff, 2, floats)[1]
+
+    assert shares(1418, 1856, 960) == 1 and shares(64, 8, 8) == 1 and shares(20000, 1000, 1000) > 1 and shares(65536, 128, 192) > 32
+    for rows in (1, 65, 1000, 65536):
+        for d, ff in ((128, 192), (8, 8), (1000, 1000), (512, 4416), (65536, 65536)):
+            for floats in (0, 1 << 16, 1 << 24, 1 << 40):
+                s = shares(rows, d, ff, floats)
+                assert 1 <= s <= 128 and (s == 1 or 2 * s * d * ff <= floats and s <= (rows + 63) // 64)
