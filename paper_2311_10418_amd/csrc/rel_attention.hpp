@@ -26,6 +26,8 @@ struct RelAttnArgs : AttnArgs {
     float* d;                                           // general kernels: D, [n_heads][q_total_rows]
     float* slots;                                       // sums of dS by distance, [block of queries][n_heads][2 reach + 1]
     float* split_part;                                  // see RelPart
+    int32_t b_splits;                                   // backward, matrix-core kernels: work-groups that share the keys (queries) of a block of queries (keys), and where they leave
+    float *part_q, *part_k;                             // their sums: dQ [share][q_total_rows][wide], dK and dV [share][k_total_rows][2][wide], wide = n_heads * head_dim
     char* aug;                                          // matrix-core kernels: what the dQ kernel hands to the dK/dV kernel
     int32_t direct, direct_k;                           // matrix-core kernels: blocks of 128 queries / keys that a sequence may have, and work-groups go by them; 0: by a list
     int32_t first_group, groups;                        // dK/dV grid: work-groups in front that sum up dbias, work-groups behind them

@@ -25,14 +25,53 @@ static int few_splits(int32_t dtype, int n_heads, int head_dim, int q_total_rows
     return (int)std::max(1LL, std::min({4LL * kRelUnits / items, (long long)kSplitMost, ((long long)max_k_len + keys - 1) / keys}));
 }
 
+// Backward on the matrix cores: work-groups that may share a block of 128 rows (the scratch has room for as many), four blocks of 64 of the other side each at least.
+static constexpr int kBackMost = 8, kBackGroups = 3 * kRelUnits;
+static long long back_groups(int n_heads, int q_total_rows, int k_total_rows, int n_seq) {
+    return ((long long)std::max(q_total_rows, k_total_rows) / 128 + n_seq) * n_heads;
+}
+static int most_back_splits(int n_heads, int q_total_rows, int k_total_rows, int longest, int n_seq) {
+    return (int)std::max(1LL, std::min({kBackGroups / back_groups(n_heads, q_total_rows, k_total_rows, n_seq), (long long)kBackMost, (long long)longest / 256}));
+}
+// As many as an estimate of dQ and dK/dV together prefers by a tenth: a work-group takes `fixed` us and `step` for each block of 64 of the other side; one to a compute unit at head size
+// 128, at 64 two in 1.6 times the time of one; under a causal mask chains are half as long on average.  Shares are joined in a launch of their own (rel_back_join_kernel).
+// Measured, us, with 1 / 2 / 3 / 4 / most shares (sequences x length, heads of size, c: causal; *: chosen): 1 x 1 565, 4 of 128 c 97 / 72 / 61 / 57 / 56 (five: *54); 1 x 1 972, 3 of 64 c 80 / 54 / 45 /
+// 41 / 40 (five: *39); 3 x 1 193, 5 of 128 c 83 / *79 / 88 / 95; 2 x 1 181, 16 of 64 c *62 / 66; 1 x 1 024, 16 of 128 *72 / 69 / 88; 4 x 600, 9 of 128 *58 / 86; 1 x 8 192, 2 of 64 c 286 / 163 / 126 / *109 / 103; 1 x 4 096,
+// 8 of 128 c 224 / *177 / 175; 1 x 512, 4 of 64 31 / *26; 1 x 2 048, 16 of 128 c *124 / 118 / 116.
+static int back_splits(const RelAttnArgs& a) {
+    const int longest = std::max(a.max_q_len, a.max_k_len), most = most_back_splits(a.n_heads, a.q_total_rows, a.k_total_rows, longest, a.n_seq);
+    const double groups = (double)back_groups(a.n_heads, a.q_total_rows, a.k_total_rows, a.n_seq), step = a.head_dim == 64 ? 2.2 : 3.05, fixed = a.head_dim == 64 ? 14 : 20;
+    const double pair = a.head_dim == 64 ? 1.6 : 2, part_us = 4 * ((double)a.q_total_rows + 2.0 * a.k_total_rows) * a.n_heads * a.head_dim / 4.5e6;
+    const int steps = (longest + 63) / 64;
+    double alone = 0, least = 0;
+    int best = 1;
+    for (int s = 1; s <= most; ++s) {
+        const double chain = step * ((steps + s - 1) / s) + fixed, each = groups * s / kRelUnits;              // work-groups to a compute unit
+        double cost;
+        if (a.mask) {
+            cost = std::max(chain, each * pair / 2 * (fixed + 0.5 * step * steps / s));
+        } else {
+            const int rounds = (int)std::ceil(each);
+            cost = (rounds / 2 * pair + rounds % 2) * chain;
+        }
+        if (s == 1) alone = least = cost;
+        else if (cost += 4 + s * part_us; cost < least && cost < 0.9 * alone) least = cost, best = s;
+    }
+    return best;
+}
+
 // Scratch: the work lists of the matrix-core kernels; what the dQ kernels hand to the dK/dV kernels, 32 bytes for each query of a head (the general ones use 4 of
-// them); the slots of dbias, for each block of 64 queries (of 32 where the general kernels have at most 512 work-groups of 64).  A forward call has the parts of
+// them); the slots of dbias, for each share of each block of 64 queries (of 32 where the general kernels have at most 512 work-groups of 64); what shares of a block leave.  A forward call has the parts of
 // split keys in the place of the last two.
 static size_t lists_size(int q_total_rows, int k_total_rows, int n_seq) { return attn_scratch_bytes(0, 0, q_total_rows, k_total_rows, n_seq); }
+static size_t slots_size(size_t blocks, int reach, int shares) { return (blocks * shares * (2 * reach + 1) * 4 + 15) & ~(size_t)15; }
+static size_t slot_blocks(int n_heads, int q_total_rows, int n_seq) { return std::max(((size_t)q_total_rows / 64 + n_seq) * n_heads, (size_t)4 * kRelUnits); }
 static size_t rel_scratch_bytes(int n_heads, int head_dim, int reach, int q_total_rows, int k_total_rows, int n_seq) {
     const size_t entries = (size_t)n_heads * q_total_rows;
-    const size_t blocks = std::max(((size_t)q_total_rows / 64 + n_seq) * n_heads, (size_t)4 * kRelUnits);
-    const size_t backward = entries * 32 + blocks * (2 * reach + 1) * 4;
+    const size_t blocks = slot_blocks(n_heads, q_total_rows, n_seq);
+    const int shares = most_back_splits(n_heads, q_total_rows, k_total_rows, std::max(q_total_rows, k_total_rows), n_seq);
+    const size_t parts = shares > 1 ? (size_t)shares * ((size_t)q_total_rows + 2 * (size_t)k_total_rows) * n_heads * head_dim * 4 : 0;
+    const size_t backward = entries * 32 + slots_size(blocks, reach, shares) + parts;
     const int splits = std::max(most_splits(true, n_heads, head_dim, q_total_rows, k_total_rows, n_seq),
                                 few_splits(DS_DTYPE_F32, n_heads, head_dim, q_total_rows, 1, k_total_rows, n_seq));      // (never fewer than the others)
     const size_t forward = splits > 1 ? entries * splits * (head_dim + 4) * 4 : 0;
@@ -64,7 +103,7 @@ static ds_status check(RelAttnArgs& a) {
             four_at_once(a.dq, size) && four_at_once(a.dk, size) && four_at_once(a.dv, size) && a.ldq % 4 == 0 && a.ldk % 4 == 0 && a.ldv % 4 == 0 && a.ldo % 4 == 0;
     char* after_lists = (char*)a.scratch + lists_size(a.q_total_rows, a.k_total_rows, a.n_seq);
     const size_t entries = (size_t)a.n_heads * a.q_total_rows;
-    a.k_splits = 1;
+    a.k_splits = a.b_splits = 1;
     a.aug = after_lists;
     a.d = (float*)after_lists;
     a.slots = (float*)(after_lists + entries * 32);
@@ -81,10 +120,10 @@ static int blocks_without_list(int max_len, int total_rows, int n_seq) {
 }
 
 // How a call goes to the kernels: fp32 arithmetic or bf16 matrix cores; work-groups that share a head's keys (forward); bf16: whether there is no work list; the
-// kernel for few queries instead (forward)
-struct RelChoice { int32_t general, k_splits, direct, few; };
+// kernel for few queries instead (forward); work-groups that share a block (backward)
+struct RelChoice { int32_t general, k_splits, direct, few, b_splits; };
 static RelChoice choose(RelAttnArgs& a, bool backward, bool force_generic) {
-    RelChoice c = {1, 1, 0, 0};
+    RelChoice c = {1, 1, 0, 0, 1};
     if (!backward && !force_generic && rel_few_supported(a) && !rel_mfma_supported(a)) {
         c.few = 1;
         c.k_splits = a.k_splits = few_splits(a.dtype, a.n_heads, a.head_dim, a.q_total_rows, a.max_q_len, a.max_k_len, a.n_seq);
@@ -99,11 +138,16 @@ static RelChoice choose(RelAttnArgs& a, bool backward, bool force_generic) {
         if (a.direct_k == 0) c.direct = 0;
     }
     a.direct = c.direct;
+    if (!c.general && backward) {
+        c.b_splits = a.b_splits = back_splits(a);
+        a.part_q = a.slots + slots_size(slot_blocks(a.n_heads, a.q_total_rows, a.n_seq), a.reach, a.b_splits) / 4;
+        a.part_k = a.part_q + (size_t)a.b_splits * a.q_total_rows * a.n_heads * a.head_dim;
+    }
     return c;
 }
 
 // For tests: what `choose` says of a call whose tensors have the least strides and are aligned: the members of RelChoice, then blocks of keys without a list (backward)
-// and columns of a work-group of the general dQ and dK/dV kernels.  Not part of the C ABI's header.
+// columns of a work-group of the general dQ and dK/dV kernels, work-groups that share a block (backward); `backward`: bit 0, bit 1: causal.  Not part of the C ABI's header.
 extern "C" void ds_rel_attention_choice(int32_t dtype, int32_t n_seq, int32_t n_heads, int32_t head_dim, int32_t max_q_len, int32_t max_k_len, int32_t q_total_rows,
                                         int32_t k_total_rows, int32_t backward, int32_t force_generic, int32_t* out) {
     RelAttnArgs a = {};
@@ -111,8 +155,10 @@ extern "C" void ds_rel_attention_choice(int32_t dtype, int32_t n_seq, int32_t n_
     a.max_q_len = std::min(max_q_len, q_total_rows); a.max_k_len = std::min(max_k_len, k_total_rows);
     a.q_total_rows = q_total_rows; a.k_total_rows = k_total_rows;
     a.ldq = a.ldk = a.ldv = a.ldo = (long long)n_heads * head_dim;
-    const RelChoice c = choose(a, backward != 0, force_generic != 0);
-    for (const int32_t v : {c.general, c.k_splits, c.direct, c.few, backward && c.direct ? a.direct_k : 0, rel_general_columns(a, a.max_q_len), rel_general_columns(a, a.max_k_len)}) *out++ = v;
+    a.reach = 1;
+    a.mask = backward >> 1 & 1;
+    const RelChoice c = choose(a, backward & 1, force_generic != 0);
+    for (const int32_t v : {c.general, c.k_splits, c.direct, c.few, (backward & 1) && c.direct ? a.direct_k : 0, rel_general_columns(a, a.max_q_len), rel_general_columns(a, a.max_k_len), c.b_splits}) *out++ = v;
 }
 
 extern "C" int64_t ds_rel_attention_scratch_bytes(int32_t n_heads, int32_t head_dim, int32_t reach, int32_t q_total_rows, int32_t k_total_rows, int32_t n_seq) {

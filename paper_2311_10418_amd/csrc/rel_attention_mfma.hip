@@ -15,6 +15,7 @@
 // 55 (450; 20 / 48 %), dQ 76 (490; 22 / 45), dK/dV 91 (545; 28 / 29); 8 of 1 638 to 2 048, 16 heads of 128, causal, 160 (685; 32 / 41), 226 (725; 35 / 33), 332 (660; 33 / 25).  Forward
 // and dK/dV take as long as ordinary attention within 4 %: what the bias adds is the table's reads at near blocks and, in dQ, the diagonal sums.
 //
+// Backward with few blocks of rows (SHARED): work-groups share a block, each with some of the other side, and leave fp32 sums in the scratch.
 // Few queries over long keys (k_splits > 1): the keys of a head are dealt out to work-groups, see RelPart.  Where the grid of all blocks that a sequence
 // may have is hardly larger than the list's (direct), there is none: its launch takes 5 us.
 #include "rel_attention.hpp"
@@ -81,7 +82,7 @@ struct RelDraw {
         ctr = const_cast<int32_t*>(a.n_items) + kCtrHeader;
         groups = a.groups;
         fixed = a.direct != 0;
-        total = (a.direct ? a.n_seq * a.direct_k : a.n_items[1]) * a.n_heads;
+        total = (a.direct ? a.n_seq * a.direct_k : a.n_items[1]) * a.b_splits * a.n_heads;
         xcd = me & 7;
         k = me >> 3;
     }
@@ -318,7 +319,7 @@ __global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void rel_fwd_mfma_kernel(Rel
 }
 
 // ------------------------------------------------------------------------------------ backward: dQ (and delta)
-template <int HD, bool CAUSAL>
+template <int HD, bool CAUSAL, bool SHARED>
 __global__ __launch_bounds__(256, 2) void rel_bwd_dq_mfma_kernel(RelAttnArgs a) {
     extern __shared__ __attribute__((aligned(16))) char smem[];
     constexpr int TILE = 64 * HD * 2;
@@ -327,7 +328,8 @@ __global__ __launch_bounds__(256, 2) void rel_bwd_dq_mfma_kernel(RelAttnArgs a) 
     const int col = lane & 31, g = lane >> 5;
     TableFill fill;
     fill.buckets(a);
-    const int item = blockIdx.x / a.n_heads, h = blockIdx.x - item * a.n_heads;
+    const int place = blockIdx.x / a.n_heads, h = blockIdx.x - place * a.n_heads;
+    const int item = SHARED ? place / a.b_splits : place, share = SHARED ? place - item * a.b_splits : 0;
     int2 it;
     if (a.direct) {
         it = direct_item(a, item, a.direct, CAUSAL);
@@ -336,22 +338,30 @@ __global__ __launch_bounds__(256, 2) void rel_bwd_dq_mfma_kernel(RelAttnArgs a) 
         it = a.items_q[item];
     }
     const int s = __builtin_amdgcn_readfirstlane(it.x), q0 = __builtin_amdgcn_readfirstlane(it.y) * 128;
-    const int ql = __builtin_amdgcn_readfirstlane(a.q_len[s]), pos = __builtin_amdgcn_readfirstlane(rel_position(a, s));
+    const int ql = __builtin_amdgcn_readfirstlane(a.q_len[s]);
+    int pos = __builtin_amdgcn_readfirstlane(rel_position(a, s)), kfirst = 0;
     const int wide = table_floats(a.reach);
     float* table = reinterpret_cast<float*>(smem + 4 * TILE);
-    float* slot = a.slots + ((size_t)item * a.n_heads + h) * (2 * a.reach + 1);
+    float* slot = a.slots + ((size_t)place * a.n_heads + h) * (2 * a.reach + 1);
     if (q0 >= ql) {                                     // (a sequence without queries, where there is no list)
         for (int i = tid; i <= 2 * a.reach; i += 256) slot[i] = 0.f;
         return;
     }
     fill.biases(a, h);
-    const int kl = rel_keys(a, __builtin_amdgcn_readfirstlane(a.k_len[s]), ql, pos);
+    int kl = rel_keys(a, __builtin_amdgcn_readfirstlane(a.k_len[s]), ql, pos);
+    if constexpr (SHARED) {                             // keys kfirst .. kfirst + kl - 1 of those that this block sees: whole tiles, as evenly as they go
+        const int seen = CAUSAL ? min(kl, max(0, pos + min(q0 + 128, ql))) : kl;
+        const long long run = ((long long)seen + 64LL * a.b_splits - 1) / (64LL * a.b_splits) * 64;
+        kfirst = (int)min(run * share, (long long)seen);
+        kl = (int)min(run, (long long)seen - kfirst);
+        pos -= kfirst;                                  // positions are counted from the first key of this work-group
+    }
     const long long qrow0 = a.q_row[s];
     const bf16_t* Q = (const bf16_t*)a.q + qrow0 * a.ldq + h * HD;
     const bf16_t* dO = (const bf16_t*)a.d_o + qrow0 * a.ldo + h * HD;
     const bf16_t* O = (const bf16_t*)a.o + qrow0 * a.ldo + h * HD;
-    const bf16_t* K = (const bf16_t*)a.k + (long long)a.k_row[s] * a.ldk + h * HD;
-    const bf16_t* V = (const bf16_t*)a.v + (long long)a.k_row[s] * a.ldv + h * HD;
+    const bf16_t* K = (const bf16_t*)a.k + ((long long)a.k_row[s] + kfirst) * a.ldk + h * HD;
+    const bf16_t* V = (const bf16_t*)a.v + ((long long)a.k_row[s] + kfirst) * a.ldv + h * HD;
     const int qw0 = q0 + wave * 32;
     const int qi = qw0 + col;
     const int qi_c = qi < ql ? qi : ql - 1;
@@ -379,7 +389,7 @@ __global__ __launch_bounds__(256, 2) void rel_bwd_dq_mfma_kernel(RelAttnArgs a) 
     }
     delta += __shfl_xor(delta, 32, 64);
     const float lse_q = a.lse[(size_t)h * a.lse_stride + qrow0 + qi_c];
-    if (g == 0 && qi < ql) {
+    if (g == 0 && qi < ql && share == 0) {
         // for the dK/dV kernel: lse/scale and delta as the sums of three bf16 values, which it appends to its contractions
         const size_t at = (size_t)h * a.lse_stride + qrow0 + qi;
         reinterpret_cast<uint4*>(a.aug_lse)[at] = three_parts(lse_q == -INFINITY ? 1e30f : lse_q * (1.0f / a.scale));
@@ -517,7 +527,10 @@ __global__ __launch_bounds__(256, 2) void rel_bwd_dq_mfma_kernel(RelAttnArgs a) 
             }
         }
     }
-    if (qi < ql) store_cols<HD>(gacc, a.scale, (bf16_t*)a.dq + (qrow0 + qi) * a.ldq + h * HD, g);
+    if (qi < ql) {
+        if constexpr (SHARED) store_cols_f32<HD>(gacc, a.part_q + ((size_t)share * a.q_total_rows + qrow0 + qi) * ((size_t)a.n_heads * HD) + h * HD, g);
+        else store_cols<HD>(gacc, a.scale, (bf16_t*)a.dq + (qrow0 + qi) * a.ldq + h * HD, g);
+    }
     to[32] += carry;
     beyond_behind = wave_sum(beyond_behind);
     beyond_front = wave_sum(beyond_front);
@@ -555,7 +568,7 @@ __global__ __launch_bounds__(256, 2) void rel_bwd_dq_mfma_kernel(RelAttnArgs a) 
 // nothing hides what lies between two items (the end of one work-group, the start of the next, dependent table reads, the first tiles); measured with ordinary attention,
 // 65 536 tokens of mean length 385: 1015 -> 962 us.  Not at head size 64, where two work-groups share a CU and the dispatcher's replacement is quicker than a draw
 // (there, one-step items 47 us, 59 with draws).  Without a list lengths are much the same, and a work-group takes one item.
-template <int HD, bool CAUSAL>
+template <int HD, bool CAUSAL, bool SHARED>
 __global__ __launch_bounds__(256, HD == 64 ? 2 : 1) void rel_bwd_dkv_mfma_kernel(RelAttnArgs a) {
     extern __shared__ __attribute__((aligned(16))) char smem[];
     constexpr int TILE = 64 * HD * 2;
@@ -578,10 +591,10 @@ __global__ __launch_bounds__(256, HD == 64 ? 2 : 1) void rel_bwd_dkv_mfma_kernel
     RelDraw draw(a);
     float* table = reinterpret_cast<float*>(smem + NS * STAGE + 64 + 64 * HD);
     if ((int)blockIdx.x < a.first_group) {              // work-groups in front: one for each head sums up dbias
-        if ((int)blockIdx.x < a.n_heads) sum_dbias<256>(a, blockIdx.x, a.direct ? a.n_seq * a.direct : a.n_items[0], reinterpret_cast<float*>(smem));
+        if ((int)blockIdx.x < a.n_heads) sum_dbias<256>(a, blockIdx.x, (a.direct ? a.n_seq * a.direct : a.n_items[0]) * a.b_splits, reinterpret_cast<float*>(smem));
         return;
     }
-    int kw0, ki, kl, ql, h, q_begin, nb, pos, table_head = -1;
+    int kw0, ki, kl, ql, h, q_begin, nb, pos, share = 0, table_head = -1;
     int k0;
     long long krow0;
     const char* aug_src;
@@ -605,8 +618,12 @@ __global__ __launch_bounds__(256, HD == 64 ? 2 : 1) void rel_bwd_dkv_mfma_kernel
     // take up the item `draw` stands at: its tables, the first three blocks, the K / V fragments
     auto begin_item = [&] {
         fill.buckets(a);
-        const int item = draw.index() / a.n_heads;
+        int item = draw.index() / a.n_heads;
         h = draw.index() - item * a.n_heads;
+        if constexpr (SHARED) {
+            share = item % a.b_splits;
+            item /= a.b_splits;
+        }
         const int2 it = a.direct ? direct_item(a, item, a.direct_k, false) : a.items_k[item];
         const int s = __builtin_amdgcn_readfirstlane(it.x);
         k0 = __builtin_amdgcn_readfirstlane(it.y) * 128;
@@ -620,6 +637,12 @@ __global__ __launch_bounds__(256, HD == 64 ? 2 : 1) void rel_bwd_dkv_mfma_kernel
         ki = kw0 + col;
         q_begin = CAUSAL ? max(0, k0 - pos) : 0;
         nb = k0 < kl ? max(0, (ql - q_begin + 63) / 64) : 0;                  // (none: keys beyond the last query of a causal sequence)
+        if constexpr (SHARED) {                         // this work-group's blocks of queries: ql is the end of the last of them
+            const int run = (nb + a.b_splits - 1) / a.b_splits, first = min(run * share, nb);
+            nb = min(run, nb - first);
+            q_begin += 64 * first;
+            ql = min(ql, q_begin + 64 * nb);
+        }
         ldQ.base = reinterpret_cast<const char*>((const bf16_t*)a.q + qrow0 * a.ldq + h * HD);
         ldO.base = reinterpret_cast<const char*>((const bf16_t*)a.d_o + qrow0 * a.ldo + h * HD);
         ldQ.n_valid = ldO.n_valid = ql;
@@ -805,6 +828,7 @@ __global__ __launch_bounds__(256, HD == 64 ? 2 : 1) void rel_bwd_dkv_mfma_kernel
     const bool store = ki < kl;
     bf16_t* dk = (bf16_t*)a.dk + (krow0 + ki) * a.ldk + h * HD;
     bf16_t* dv = (bf16_t*)a.dv + (krow0 + ki) * a.ldv + h * HD;
+    float* part = SHARED ? a.part_k + ((size_t)share * a.k_total_rows + krow0 + ki) * (2 * (size_t)a.n_heads * HD) + h * HD : nullptr;
     bool more = false;
     if constexpr (PS) {
         if (tid == 0) s_next[turn] = next;
@@ -816,12 +840,42 @@ __global__ __launch_bounds__(256, HD == 64 ? 2 : 1) void rel_bwd_dkv_mfma_kernel
         if (more) begin_item();
     }
     if (store) {
-        store_cols<HD>(dkacc, a.scale, dk, g);
-        store_cols<HD>(dvacc, 1.0f, dv, g);
+        if constexpr (SHARED) {
+            store_cols_f32<HD>(dkacc, part, g);
+            store_cols_f32<HD>(dvacc, part + (size_t)a.n_heads * HD, g);
+        } else {
+            store_cols<HD>(dkacc, a.scale, dk, g);
+            store_cols<HD>(dvacc, 1.0f, dv, g);
+        }
     }
     if (!more) break;
     }   // for (;;): the next item
     if (PS) draw.finish();
+}
+
+// Backward: what the work-groups that shared a block found, in their order; blockIdx.z 0: dQ, 1: dK and dV, four features to a thread
+template <int HD> __global__ __launch_bounds__(256) void rel_back_join_kernel(RelAttnArgs a) {
+    const int s = blockIdx.y;
+    const bool keys = blockIdx.z != 0;
+    const long long row0 = keys ? a.k_row[s] : a.q_row[s], total = keys ? a.k_total_rows : a.q_total_rows;
+    const int wide = a.n_heads * HD, per = (keys ? 2 : 1) * wide / 4;
+    const long long n = (long long)(keys ? a.k_len[s] : a.q_len[s]) * per;
+    const float* from = keys ? a.part_k : a.part_q;
+    const size_t step = (size_t)total * per * 4;
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long long)gridDim.x * 256) {
+        const long long row = row0 + i / per;
+        const int c = (int)(i % per) * 4;
+        const float* p = from + (size_t)row * per * 4 + c;
+        f32x4_t sum = *reinterpret_cast<const f32x4_t*>(p);
+#pragma unroll 4
+        for (int k = 1; k < a.b_splits; ++k) sum += *reinterpret_cast<const f32x4_t*>(p + k * step);
+        const bool value = keys && c >= wide;
+        bf16_t* to = !keys ? (bf16_t*)a.dq + row * a.ldq + c : value ? (bf16_t*)a.dv + row * a.ldv + (c - wide) : (bf16_t*)a.dk + row * a.ldk + c;
+        bf16x4_t x;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = (bf16_t)(value ? sum[e] : sum[e] * a.scale);
+        *reinterpret_cast<bf16x4_t*>(to) = x;
+    }
 }
 
 template <int HD, bool CAUSAL>
@@ -836,25 +890,30 @@ ds_status fwd_launch(const RelAttnArgs& a, hipStream_t st) {
     return DS_OK;
 }
 
-template <int HD, bool CAUSAL>
+template <int HD, bool CAUSAL, bool SHARED>
 ds_status bwd_launch(const RelAttnArgs& a, hipStream_t st) {
     static std::atomic<uint64_t> allowed_q{0}, allowed_kv{0};
-    auto kq = rel_bwd_dq_mfma_kernel<HD, CAUSAL>;
-    auto kkv = rel_bwd_dkv_mfma_kernel<HD, CAUSAL>;
+    auto kq = rel_bwd_dq_mfma_kernel<HD, CAUSAL, SHARED>;
+    auto kkv = rel_bwd_dkv_mfma_kernel<HD, CAUSAL, SHARED>;
     const int smem_q = 4 * (64 * HD * 2) + 9 * table_floats(a.reach) * 4;
     const int smem_kv = 4 * (2 * (64 * HD * 2) + 2048) + 64 + 64 * HD + table_floats(a.reach) * 4;      // stages, draws, zeros, table
     ds_status r = allow_dynamic_lds(kq, kAllLds, allowed_q);
     if (r != DS_OK) return r;
     r = allow_dynamic_lds(kkv, kAllLds, allowed_kv);
     if (r != DS_OK) return r;
-    hipLaunchKernelGGL(kq, dim3((unsigned)(a.direct ? a.n_seq * a.direct : a.max_items_q) * a.n_heads), dim3(256), smem_q, st, a);
+    hipLaunchKernelGGL(kq, dim3((unsigned)(a.direct ? a.n_seq * a.direct : a.max_items_q) * a.b_splits * a.n_heads), dim3(256), smem_q, st, a);
     DS_LAUNCH_CHECK();
-    const unsigned items_kv = (unsigned)(a.direct ? a.n_seq * a.direct_k : a.max_items_k) * a.n_heads;
+    const unsigned items_kv = (unsigned)(a.direct ? a.n_seq * a.direct_k : a.max_items_k) * a.b_splits * a.n_heads;
     RelAttnArgs b = a;
     b.first_group = (a.n_heads + 7) / 8 * 8;            // (the rest keeps its XCDs)
     b.groups = dkv_persistent(HD) && !a.direct ? (int32_t)persistent_grid(items_kv) : (int32_t)items_kv;
     hipLaunchKernelGGL(kkv, dim3((unsigned)b.first_group + b.groups), dim3(256), smem_kv, st, b);
     DS_LAUNCH_CHECK();
+    if constexpr (SHARED) {
+        const long long pieces = std::max((long long)a.max_q_len, 2LL * a.max_k_len) * a.n_heads * (HD / 4);
+        hipLaunchKernelGGL(rel_back_join_kernel<HD>, dim3((unsigned)std::min((pieces + 255) / 256, 2048LL), a.n_seq, 2), dim3(256), 0, st, a);
+        DS_LAUNCH_CHECK();
+    }
     return DS_OK;
 }
 }  // namespace
@@ -892,6 +951,9 @@ ds_status rel_bwd_mfma(const RelAttnArgs& a0, hipStream_t st) {
     RelAttnArgs a = a0;
     const ds_status r = prepare(a, true, st);
     if (r != DS_OK) return r;
-    if (a.head_dim == 128) return a.mask ? bwd_launch<128, true>(a, st) : bwd_launch<128, false>(a, st);
-    return a.mask ? bwd_launch<64, true>(a, st) : bwd_launch<64, false>(a, st);
+    auto by_shares = [&](auto hd, auto causal) {
+        return a.b_splits > 1 ? bwd_launch<decltype(hd)::value, decltype(causal)::value, true>(a, st) : bwd_launch<decltype(hd)::value, decltype(causal)::value, false>(a, st);
+    };
+    auto by_mask = [&](auto hd) { return a.mask ? by_shares(hd, std::true_type{}) : by_shares(hd, std::false_type{}); };
+    return a.head_dim == 128 ? by_mask(std::integral_constant<int, 128>{}) : by_mask(std::integral_constant<int, 64>{});
 }

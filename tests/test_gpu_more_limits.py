@@ -32,10 +32,35 @@ def test_sequences_of_all_lengths_without_a_list(hd):
     for ql, kl, causal in (([400, 300, 390, 385, 257, 300], [300, 400, 390, 1, 390, 385], False), ([300, 257, 384, 290], [300, 257, 384, 290], True)):
         c = Case(32, BF, 2, hd, ql, kl, causal, gap=0)
         for backward in (0, 1):
-            out = (ctypes.c_int32 * 7)()
+            out = (ctypes.c_int32 * 8)()
             ds.lib().ds_rel_attention_choice(1, len(ql), 2, hd, max(ql), max(kl), c.Tq, c.Tk, backward, 0, out)
             assert out[2] > 0
         c.run(False, accumulate=causal)
+
+
+# query lengths, key lengths, causal, positions
+SHARED = [([700], [700], False, None), ([1500], [1500], True, None), ([1100, 3, 0, 700], [900, 1100, 50, 0], False, None), ([1030, 1100], [1030, 1100], True, None), ([520], [2000], True, [1480]),
+          ([60], [1300], False, [-700]), ([1300], [70], True, [-300]), ([2000, 1, 30, 2, 15], [2000, 1, 30, 2, 15], True, None), ([900], [1], False, None), ([1], [900], True, [899])]
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("case", SHARED, ids=lambda c: "-".join(map(str, c)).replace(" ", ""))
+def test_work_groups_share_blocks(case, hd):
+    """Backward with few blocks of rows: long ones, ends of sequences and positions that fall into any share, shares without anything."""
+    ql, kl, causal, pos = case
+    c = Case(36, BF, 1, hd, ql, kl, causal, pos=pos)
+    out = (ctypes.c_int32 * 8)()
+    ds.lib().ds_rel_attention_choice(1, len(ql), 1, hd, max(ql), max(kl), c.Tq, c.Tk, 1 + 2 * causal, 0, out)
+    assert out[7] > 1
+    c.run(False, accumulate=causal)
+    first = [t.clone() for t in (c.dq, c.dk, c.dv)]
+    for t in (c.dq, c.dk, c.dv):
+        t.fill_(9.0)
+    c.scratch.fill_(255)
+    c.backward()
+    torch.cuda.synchronize()
+    for s, t in zip(first, (c.dq, c.dk, c.dv)):
+        assert torch.equal(s, t)
 
 
 @pytest.mark.parametrize("hd", [64, 128])

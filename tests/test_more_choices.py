@@ -5,12 +5,12 @@ import pytest
 
 from paper_2311_10418_amd import binding as ds
 
-REL = ("general", "splits", "direct", "few", "direct_k", "dq_columns", "dkv_columns")
+REL = ("general", "splits", "direct", "few", "direct_k", "dq_columns", "dkv_columns", "shares")
 
 
-def rel(bf16=True, n_seq=16, heads=16, hd=64, max_q=100, max_k=100, q_rows=None, k_rows=None, backward=False, generic=False):
+def rel(bf16=True, n_seq=16, heads=16, hd=64, max_q=100, max_k=100, q_rows=None, k_rows=None, backward=False, generic=False, causal=False):
     out = (ctypes.c_int32 * len(REL))()
-    ds.lib().ds_rel_attention_choice(int(bf16), n_seq, heads, hd, max_q, max_k, q_rows or n_seq * max_q, k_rows or n_seq * max_k, int(backward), int(generic), out)
+    ds.lib().ds_rel_attention_choice(int(bf16), n_seq, heads, hd, max_q, max_k, q_rows or n_seq * max_q, k_rows or n_seq * max_k, int(backward) + 2 * int(causal), int(generic), out)
     return dict(zip(REL, out))
 
 
@@ -67,6 +67,24 @@ def test_no_list():
             for q_rows in (max_q, n_seq * max_q // 2 + max_q, n_seq * max_q, n_seq * max_q + 7):
                 c = rel(n_seq=n_seq, max_q=max_q, max_k=max_q, q_rows=q_rows, k_rows=q_rows, backward=True)
                 assert c["direct"] * n_seq <= q_rows // 64 + n_seq and c["direct_k"] * n_seq <= q_rows // 64 + n_seq
+
+
+def test_work_groups_share_blocks():
+    def shares(n_seq, length, heads, hd, **more):
+        return rel(n_seq=n_seq, heads=heads, hd=hd, max_q=length, max_k=length, backward=True, **more)["shares"]
+
+    assert shares(1, 1565, 4, 128) > 1 and shares(1, 511, 4, 64) == 1 and shares(1, 512, 4, 64) == 2 and shares(4, 600, 9, 128) == 1 and shares(31, 523, 16, 64) == 1
+    assert shares(1, 1565, 4, 128, bf16=False) == shares(1, 1565, 4, 128, generic=True) == shares(1, 1565, 4, 96) == 1
+    assert shares(1, 1565, 4, 128, causal=True) > 1 and shares(3, 1193, 5, 128, causal=True) == 2 and shares(2, 1181, 16, 64, causal=True) == 1
+    assert rel(n_seq=1, heads=4, max_q=1565, max_k=1565)["shares"] == 1                     # forward
+    for n_seq in (1, 2, 7):
+        for length in (100, 600, 3000, 20000):
+            for heads in (1, 3, 16):
+                for hd in (64, 128):
+                    s = max(shares(n_seq, length, heads, hd), shares(n_seq, length, heads, hd, causal=True))
+                    assert 1 <= s <= 8 and (s == 1 or s * (n_seq * length // 128 + n_seq) * heads <= 3 * 256 and length >= 256 * s)
+                    rows = n_seq * length
+                    assert ds.ds_rel_attention_scratch_bytes(heads, hd, 128, rows, rows, n_seq) >= 4 * 3 * s * rows * heads * hd * (s > 1)
 
 
 def test_general_columns():
