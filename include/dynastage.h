@@ -587,8 +587,8 @@ int64_t ds_rel_attention_scratch_bytes(int32_t n_heads, int32_t head_dim, int32_
  * Precision: bf16 heads of 64 and 128 with 16-byte aligned rows go to the matrix cores, where probabilities and their gradients are rounded to bf16 as they are
  * multiplied (at most 2^-8 of each); every other call, and with force_generic != 0 all of them, to kernels that compute in fp32.  Backward takes probabilities from lse:
  * they are off by up to 2^-22 of a score's size (after scaling, with its bias).
- * Speed: at most 64 queries over long keys (tokens on a cache) are shared out over work-groups if the q tensor has at most 64 rows for each sequence; the backward pass of few blocks
- * of 128 rows shares out the other side likewise.
+ * Speed: at most 64 queries over long keys (tokens on a cache) are shared out over work-groups if the q tensor has at most 64 rows for each sequence; so is the other
+ * side of blocks of 128 rows where those are few, in both directions.
  * Values that are not finite: a row is affected by the rows it sees.  The bf16 matrix-core kernels multiply whole blocks by probabilities that are 0 where mask = 1
  * hides a token, so that an infinity or NaN may also reach rows up to 63 tokens in front of it in o, up to 31 in dq (31 behind it in dk and dv). */
 ds_status ds_rel_attention_fwd(int32_t dtype, int32_t n_seq, int32_t n_heads, int32_t head_dim, int32_t mask, const int32_t* q_row,

@@ -33,6 +33,7 @@ struct RelAttnArgs : AttnArgs {
     int32_t first_group, groups;                        // dK/dV grid: work-groups in front that sum up dbias, work-groups behind them
 };
 
+constexpr int kRelShares = 8;                           // most work-groups that share a block of 128 rows in the matrix-core kernels
 // Work-groups that share the keys of a sequence and head leave, for each query, its maximum (exp2 domain), sum and unscaled output.
 struct RelPart { float *stat, *o; };
 __device__ __forceinline__ RelPart rel_part(const RelAttnArgs& a, int h, long long row, int split) {

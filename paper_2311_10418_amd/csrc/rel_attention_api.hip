@@ -25,22 +25,48 @@ static int few_splits(int32_t dtype, int n_heads, int head_dim, int q_total_rows
     return (int)std::max(1LL, std::min({4LL * kRelUnits / items, (long long)kSplitMost, ((long long)max_k_len + keys - 1) / keys}));
 }
 
-// Backward on the matrix cores: work-groups that may share a block of 128 rows (the scratch has room for as many), four blocks of 64 of the other side each at least.
-static constexpr int kBackMost = 8, kBackGroups = 3 * kRelUnits;
-static long long back_groups(int n_heads, int q_total_rows, int k_total_rows, int n_seq) {
+// The matrix-core kernels where blocks of 128 rows are few: work-groups that may share a block (the scratch has room for as many), four blocks of 64 of the other side each at least,
+// 56 MiB of sums at most.
+static constexpr int kShareGroups = 3 * kRelUnits;
+static constexpr long long kShareBytes = 56LL << 20;
+static long long share_groups(int n_heads, int q_total_rows, int k_total_rows, int n_seq) {
     return ((long long)std::max(q_total_rows, k_total_rows) / 128 + n_seq) * n_heads;
 }
-static int most_back_splits(int n_heads, int q_total_rows, int k_total_rows, int longest, int n_seq) {
-    return (int)std::max(1LL, std::min({kBackGroups / back_groups(n_heads, q_total_rows, k_total_rows, n_seq), (long long)kBackMost, (long long)longest / 256}));
+static int most_back_splits(int n_heads, int head_dim, int q_total_rows, int k_total_rows, int longest, int n_seq) {
+    const long long bytes = 4 * (q_total_rows + 2LL * k_total_rows) * n_heads * head_dim;
+    return (int)std::max(1LL, std::min({kShareGroups / share_groups(n_heads, q_total_rows, k_total_rows, n_seq), (long long)kRelShares, (long long)longest / 256, kShareBytes / bytes}));
+}
+// Forward with more than 64 queries, bf16: as many shares of the keys as an estimate prefers by a tenth: a work-group takes 4 us and `step` for each block of 64 keys, each more on a compute unit 0.45
+// of one alone; under a causal mask half as long on average; the shares are written, read and joined.
+// Measured, us, with 1 / 2 / 3 / 4 / most shares (sequences x length, heads of size, c: causal; *: chosen): 1 x 1 565, 4 of 128 c 33 / 26 / *23 / 23 / 24; 1 x 8 192, 2 of 64 c 109 / 67 / 50 / 43 / *40; 1 x 4 096,
+// 8 of 128 c 80 / *65; 1 x 1 024, 4 of 128 24 / 20 / 19 / *18; 4 x 600, 9 of 128 *21 / 30; 2 x 1 181, 16 of 64 c *22 / 29; 1 x 2 048, 16 of 128 c *44 / 43; 1 x 512, 4 of 64 *12.7 / 11.7.
+static int most_fwd_splits(int n_heads, int head_dim, int q_total_rows, int max_k_len, int n_seq) {
+    const long long bytes = 4LL * q_total_rows * n_heads * (head_dim + 4);
+    return (int)std::max(1LL, std::min({kShareGroups / share_groups(n_heads, q_total_rows, 0, n_seq), (long long)kRelShares, (long long)max_k_len / 256, kShareBytes / bytes}));
+}
+static int fwd_splits(const RelAttnArgs& a) {
+    const int most = most_fwd_splits(a.n_heads, a.head_dim, a.q_total_rows, a.max_k_len, a.n_seq), steps = (a.max_k_len + 63) / 64;
+    const double groups = (double)share_groups(a.n_heads, a.q_total_rows, 0, a.n_seq), step = a.head_dim == 64 ? 0.85 : 1.15;
+    const double part_us = 2.0 * 4 * a.q_total_rows * a.n_heads * (a.head_dim + 4) / 4.5e6;
+    double alone = 0, least = 0;
+    int best = 1;
+    for (int s = 1; s <= most; ++s) {
+        const double chain = step * ((steps + s - 1) / s) + 4, each = groups * s / kRelUnits;
+        double cost = (0.55 + 0.45 * std::max(1.0, std::ceil(each))) * chain;
+        if (a.mask) cost = std::max(chain, (0.55 + 0.45 * std::max(1.0, each)) * (4 + 0.5 * step * steps / s));
+        if (s == 1) alone = least = cost;
+        else if (cost += 4 + s * part_us; cost < least && cost < 0.9 * alone) least = cost, best = s;
+    }
+    return best;
 }
 // As many as an estimate of dQ and dK/dV together prefers by a tenth: a work-group takes `fixed` us and `step` for each block of 64 of the other side; one to a compute unit at head size
 // 128, at 64 two in 1.6 times the time of one; under a causal mask chains are half as long on average.  Shares are joined in a launch of their own (rel_back_join_kernel).
 // Measured, us, with 1 / 2 / 3 / 4 / most shares (sequences x length, heads of size, c: causal; *: chosen): 1 x 1 565, 4 of 128 c 97 / 72 / 61 / 57 / 56 (five: *54); 1 x 1 972, 3 of 64 c 80 / 54 / 45 /
 // 41 / 40 (five: *39); 3 x 1 193, 5 of 128 c 83 / *79 / 88 / 95; 2 x 1 181, 16 of 64 c *62 / 66; 1 x 1 024, 16 of 128 *72 / 69 / 88; 4 x 600, 9 of 128 *58 / 86; 1 x 8 192, 2 of 64 c 286 / 163 / 126 / *109 / 103; 1 x 4 096,
-// 8 of 128 c 224 / *177 / 175; 1 x 512, 4 of 64 31 / *26; 1 x 2 048, 16 of 128 c *124 / 118 / 116.
+// 8 of 128 c *224 / 177 / 175 (beyond 56 MiB); 1 x 512, 4 of 64 31 / *26; 1 x 2 048, 16 of 128 c *124 / 118 / 116.
 static int back_splits(const RelAttnArgs& a) {
-    const int longest = std::max(a.max_q_len, a.max_k_len), most = most_back_splits(a.n_heads, a.q_total_rows, a.k_total_rows, longest, a.n_seq);
-    const double groups = (double)back_groups(a.n_heads, a.q_total_rows, a.k_total_rows, a.n_seq), step = a.head_dim == 64 ? 2.2 : 3.05, fixed = a.head_dim == 64 ? 14 : 20;
+    const int longest = std::max(a.max_q_len, a.max_k_len), most = most_back_splits(a.n_heads, a.head_dim, a.q_total_rows, a.k_total_rows, longest, a.n_seq);
+    const double groups = (double)share_groups(a.n_heads, a.q_total_rows, a.k_total_rows, a.n_seq), step = a.head_dim == 64 ? 2.2 : 3.05, fixed = a.head_dim == 64 ? 14 : 20;
     const double pair = a.head_dim == 64 ? 1.6 : 2, part_us = 4 * ((double)a.q_total_rows + 2.0 * a.k_total_rows) * a.n_heads * a.head_dim / 4.5e6;
     const int steps = (longest + 63) / 64;
     double alone = 0, least = 0;
@@ -64,16 +90,17 @@ static int back_splits(const RelAttnArgs& a) {
 // them); the slots of dbias, for each share of each block of 64 queries (of 32 where the general kernels have at most 512 work-groups of 64); what shares of a block leave.  A forward call has the parts of
 // split keys in the place of the last two.
 static size_t lists_size(int q_total_rows, int k_total_rows, int n_seq) { return attn_scratch_bytes(0, 0, q_total_rows, k_total_rows, n_seq); }
-static size_t slots_size(size_t blocks, int reach, int shares) { return (blocks * shares * (2 * reach + 1) * 4 + 15) & ~(size_t)15; }
-static size_t slot_blocks(int n_heads, int q_total_rows, int n_seq) { return std::max(((size_t)q_total_rows / 64 + n_seq) * n_heads, (size_t)4 * kRelUnits); }
+static size_t slots_size(int n_heads, int q_total_rows, int n_seq, int reach, int shares) {
+    const size_t blocks = std::max(((size_t)q_total_rows / 64 + n_seq) * n_heads * shares, (size_t)4 * kRelUnits);
+    return (blocks * (2 * reach + 1) * 4 + 15) & ~(size_t)15;
+}
 static size_t rel_scratch_bytes(int n_heads, int head_dim, int reach, int q_total_rows, int k_total_rows, int n_seq) {
     const size_t entries = (size_t)n_heads * q_total_rows;
-    const size_t blocks = slot_blocks(n_heads, q_total_rows, n_seq);
-    const int shares = most_back_splits(n_heads, q_total_rows, k_total_rows, std::max(q_total_rows, k_total_rows), n_seq);
+    const int shares = most_back_splits(n_heads, head_dim, q_total_rows, k_total_rows, std::max(q_total_rows, k_total_rows), n_seq);
     const size_t parts = shares > 1 ? (size_t)shares * ((size_t)q_total_rows + 2 * (size_t)k_total_rows) * n_heads * head_dim * 4 : 0;
-    const size_t backward = entries * 32 + slots_size(blocks, reach, shares) + parts;
-    const int splits = std::max(most_splits(true, n_heads, head_dim, q_total_rows, k_total_rows, n_seq),
-                                few_splits(DS_DTYPE_F32, n_heads, head_dim, q_total_rows, 1, k_total_rows, n_seq));      // (never fewer than the others)
+    const size_t backward = entries * 32 + slots_size(n_heads, q_total_rows, n_seq, reach, shares) + parts;
+    const int splits = std::max({most_splits(true, n_heads, head_dim, q_total_rows, k_total_rows, n_seq), most_fwd_splits(n_heads, head_dim, q_total_rows, k_total_rows, n_seq),
+                                 few_splits(DS_DTYPE_F32, n_heads, head_dim, q_total_rows, 1, k_total_rows, n_seq)});    // (never fewer than the others)
     const size_t forward = splits > 1 ? entries * splits * (head_dim + 4) * 4 : 0;
     return lists_size(q_total_rows, k_total_rows, n_seq) + std::max(backward, forward);
 }
@@ -131,6 +158,7 @@ static RelChoice choose(RelAttnArgs& a, bool backward, bool force_generic) {
     }
     c.general = force_generic || !rel_mfma_supported(a);
     if (!backward && a.max_q_len <= kSplitQueries) c.k_splits = most_splits(c.general, a.n_heads, a.head_dim, a.q_total_rows, a.max_k_len, a.n_seq);
+    if (!c.general && !backward && a.max_q_len > kSplitQueries) c.k_splits = fwd_splits(a);
     a.k_splits = c.k_splits;
     if (!c.general) c.direct = blocks_without_list(a.max_q_len, a.q_total_rows, a.n_seq);
     if (c.direct && backward) {
@@ -140,7 +168,7 @@ static RelChoice choose(RelAttnArgs& a, bool backward, bool force_generic) {
     a.direct = c.direct;
     if (!c.general && backward) {
         c.b_splits = a.b_splits = back_splits(a);
-        a.part_q = a.slots + slots_size(slot_blocks(a.n_heads, a.q_total_rows, a.n_seq), a.reach, a.b_splits) / 4;
+        a.part_q = a.slots + slots_size(a.n_heads, a.q_total_rows, a.n_seq, a.reach, a.b_splits) / 4;
         a.part_k = a.part_q + (size_t)a.b_splits * a.q_total_rows * a.n_heads * a.head_dim;
     }
     return c;

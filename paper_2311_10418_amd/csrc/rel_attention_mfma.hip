@@ -15,7 +15,7 @@
 // 55 (450; 20 / 48 %), dQ 76 (490; 22 / 45), dK/dV 91 (545; 28 / 29); 8 of 1 638 to 2 048, 16 heads of 128, causal, 160 (685; 32 / 41), 226 (725; 35 / 33), 332 (660; 33 / 25).  Forward
 // and dK/dV take as long as ordinary attention within 4 %: what the bias adds is the table's reads at near blocks and, in dQ, the diagonal sums.
 //
-// Backward with few blocks of rows (SHARED): work-groups share a block, each with some of the other side, and leave fp32 sums in the scratch.
+// Few blocks of rows: work-groups share a block, each with some of the other side, and leave fp32 sums in the scratch (forward k_splits, backward b_splits and SHARED).
 // Few queries over long keys (k_splits > 1): the keys of a head are dealt out to work-groups, see RelPart.  Where the grid of all blocks that a sequence
 // may have is hardly larger than the list's (direct), there is none: its launch takes 5 us.
 #include "rel_attention.hpp"
@@ -119,9 +119,10 @@ __global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void rel_fwd_mfma_kernel(Rel
     fill.buckets(a);
     int item = blockIdx.x / a.n_heads;
     const int h = blockIdx.x - item * a.n_heads, split = a.k_splits > 1 ? item % a.k_splits : 0;
+    if (a.k_splits > 1) item /= a.k_splits;
     int2 it;
-    if (a.direct) {                                     // no list; work-groups that share keys: one block of queries to a sequence
-        it = direct_item(a, a.k_splits > 1 ? item / a.k_splits : item, a.direct, CAUSAL);
+    if (a.direct) {
+        it = direct_item(a, item, a.direct, CAUSAL);
     } else {
         it = a.items_q[item];                           // (within the list's capacity; read beside its length, not behind it)
         if (item >= a.n_items[0]) return;
@@ -131,7 +132,8 @@ __global__ __launch_bounds__(256, HD == 64 ? 3 : 2) void rel_fwd_mfma_kernel(Rel
     if (q0 >= ql) return;
     fill.biases(a, h);
     int kl = rel_keys(a, __builtin_amdgcn_readfirstlane(a.k_len[s]), ql, pos0), kfirst = 0;
-    if (a.k_splits > 1) {                               // keys kfirst .. kfirst + kl - 1: whole tiles, as evenly as they go
+    if (a.k_splits > 1) {                               // keys kfirst .. kfirst + kl - 1 of those that this block sees: whole tiles, as evenly as they go
+        if (CAUSAL) kl = min(kl, max(0, pos0 + min(q0 + 128, ql)));
         const long long run = ((long long)kl + 64LL * a.k_splits - 1) / (64LL * a.k_splits) * 64;
         kfirst = (int)min(run * split, (long long)kl);
         kl = (int)min(run, (long long)kl - kfirst);
@@ -853,6 +855,49 @@ __global__ __launch_bounds__(256, HD == 64 ? 2 : 1) void rel_bwd_dkv_mfma_kernel
     if (PS) draw.finish();
 }
 
+// Forward of many queries: what at most kRelShares work-groups that shared a block found, four features to a thread (rel_join is for few queries: a wavefront for each head of each)
+template <int HD> __global__ __launch_bounds__(256) void rel_rows_join_kernel(RelAttnArgs a) {
+    const int s = blockIdx.y, per = a.n_heads * (HD / 4), n = a.k_splits;
+    const long long row0 = a.q_row[s], all = (long long)a.q_len[s] * per;
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < all; i += (long long)gridDim.x * 256) {
+        const long long row = row0 + i / per;
+        const int at = (int)(i % per), h = at / (HD / 4), d = at % (HD / 4) * 4;
+        const RelPart p = rel_part(a, h, row, 0);
+        f32x4_t v[kRelShares];
+        float2 st[kRelShares];
+#pragma unroll
+        for (int k = 0; k < kRelShares; ++k)
+            if (k < n) {
+                st[k] = *reinterpret_cast<const float2*>(p.stat + k * (HD + 4));
+                v[k] = *reinterpret_cast<const f32x4_t*>(p.o + k * (HD + 4) + d);
+            }
+        float top = -INFINITY, sum = 0.f;
+#pragma unroll
+        for (int k = 0; k < kRelShares; ++k)
+            if (k < n && st[k].y != 0.f) top = fmaxf(top, st[k].x);
+        f32x4_t o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < kRelShares; ++k)
+            if (k < n) {                                // (a share without keys has sum 0, and its maximum does not count)
+                const float w = st[k].y == 0.f ? 0.f : __builtin_amdgcn_exp2f(st[k].x - top);
+                sum = __builtin_fmaf(w, st[k].y, sum);
+                o += w * v[k];
+            }
+        const float r = sum == 0.f ? 0.f : 1.0f / sum;
+        bf16x4_t x;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = (bf16_t)(o[e] * r);
+        *reinterpret_cast<bf16x4_t*>((bf16_t*)a.o + row * a.ldo + h * HD + d) = x;
+        if (d == 0) a.lse[(size_t)h * a.lse_stride + row] = (top + __builtin_amdgcn_logf(sum)) * kLn2;
+    }
+}
+template <int HD> ds_status rows_join(const RelAttnArgs& a, hipStream_t st) {
+    const long long pieces = (long long)a.max_q_len * a.n_heads * (HD / 4);
+    hipLaunchKernelGGL(rel_rows_join_kernel<HD>, dim3((unsigned)std::min((pieces + 255) / 256, 2048LL), a.n_seq), dim3(256), 0, st, a);
+    DS_LAUNCH_CHECK();
+    return DS_OK;
+}
+
 // Backward: what the work-groups that shared a block found, in their order; blockIdx.z 0: dQ, 1: dK and dV, four features to a thread
 template <int HD> __global__ __launch_bounds__(256) void rel_back_join_kernel(RelAttnArgs a) {
     const int s = blockIdx.y;
@@ -885,7 +930,7 @@ ds_status fwd_launch(const RelAttnArgs& a, hipStream_t st) {
     const int smem = 4 * (64 * HD * 2) + table_floats(a.reach) * 4;
     ds_status r = allow_dynamic_lds(kern, kAllLds, allowed);
     if (r != DS_OK) return r;
-    hipLaunchKernelGGL(kern, dim3((unsigned)(a.direct ? a.n_seq * a.direct * a.k_splits : a.max_items_q) * a.n_heads), dim3(256), smem, st, a);
+    hipLaunchKernelGGL(kern, dim3((unsigned)(a.direct ? a.n_seq * a.direct : a.max_items_q) * a.k_splits * a.n_heads), dim3(256), smem, st, a);
     DS_LAUNCH_CHECK();
     return DS_OK;
 }
@@ -928,7 +973,7 @@ bool rel_mfma_supported(const RelAttnArgs& a) {
     if (a.d_o && !(a.scale >= 0x1p-20f && a.scale <= 0x1p20f)) return false;        // (log-sum-exps reach the dK/dV kernel divided by it)
     // work-items of a launch: 32 bits
     const long long items = (long long)std::max(a.q_total_rows, a.k_total_rows) / 128 + (long long)a.n_seq * 2;
-    return items * a.n_heads + a.n_heads + 8 < 1LL << 23;       // (shares of keys: 512 work-groups at most)
+    return items * a.n_heads + a.n_heads + 8 < 1LL << 23;       // (shares only where work-groups are few)
 }
 
 static ds_status prepare(RelAttnArgs& a, bool backward, hipStream_t st) {
@@ -944,7 +989,9 @@ ds_status rel_fwd_mfma(const RelAttnArgs& a0, hipStream_t st) {
     if (r != DS_OK) return r;
     if (a.head_dim == 128) r = a.mask ? fwd_launch<128, true>(a, st) : fwd_launch<128, false>(a, st);
     else r = a.mask ? fwd_launch<64, true>(a, st) : fwd_launch<64, false>(a, st);
-    return r != DS_OK || a.k_splits == 1 ? r : rel_join(a, st);
+    if (r != DS_OK || a.k_splits == 1) return r;
+    if (a.max_q_len <= 64 || a.k_splits > kRelShares) return rel_join(a, st);
+    return a.head_dim == 128 ? rows_join<128>(a, st) : rows_join<64>(a, st);
 }
 
 ds_status rel_bwd_mfma(const RelAttnArgs& a0, hipStream_t st) {

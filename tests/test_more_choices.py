@@ -38,7 +38,7 @@ def test_single_tokens():
 
 def test_work_groups_share_keys():
     assert rel(max_q=8, max_k=128)["splits"] == 1 and rel(max_q=8, max_k=129)["splits"] == 2
-    assert rel(max_q=64, max_k=4000)["splits"] == 2 and rel(max_q=65, max_k=4000)["splits"] == 1 and rel(max_q=8, max_k=4000, q_rows=16 * 64 + 1)["splits"] == 1
+    assert rel(max_q=64, max_k=4000)["splits"] == 2 and rel(max_q=8, max_k=4000, q_rows=16 * 64 + 1)["splits"] == 1
     assert rel(n_seq=17, max_q=8, max_k=4000)["splits"] == 1 and rel(n_seq=9, hd=128, max_q=8, max_k=4000)["splits"] == 1 and rel(n_seq=8, hd=128, max_q=8, max_k=4000)["splits"] == 2
     assert rel(bf16=False, max_q=8, max_k=4000)["splits"] == 3 and rel(n_seq=1, heads=1, max_q=8, max_k=10000)["splits"] == 64 and rel(n_seq=1, heads=1, max_q=8, max_k=300)["splits"] == 5
     assert rel(max_q=8, max_k=4000, backward=True)["splits"] == 1
@@ -48,7 +48,7 @@ def test_scratch_holds_the_shares():
     for bf16 in (False, True):
         for hd in (32, 64, 96, 128):
             for n_seq in (1, 3, 16, 40):
-                for max_q in (1, 5, 64):
+                for max_q in (1, 5, 64, 65, 1000):
                     for max_k in (1, 200, 5000):
                         c = rel(bf16, n_seq, 4, hd, max_q, max_k)
                         need = 4 * n_seq * max_q * c["splits"] * (hd + 4) * 4 if c["splits"] > 1 else 0
@@ -76,13 +76,15 @@ def test_work_groups_share_blocks():
     assert shares(1, 1565, 4, 128) > 1 and shares(1, 511, 4, 64) == 1 and shares(1, 512, 4, 64) == 2 and shares(4, 600, 9, 128) == 1 and shares(31, 523, 16, 64) == 1
     assert shares(1, 1565, 4, 128, bf16=False) == shares(1, 1565, 4, 128, generic=True) == shares(1, 1565, 4, 96) == 1
     assert shares(1, 1565, 4, 128, causal=True) > 1 and shares(3, 1193, 5, 128, causal=True) == 2 and shares(2, 1181, 16, 64, causal=True) == 1
-    assert rel(n_seq=1, heads=4, max_q=1565, max_k=1565)["shares"] == 1                     # forward
+    assert rel(n_seq=1, heads=4, max_q=1565, max_k=1565)["shares"] == 1                     # forward: shares of keys
+    assert rel(n_seq=1, heads=4, hd=128, max_q=1565, max_k=1565, causal=True)["splits"] > 1 and rel(n_seq=1, heads=4, hd=128, max_q=1565, max_k=511)["splits"] == 1
+    assert rel(n_seq=4, heads=9, hd=128, max_q=600, max_k=600)["splits"] == 1 and rel(n_seq=1, heads=4, max_q=1565, max_k=1565, bf16=False)["splits"] == 1
     for n_seq in (1, 2, 7):
         for length in (100, 600, 3000, 20000):
             for heads in (1, 3, 16):
                 for hd in (64, 128):
                     s = max(shares(n_seq, length, heads, hd), shares(n_seq, length, heads, hd, causal=True))
-                    assert 1 <= s <= 8 and (s == 1 or s * (n_seq * length // 128 + n_seq) * heads <= 3 * 256 and length >= 256 * s)
+                    assert 1 <= s <= 8 and (s == 1 or s * (n_seq * length // 128 + n_seq) * heads <= 3 * 256 and length >= 256 * s and 12 * s * n_seq * length * heads * hd <= 56 << 20)
                     rows = n_seq * length
                     assert ds.ds_rel_attention_scratch_bytes(heads, hd, 128, rows, rows, n_seq) >= 4 * 3 * s * rows * heads * hd * (s > 1)
 
