@@ -588,7 +588,7 @@ int64_t ds_rel_attention_scratch_bytes(int32_t n_heads, int32_t head_dim, int32_
  * multiplied (at most 2^-8 of each); every other call, and with force_generic != 0 all of them, to kernels that compute in fp32.  Backward takes probabilities from lse:
  * they are off by up to 2^-22 of a score's size (after scaling, with its bias).
  * Speed: at most 64 queries over long keys (tokens on a cache) are shared out over work-groups if the q tensor has at most 64 rows for each sequence; so is the other
- * side of blocks of 128 rows where those are few, in both directions.
+ * side of blocks of 128 rows where those are few, in both directions (56 MiB of the scratch at most).
  * Values that are not finite: a row is affected by the rows it sees.  The bf16 matrix-core kernels multiply whole blocks by probabilities that are 0 where mask = 1
  * hides a token, so that an infinity or NaN may also reach rows up to 63 tokens in front of it in o, up to 31 in dq (31 behind it in dk and dv). */
 ds_status ds_rel_attention_fwd(int32_t dtype, int32_t n_seq, int32_t n_heads, int32_t head_dim, int32_t mask, const int32_t* q_row,
@@ -652,7 +652,7 @@ ds_status ds_resid_norm_bwd(int32_t dtype, int32_t rms, int32_t rows, int32_t d,
                             int32_t accumulate, void* hip_stream);
 int64_t ds_resid_norm_bwd_scratch_floats(int32_t rows, int32_t d);
 
-/* The gated feed-forward block, both projections, activation and product in one kernel:
+/* The gated feed-forward block, both projections, activation and product in one kernel (rows = 0: nothing happens):
  *     G = x Wg^T + bg,   U = x Wu^T + bu,   H = act(G) . U
  * x: [rows, d]; wg, wu: [d_ff, d], as forward products read them (one row per output); bg, bu: [d_ff] or NULL; h: [rows, d_ff].  All of the type dtype,
  * row-major, contiguous, 16-byte aligned; d and d_ff multiples of 8, at most 65 536; ceil(rows / 64) * ceil(max(d, d_ff) / 64) at most 2^23.  The activation sees the sums before they

@@ -48,7 +48,7 @@ ds_status check(int32_t dtype, int32_t rows, int32_t d, int32_t ff, std::initial
     if (rows < 0 || rows > kRows || d <= 0 || d % 8 || d > kWide || ff <= 0 || ff % 8 || ff > kWide) return DS_EINVAL;
     if (((int64_t)rows + 63) / 64 * ((std::max(d, ff) + 63) / 64) > 0x7fffffff / 256) return DS_EINVAL;       // (work-items of a launch)
     for (const void* p : needed)
-        if (!p || ((uintptr_t)p & 15)) return DS_EINVAL;
+        if ((!p && rows > 0) || ((uintptr_t)p & 15)) return DS_EINVAL;           // (a tensor without rows has no address)
     for (const void* p : others)
         if ((uintptr_t)p & 15) return DS_EINVAL;
     if (workspace_floats < 0 || (workspace_floats > 0 && (!workspace || ((uintptr_t)workspace & 15)))) return DS_EINVAL;

@@ -60,7 +60,7 @@ struct RowLoader {
     // k0: a multiple of 64 below K
     __device__ __forceinline__ void issue(uint32_t lds, int k0, int K) const {
         const uint32_t skip = (uint32_t)k0 * 2u;
-        const i32x4_t buf = make_raw_buffer(base + skip - 3072, bytes ? bytes - skip + 3072u : 0u);
+        const i32x4_t buf = make_raw_buffer(base + skip - 3 * 1024, bytes ? bytes - skip + 3 * 1024u : 0u);
         if (k0 + TK <= K) {
             lds_dma16_buffer_group<4>(buf, off, lds);
         } else {
@@ -188,7 +188,7 @@ struct ColumnLoader {
     // rows k0 .. k0 + 63 of those below k_end (k0 < k_end)
     __device__ __forceinline__ void issue(uint32_t lds, int k0, int k_end) const {
         const uint32_t bytes = (uint32_t)(min(TK, k_end - k0) - 1) * (uint32_t)ld2 + (uint32_t)cols_left2;
-        lds_dma16_buffer_group<4>(make_raw_buffer(base + (long long)k0 * ld2 - 3072, bytes + 3072u), off, lds);
+        lds_dma16_buffer_group<4>(make_raw_buffer(base + (long long)k0 * ld2 - 3 * 1024, bytes + 3 * 1024u), off, lds);
     }
 };
 

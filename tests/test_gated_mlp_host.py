@@ -32,12 +32,13 @@ SIZES = [dict(dtype=2), dict(dtype=-1), dict(rows=-1), dict(rows=2 ** 31 - 1), d
 @pytest.mark.parametrize("call,needed,others", [(_fwd, ("x", "wg", "wu", "h"), ("bg", "bu", "g", "u")), (_bwd, ("dh", "g", "u", "wg", "wu", "dg", "du", "dx"), ()),
                                                 (_wgrad, ("x", "dg", "du", "dwg", "dwu"), ("dbg", "dbu"))])
 def test_refusals(call, needed, others):
-    for kw in SIZES + [{n: None} for n in needed] + [{n: P + 8} for n in needed + others] + ([] if call is _wgrad else [dict(act=3), dict(act=-1)]):
+    for kw in SIZES + [{n: None, "rows": 4} for n in needed] + [{n: P + 8} for n in needed + others] + ([] if call is _wgrad else [dict(act=3), dict(act=-1)]):
         assert call(**kw) == BAD, kw
 
 
 def test_pairs_and_nothing_to_do():
     assert _fwd() == _bwd() == ds.DS_OK                         # no rows
+    assert _fwd(x=None, h=None) == _bwd(dh=None, g=None, u=None, dg=None, du=None, dx=None) == ds.DS_OK
     assert _fwd(g=P) == BAD and _fwd(u=P) == BAD
     assert _wgrad(rows=0) == BAD and _wgrad(accumulate=2) == BAD and _wgrad(dbg=P) == BAD and _wgrad(dbu=P) == BAD
     assert _wgrad(dbg=P, dbu=P) == BAD and _wgrad(dbg=P, dbu=P, workspace=P, floats=128 * 128 - 1) == BAD

@@ -161,6 +161,13 @@ def test_gated_block_behind_2_31_elements(dt, rows):
         assert np.all(np.abs(to_np(dx[-700:]) - ref) <= 2.0 ** -8 * np.abs(ref) + 2 * ff * U * size)
 
 
+@pytest.mark.parametrize("dt", [BF, F32])
+def test_gated_block_without_rows(dt):
+    x, h, w = torch.zeros((0, 64), dtype=dt, device=DEV), torch.zeros((0, 128), dtype=dt, device=DEV), torch.ones((128, 64), dtype=dt, device=DEV)
+    ds.ds_gated_mlp_fwd(x, w, w, h)
+    ds.ds_gated_mlp_bwd(h, h, h, w.t().contiguous(), w.t().contiguous(), h, h, x)
+
+
 @pytest.mark.parametrize("floats", [0, 4, 16, 20, 1000, 70000, 1 << 20])
 def test_gated_block_with_any_workspace(floats):
     """Large tiles with and without room for their counters and for partial sums."""
