@@ -10,7 +10,7 @@ constexpr int kRelReach = 1024, kRelBuckets = 1024, kRelLongest = 1 << 28;
 // matrix-core kernels as many as make two for every compute unit at head size 64, one at 128; general ones three.
 // Tokens on a cache, 16 heads, us, 1 / 2 / 3 / 4 to a compute unit: bf16, heads of 64, 16 sequences of 1 019 keys, one query  - / 19.0 / 17.6 / 20.9, of 16 384  - / 206 / 213 / 266,
 // one of 32 768  - / 32 / 36 / 43; heads of 128, 25.5 / 29.2 / 30.1 / 31.2, 431 / 390 / 435 / 387, 49 / 52 / 57 / 62; fp32, four queries, 1 019 keys: heads of 64  - / 41 / 36 / 44, of 128
-// 106 / 65 / 56 / 69.
+// 106 / 65 / 56 / 69.  (With a join that took shares beyond 16 one by one: at one of 32 768 it is 29 now, not 32.)
 static constexpr int kSplitQueries = 64, kSplitMost = 64;
 static int most_splits(bool general, int n_heads, int head_dim, int q_total_rows, int max_k_len, int n_seq) {
     const long long items = (long long)n_seq * n_heads;

@@ -7,8 +7,8 @@
 // lanes); each group of lanes keeps a softmax of its own (maximum, sum, output) and they meet in LDS at the end, those of the work-groups in rel_join.
 // fp32 arithmetic throughout.  Keys that a mask hides are not read.
 //
-// fp32, 16 heads, us (TB/s), before with the general kernels -> now: heads of 64, one sequence of 1 024 keys 10.1 -> 7.3, of 32 768 72 -> 59 (4.6), 16 of 1 019 40 -> 27 (4.9), 16 of 16 384
-// 458 -> 400 (5.4); heads of 128, 13.3 -> 8.0, 208 -> 115 (4.7), 106 -> 49 (5.4), 1 579 -> 699 (6.1).
+// fp32, 16 heads, us (TB/s), before with the general kernels -> now: heads of 64, one sequence of 1 024 keys 10.1 -> 7.3, of 32 768 72 -> 52 (5.2), 16 of 1 019 40 -> 27 (4.9), 16 of 16 384
+// 458 -> 400 (5.4); heads of 128, 13.3 -> 8.0, 208 -> 108 (5.0), 106 -> 49 (5.4), 1 579 -> 699 (6.1).
 #include "rel_attention.hpp"
 #include <initializer_list>
 

@@ -292,7 +292,9 @@ template <class T> __global__ __launch_bounds__(256) void rel_join_kernel(RelAtt
     const int hd = a.head_dim, n = a.k_splits;
     const size_t step = hd + 4;
     const RelPart p = rel_part(a, h, row, 0);
-    constexpr int kAtOnce = 16;                         // outputs on their way before the statistics are there
+    // outputs on their way together, the first of them before the statistics are there (those beyond 16 one by one: single tokens of 4 heads of 64, fp32, two caches of 8 192 keys 22.9 -> 13.2 us;
+    // 16 heads, one of 32 768 61 -> 52)
+    constexpr int kAtOnce = 16;
     const bool on = 2 * lane < hd;
     const float* from = p.o + (on ? 2 * lane : 0);
     auto load = [&](int i) { return *reinterpret_cast<const float2*>(from + min(i, n - 1) * step); };
@@ -308,8 +310,13 @@ template <class T> __global__ __launch_bounds__(256) void rel_join_kernel(RelAtt
 #pragma unroll
     for (int i = 0; i < kAtOnce; ++i)
         if (i < n) add(v[i], weight(i));
-#pragma unroll 8
-    for (int i = kAtOnce; i < n; ++i) add(load(i), weight(i));
+    for (int first = kAtOnce; first < n; first += kAtOnce) {
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) v[i] = load(first + i);
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i)
+            if (first + i < n) add(v[i], weight(first + i));
+    }
     const float r = sum == 0.f ? 0.f : 1.0f / sum;
     if (on) {
         T* to = (T*)a.o + row * a.ldo + (long long)h * hd + 2 * lane;
