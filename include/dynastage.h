@@ -576,7 +576,7 @@ int64_t ds_rel_attention_scratch_bytes(int32_t n_heads, int32_t head_dim, int32_
  *     S_ij = scale * q_i . k_j + bias[bucket[clamp(j - p_i, -reach, reach) + reach]][h],   P = softmax(S),   O = P V,   p_i = q_pos[s] + i.
  * Query i of sequence s stands at position p_i (q_pos: DEVICE int32[n_seq], or NULL: zeros; negative ones too), key j at position j.  mask = 1 hides keys with
  * j > p_i.  With q_pos the queries may be the last tokens of a longer sequence whose keys lie in a cache, down to a single one.
- * head_dim: a multiple of 8, at most 128.  scale: positive.  bias: [n_buckets, n_heads] of the tensors' type, contiguous; entries of -inf, or below -2.3e38 (a
+ * head_dim: a multiple of 8, at most 128.  scale: positive, at most 2.3e38 (refused where scale * log2 e is infinite).  bias: [n_buckets, n_heads] of the tensors' type, contiguous; entries of -inf, or below -2.3e38 (a
  * type's lowest value), hide what has their bucket.  bucket: DEVICE int32[2 * reach + 1] (ds_rel_buckets makes the usual ones, reach = max_distance; any other table will do, entries outside of
  * 0 .. n_buckets - 1 are clamped).  n_buckets and reach: at most 1024.
  * lse: float32 [n_heads, q_total_rows].  A row that sees no key has zeros in o (and gradients) and -inf in lse.

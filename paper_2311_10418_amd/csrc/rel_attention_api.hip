@@ -113,7 +113,7 @@ static ds_status check(RelAttnArgs& a) {
     if (a.mask != 0 && a.mask != 1) return DS_EINVAL;
     if (!a.q_row || !a.q_len || !a.k_row || !a.k_len || !a.q || !a.k || !a.v || !a.bias || !a.bucket || !a.o || !a.lse) return DS_EINVAL;
     if (a.reach < 1 || a.reach > kRelReach || a.n_buckets < 1 || a.n_buckets > kRelBuckets) return DS_EINVAL;
-    if (!(a.scale > 0.f) || std::isinf(a.scale)) return DS_EINVAL;
+    if (!(a.scale > 0.f) || std::isinf(a.scale * 1.4426950408889634f)) return DS_EINVAL;        // (the kernels multiply scores by this; infinite, it makes NaN of a score of 0)
     if (a.max_q_len <= 0 || a.max_k_len <= 0 || a.q_total_rows <= 0 || a.k_total_rows <= 0) return DS_EINVAL;
     if (a.n_seq > 65534 || a.n_heads > 65535) return DS_EINVAL;
     const long long wide = (long long)a.n_heads * a.head_dim;
