@@ -77,10 +77,11 @@ template <class T, int LANES> __global__ __launch_bounds__(256) void rel_few_ker
     for (int i = t; i <= 2 * a.reach; i += 256) table[i] = rel_bias(a, h, i);
     __syncthreads();
     float q[N], o[N], m = -INFINITY, l = 0.f;
+    const float c = a.scale * 1.4426950408889634f;      // (times the sum, as in the other kernels: times the query it might overflow where the score does not)
     qp.get(q);
 #pragma unroll
     for (int j = 0; j < N; ++j) {
-        q[j] = in ? q[j] * (a.scale * 1.4426950408889634f) : 0.f;
+        q[j] = in ? q[j] : 0.f;
         o[j] = 0.f;
     }
     for (int from = first; from < end; from += GROUPS * kLoads) {
@@ -93,7 +94,7 @@ template <class T, int LANES> __global__ __launch_bounds__(256) void rel_few_ker
 #pragma unroll
             for (int j = 0; j < N; ++j) dot = __builtin_fmaf(q[j], in ? f[j] : 0.f, dot);
             const int j = from + key + u * KEYS;
-            x[u] = j < end ? sum_lanes<LANES>(dot) + table[min(max(j - pos, -a.reach), a.reach) + a.reach] : -INFINITY;
+            x[u] = j < end ? __builtin_fmaf(sum_lanes<LANES>(dot), c, table[min(max(j - pos, -a.reach), a.reach) + a.reach]) : -INFINITY;
             up = fmaxf(up, x[u]);
         }
         const float use = up == -INFINITY ? 0.f : up, alpha = __builtin_amdgcn_exp2f(m - use);
