@@ -589,7 +589,9 @@ int64_t ds_rel_attention_scratch_bytes(int32_t n_heads, int32_t head_dim, int32_
  * they are off by up to 2^-22 of a score's size (after scaling, with its bias).
  * Speed: at most 64 queries over long keys (tokens on a cache) are shared out over work-groups if the q tensor has at most 64 rows for each sequence; so is the other
  * side of blocks of 128 rows where those are few, in both directions (56 MiB of the scratch at most).
- * Values that are not finite: a row is affected by the rows it sees.  The bf16 matrix-core kernels multiply whole blocks by probabilities that are 0 where mask = 1
+ * Values that are not finite: a row is affected by the rows it sees.  A bias is a term of the score, not a mask: tokens that only a bias of -inf hides may count as
+ * seen here (NaN - inf and 0 x inf are NaN, also where it hides all that a row might see).  Finite biases above 2.3e38 are taken as +inf.
+ * The bf16 matrix-core kernels multiply whole blocks by probabilities that are 0 where mask = 1
  * hides a token, so that an infinity or NaN may also reach rows up to 63 tokens in front of it in o, up to 31 in dq (31 behind it in dk and dv). */
 ds_status ds_rel_attention_fwd(int32_t dtype, int32_t n_seq, int32_t n_heads, int32_t head_dim, int32_t mask, const int32_t* q_row,
                                const int32_t* q_len, const int32_t* k_row, const int32_t* k_len, const int32_t* q_pos, int32_t max_q_len,
@@ -659,8 +661,8 @@ int64_t ds_resid_norm_bwd_scratch_floats(int32_t rows, int32_t d);
  * are rounded.  act: DS_ACT_GELU (tanh form), DS_ACT_SILU, DS_ACT_RELU.
  * g, u: [rows, d_ff], what the backward pass needs of G and U, or both NULL: nothing is kept.
  * row_valid: NULL, or DEVICE int32[rows]: rows with a negative entry are zeros in every output, whatever the inputs hold there (NaN too; dx: where the weights are finite).
- * workspace: DEVICE float32, 16-byte aligned, or NULL: room for partial sums and tile counters; ds_gated_mlp_workspace_floats is as much as any of the three calls uses, and a
- * smaller one is used as far as it goes.  Calls that share a workspace must not overlap.
+ * workspace: DEVICE float32, 16-byte aligned, or NULL: room for partial sums and tile counters.  ds_gated_mlp_workspace_floats is enough for any of the three calls; a smaller one
+ * is used as far as it goes, a larger one too where there is more to share out (the order of sums, and with it their last bits, depends on its size).  Calls that share a workspace must not overlap.
  * force_generic != 0 takes every product in fp32 matrix instructions; without it fp32 products may be made of bf16 parts of each value, as those of ds_gemm.  Forward, at most 64 rows go
  * to a kernel that reads the weights once. */
 enum { DS_ACT_GELU = 0, DS_ACT_SILU = 1, DS_ACT_RELU = 2 };
