@@ -592,7 +592,8 @@ int64_t ds_rel_attention_scratch_bytes(int32_t n_heads, int32_t head_dim, int32_
  * Values that are not finite: a row is affected by the rows it sees.  A bias is a term of the score, not a mask: tokens that only a bias of -inf hides may count as
  * seen here (NaN - inf and 0 x inf are NaN, also where it hides all that a row might see).  Finite biases above 2.3e38 are taken as +inf.
  * The bf16 matrix-core kernels multiply whole blocks by probabilities that are 0 where mask = 1
- * hides a token, so that an infinity or NaN may also reach rows up to 63 tokens in front of it in o, up to 31 in dq (31 behind it in dk and dv). */
+ * hides a token, so that an infinity or NaN may also reach rows up to 63 tokens in front of it in o, up to 31 in dq (31 behind it in dk and dv); where the position of a
+ * sequence's first query is not a multiple of 32, up to 94 and 62. */
 ds_status ds_rel_attention_fwd(int32_t dtype, int32_t n_seq, int32_t n_heads, int32_t head_dim, int32_t mask, const int32_t* q_row,
                                const int32_t* q_len, const int32_t* k_row, const int32_t* k_len, const int32_t* q_pos, int32_t max_q_len,
                                int32_t max_k_len, const void* q, int32_t ldq, const void* k, int32_t ldk, const void* v, int32_t ldv, float scale,

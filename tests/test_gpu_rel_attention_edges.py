@@ -1,4 +1,4 @@
-"""Attention with a relative position bias at scales near the ends of their range.  Tolerances as in test_gpu_rel_attention.py."""
+"""Attention with a relative position bias at scales near the ends of their range, and how far values that are not finite reach.  Tolerances as in test_gpu_rel_attention.py."""
 import numpy as np
 import pytest
 import torch
@@ -43,3 +43,46 @@ def test_largest_scale(dt, hd, generic):
         c.scale = 1.0                                   # (for the check: 0 times anything)
         c.check(generic, back=False)
         assert np.isfinite(to_np(c.lse)).all()
+
+
+# queries at any position see blocks of 64 (32) keys that begin at a multiple of 64 (32): where positions are not a multiple of 32 a block that the last of 32 queries sees
+# lies 31 tokens further in front of the first of them
+@pytest.mark.parametrize("bad", [float("inf"), float("nan")])
+@pytest.mark.parametrize("pos", [0, 64, 1, 45, 31])
+@pytest.mark.parametrize("length", [300, 1100])
+@pytest.mark.parametrize("hd", [64, 128])
+def test_how_far_hidden_values_that_are_not_finite_reach(hd, length, pos, bad):
+    """bf16 matrix-core kernels under a causal mask: rows further off than the header says keep their bits, in o, dq, dk and dv."""
+    front, back = (63, 31) if pos % 32 == 0 else (94, 62)
+    ref = Case(43, BF, 2, hd, [length], [length + pos], True, pos=[pos] if pos else None).tensors()
+    ref.forward()
+    ref.backward()
+    q0, k0 = ref.q_row[0], ref.k_row[0]
+    at = torch.arange(length, device="cuda") + pos          # positions of the queries
+    keys = torch.arange(length + pos, device="cuda")
+    farthest = {"o": 0, "dq": 0, "dk": 0, "dv": 0}
+
+    def differ(name, got, want, off):
+        """The largest distance of a row that differs; off: distance of each row, positive where the value is hidden from it."""
+        rows = (got != want).any(dim=1) & (off > 0)
+        far = int(off[rows].max()) if bool(rows.any()) else 0
+        farthest[name] = max(farthest[name], far)
+
+    for t in sorted({127, 128, 159, 191, 200, 223, 255, length + pos - 1, length // 2 + pos}):
+        c = Case(43, BF, 2, hd, [length], [length + pos], True, pos=[pos] if pos else None)
+        c.k[k0 + t] = c.v[k0 + t] = bad
+        c.tensors()
+        c.forward()
+        differ("o", c.o[q0:q0 + length], ref.o[q0:q0 + length], t - at)
+        c.o, c.lse = ref.o, ref.lse
+        c.backward()
+        differ("dq", c.dq[q0:q0 + length], ref.dq[q0:q0 + length], t - at)
+        i = min(t, length - 1)
+        c = Case(43, BF, 2, hd, [length], [length + pos], True, pos=[pos] if pos else None)
+        c.q[q0 + i] = c.d_o[q0 + i] = bad
+        c.tensors()
+        c.o, c.lse = ref.o, ref.lse
+        c.backward()
+        for n in ("dk", "dv"):
+            differ(n, getattr(c, n)[k0:k0 + length + pos], getattr(ref, n)[k0:k0 + length + pos], keys - (pos + i))
+    assert farthest["o"] <= front and max(farthest["dq"], farthest["dk"], farthest["dv"]) <= back
