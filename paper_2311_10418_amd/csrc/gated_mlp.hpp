@@ -66,3 +66,5 @@ ds_status glu_dx_f32(const GluArgs& a, float* ws, size_t ws_floats, hipStream_t 
 ds_status glu_fwd_big(const GluArgs& a, float* ws, size_t ws_floats, hipStream_t st);
 ds_status glu_dx_big(const GluArgs& a, float* ws, size_t ws_floats, hipStream_t st);
 double glu_big_cost(int M, int columns, int K, size_t ws_floats);
+// how such a product divides its tiles: whole ones, those whose contraction is cut up, pieces of it, whether work-groups are persistent
+void glu_big_division(const GluArgs& a, bool dx, size_t ws_floats, int32_t* out);

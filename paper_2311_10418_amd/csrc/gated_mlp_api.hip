@@ -118,6 +118,14 @@ extern "C" void ds_gated_mlp_choice(int32_t rows, int32_t d, int32_t d_ff, int32
     out[1] = c.splits;
 }
 
+// For tests: `choose`'s first member, then (of the 256 x 256 tiles, taken or not) glu_big_division.  Not part of the C ABI's header.
+extern "C" void ds_gated_mlp_division(int32_t rows, int32_t d, int32_t d_ff, int32_t dx, int64_t workspace_floats, int32_t* out) {
+    GluArgs a = {};
+    a.rows = rows; a.d = d; a.ff = d_ff;
+    out[0] = choose(a, dx != 0, (size_t)workspace_floats).big;
+    glu_big_division(a, dx != 0, (size_t)workspace_floats, out + 1);
+}
+
 extern "C" ds_status ds_gated_mlp_fwd(int32_t dtype, int32_t act, int32_t rows, int32_t d, int32_t d_ff, const void* x, const void* wg, const void* wu, const void* bg,
                                       const void* bu, const int32_t* row_valid, void* h, void* g, void* u, float* workspace, int64_t workspace_floats,
                                       int32_t force_generic, void* hip_stream) {

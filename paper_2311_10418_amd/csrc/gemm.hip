@@ -986,6 +986,9 @@ __global__ __launch_bounds__(256) void glu_tail_finish_kernel(int M, int N, int 
 __global__ void glu_clear_kernel(int* ctr) {
     if (threadIdx.x < 16) ctr[threadIdx.x] = 0;
 }
+// What of a workspace partial sums may have (the counters lie behind), and how the tiles are divided
+size_t glu_room(size_t floats) { return floats > 16 ? (floats - 16) & ~(size_t)3 : 0; }
+BigPlan glu_plan(bool dx, int M, int N, int K, size_t room) { return plan_big(false, DS_EPI_NONE, M, dx ? N : (N + 127) / 128 * BN, dx ? 2 * K : K, room); }
 // The gated block's products with 256 x 256 tiles: launch_nt with a tile's columns counted as the kernel counts them.  The tile counters of the persistent form lie at the
 // end of the caller's workspace, whose calls do not overlap, and are cleared here (2 us): two captured graphs never share any.
 template <int EPI, int GLU>
@@ -998,8 +1001,8 @@ ds_status launch_glu(int M, int N, int K, const void* A, const void* B, void* C,
     if (r != DS_OK) return r;
     r = allow_dynamic_lds(kern_ps, RING, allowed_ps);
     if (r != DS_OK) return r;
-    const size_t room = split_ws && split_ws_floats > 16 ? (split_ws_floats - 16) & ~(size_t)3 : 0;
-    const BigPlan plan = plan_big(false, EPI, M, GLU == 1 ? (N + 127) / 128 * BN : N, GLU == 2 ? 2 * K : K, room);
+    const size_t room = split_ws ? glu_room(split_ws_floats) : 0;
+    const BigPlan plan = glu_plan(GLU == 2, M, N, K, room);
     const int tiles = plan.tiles_m * plan.tiles_n, n_cu = gemm_cu_count();
     int* ctr = room && nt_persistent(plan) ? reinterpret_cast<int*>(split_ws + room) : nullptr;
     if (ctr) {
@@ -1245,6 +1248,14 @@ ds_status glu_fwd_big(const GluArgs& a, float* ws, size_t ws_floats, hipStream_t
 ds_status glu_dx_big(const GluArgs& a, float* ws, size_t ws_floats, hipStream_t st) {
     const GluOperands o = {(const bf16_t*)a.du, (const bf16_t*)a.wu, nullptr, nullptr, nullptr};
     return launch_glu<DS_EPI_NONE, 2>(a.rows, a.d, a.ff, a.dg, a.wg, a.dx, GemmEpi{}, o, ws, ws_floats, st);
+}
+void glu_big_division(const GluArgs& a, bool dx, size_t ws_floats, int32_t* out) {
+    const size_t room = glu_room(ws_floats);
+    const BigPlan plan = dx ? glu_plan(true, a.rows, a.d, a.ff, room) : glu_plan(false, a.rows, a.ff, a.d, room);
+    out[0] = plan.n_main;
+    out[1] = plan.tiles_m * plan.tiles_n - plan.n_main;
+    out[2] = plan.tail_splits;
+    out[3] = room && nt_persistent(plan);
 }
 double glu_big_cost(int M, int columns, int K, size_t ws_floats) { return big_cost(plan_big(false, DS_EPI_NONE, M, columns, K, ws_floats), false, M, columns); }
 
