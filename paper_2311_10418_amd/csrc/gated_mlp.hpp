@@ -61,6 +61,7 @@ ds_status glu_wgrad_tile(const GluWgrad& a, hipStream_t st);
 bool glu_f32_supported(const GluArgs& a);
 ds_status glu_fwd_f32(const GluArgs& a, hipStream_t st);
 ds_status glu_dx_f32(const GluArgs& a, float* ws, size_t ws_floats, hipStream_t st);
+int glu_dx_f32_columns(const GluArgs& a);              // columns of a tile of dx; 0: two products instead
 // the same with 256 x 256 tiles (gemm.hip): d and d_ff multiples of 64, dx: d of 256; and the estimate of their time in microseconds, of `columns` (a multiple of 256)
 // weight rows and a contraction over K
 ds_status glu_fwd_big(const GluArgs& a, float* ws, size_t ws_floats, hipStream_t st);

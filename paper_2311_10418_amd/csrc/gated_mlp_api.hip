@@ -126,6 +126,13 @@ extern "C" void ds_gated_mlp_division(int32_t rows, int32_t d, int32_t d_ff, int
     glu_big_division(a, dx != 0, (size_t)workspace_floats, out + 1);
 }
 
+// For tests: columns of a tile of dx in fp32, 0: two products, -1: fp32 matrix instructions.  Not part of the C ABI's header.
+extern "C" int32_t ds_gated_mlp_f32_columns(int32_t rows, int32_t d, int32_t d_ff) {
+    GluArgs a = {};
+    a.dtype = DS_DTYPE_F32; a.rows = rows; a.d = d; a.ff = d_ff;
+    return split_f32(a, true) ? glu_dx_f32_columns(a) : -1;
+}
+
 extern "C" ds_status ds_gated_mlp_fwd(int32_t dtype, int32_t act, int32_t rows, int32_t d, int32_t d_ff, const void* x, const void* wg, const void* wu, const void* bg,
                                       const void* bu, const int32_t* row_valid, void* h, void* g, void* u, float* workspace, int64_t workspace_floats,
                                       int32_t force_generic, void* hip_stream) {

@@ -736,15 +736,20 @@ ds_status glu_fwd_f32(const GluArgs& a, hipStream_t st) {
         return launch_glu<decltype(act)::value, G_BN, 1>(64, a.rows, a.ff, a.d, (const float*)a.x, (const float*)a.wg, (float*)a.h, p, o, st);
     });
 }
+int glu_dx_f32_columns(const GluArgs& a) {
+    const long long rows = (a.rows + 63) / 64, wide = (a.d + 127) / 128, narrow = (a.d + 63) / 64;
+    const int n_cu = gemm_cu_count();
+    if (rows * wide >= 2 * n_cu && 2 * wide - narrow <= narrow / 8) return 128;
+    return rows * narrow >= n_cu * 7 / 8 ? 64 : 0;
+}
 ds_status glu_dx_f32(const GluArgs& a, float* ws, size_t ws_floats, hipStream_t st) {
     GemmEpi p{};
     p.row_valid = a.row_valid;
     const GluOperandsF32 o = {(const float*)a.du, (const float*)a.wu, nullptr, nullptr, nullptr};
     const float *dg = (const float*)a.dg, *wg = (const float*)a.wg;
-    const long long rows = (a.rows + 63) / 64, wide = (a.d + 127) / 128, narrow = (a.d + 63) / 64;
-    const int n_cu = gemm_cu_count();
-    if (rows * wide >= 2 * n_cu && 2 * wide - narrow <= narrow / 8) return launch_glu<DS_EPI_NONE, 128, 2>(128, a.rows, a.d, a.ff, dg, wg, (float*)a.dx, p, o, st);
-    if (rows * narrow >= n_cu * 7 / 8) return launch_glu<DS_EPI_NONE, 64, 2>(64, a.rows, a.d, a.ff, dg, wg, (float*)a.dx, p, o, st);
+    const int columns = glu_dx_f32_columns(a);
+    if (columns == 128) return launch_glu<DS_EPI_NONE, 128, 2>(128, a.rows, a.d, a.ff, dg, wg, (float*)a.dx, p, o, st);
+    if (columns == 64) return launch_glu<DS_EPI_NONE, 64, 2>(64, a.rows, a.d, a.ff, dg, wg, (float*)a.dx, p, o, st);
     // few work-groups: two products, which cut their contractions
     ds_status r = launch_gemm_f32_mfma(0, 1, a.rows, a.d, a.ff, a.dg, a.wg, a.dx, DS_EPI_NONE, GemmEpi{}, ws, ws_floats, st);
     if (r != DS_OK) return r;
