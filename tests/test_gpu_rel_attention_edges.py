@@ -86,3 +86,14 @@ def test_how_far_hidden_values_that_are_not_finite_reach(hd, length, pos, bad):
         for n in ("dk", "dv"):
             differ(n, getattr(c, n)[k0:k0 + length + pos], getattr(ref, n)[k0:k0 + length + pos], keys - (pos + i))
     assert farthest["o"] <= front and max(farthest["dq"], farthest["dk"], farthest["dv"]) <= back
+
+
+@pytest.mark.parametrize("dt,hd,generic", [(BF, 64, False), (BF, 128, False), (BF, 64, True), (F32, 64, False), (F32, 32, False)])
+def test_row_strides_that_put_tensors_beyond_2_31_elements(dt, hd, generic):
+    """Column ranges of tensors with 2^20 columns more: the last of 2 100 rows begin behind 2^31 elements."""
+    c = Case(44, dt, 2, hd, [1200, 900], [1000, 1200], False, pad_cols=1 << 20)
+    assert min(c.Tq, c.Tk) > 2048 + 50
+    c.run(generic)
+    torch.cuda.synchronize()
+    c = Case(45, dt, 2, hd, [1, 1], [1000, 1100], True, pos=[999, 1099], pad_cols=1 << 20)
+    c.run(generic, back=False)
