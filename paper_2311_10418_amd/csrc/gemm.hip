@@ -154,8 +154,9 @@ __host__ __device__ __forceinline__ void nt_tile_coords(int logical, int tiles_m
 //      others Wu's for the same 64 columns (each wavefront fetches 64 of one matrix), so that the two halves of its accumulators are G and U of the same
 //      outputs: one even and one odd pass of the epilogue.  N is the width of H, a multiple of 64: a wavefront has all its columns or none.
 //   2  dx: the K loop runs through (A, B) and then through (second_a, second_b); K is the length of one of them.
-// Measured, 65 629 x 1024 x 2816, us (TFLOP/s; share of the cycles with the matrix pipe busy): forward with G and U kept 722 (1 049; 51 %), dx 546 (1 387; 69 %).  Bound by the epilogue
-// (1: three tensors of 370 MB leave in bursts behind a contraction of only 1024) and by the clock under load.
+// Measured, 65 629 x 1024 x 2816, us (TFLOP/s; share of the compute units' busy cycles with the matrix pipe busy): forward with G and U kept 698 - 722 (1 049 - 1 085; 53 %), dx 546 (1 387;
+// 75 %).  What 1 loses against 2 it loses in the epilogue, behind a contraction of only 1024: its three tensors are 1.1 GB, and the entries of row_valid (read where there is none, too) are loaded
+// between the stores and used at once.  Memory operations are counted in order, so that each of those loads is a wait for the stores before it, 24 times a tile; the plain epilogue has none.
 struct GluOperands {
     const bf16_t *second_a, *second_b;              // forward: B is Wg, second_b Wu
     const bf16_t* bu;                               // forward: bias of U (that of G is p.bias)

@@ -10,7 +10,8 @@
 // the wavefront's own in LDS, 16 lanes (16 distances) at a time.
 //
 // Bound by the trips between memory, LDS and the products at short sequences (a tile of 64 rows costs 2.5 us of which the matrix instructions are 1, and a kernel has 5 us besides): fp32, 23
-// sequences of 88 to 177, 4 heads of 64, causal, dQ 23 us and dK/dV 26 (matrix pipe 8 and 10 % of the cycles).
+// sequences of 88 to 177, 4 heads of 64, causal, dQ 23 us and dK/dV 26 (matrix pipe 8 and 10 % of the cycles).  dK/dV with work-groups of 32 columns, which such calls take, has 136 registers
+// at head size 64: three wavefronts to a SIMD, and so one work-group of eight to a compute unit.  With 64 columns it has 128 and spills 3 or 4.
 //
 // Causal masks and values that are not finite: as in the general kernels of differential attention, a wavefront whose sums are not finite in the end takes its
 // columns one by one (rel_attention_rows.hpp), so that a row is affected by the rows it sees and by no others.

@@ -10,10 +10,13 @@
 // 16 heads of 64.)  Work-groups leave their sums in a slot; work-groups in front of the dK/dV grid add the slots up.
 // dK/dV: the loop over the blocks of queries is cut by distance, so that steps stay straight code: steps with the table and steps with one number.
 //
-// What bounds them: vector instructions beside the matrix pipe (exponential, FMA, maximum and packing of every score), which share a SIMD's issue.  Measured, us
-// (TFLOP/s of the products that they do; share of the cycles with the matrix pipe / with the vector ALU busy): 31 sequences of 366 to 523, 16 heads of 64, bidirectional, forward
-// 55 (450; 20 / 48 %), dQ 76 (490; 22 / 45), dK/dV 91 (545; 28 / 29); 8 of 1 638 to 2 048, 16 heads of 128, causal, 160 (685; 32 / 41), 226 (725; 35 / 33), 332 (660; 33 / 25).  Forward
-// and dK/dV take as long as ordinary attention within 4 %: what the bias adds is the table's reads at near blocks and, in dQ, the diagonal sums.
+// What bounds them: forward and dQ at head size 64 the issue of a SIMD, which vector instructions (exponential, FMA, maximum and packing of every score) share with the matrix pipe's; the
+// others, with one or two wavefronts to a SIMD, that and waits for fragments and transfers.  Measured, us (TFLOP/s of the products that they do; share of the compute units' busy cycles
+// with the matrix pipe / with the vector ALU busy / with any instruction issued): 31 sequences of 366 to 523, 16 heads of 64, bidirectional, forward 55 (450; 26 / 63 / 94 %), dQ 76 (490; 28 / 58 / 93),
+// dK/dV 91 (545; 35 / 36 / 63); 8 of 1 638 to 2 048, 16 heads of 128, causal, 160 (685; 42 / 54 / 80), 226 (725; 42 / 41 / 65), 332 (660; 38 / 29 / 44).  A fifth of a launch (heads of 128, dK/dV: an
+// eighth) compute units have no work: its start and its last round.  Forward and dK/dV take as long as ordinary attention within 4 %: what the bias adds is the table's reads at near blocks and,
+// in dQ, the diagonal sums.
+// Registers: dK/dV at head size 64 without a mask has all 256 and spills 4 or 5 more; at 128 it keeps 192 to 240 in accumulation registers, 64 of which move over in every step.
 //
 // Few blocks of rows: work-groups share a block, each with some of the other side, and leave fp32 sums in the scratch (forward k_splits, backward b_splits and SHARED).
 // Few queries over long keys (k_splits > 1): the keys of a head are dealt out to work-groups, see RelPart.  Where the grid of all blocks that a sequence
