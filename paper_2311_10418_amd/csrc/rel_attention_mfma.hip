@@ -12,8 +12,8 @@
 //
 // What bounds them: forward and dQ at head size 64 the issue of a SIMD, which vector instructions (exponential, FMA, maximum and packing of every score) share with the matrix pipe's; the
 // others, with one or two wavefronts to a SIMD, that and waits for fragments and transfers.  Measured, us (TFLOP/s of the products that they do; share of the compute units' busy cycles
-// with the matrix pipe / with the vector ALU busy / with any instruction issued): 31 sequences of 366 to 523, 16 heads of 64, bidirectional, forward 55 (450; 26 / 63 / 94 %), dQ 76 (490; 28 / 58 / 93),
-// dK/dV 91 (545; 35 / 36 / 63); 8 of 1 638 to 2 048, 16 heads of 128, causal, 160 (685; 42 / 54 / 80), 226 (725; 42 / 41 / 65), 332 (660; 38 / 29 / 44).  A fifth of a launch (heads of 128, dK/dV: an
+// with the matrix pipe / with the vector ALU busy / with any instruction issued): 31 sequences of 366 to 523, 16 heads of 64, bidirectional, forward 55 (450; 26 / 63 / 95 %), dQ 76 (490; 28 / 58 / 93),
+// dK/dV 91 (545; 35 / 36 / 63); 8 of 1 638 to 2 048, 16 heads of 128, causal, 160 (685; 42 / 54 / 80), 226 (725; 42 / 41 / 65), 332 (660; 38 / 28 / 44).  A fifth of a launch (heads of 128, dK/dV: an
 // eighth) compute units have no work: its start and its last round.  Forward and dK/dV take as long as ordinary attention within 4 %: what the bias adds is the table's reads at near blocks and,
 // in dQ, the diagonal sums.
 // Registers: dK/dV at head size 64 without a mask has all 256 and spills 4 or 5 more; at 128 it keeps 192 to 240 in accumulation registers, 64 of which move over in every step.
