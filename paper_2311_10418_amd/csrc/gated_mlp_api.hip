@@ -7,7 +7,8 @@
 
 namespace {
 
-// dG and dU, 8 elements to a thread.  dg may be g, du may be u.  Bound by memory: three tensors read, two written
+// dG and dU, 8 elements to a thread.  They are outputs, which the weight gradients take, and dx is made of them as they are stored: in bf16 the matrix instructions would round them as they
+// are multiplied all the same (error of dx against 64 bits, relative, 0.0023; rounded once from fp32 it would be 0.0017).  dg may be g, du may be u.  Bound by memory: three tensors read, two written
 // (65 629 x 2816 in bf16: 309 us, 6.0 TB/s).
 template <class T, int ACT>
 __global__ __launch_bounds__(256) void glu_grad_kernel(long long n8, int ff8, const T* __restrict__ dh, const T* g, const T* u, const int32_t* __restrict__ row_valid, T* dg, T* du) {
